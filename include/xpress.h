@@ -47,7 +47,7 @@ typedef enum {
   XP_ENOMEM = -4         /* device allocation of the workspace failed              */
 } xp_status;
 
-typedef enum { XP_F32 = 0, XP_BF16 = 1 } xp_dtype;
+typedef enum { XP_F32 = 0, XP_BF16 = 1, XP_E4M3 = 2 /* 8-bit caches only */ } xp_dtype;
 
 /* flags of xp_refine_block */
 #define XP_EARLY_EXIT   1u  /* skip the remaining passes once every sequence is at its fixed point */
@@ -57,6 +57,10 @@ typedef enum { XP_F32 = 0, XP_BF16 = 1 } xp_dtype;
 #define XP_DEVERR_TOKEN 1u  /* a token id outside [0, V) was read and replaced by 0 */
 #define XP_DEVERR_TEMPERATURE 2u  /* a sampled row's temperature was not finite and > 0; 1 was used */
 #define XP_DEVERR_FILTER 4u       /* a sampled row's top_k < 0 or top_p <= 0 (or NaN); not applied */
+#define XP_DEVERR_PAGE 8u     /* a page id outside [0, n_pages) where a key is; page 0 was read, or no slot given */
+#define XP_DEVERR_SLOT 16u    /* a slot outside the cache, not written; or more new tokens than slots */
+#define XP_DEVERR_POOL 32u    /* too few free pages (requests not served), or a pool count out of range */
+#define XP_DEVERR_LENGTH 64u  /* a length, token range or page count out of range; clamped or left alone */
 
 typedef struct xp_handle xp_handle;
 
@@ -358,6 +362,180 @@ xp_status xp_layer_forward_noalloc(const xp_layer_weights* w, int32_t batch, int
                                    int32_t causal, const void* x, const void* k_cache,
                                    const void* v_cache, int32_t C_max, const int32_t* ctx_len,
                                    float* h_f32, void* h_bf16, void* stream);
+
+/*
+ * The paged context cache: the keys and values that context layers attend to,
+ * kept in pages so that requests grow by the tokens that verification accepts,
+ * shrink by those it rejects, and share a common prefix.
+ *
+ *   k_cache, v_cache [n_pages][n_kv][page_size][head_dim]   caller-owned
+ *       XP_BF16, or XP_E4M3 with a scale per KV head (k_scale, v_scale [n_kv]
+ *       float, > 0; NULL: 1): the value of an entry is e4m3 times the scale
+ *   table [..][table_ld] int32   the pages of each request, in order; key j of
+ *       request b is row j % page_size of page table[b][j / page_size]
+ *   a slot is page * page_size + row
+ *
+ * Built: head_dim 64 or 128; any whole group n_heads / n_kv up to 64;
+ * page_size 16, 32, 64, 128 or 256; n_pages * page_size below 2^31.
+ */
+typedef struct {
+  int32_t n_heads, n_kv, head_dim;
+  int32_t page_size, n_pages;
+  int32_t dtype;                     /* xp_dtype of the caches: XP_BF16 or XP_E4M3 */
+} xp_kv_shape;
+
+typedef struct xp_kv xp_kv;
+
+/*
+ * Create a handle for calls of up to max_batch (<= 4096) requests, max_tokens
+ * (<= 2^20) new tokens and requests of up to max_len (<= 2^22) keys on the
+ * current device; allocates the workspace (freed by xp_kv_destroy; with
+ * shared = 1 also 8 * (head_dim + 2) bytes a token and query head for
+ * xp_kv_attn_shared).  Synchronous.  Calls on one handle share its workspace:
+ * issue them in stream order, and replay captured graphs of them in that order
+ * too.  A call runs with the handle's device as the current one.
+ * Errors: XP_EINVAL (null pointers, sizes), XP_EUNSUPPORTED (shapes outside the
+ * built set), XP_ENOMEM, XP_EHIP.  *out is NULL on error; xp_kv_last_error(NULL)
+ * names the problem.
+ */
+xp_status xp_kv_create(const xp_kv_shape* shape, int32_t max_batch, int32_t max_tokens,
+                       int32_t max_len, int32_t shared, xp_kv** out);
+
+/* Free the handle and its workspace (waits for the device first).  NULL is a no-op. */
+void xp_kv_destroy(xp_kv* kv);
+
+/* Message of the last failed call on `kv` (NULL: of this thread's last failed xp_kv_create). */
+const char* xp_kv_last_error(const xp_kv* kv);
+
+/*
+ * Pages and slots of n requests from their lengths, on the device.
+ *
+ *   lens [n], add [n] int32   tokens that request b has in the cache, and new
+ *       tokens it is to hold beside them.  After verification: the accepted
+ *       length and the next block's; add = 0 trims, lens = add = 0 ends a request
+ *   table [n][table_ld] in/out, held [n] in/out   pages, and how many are held;
+ *       entries from held[b] on are written -1 where pages leave
+ *   pool [n_pages] in/out, pool_n [1] in/out   the free pages, a stack whose top
+ *       is pool[pool_n - 1]
+ *   cu [n + 1] or NULL        exclusive sums of add
+ *   kv_len [n] or NULL        lens + add
+ *   slots [max_slots] or NULL slot of new token i of request b at cu[b] + i; -1
+ *       from cu[n] on
+ *
+ * Request b holds ceil((lens + add) / page_size) pages afterwards.  First all
+ * surplus pages are returned: with r_0 .. r_{R-1} those in request order, each
+ * request's by ascending index, r_i comes to lie at pool[pool_n + R - 1 - i].
+ * Then requests that need pages take them from the top, in request order and
+ * ascending index: taking what was just returned restores it.  A request whose
+ * pages, with all that requests before it ask for, exceed the free ones is not
+ * served, nor is any later one that needs pages: it keeps what it holds, its
+ * kv_len is lens, its slots are -1, and XP_DEVERR_POOL is set.  A request whose
+ * numbers are out of range (negative, beyond max_len or table_ld pages) is left
+ * alone with kv_len 0 and no tokens in cu (XP_DEVERR_LENGTH).
+ * Asynchronous on `stream`; no allocation; the same call gives the same pages.
+ * Errors: XP_EINVAL before any launch, XP_EHIP.
+ */
+xp_status xp_kv_map(xp_kv* kv, int32_t n, const int32_t* lens, const int32_t* add, int32_t* table,
+                    int64_t table_ld, int32_t* held, int32_t* pool, int32_t* pool_n, int32_t* cu,
+                    int32_t* kv_len, int32_t* slots, int32_t max_slots, void* stream);
+
+/*
+ * Write the K and V rows of `tokens` tokens to their slots.
+ *
+ *   k, v   [tokens][n_kv][head_dim] bf16, token rows k_ld, v_ld elements apart
+ *          (slices of a fused projection's rows; multiples of 8, 16-byte aligned)
+ *   slots  [tokens] int32   -1: the token has no place; another one outside the
+ *          cache is skipped and sets XP_DEVERR_SLOT.  Slots given twice: each KV
+ *          head's row is that of either token.
+ * An 8-bit cache stores the e4m3 value nearest to k / k_scale (ties to even, one
+ * rounding), at most 448 in magnitude; NaN stays.
+ * Errors: XP_EINVAL before any launch, XP_EHIP.
+ */
+xp_status xp_kv_write(xp_kv* kv, int32_t tokens, const void* k, int64_t k_ld, const void* v,
+                      int64_t v_ld, const int32_t* slots, void* k_cache, void* v_cache,
+                      const float* k_scale, const float* v_scale, void* stream);
+
+/*
+ * Attention of new tokens over the pages of their requests: single tokens,
+ * drafted blocks, prompts, any mix of them in one call.
+ *
+ *   tokens, q   q [tokens][n_heads][head_dim] bf16, token rows q_ld elements apart
+ *   cu_q        [n + 1] int32: the tokens of request b are cu_q[b] .. cu_q[b + 1]
+ *               - 1; NULL: max_q each (tokens = n max_q).  Tokens from cu_q[n]
+ *               on are left as they are.
+ *   max_q       the most tokens of a request (it sizes the row tiles; a wrong
+ *               one costs time only)
+ *   kv_len      [n] int32: keys of request b, the new tokens' own among them
+ *   causal      1 or 0 (the drafter's bidirectional block)
+ *   window      0: none; W: a token at position p sees keys j > p - W only
+ *   sinks       with a window, keys j < sinks stay visible
+ *   scale       of q.k; 0: 1 / sqrt(head_dim)
+ *   out         [tokens][n_heads][head_dim] bf16, token rows out_ld apart
+ *   lse         [tokens][n_heads] float or NULL: log sum exp of the scaled scores
+ *
+ * Query head h reads KV head h / (n_heads / n_kv).  Token i of request b has
+ * position p = kv_len[b] - q_len[b] + i and sees key j iff j < kv_len[b], j <= p
+ * if causal, and j > p - window or j < sinks if there is a window.  A token that
+ * sees no key gives 0 (lse -inf).  Keys that a token does not see do not enter
+ * its result, whatever they hold.  Scores and sums are fp32; the numerators enter
+ * the product with V as two bf16 parts, as one in calls of more than 128 rows
+ * (max_q times the heads of a group).
+ * Pages outside [0, n_pages) where a key is read are replaced by 0 and set
+ * XP_DEVERR_PAGE; lengths outside [0, max_len] are clamped (XP_DEVERR_LENGTH).
+ * The same call gives the same bits; a request's summation order follows the
+ * lengths of all requests of the call.
+ * Errors: XP_EINVAL before any launch (null or misaligned pointers, sizes), XP_EHIP.
+ */
+xp_status xp_kv_attn(xp_kv* kv, int32_t n, int32_t tokens, int32_t max_q, const void* q,
+                     int64_t q_ld, const int32_t* cu_q, const int32_t* kv_len,
+                     const int32_t* table, int64_t table_ld, const void* k_cache,
+                     const void* v_cache, const float* k_scale, const float* v_scale,
+                     int32_t causal, int32_t window, int32_t sinks, float scale, void* out,
+                     int64_t out_ld, float* lse, void* stream);
+
+/*
+ * The same for requests that begin with common prefixes: group g is requests
+ * group_start[g] .. group_start[g + 1] - 1 (neighbours; [groups + 1] int32), whose
+ * first shared_len[g] ([groups] int32) keys are the same pages.  They are read
+ * once for the whole group, through its first request's table.  shared_len may
+ * end inside a page and reach into the new tokens; it is clamped to the shortest
+ * member (XP_DEVERR_LENGTH).  Requests outside every group, and groups of length
+ * 0, are attended as in xp_kv_attn.  The result differs from xp_kv_attn's in
+ * summation order only.
+ */
+xp_status xp_kv_attn_shared(xp_kv* kv, int32_t n, int32_t tokens, int32_t max_q, int32_t groups,
+                            const int32_t* group_start, const int32_t* shared_len, const void* q,
+                            int64_t q_ld, const int32_t* cu_q, const int32_t* kv_len,
+                            const int32_t* table, int64_t table_ld, const void* k_cache,
+                            const void* v_cache, const float* k_scale, const float* v_scale,
+                            int32_t causal, int32_t window, int32_t sinks, float scale, void* out,
+                            int64_t out_ld, float* lse, void* stream);
+
+/* Read and clear the handle's device error word into *out (host).  Synchronizes `stream`. */
+xp_status xp_kv_device_errors(xp_kv* kv, uint32_t* out, void* stream);
+
+/*
+ * xp_layer_forward over the paged context cache: the block's own keys and values
+ * are written to the pages of positions ctx_len[b] .. ctx_len[b] + B - 1, then
+ * every query attends to its request's pages, with xp_kv_attn's causal, window
+ * and sinks.  Once verification has accepted n of the block, ctx_len[b] + n keys
+ * are the context of the next one.
+ *   kv       a handle of the layer's heads and head_dim 128 on this device, its
+ *            max_tokens at least batch B; used in stream order like the layer
+ *   table    [batch][table_ld]: pages for ctx_len[b] + B keys each (xp_kv_map
+ *            with add = B); keys beyond the table's pages are not written and set
+ *            XP_DEVERR_LENGTH or XP_DEVERR_PAGE in kv's device error word
+ *   x, ctx_len, h_f32, h_bf16, causal   as for xp_layer_forward
+ * A bf16 cache gives xp_layer_forward's output up to fp32 summation order and, for
+ * blocks whose B n_heads / n_kv rows exceed 128, the single bf16 part of the
+ * numerators; an 8-bit one reads the block's own keys rounded too.
+ * Errors: XP_EINVAL before any launch, XP_EHIP; xp_layer_last_error(L).
+ */
+xp_status xp_layer_forward_paged(xp_layer* L, xp_kv* kv, int32_t batch, int32_t B, int32_t causal,
+                                 int32_t window, int32_t sinks, const void* x, void* k_cache,
+                                 void* v_cache, const float* k_scale, const float* v_scale,
+                                 const int32_t* table, int64_t table_ld, const int32_t* ctx_len,
+                                 float* h_f32, void* h_bf16, void* stream);
 
 /*
  * Measurement probes (not part of the method).  They give the measured peaks

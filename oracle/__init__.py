@@ -6,3 +6,4 @@ imports it and shares no code with it.
 """
 from .xpress_ref import *  # noqa: F401,F403
 from . import layer_ref  # noqa: F401,E402  (the context layer)
+from . import kv_ref  # noqa: F401,E402  (the paged context cache)

@@ -1,0 +1,1033 @@
+// Attention over the paged context cache: single tokens, drafted blocks and
+// prompts, with an optional sliding window and first keys that stay visible,
+// and with prefixes that several sequences share.
+//
+// Row (token i of sequence b, head h) has position p = kv_len[b] - q_len[b] + i
+// and sees key j iff
+//   j < kv_len[b]  and  (not causal or j <= p)  and
+//   (window == 0 or j > p - window or j < sinks);
+// o = sum_j softmax_j(scale q.k_j) v_j over these, 0 if there are none.
+//
+// Work list (k_kv_plan).  The rows of a KV head's group, (token, head) pairs,
+// are cut into tiles of up to R rows; a tile walks the 64-key tiles that any of
+// its rows sees.  (row tile, KV head, key tile) in this order is a list of units
+// that k_kv_attn cuts into equal shares, one a workgroup, whatever the lengths:
+// long and short contexts, prompts beside single tokens, causal triangles and
+// windows all carry the same load.  A share that begins or ends inside a (row
+// tile, KV head) segment leaves a partial (O, reference maximum, sum), and
+// k_kv_join adds the parts of every cut segment in order; a segment inside one
+// share is written at once.  The same call gives the same bits.
+//
+// With shared prefixes a group's prefix keys are segments of their own, whose
+// rows are all tokens of the group: they are read once for all of them.  Each
+// sequence's own segments then begin behind the prefix, and k_kv_join_rows adds
+// both results of every row.
+#include <algorithm>
+#include <cmath>
+
+#include "xp_kv.h"
+
+namespace xp {
+
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+// read-only data at wave-uniform addresses: scalar loads
+#define XP_AS4 __attribute__((address_space(4)))
+typedef const XP_AS4 int32_t* scalar_i32;
+
+__device__ __forceinline__ scalar_i32 as_scalar(const void* p) {
+  return (scalar_i32)(uintptr_t)p;
+}
+__device__ __forceinline__ float fsum_xor32(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ int imin(int a, int b) { return a < b ? a : b; }
+__device__ __forceinline__ int imax(int a, int b) { return a > b ? a : b; }
+
+// What the kernels read of a call.
+struct KvDev {
+  const uint16_t* q;
+  int64_t q_ld;
+  uint16_t* out;
+  int64_t out_ld;
+  float* lse;
+  const char* kc;
+  const char* vc;
+  const float* k_scale;
+  const float* v_scale;
+  const int32_t* table;
+  int64_t table_ld;
+  int nh, nkv, grp, logP, n_pages, cols;
+  int causal, window, sinks;
+  float scale2;                      // scale log2(e)
+  int total_q, groups;
+  int64_t row0;                      // partial rows before those of whole segments
+  KvAttnWs w;
+  uint32_t* err;
+};
+
+// ---------------------------------------------------------------------------
+// The work list.  One workgroup: item i is sequence i (its rows behind a
+// shared prefix, if it has one) or group i - n (its prefix); the items' row
+// tiles, the entries' key ranges, the sums of both, and where each share begins.
+// Bound by latency: a few block scans and one search per entry and share.
+// ---------------------------------------------------------------------------
+constexpr int kPlanThreads = 1024;
+constexpr int kPlanWaves = kPlanThreads / kWave;
+constexpr int kPlanCum = 4096;       // entries whose sums stay in LDS
+constexpr int kPlanMinShare = 4;     // units a share has at least
+
+// exclusive sum over the workgroup of each thread's v; *total their sum
+__device__ __forceinline__ int block_scan(int v, int* lds, int* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int x = v;
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const int y = __shfl_up(x, o, kWave);
+    if (lane >= o) x += y;
+  }
+  __syncthreads();
+  if (lane == kWave - 1) lds[wave] = x;
+  __syncthreads();
+  int before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kPlanWaves; ++w) {
+    const int t = lds[w];
+    before += w < wave ? t : 0;
+    all += t;
+  }
+  *total = all;
+  return before + x - v;
+}
+
+// the last index in [0, n) whose a[] is at most x (a[0] <= x, a non-decreasing)
+template <typename P>
+__device__ __forceinline__ int last_at_most(P a, int n, int x) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int m = (lo + hi) >> 1;
+    if (a[m] <= x) lo = m;
+    else hi = m;
+  }
+  return lo;
+}
+
+struct KvPlan {
+  int n, total_q, max_q, kv_add, cap, R, grp, nkv, causal, window, sinks, groups, entries, shares;
+  const int32_t* cu_q;
+  const int32_t* kv_len;
+  const int32_t* group_start;
+  const int32_t* shared_len;
+  KvAttnWs w;
+  uint32_t* err;
+};
+
+__device__ __forceinline__ int clampi(int x, int lo, int hi) { return imin(imax(x, lo), hi); }
+
+template <bool SHARED>
+__global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d) {
+  constexpr int kItems = SHARED ? 2 * kKvMaxBatch : kKvMaxBatch;
+  __shared__ int off[kItems + 1];                 // entries before each item
+  __shared__ int floors[SHARED ? kKvMaxBatch : 1];   // keys of the sequence that its prefix holds
+  __shared__ int gmin[SHARED ? kKvMaxBatch : 1];  // a group's positions: least and greatest
+  __shared__ int gmax[SHARED ? kKvMaxBatch : 1];
+  __shared__ int glen[SHARED ? kKvMaxBatch : 1];  // and its prefix keys
+  __shared__ int cums[kPlanCum];
+  __shared__ int red[kPlanWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int n = d.n;
+  uint32_t bad = 0;
+  auto first = [&](int b) {                       // first token of sequence b
+    return d.cu_q != nullptr ? clampi(d.cu_q[b], 0, d.total_q) : imin(b * d.max_q, d.total_q);
+  };
+  auto keys = [&](int b) {                        // its keys
+    const int x = d.kv_len[b];
+    if (x < 0 || x > d.cap - d.kv_add) bad |= XP_DEVERR_LENGTH;
+    return clampi(x, 0, imax(d.cap - d.kv_add, 0)) + imin(d.kv_add, d.cap);
+  };
+  auto tokens = [&](int b, int t0) { return imax(first(b + 1) - t0, 0); };
+  if constexpr (SHARED) {
+    for (int b = tid; b < n; b += kPlanThreads) {
+      floors[b] = 0;
+      d.w.sgrp[b] = -1;
+      d.w.stok[b] = first(b);
+    }
+    __syncthreads();
+    // a wave per group: its members' positions, and a prefix that none is shorter than
+    for (int g = wave; g < d.groups; g += kPlanWaves) {
+      const int s0 = clampi(d.group_start[g], 0, n), s1 = clampi(d.group_start[g + 1], s0, n);
+      int pmin = 0x7fffffff, pmax = -0x7fffffff, kmin = d.cap;
+      for (int b = s0 + lane; b < s1; b += kWave) {
+        const int t0 = first(b), ql = tokens(b, t0), kv = keys(b);
+        if (ql == 0) continue;
+        pmin = imin(pmin, kv - ql);
+        pmax = imax(pmax, kv - 1);
+        kmin = imin(kmin, kv);
+      }
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) {
+        pmin = imin(pmin, __shfl_xor(pmin, o, kWave));
+        pmax = imax(pmax, __shfl_xor(pmax, o, kWave));
+        kmin = imin(kmin, __shfl_xor(kmin, o, kWave));
+      }
+      const int want = d.shared_len[g], len = clampi(want, 0, kmin);
+      if (want != len) bad |= XP_DEVERR_LENGTH;
+      for (int b = s0 + lane; b < s1; b += kWave) {
+        floors[b] = len;
+        d.w.sgrp[b] = len > 0 ? g : -1;
+      }
+      if (lane == 0) {
+        gmin[g] = pmin;
+        gmax[g] = pmax;
+        glen[g] = len;
+        d.w.gtok[g] = first(s0);
+      }
+    }
+    for (int b = wave; b < n; b += kPlanWaves) {  // every token's position and sequence
+      const int t0 = first(b), ql = tokens(b, t0), p0 = keys(b) - ql;
+      for (int i = lane; i < ql; i += kWave) {
+        d.w.pos[t0 + i] = p0 + i;
+        d.w.tseq[t0 + i] = b;
+      }
+    }
+    __syncthreads();
+  }
+  // entries of each item
+  const int items = n + (SHARED ? d.groups : 0);
+  int T = 0;
+  for (int i0 = 0; i0 < items; i0 += kPlanThreads) {
+    const int i = i0 + tid;
+    int nt = 0;
+    if (i < items) {
+      int tk;
+      if (i < n) {
+        tk = tokens(i, first(i));
+      } else {
+        const int g = i - n;
+        const int s0 = clampi(d.group_start[g], 0, n), s1 = clampi(d.group_start[g + 1], s0, n);
+        tk = glen[g] > 0 ? imax(first(s1) - first(s0), 0) : 0;
+      }
+      nt = (int)(((int64_t)tk * d.grp + d.R - 1) / d.R);
+    }
+    int all;
+    const int before = block_scan(nt, red, &all);
+    if (i < items) off[i] = T + before;
+    T += all;
+  }
+  if (tid == 0) off[items] = T;
+  if (T > d.entries) {                            // token ranges that overlap
+    T = d.entries;
+    bad |= XP_DEVERR_LENGTH;
+  }
+  __syncthreads();
+  if constexpr (SHARED)
+    for (int i = tid; i <= items; i += kPlanThreads) d.w.off[i] = off[i];
+  // their key ranges
+  int W = 0;
+  for (int e0 = 0; e0 < T; e0 += kPlanThreads) {
+    const int e = e0 + tid;
+    int units = 0;
+    if (e < T) {
+      const int i = last_at_most(off, items, e);
+      const bool prefix = SHARED && i >= n;
+      KvEntry x{};
+      x.row0 = (e - off[i]) * d.R;
+      int pa, pb;                                 // positions of the tile's tokens
+      if (!prefix) {
+        x.tok0 = first(i);
+        const int tk = tokens(i, x.tok0);
+        x.seq = i;
+        x.nrows = imin(tk * d.grp - x.row0, d.R);
+        x.ceil = keys(i);
+        x.p0 = x.ceil - tk;
+        x.floor = SHARED ? floors[i] : 0;
+        pa = x.p0 + x.row0 / d.grp;
+        pb = x.p0 + (x.row0 + x.nrows - 1) / d.grp;
+      } else {
+        const int g = i - n;
+        const int s0 = clampi(d.group_start[g], 0, n), s1 = clampi(d.group_start[g + 1], s0, n);
+        x.tok0 = first(s0);
+        x.seq = s0;
+        x.nrows = imin((first(s1) - x.tok0) * d.grp - x.row0, d.R);
+        x.prefix = 1;
+        x.ceil = glen[g];
+        pa = gmin[g];
+        pb = gmax[g];
+      }
+      x.hi = d.causal ? imin(x.ceil, pb + 1) : x.ceil;
+      x.lo = d.window > 0 ? imax(pa - d.window + 1, x.floor) : x.floor;
+      x.s = d.window > 0 ? imax(imin(d.sinks, x.hi), x.floor) : x.floor;
+      const bool sink = x.s > x.floor;
+      const int fl = x.floor / kKvTile;
+      x.a0 = sink ? fl : x.lo / kKvTile;
+      const int a1 = sink ? (x.s + kKvTile - 1) / kKvTile : x.a0;
+      x.n1 = a1 - x.a0;
+      x.b0 = imax(x.lo / kKvTile, a1);
+      const int b1 = x.hi > x.lo ? (x.hi + kKvTile - 1) / kKvTile : 0;
+      // no row sees a key: one tile, wholly masked, writes the zeros
+      x.tiles = imax(x.n1 + imax(b1 - x.b0, 0), 1);
+      d.w.ent[e] = x;
+      units = x.tiles * d.nkv;
+    }
+    int all;
+    const int before = block_scan(units, red, &all);
+    if (e < T) {
+      if (e < kPlanCum) cums[e] = W + before;
+      d.w.cum[e] = W + before;
+    }
+    W += all;
+  }
+  if (tid == 0) {
+    d.w.cum[T] = W;
+    const int S = imax((W + d.shares - 1) / d.shares, kPlanMinShare);
+    d.w.hdr[0] = W;
+    d.w.hdr[1] = S;
+    d.w.hdr[2] = T;
+  }
+  __syncthreads();                                // also the entries, for this workgroup
+  const int S = imax((W + d.shares - 1) / d.shares, kPlanMinShare);
+  for (int s = tid; s <= d.shares; s += kPlanThreads) {
+    KvShare r{};
+    r.f = (int64_t)s * S < W ? s * S : W;
+    if (r.f < W) {
+      r.e = T <= kPlanCum ? last_at_most((const int*)cums, T, r.f)
+                          : last_at_most((const int32_t*)d.w.cum, T, r.f);
+      const int tiles = d.w.ent[r.e].tiles;
+      const int in = r.f - (T <= kPlanCum ? cums[r.e] : d.w.cum[r.e]);
+      r.kvh = in / tiles;
+      r.j = in - r.kvh * tiles;
+    }
+    d.w.share[s] = r;
+  }
+  if (bad) atomicOr(d.err, bad);
+}
+
+// ---------------------------------------------------------------------------
+// The attention.
+// ---------------------------------------------------------------------------
+// Layout of a stage: a tile's 64 K rows, then its 64 V rows, of RB bytes; the
+// 16-byte chunk c of row r at position c ^ swz(r), so that neither the K reads
+// (16 rows, one chunk) nor the transposing V reads (4 or 8 rows, 4 or 2 chunks)
+// meet in a bank.
+template <int HD, bool F8>
+struct KvRows {
+  static constexpr int RB = HD * (F8 ? 1 : 2);
+  static constexpr int CPR = RB / 16;
+  static constexpr int kHalf = kKvTile * CPR;     // 16-byte slots of K, of V
+  static constexpr int kStage = 2 * kHalf;
+  static constexpr int IPG = CPR / 4;             // 1 KB loads of 16 rows
+  __device__ static __forceinline__ int swz(int r) {
+    if constexpr (CPR == 16) return ((r & 3) << 2) | ((r >> 2) & 3);
+    else if constexpr (CPR == 8 && !F8) return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+    else if constexpr (CPR == 8)
+      return (((r >> 1) & 1) << 2) | (((r >> 3) & 1) << 1) | ((r >> 2) & 1);
+    else return (((r >> 3) & 1) << 1) | ((r >> 2) & 1);
+  }
+};
+
+__device__ __forceinline__ floatx16 mma32(u32x4 a, u32x4 b, floatx16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                 __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+// 8 e4m3 values to bf16 (exact)
+__device__ __forceinline__ u32x4 f8_bf16x8(uint32_t a, uint32_t b) {
+  return u32x4{
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, false)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.f, true)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, false)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, true))};
+}
+__device__ __forceinline__ uint32_t lds_byte(const void* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
+}
+
+// V operands of one 16-key step for ND blocks of 32 dims: the addresses a[] of
+// the lane's part of each (b[]: of the keys 8 further), with the wait for the
+// reads.  Written out because the compiler takes its transposing-read builtin
+// for a use of the global-to-LDS loads in flight and waits for all of them.
+template <int ND, int OFF>
+__device__ __forceinline__ void lds_v16(const uint32_t* a, const uint32_t* b, u32x4* v) {
+  uint2 r[2 * ND];
+  if constexpr (ND == 4) {
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %8 offset:%16\n\tds_read_b64_tr_b16 %1, %12 offset:%16\n\t"
+        "ds_read_b64_tr_b16 %2, %9 offset:%16\n\tds_read_b64_tr_b16 %3, %13 offset:%16\n\t"
+        "ds_read_b64_tr_b16 %4, %10 offset:%16\n\tds_read_b64_tr_b16 %5, %14 offset:%16\n\t"
+        "ds_read_b64_tr_b16 %6, %11 offset:%16\n\tds_read_b64_tr_b16 %7, %15 offset:%16\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]),
+          "=&v"(r[6]), "=&v"(r[7])
+        : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]),
+          "n"(OFF)
+        : "memory");
+  } else {
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %4 offset:%8\n\tds_read_b64_tr_b16 %1, %6 offset:%8\n\t"
+        "ds_read_b64_tr_b16 %2, %5 offset:%8\n\tds_read_b64_tr_b16 %3, %7 offset:%8\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3])
+        : "v"(a[0]), "v"(a[1]), "v"(b[0]), "v"(b[1]), "n"(OFF)
+        : "memory");
+  }
+#pragma unroll
+  for (int i = 0; i < ND; ++i) v[i] = u32x4{r[2 * i].x, r[2 * i].y, r[2 * i + 1].x, r[2 * i + 1].y};
+}
+// the same of 8-bit rows: one read brings both groups of four keys
+template <int ND, int OFF>
+__device__ __forceinline__ void lds_v8(const uint32_t* a, u32x4* v) {
+  uint2 r[ND];
+  if constexpr (ND == 4) {
+    asm volatile(
+        "ds_read_b64_tr_b8 %0, %4 offset:%8\n\tds_read_b64_tr_b8 %1, %5 offset:%8\n\t"
+        "ds_read_b64_tr_b8 %2, %6 offset:%8\n\tds_read_b64_tr_b8 %3, %7 offset:%8\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3])
+        : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "n"(OFF)
+        : "memory");
+  } else {
+    asm volatile(
+        "ds_read_b64_tr_b8 %0, %2 offset:%4\n\tds_read_b64_tr_b8 %1, %3 offset:%4\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(r[0]), "=&v"(r[1])
+        : "v"(a[0]), "v"(a[1]), "n"(OFF)
+        : "memory");
+  }
+#pragma unroll
+  for (int i = 0; i < ND; ++i) v[i] = f8_bf16x8(r[i].x, r[i].y);
+}
+
+// some 16-bit (8-bit) value of x is an infinity or NaN
+template <bool F8>
+__device__ __forceinline__ bool has_nonfinite(u32x4 x) {
+  bool any = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (F8) {
+      const uint32_t y = ~x[i] & 0x7f7f7f7fu;     // 0 where all seven bits are ones
+      any |= ((y - 0x01010101u) & ~y & 0x80808080u) != 0u;
+    } else {
+      any |= (x[i] & 0x7f800000u) == 0x7f800000u || (x[i] & 0x7f80u) == 0x7f80u;
+    }
+  }
+  return any;
+}
+
+// A row's view of the keys: [lo, lo + n) and [floor, floor + s).
+struct KvSees {
+  int lo, floor;
+  uint32_t n, s;
+  __device__ __forceinline__ bool operator()(int key) const {
+    return ((uint32_t)(key - lo) < n) | ((uint32_t)(key - floor) < s);
+  }
+};
+
+// WR x WK waves: wave (wr, wk) takes rows 32 wr .. + 31 of the tile and the
+// wk-th part of each tile's keys.  S^T = K Q^T and O^T = V^T P^T on
+// v_mfma_f32_32x32x16_bf16: a lane holds one query row (l % 32) in both, so the
+// softmax's statistics are the lane's own but for one exchange with lane l ^ 32,
+// and the numerators go from the accumulators of S straight into the B operand
+// (its k order is that of the keys 16 t + 4 (l / 32) + 0..3 and + 8, which the
+// transposing reads of V follow).  Scores are kept in base 2.  A row's reference
+// maximum moves only when a score exceeds it by more than 2^8, so most tiles
+// rescale nothing.  Numerators enter P V as PARTS bf16 parts: two (16
+// significant bits) where the call is bound by memory.
+// Tiles wait in an LDS ring of NST stages filled by global_load_lds; the keys
+// that no row of the tile sees are loaded as zeros, whatever lies there.
+template <int HD, bool F8, int WR, int WK, int NST, int PARTS>
+__global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
+  using SH = KvRows<HD, F8>;
+  constexpr int NW = WR * WK, R = 32 * WR, KB = 2 / WK, ND = HD / 32, NKS = HD / 16;
+  constexpr int RB = SH::RB, CPR = SH::CPR, IPG = SH::IPG;
+  constexpr int NG = 8 / NW;                      // groups of 16 rows that a wave loads
+  static_assert(NG * NW == 8 && KB * WK == 2, "waves");
+  constexpr int PER = NG * IPG;                   // loads of a wave for a stage
+  static_assert((NST - 2) * PER < 64, "vmcnt field");
+  constexpr int kMerge = (HD / 2 + 2) * kWave;    // floats a wave hands over
+  static_assert(WK == 1 || WR * kMerge * 4 <= NST * SH::kStage * 16, "merge in LDS");
+  __shared__ __align__(256) u32x4 lds[NST * SH::kStage];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wr = wave % WR, wk = wave / WR;
+  const int h = lane >> 5, li = lane & 31;
+  // neighbouring shares on one XCD: they read the same sequence's keys
+  const int sidx = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+  const scalar_i32 sh = as_scalar(d.w.share + sidx);
+  int f = sh[0], e = sh[1], kvh = sh[2], j = sh[3];
+  const int f1 = sh[4];
+  if (f >= f1) return;                            // whole workgroup
+  // byte offsets of the lane's chunk in the loads of 16 rows
+  uint32_t lp[IPG];
+#pragma unroll
+  for (int i = 0; i < IPG; ++i) {
+    const int r = i * (kWave / CPR) + lane / CPR;
+    lp[i] = (uint32_t)(r * RB + 16 * ((lane % CPR) ^ SH::swz(r)));
+  }
+  // V reads: the lane's byte addresses within a stage for each block of 32 dims
+  uint32_t va[ND], vb[ND];
+#pragma unroll
+  for (int db = 0; db < ND; ++db) {
+    if constexpr (F8) {
+      const int jj = (lane & 15) >> 1, r = 4 * h + (jj & 3) + 8 * (jj >> 2);
+      va[db] = r * RB + 16 * ((2 * db + ((lane >> 4) & 1)) ^ SH::swz(r)) + 8 * (lane & 1);
+      vb[db] = 0;
+    } else {
+      const int r = 4 * h + ((lane & 15) >> 2);
+      const int c = 4 * db + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+      va[db] = r * RB + 16 * (c ^ SH::swz(r)) + 8 * (lane & 1);
+      vb[db] = (r + 8) * RB + 16 * (c ^ SH::swz(r + 8)) + 8 * (lane & 1);
+    }
+  }
+  const int P1 = (1 << d.logP) - 1;
+  for (;;) {
+  const scalar_i32 en = as_scalar(d.w.ent + e);
+  const int tok0 = en[0], row0 = en[1], nrows = en[2], seq = en[3], p0 = en[4], prefix = en[5];
+  const int kfloor = en[6], kceil = en[7], ks_ = en[8], klo = en[9], khi = en[10], tiles = en[11];
+  const int a0 = en[12], n1 = en[13], b0 = en[14];
+  const int nj = imin(tiles - j, f1 - f);         // tiles of this part (>= 1)
+  const bool whole = j == 0 && nj == tiles;
+  auto tile_key = [&](int t) { return kKvTile * (t < n1 ? a0 + t : b0 + t - n1); };
+
+  // ---- the wave's query rows (B operand): row li of its 32 ----
+  const int rr = 32 * wr + li;
+  const bool live = 32 * wr < nrows;              // wave-uniform
+  const bool rv = rr < nrows;
+  const int row = row0 + (rv ? rr : 0);
+  const int tk = row / d.grp, head = kvh * d.grp + (row - tk * d.grp);
+  const int64_t tok = tok0 + tk;
+  u32x4 qf[NKS];
+  {
+    const uint16_t* qs = d.q + tok * d.q_ld + (int64_t)head * HD;
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) {
+      const int dim = F8 ? 32 * (ks >> 1) + 16 * h + 8 * (ks & 1) : 16 * ks + 8 * h;
+      qf[ks] = ld16(qs + dim);
+    }
+  }
+  const int p = prefix ? d.w.pos[tok] : p0 + tk;
+  const int hi = rv ? (d.causal ? imin(p + 1, kceil) : kceil) : kfloor;
+  const int lo = d.window > 0 ? imax(p - d.window + 1, kfloor) : kfloor;
+  const KvSees sees{lo, kfloor, (uint32_t)imax(hi - lo, 0),
+                    d.window > 0 ? (uint32_t)imax(imin(d.sinks, hi) - kfloor, 0) : 0u};
+  // keys that every row of the wave sees: [wlo, whi), and [kfloor, wsink); and
+  // beyond wend, or between the sinks and wbeg, none sees any
+  int whi, wend, wlo, wbeg;
+  {
+    int pmin = rv ? p : 0x7fffffff, pmax = rv ? p : -0x7fffffff;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      pmin = imin(pmin, __shfl_xor(pmin, o, kWave));
+      pmax = imax(pmax, __shfl_xor(pmax, o, kWave));
+    }
+    pmin = __builtin_amdgcn_readfirstlane(pmin);
+    pmax = __builtin_amdgcn_readfirstlane(pmax);
+    whi = d.causal ? imin(pmin < 0x7fffffff ? pmin + 1 : pmin, kceil) : kceil;
+    wend = d.causal ? imin(pmax + 1, kceil) : kceil;
+    wlo = d.window > 0 ? imax(pmax - d.window + 1, kfloor) : kfloor;
+    wbeg = d.window > 0 ? imax(pmin - d.window + 1, kfloor) : kfloor;
+  }
+  const int wsink = d.window > 0 ? d.sinks : 0;
+  const float scale2 = d.scale2 * (F8 && d.k_scale != nullptr ? d.k_scale[kvh] : 1.f);
+
+  // ---- loads ----
+  const scalar_i32 tb = as_scalar(d.table + (int64_t)seq * d.table_ld);
+  int pg[NG];
+  auto pages = [&](int t) {                       // page ids of the wave's rows of tile t
+#pragma unroll
+    for (int g = 0; g < NG; ++g)
+      pg[g] = tb[imin((tile_key(t) + 16 * ((wave * NG + g) & 3)) >> d.logP, d.cols - 1)];
+  };
+  auto issue = [&](int t, int slot) __attribute__((always_inline)) {
+    const int k0 = tile_key(t);
+    const bool inner = k0 >= kfloor && k0 + kKvTile <= khi && (k0 >= klo || k0 + kKvTile <= ks_);
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      const int gi = wave * NG + g, rb = 16 * (gi & 3), g0 = k0 + rb;
+      int page = pg[g];
+      if ((uint32_t)page >= (uint32_t)d.n_pages) {
+        const int from = imax(g0, kfloor), to = imin(g0 + 16, khi);
+        if (from < to && (to > klo || from < ks_) && lane == 0) atomicOr(d.err, XP_DEVERR_PAGE);
+        page = 0;
+      }
+      const char* base = (gi >= 4 ? d.vc : d.kc) +
+                         ((((int64_t)page * d.nkv + kvh) << d.logP) + (g0 & P1)) * RB;
+      u32x4* dst = lds + slot * SH::kStage + (gi >= 4 ? SH::kHalf : 0) + rb * CPR;
+      if (inner) {
+#pragma unroll
+        for (int i = 0; i < IPG; ++i) lds_dma16(base + lp[i], dst + 64 * i);
+      } else {
+#pragma unroll
+        for (int i = 0; i < IPG; ++i) {
+          const int key = g0 + i * (kWave / CPR) + lane / CPR;
+          const bool any = key >= kfloor && key < khi && (key >= klo || key < ks_);
+          lds_dma16(any ? base + lp[i] : d.w.zero + 16 * (lane & 15), dst + 64 * i);
+        }
+      }
+    }
+  };
+  pages(j);
+#pragma unroll
+  for (int t = 0; t < NST - 1; ++t)
+    if (t < nj) {                                 // whole workgroup
+      issue(j + t, t);
+      pages(j + imin(t + 1, nj - 1));
+    }
+
+  float m_run = -INFINITY, l_run = 0.f;           // the row's; l of this half's keys
+  floatx16 o[ND];
+#pragma unroll
+  for (int db = 0; db < ND; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
+
+  int slot = 0;
+#pragma unroll 1
+  for (int t = 0; t < nj; ++t) {
+    // tile t landed (every wave's loads), and every wave is done with t - 1,
+    // whose slot takes tile t + NST - 1
+    asm volatile("" ::: "memory");
+    if (t + NST - 2 < nj) __builtin_amdgcn_s_waitcnt(0x0070 | (((NST - 2) * PER) & 15) | ((((NST - 2) * PER) >> 4) << 14));
+    else __builtin_amdgcn_s_waitcnt(0x0070);
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (t + NST - 1 < nj) {
+      issue(j + t + NST - 1, slot == 0 ? NST - 1 : slot - 1);
+      pages(j + imin(t + NST, nj - 1));
+    }
+    const u32x4* Ks = lds + slot * SH::kStage + 32 * wk * CPR;
+    const u32x4* Vs = Ks + SH::kHalf;
+    slot = slot + 1 == NST ? 0 : slot + 1;
+    const int k0 = tile_key(j + t) + 32 * wk;
+    constexpr int NK = 32 * KB;                   // the wave's keys of the tile
+    // tiles that no row of the wave sees
+    if (!live || k0 >= wend || (k0 + NK <= wbeg && k0 >= wsink)) continue;
+    const bool full = k0 >= kfloor && k0 + NK <= whi && (k0 >= wlo || k0 + NK <= wsink);
+    floatx16 sc[KB];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      const int kr = 32 * kb + li, sw = SH::swz(kr);
+      floatx16 acc;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[i] = 0.f;
+      if constexpr (F8) {
+#pragma unroll
+        for (int kp = 0; kp < NKS / 2; ++kp) {
+          const u32x4 x = Ks[kr * CPR + ((2 * kp + h) ^ sw)];
+          acc = mma32(f8_bf16x8(x.x, x.y), qf[2 * kp], acc);
+          acc = mma32(f8_bf16x8(x.z, x.w), qf[2 * kp + 1], acc);
+        }
+      } else {
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) acc = mma32(Ks[kr * CPR + ((2 * ks + h) ^ sw)], qf[ks], acc);
+      }
+      sc[kb] = acc;
+    }
+    if (!full) {
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          sc[kb][i] = sees(k0 + 32 * kb + 8 * (i / 4) + 4 * h + i % 4) ? sc[kb][i] : -INFINITY;
+    }
+    constexpr float kLazy = 8.f;
+    float mt = -INFINITY;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mt = fmaxf(mt, sc[kb][i]);
+    mt = fmax_xor32(mt) * scale2;
+    if (__ballot(mt > m_run + kLazy) != 0) {      // wave-uniform
+      const float mref = fmaxf(m_run, mt);
+      const float alpha = __builtin_amdgcn_exp2f(m_run - (mref == -INFINITY ? 0.f : mref));
+      l_run *= alpha;
+#pragma unroll
+      for (int db = 0; db < ND; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
+      m_run = mref;
+    }
+    // with no visible key yet (m = -inf) every exponent below is -inf: 0
+    const float mxs = m_run == -INFINITY ? 0.f : m_run;
+    float ls = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        sc[kb][i] = __builtin_amdgcn_exp2f(fmaf(sc[kb][i], scale2, -mxs));
+        ls += sc[kb][i];
+      }
+    l_run += ls;
+    bool odd = false;                             // infinities or NaN among the tile's V
+    if (!full) {
+#pragma unroll 1
+      for (int i = lane; i < NK * CPR; i += kWave) odd |= has_nonfinite<F8>(Vs[i]);
+      odd = __ballot(odd) != 0;
+    }
+    if (!odd) {
+      const uint32_t vs0 = lds_byte(Vs);
+      uint32_t xa[ND], xb[ND];
+#pragma unroll
+      for (int db = 0; db < ND; ++db) {
+        xa[db] = va[db] + vs0;
+        xb[db] = vb[db] + vs0;
+      }
+      auto step = [&](auto u_) __attribute__((always_inline)) {
+        constexpr int u = decltype(u_)::value, kb = u / 2, i0 = 8 * (u % 2);
+        u32x4 v[ND], ph, pl;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float e0 = sc[kb][i0 + 2 * i], e1 = sc[kb][i0 + 2 * i + 1];
+          ph[i] = pk_bf16(e0, e1);
+          if constexpr (PARTS == 2)
+            pl[i] = pk_bf16(e0 - __uint_as_float(ph[i] << 16),
+                            e1 - __uint_as_float(ph[i] & 0xFFFF0000u));
+        }
+        if constexpr (F8) lds_v8<ND, 16 * u * RB>(xa, v);
+        else lds_v16<ND, 16 * u * RB>(xa, xb, v);
+#pragma unroll
+        for (int db = 0; db < ND; ++db) {
+          if constexpr (PARTS == 2) o[db] = mma32(v[db], pl, o[db]);
+          o[db] = mma32(v[db], ph, o[db]);
+        }
+      };
+      step(std::integral_constant<int, 0>{});
+      step(std::integral_constant<int, 1>{});
+      if constexpr (KB == 2) {
+        step(std::integral_constant<int, 2>{});
+        step(std::integral_constant<int, 3>{});
+      }
+    } else {
+      // Rows must not meet the values of keys that they do not see (0 times an
+      // infinity is no number): key by key, each row its own.  Only tiles on the
+      // border of some row's view come here, and only if they hold such values.
+      const char* vbytes = reinterpret_cast<const char*>(Vs);
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+#pragma unroll 1
+        for (int x = 0; x < 32; ++x) {
+          const int i = 4 * (x >> 3) + (x & 3), hh = (x >> 2) & 1, r = 32 * kb + x;
+          float ei = 0.f;
+#pragma unroll
+          for (int y = 0; y < 16; ++y) ei = y == i ? sc[kb][y] : ei;
+          const float pk = __shfl(ei, li + 32 * hh, kWave);
+          if (!sees(k0 + r)) continue;
+#pragma unroll
+          for (int db = 0; db < ND; ++db)
+#pragma unroll
+            for (int y = 0; y < 16; ++y) {
+              const int dim = 32 * db + 8 * (y / 4) + 4 * h + y % 4;
+              const int c = F8 ? dim >> 4 : dim >> 3;
+              const char* at = vbytes + r * RB + 16 * (c ^ SH::swz(r));
+              float v;
+              if constexpr (F8) {
+                const uint32_t b = *reinterpret_cast<const uint8_t*>(at + (dim & 15));
+                v = __builtin_amdgcn_cvt_f32_fp8(b, 0);
+              } else {
+                v = bf16_to_f32(*reinterpret_cast<const uint16_t*>(at + 2 * (dim & 7)));
+              }
+              o[db][y] = fmaf(pk, v, o[db][y]);
+            }
+        }
+      }
+    }
+  }
+  l_run = fsum_xor32(l_run);
+  if constexpr (WK == 2) {
+    // the second key half hands (m, l, O) to the first through the ring's LDS:
+    // O = 2^(m0 - M) O0 + 2^(m1 - M) O1, l likewise, M = max(m0, m1)
+    __syncthreads();                              // every wave's reads of the ring done
+    float* mg = reinterpret_cast<float*>(lds) + wr * kMerge + lane;
+    if (wk == 1) {
+#pragma unroll
+      for (int db = 0; db < ND; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mg[(16 * db + i) * kWave] = o[db][i];
+      mg[HD / 2 * kWave] = m_run;
+      mg[(HD / 2 + 1) * kWave] = l_run;
+    }
+    __syncthreads();
+    if (wk == 0) {
+      const float m1 = mg[HD / 2 * kWave], l1 = mg[(HD / 2 + 1) * kWave];
+      const float M = fmaxf(m_run, m1), Ms = M == -INFINITY ? 0.f : M;
+      const float w0 = __builtin_amdgcn_exp2f(m_run - Ms), w1 = __builtin_amdgcn_exp2f(m1 - Ms);
+      m_run = M;
+      l_run = w0 * l_run + w1 * l1;
+#pragma unroll
+      for (int db = 0; db < ND; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[db][i] = w0 * o[db][i] + w1 * mg[(16 * db + i) * kWave];
+    }
+  }
+  // ---- results: the rows themselves, or what k_kv_join(_rows) adds up ----
+  if (rv && wk == 0) {
+    if (whole && d.groups == 0) {
+      const float inv = l_run == 0.f ? 0.f
+                                     : (F8 && d.v_scale != nullptr ? d.v_scale[kvh] : 1.f) / l_run;
+      uint16_t* op = d.out + tok * d.out_ld + (int64_t)head * HD + 4 * h;
+#pragma unroll
+      for (int db = 0; db < ND; ++db)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint2 v{pk_bf16(o[db][4 * i] * inv, o[db][4 * i + 1] * inv),
+                        pk_bf16(o[db][4 * i + 2] * inv, o[db][4 * i + 3] * inv)};
+          *reinterpret_cast<uint2*>(op + 32 * db + 8 * i) = v;
+        }
+      if (d.lse != nullptr && h == 0)
+        d.lse[tok * d.nh + head] = l_run == 0.f
+            ? -INFINITY : (m_run + __builtin_amdgcn_logf(l_run)) * 0.69314718055994531f;
+    } else {
+      const int64_t prow = whole ? d.row0 + ((int64_t)prefix * d.total_q + tok) * d.nh + head
+                                 : (int64_t)(2 * sidx + (j == 0 ? 1 : 0)) * R + rr;
+      float* op = d.w.part + prow * HD + 4 * h;
+#pragma unroll
+      for (int db = 0; db < ND; ++db)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<floatx4*>(op + 32 * db + 8 * i) =
+              floatx4{o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]};
+      if (h == 0) *reinterpret_cast<float2*>(d.w.ml + 2 * prow) = float2{m_run, l_run};
+    }
+  }
+  // ---- on to the next segment of the share ----
+  f += nj;
+  if (f >= f1) return;                            // whole workgroup
+  j = 0;
+  if (++kvh == d.nkv) {
+    kvh = 0;
+    ++e;
+  }
+  __syncthreads();                                // the ring is read, the merge done
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Joining.  Part (m_i, l_i, O_i) of a row: O = sum 2^(m_i - M) O_i, l likewise,
+// M = max m_i, parts in order.
+// ---------------------------------------------------------------------------
+struct KvSum {
+  float m = -INFINITY, l = 0.f;
+  floatx4 o{0.f, 0.f, 0.f, 0.f};
+  __device__ __forceinline__ void add(float m1, float l1, floatx4 o1) {
+    const float M = fmaxf(m, m1), Ms = M == -INFINITY ? 0.f : M;
+    const float w0 = __builtin_amdgcn_exp2f(m - Ms), w1 = __builtin_amdgcn_exp2f(m1 - Ms);
+    m = M;
+    l = w0 * l + w1 * l1;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = w0 * o[i] + w1 * o1[i];
+  }
+};
+
+// the parts of row rr of the segment of units [a, a + tiles), cut at multiples of
+// S: the first at the end of share a / S, the others at the beginning of theirs
+template <int HD>
+__device__ __forceinline__ void add_parts(const KvDev& d, int R, int a, int tiles, int S, int rr,
+                                          int c, KvSum& x) {
+  const int s0 = a / S, s1 = (a + tiles - 1) / S;
+  constexpr int U = 4;
+  for (int s = s0; s <= s1; s += U) {             // loads of U parts in flight
+    float2 ml[U];
+    floatx4 o[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int su = imin(s + u, s1);
+      const int64_t prow = (int64_t)(2 * su + (su == s0 ? 1 : 0)) * R + rr;
+      ml[u] = *reinterpret_cast<const float2*>(d.w.ml + 2 * prow);
+      o[u] = *reinterpret_cast<const floatx4*>(d.w.part + prow * HD + c);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (s + u <= s1) x.add(ml[u].x, ml[u].y, o[u]);
+  }
+}
+
+template <int HD>
+__device__ __forceinline__ void write_row(const KvDev& d, int64_t tok, int head, int c,
+                                          const KvSum& x) {
+  const int kvh = head / d.grp;
+  const float inv = x.l == 0.f ? 0.f : (d.v_scale != nullptr ? d.v_scale[kvh] : 1.f) / x.l;
+  *reinterpret_cast<uint2*>(d.out + tok * d.out_ld + (int64_t)head * HD + c) =
+      uint2{pk_bf16(x.o[0] * inv, x.o[1] * inv), pk_bf16(x.o[2] * inv, x.o[3] * inv)};
+  if (d.lse != nullptr && c == 0)
+    d.lse[tok * d.nh + head] = x.l == 0.f
+        ? -INFINITY : (x.m + __builtin_amdgcn_logf(x.l)) * 0.69314718055994531f;
+}
+
+// Workgroup (s, y): the segment that share s begins inside of, if no share
+// before s does; rows HD / 4 threads each.
+template <int HD>
+__global__ __launch_bounds__(256) void k_kv_join(const KvDev d, int R) {
+  constexpr int TPR = HD / 4, RPB = 256 / TPR;
+  const int s = blockIdx.x + 1;
+  const scalar_i32 sh = as_scalar(d.w.share + s), hd = as_scalar(d.w.hdr);
+  const int f = sh[0], e = sh[1], kvh = sh[2], j = sh[3], S = hd[1];
+  if (f >= hd[0] || j == 0) return;               // past the end, or nothing is cut here
+  const int a = f - j;
+  if (a < f - S) return;                          // cut before: an earlier workgroup's
+  const scalar_i32 en = as_scalar(d.w.ent + e);
+  const int tok0 = en[0], row0 = en[1], nrows = en[2], tiles = en[11];
+  const int rr = blockIdx.y * RPB + threadIdx.x / TPR, c = 4 * (threadIdx.x % TPR);
+  if (rr >= nrows) return;
+  KvSum x;
+  add_parts<HD>(d, R, a, tiles, S, rr, c, x);
+  const int row = row0 + rr, tk = row / d.grp;
+  write_row<HD>(d, tok0 + tk, kvh * d.grp + (row - tk * d.grp), c, x);
+}
+
+// Calls with shared prefixes: every row, its prefix's result and its own.
+template <int HD>
+__global__ __launch_bounds__(256) void k_kv_join_rows(const KvDev d, int R, int n,
+                                                      const int32_t* __restrict__ cu_q) {
+  constexpr int TPR = HD / 4, RPB = 256 / TPR;
+  const int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
+  const int c = 4 * (threadIdx.x % TPR);
+  if (row >= (int64_t)d.total_q * d.nh) return;
+  const int tok = (int)(row / d.nh), head = (int)(row - (int64_t)tok * d.nh);
+  const int b = d.w.tseq[tok];
+  if ((uint32_t)b >= (uint32_t)n) return;         // behind the last sequence
+  const int kvh = head / d.grp, hg = head - kvh * d.grp, g = d.w.sgrp[b], S = d.w.hdr[1];
+  KvSum x;
+#pragma unroll 1
+  for (int k = g >= 0 ? 0 : 1; k < 2; ++k) {      // the prefix, then the sequence's own keys
+    const int lr = (tok - (k == 0 ? d.w.gtok[g] : d.w.stok[b])) * d.grp + hg;
+    const int e = d.w.off[k == 0 ? n + g : b] + lr / R;
+    if (e >= d.w.hdr[2]) continue;                // dropped: token ranges that overlap
+    const int tiles = d.w.ent[e].tiles, a = d.w.cum[e] + kvh * tiles;
+    if (a / S == (a + tiles - 1) / S) {
+      const int64_t prow = d.row0 + ((int64_t)(1 - k) * d.total_q + tok) * d.nh + head;
+      const float2 ml = *reinterpret_cast<const float2*>(d.w.ml + 2 * prow);
+      x.add(ml.x, ml.y, *reinterpret_cast<const floatx4*>(d.w.part + prow * HD + c));
+    } else {
+      add_parts<HD>(d, R, a, tiles, S, lr % R, c, x);
+    }
+  }
+  write_row<HD>(d, tok, head, c, x);
+}
+
+// no sequence yet for any token (a fill kernel: a captured memset is not one)
+__global__ void k_kv_unseen(int32_t* __restrict__ tseq, int n) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i < n) tseq[i] = -1;
+}
+
+// ---------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------
+// Rows of a workgroup by the rows that a sequence of max_q tokens (a group of
+// sequences) brings: the fewest waves that hold them, so that short ones leave
+// room for a second workgroup and its loads.
+static int kv_rows(int64_t rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
+static int kv_shares(const xp_kv* kv, int R) {
+  return std::max(8, kv->cus * (R == 256 ? 1 : 2) / 8 * 8);
+}
+
+void kv_attn_sizes(const xp_kv* kv, int64_t* rows, int* entries, int* shares) {
+  const int64_t all = (int64_t)kv->max_tokens * kv->grp;
+  const int R = kv_rows(all);
+  *rows = 0;
+  for (int r = 32; r <= R; r *= 2) *rows = std::max(*rows, (int64_t)2 * kv_shares(kv, r) * r);
+  if (R == 256) *rows = std::max(*rows, (int64_t)2 * kv_shares(kv, 256) * 256);
+  // every sequence and every group rounds its rows up to whole tiles
+  *entries = (int)(((all + 31) / 32) * (kv->shared ? 2 : 1) + kv->max_batch * (kv->shared ? 2 : 1));
+  *shares = kv_shares(kv, 32);
+}
+
+hipError_t launch_kv_attn(const xp_kv* kv, const KvAttnArgs& a, hipStream_t st) {
+  int64_t hint = (int64_t)a.max_q * kv->grp;
+  if (a.groups > 0) hint = std::max(hint, (int64_t)a.total_q / a.groups * kv->grp);
+  const int R = kv_rows(hint), shares = kv_shares(kv, R);
+  hipError_t e;
+  KvPlan p{};
+  p.n = a.n;
+  p.total_q = a.total_q;
+  p.max_q = a.max_q;
+  p.kv_add = a.kv_add;
+  const int cols = (int)std::min<int64_t>(kv->max_pages, a.table_ld);
+  p.cap = (int)std::min<int64_t>((int64_t)cols << kv->logP, kKvMaxLen);
+  p.R = R;
+  p.grp = kv->grp;
+  p.nkv = kv->nkv;
+  p.causal = a.causal;
+  p.window = a.window;
+  p.sinks = a.sinks;
+  p.groups = a.groups;
+  p.entries = kv->entries;
+  p.shares = shares;
+  p.cu_q = a.cu_q;
+  p.kv_len = a.kv_len;
+  p.group_start = a.group_start;
+  p.shared_len = a.shared_len;
+  p.w = kv->a;
+  p.err = kv->err;
+  if (a.groups > 0) {
+    hipLaunchKernelGGL(k_kv_unseen, dim3((a.total_q + 255) / 256), dim3(256), 0, st, kv->a.tseq,
+                       a.total_q);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    hipLaunchKernelGGL(k_kv_plan<true>, dim3(1), dim3(kPlanThreads), 0, st, p);
+  } else {
+    hipLaunchKernelGGL(k_kv_plan<false>, dim3(1), dim3(kPlanThreads), 0, st, p);
+  }
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+
+  KvDev d{};
+  d.q = a.q;
+  d.q_ld = a.q_ld;
+  d.out = a.out;
+  d.out_ld = a.out_ld;
+  d.lse = a.lse;
+  d.kc = (const char*)a.kc;
+  d.vc = (const char*)a.vc;
+  d.k_scale = a.k_scale;
+  d.v_scale = a.v_scale;
+  d.table = a.table;
+  d.table_ld = a.table_ld;
+  d.nh = kv->nh;
+  d.nkv = kv->nkv;
+  d.grp = kv->grp;
+  d.logP = kv->logP;
+  d.n_pages = kv->n_pages;
+  d.cols = cols;
+  d.causal = a.causal;
+  d.window = a.window;
+  d.sinks = a.sinks;
+  d.scale2 = (a.scale > 0.f ? a.scale : 1.f / std::sqrt((float)kv->hd)) * 1.4426950408889634f;
+  d.total_q = a.total_q;
+  d.groups = a.groups;
+  d.row0 = kv->rows;
+  d.w = kv->a;
+  d.err = kv->err;
+#define XP_KV(HD_, F8_, WR_, WK_, NST_, PARTS_)                                                  \
+  hipLaunchKernelGGL((k_kv_attn<HD_, F8_, WR_, WK_, NST_, PARTS_>), dim3(shares),                \
+                     dim3((WR_) * (WK_) * kWave), 0, st, d)
+#define XP_KV_R(HD_, F8_, N2_)                                                                   \
+  do {                                                                                           \
+    if (R == 32) XP_KV(HD_, F8_, 1, 2, N2_, 2);                                                  \
+    else if (R == 64) XP_KV(HD_, F8_, 2, 2, N2_, 2);                                             \
+    else if (R == 128) XP_KV(HD_, F8_, 4, 1, N2_, 2);                                            \
+    else XP_KV(HD_, F8_, 8, 1, 4, 1);                                                            \
+  } while (0)
+  const bool f8 = kv->dtype == XP_E4M3;
+  if (kv->hd == 128) {
+    if (f8) XP_KV_R(128, true, 4);
+    else XP_KV_R(128, false, 2);
+  } else {
+    if (f8) XP_KV_R(64, true, 4);
+    else XP_KV_R(64, false, 4);
+  }
+#undef XP_KV_R
+#undef XP_KV
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  if (a.groups > 0) {
+    const int rpb = 1024 / kv->hd;
+    const dim3 grid((unsigned)(((int64_t)a.total_q * kv->nh + rpb - 1) / rpb));
+    if (kv->hd == 128)
+      hipLaunchKernelGGL(k_kv_join_rows<128>, grid, dim3(256), 0, st, d, R, a.n, a.cu_q);
+    else
+      hipLaunchKernelGGL(k_kv_join_rows<64>, grid, dim3(256), 0, st, d, R, a.n, a.cu_q);
+  } else {
+    const dim3 grid(shares - 1, R * kv->hd / 1024);
+    if (kv->hd == 128) hipLaunchKernelGGL(k_kv_join<128>, grid, dim3(256), 0, st, d, R);
+    else hipLaunchKernelGGL(k_kv_join<64>, grid, dim3(256), 0, st, d, R);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace xp

@@ -38,6 +38,7 @@
 #include <type_traits>
 
 #include "xp_internal.h"
+#include "xp_kv.h"
 #include "xp_layer_plan.h"
 
 namespace xp {
@@ -1312,14 +1313,27 @@ static xp_status check_call(xp_layer* Lerr, int32_t batch, int32_t B, int32_t ca
   return XP_OK;
 }
 
+// The context of a paged forward: the block's keys and values go to the pages
+// first, and the attention reads them there.
+struct PagedContext {
+  xp_kv* kv;
+  void *kc, *vc;
+  const float *ks, *vs;
+  const int32_t* table;
+  int64_t table_ld;
+  int window, sinks;
+};
+
 // The launch sequence of one forward over `batch` blocks of B positions with
-// the attention chunking `ap`, on the buffers `b` (which hold at least the
+// the attention chunking `ap` (pg: over the pages instead, C_max the most
+// context keys that leave room for the block), on the buffers `b` (which hold at least the
 // call's positions and ap.parts partials).  Errors go to Lerr (NULL: the
 // thread's message).
 static xp_status forward(const xp_layer& L, const LayerBufs& b, const AttnPlan& ap,
                          xp_layer* Lerr, int32_t batch, int32_t B, int32_t causal, const void* x,
                          const void* k_cache, const void* v_cache, int32_t C_max,
-                         const int32_t* ctx_len, float* h_f32, void* h_bf16, hipStream_t st) {
+                         const int32_t* ctx_len, float* h_f32, void* h_bf16, hipStream_t st,
+                         const PagedContext* pg = nullptr) {
   const int M = batch * B, H = L.H, nh = L.nh, nkv = L.nkv, F = L.ffn, grp = L.grp;
   const int nhd = nh * kHd, kvd = nkv * kHd, ldq = nhd + 2 * kvd;
   const int npb = (B + kTile - 1) / kTile;
@@ -1358,6 +1372,33 @@ static xp_status forward(const xp_layer& L, const LayerBufs& b, const AttnPlan& 
           hipLaunchKernelGGL(k_qkrope, dim3(M, qy), dim3(256), 0, st, sq > 1 ? b.part : b.qkv, sq,
                              (size_t)M * ldq, ldq, B, nh, nkv, ctx_len, C_max, L.g_q, L.g_k,
                              L.eps, lt, b.qn, b.kb, b.vb, batch, pre));
+  if (pg != nullptr) {
+    e = launch_kv_write(pg->kv, M, b.kb, b.vb, kvd, kvd, nullptr, pg->table, pg->table_ld, ctx_len,
+                        B, pg->kc, pg->vc, pg->ks, pg->vs, st);
+    if (e != hipSuccess)
+      return layer_fail(Lerr, XP_EHIP, "cache write launch failed: %s", hipGetErrorString(e));
+    KvAttnArgs ka{};
+    ka.n = batch;
+    ka.total_q = M;
+    ka.max_q = B;
+    ka.kv_len = ctx_len;
+    ka.kv_add = B;
+    ka.table = pg->table;
+    ka.table_ld = pg->table_ld;
+    ka.q = b.qn;
+    ka.q_ld = nhd;
+    ka.kc = pg->kc;
+    ka.vc = pg->vc;
+    ka.k_scale = pg->ks;
+    ka.v_scale = pg->vs;
+    ka.causal = causal;
+    ka.window = pg->window;
+    ka.sinks = pg->sinks;
+    ka.out = b.attn;
+    ka.out_ld = nhd;
+    if ((e = launch_kv_attn(pg->kv, ka, st)) != hipSuccess)
+      return layer_fail(Lerr, XP_EHIP, "paged attention launch failed: %s", hipGetErrorString(e));
+  } else {
 #define XP_ATTN(GG, PB)                                                                      \
   hipLaunchKernelGGL((k_attn<GG, PB>), dim3(ap.W),                                            \
                      dim3(attn_waves(GG, PB) * kWave), 0, st,                                 \
@@ -1396,6 +1437,7 @@ static xp_status forward(const xp_layer& L, const LayerBufs& b, const AttnPlan& 
   else XP_STEP("attention combine", XP_COMB1(8, 1));
 #undef XP_COMB1
 #undef XP_COMB
+  }
   XP_LINEAR("output", b, L.Wo, nullptr, nullptr, H, 0, H, nhd, b.attn, M, b.x32, H, b.x1,
             nullptr, H, false, &so, st);
   // x1 = Wo attn + x: written by the projection, or here from its slabs
@@ -1439,6 +1481,50 @@ extern "C" xp_status xp_layer_forward(xp_layer* L, int32_t batch, int32_t B, int
                       L->max_ctx > 0 ? L->max_ctx : 1);
   return forward(*L, L->b, attn_plan_default(*L, batch, B, C_max), L, batch, B, causal, x,
                  k_cache, v_cache, C_max, ctx_len, h_f32, h_bf16, (hipStream_t)stream);
+}
+
+extern "C" xp_status xp_layer_forward_paged(xp_layer* L, xp_kv* kv, int32_t batch, int32_t B,
+                                            int32_t causal, int32_t window, int32_t sinks,
+                                            const void* x, void* k_cache, void* v_cache,
+                                            const float* k_scale, const float* v_scale,
+                                            const int32_t* table, int64_t table_ld,
+                                            const int32_t* ctx_len, float* h_f32, void* h_bf16,
+                                            void* stream) {
+  if (L == nullptr) return XP_EINVAL;
+  if (kv == nullptr || table == nullptr || table_ld < 1)
+    return layer_fail(L, XP_EINVAL, "kv, table and table_ld >= 1 are required");
+  // the most context keys that leave room for the block
+  const int64_t cap = std::min<int64_t>(kv->max_pages, table_ld) << kv->logP;
+  const int C_max = (int)std::min<int64_t>(cap, 1 << 20) - B;
+  const xp_status cs = check_call(L, batch, B, causal, x, k_cache, v_cache, std::max(C_max, 1),
+                                  ctx_len, h_f32, h_bf16);
+  if (cs != XP_OK) return cs;
+  if (C_max < 0)
+    return layer_fail(L, XP_EINVAL, "a table of %lld pages has no room for a block of %d",
+                      (long long)table_ld, B);
+  if (batch > L->max_batch || B > L->max_B || batch > kv->max_batch ||
+      (int64_t)batch * B > kv->max_tokens)
+    return layer_fail(L, XP_EINVAL,
+                      "batch=%d (1..%d, cache %d) or B=%d (1..%d, cache %d tokens) outside the "
+                      "created maxima", batch, L->max_batch, kv->max_batch, B, L->max_B,
+                      kv->max_tokens);
+  if (kv->nh != L->nh || kv->nkv != L->nkv || kv->hd != kHd)
+    return layer_fail(L, XP_EINVAL, "the cache has heads %d/%d x %d, the layer %d/%d x %d", kv->nh,
+                      kv->nkv, kv->hd, L->nh, L->nkv, kHd);
+  if (!kv_units_fit(kv, batch * B, batch, 0, table_ld))
+    return layer_fail(L, XP_EINVAL, "the call's tokens and the tables' pages reach 2^31 key tiles");
+  if (window < 0 || window > kKvMaxLen || sinks < 0 || sinks > kKvMaxLen)
+    return layer_fail(L, XP_EINVAL, "window=%d or sinks=%d out of range 0..2^22", window, sinks);
+  if (kv->dtype == XP_BF16 && (k_scale != nullptr || v_scale != nullptr))
+    return layer_fail(L, XP_EINVAL, "a bf16 cache has no scales");
+  int dev = -1;
+  const hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return layer_fail(L, XP_EHIP, "device query failed: %s", hipGetErrorString(e));
+  if (dev != kv->device)
+    return layer_fail(L, XP_EINVAL, "the current device is %d, the cache's %d", dev, kv->device);
+  const PagedContext pg{kv, k_cache, v_cache, k_scale, v_scale, table, table_ld, window, sinks};
+  return forward(*L, L->b, AttnPlan{}, L, batch, B, causal, x, k_cache, v_cache, C_max, ctx_len,
+                 h_f32, h_bf16, (hipStream_t)stream, &pg);
 }
 
 // ---------------------------------------------------------------------------

@@ -20,15 +20,18 @@ LIB_PATH = os.environ.get("XPRESS_LIB") or os.path.join(
     os.path.dirname(os.path.abspath(__file__)), "libxpress.so")
 
 XP_OK, XP_EINVAL, XP_EUNSUPPORTED, XP_EHIP, XP_ENOMEM = 0, -1, -2, -3, -4
-XP_F32, XP_BF16 = 0, 1
+XP_F32, XP_BF16, XP_E4M3 = 0, 1, 2
 XP_EARLY_EXIT, XP_WRITE_LOGITS = 1, 2
 XP_DEVERR_TOKEN, XP_DEVERR_TEMPERATURE, XP_DEVERR_FILTER = 1, 2, 4
+XP_DEVERR_PAGE, XP_DEVERR_SLOT, XP_DEVERR_POOL, XP_DEVERR_LENGTH = 8, 16, 32, 64
 
 EXPORTS = ("xp_create", "xp_destroy", "xp_last_error", "xp_status_string",
            "xp_refine_block", "xp_verify_block", "xp_device_errors", "xp_timing_enable",
            "xp_timing_read", "xp_probe_hbm_read", "xp_probe_mfma_bf16", "xp_toeplitz_mixer",
            "xp_layer_create", "xp_layer_forward", "xp_layer_destroy", "xp_layer_last_error",
-           "xp_layer_forward_noalloc")
+           "xp_layer_forward_noalloc", "xp_kv_create", "xp_kv_destroy", "xp_kv_last_error",
+           "xp_kv_map", "xp_kv_write", "xp_kv_attn", "xp_kv_attn_shared", "xp_kv_device_errors",
+           "xp_layer_forward_paged")
 LAYER_WEIGHT_NAMES = ("g_attn", "Wq", "Wk", "Wv", "g_q", "g_k", "Wo", "g_mlp", "Wg", "Wu", "Wd")
 STAGES = ("prep", "lmhead", "select", "rspace", "read", "verify")
 
@@ -52,6 +55,11 @@ class _LayerWeights(ctypes.Structure):
         ("eps", ctypes.c_float), ("rope_theta", ctypes.c_float)] + [
         (n, ctypes.c_void_p) for n in ("g_attn", "Wq", "Wk", "Wv", "g_q", "g_k", "Wo", "g_mlp",
                                        "Wg", "Wu", "Wd")]
+
+
+class _KvShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_heads", "n_kv", "head_dim", "page_size",
+                                              "n_pages", "dtype")]
 
 
 _lib = None
@@ -102,6 +110,28 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     L.xp_layer_forward_noalloc.argtypes = [ctypes.POINTER(_LayerWeights), i32, i32, i32, vp, vp,
                                            vp, i32, vp, vp, vp, vp]
     L.xp_layer_forward_noalloc.restype = i32
+    i64 = ctypes.c_int64
+    L.xp_kv_create.argtypes = [ctypes.POINTER(_KvShape), i32, i32, i32, i32, ctypes.POINTER(vp)]
+    L.xp_kv_create.restype = i32
+    L.xp_kv_destroy.argtypes = [vp]
+    L.xp_kv_destroy.restype = None
+    L.xp_kv_last_error.argtypes = [vp]
+    L.xp_kv_last_error.restype = ctypes.c_char_p
+    L.xp_kv_map.argtypes = [vp, i32, vp, vp, vp, i64, vp, vp, vp, vp, vp, vp, i32, vp]
+    L.xp_kv_map.restype = i32
+    L.xp_kv_write.argtypes = [vp, i32, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp]
+    L.xp_kv_write.restype = i32
+    attn = [vp, i64, vp, vp, vp, i64, vp, vp, vp, vp, i32, i32, i32, ctypes.c_float, vp, i64, vp,
+            vp]
+    L.xp_kv_attn.argtypes = [vp, i32, i32, i32] + attn
+    L.xp_kv_attn.restype = i32
+    L.xp_kv_attn_shared.argtypes = [vp, i32, i32, i32, i32, vp, vp] + attn
+    L.xp_kv_attn_shared.restype = i32
+    L.xp_layer_forward_paged.argtypes = [vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp,
+                                         i64, vp, vp, vp, vp]
+    L.xp_layer_forward_paged.restype = i32
+    L.xp_kv_device_errors.argtypes = [vp, ctypes.POINTER(u32), vp]
+    L.xp_kv_device_errors.restype = i32
     _lib = L
     return L
 
@@ -376,9 +406,212 @@ class Layer:
             raise XpError(st, "xp_layer_forward: " + L.xp_layer_last_error(self._h).decode())
         return h_f32, h_bf16
 
+    def forward_paged(self, x, kv, k_cache, v_cache, table, ctx_len, causal=True, window=0,
+                      sinks=0, k_scale=None, v_scale=None, h_f32=None, h_bf16=None, stream=None):
+        """forward() over the pages of `kv` (a PagedKV of the layer's heads): the
+        block's keys and values are written to positions ctx_len .. + B - 1 of
+        their requests' tables, then attended to (xp_layer_forward_paged)."""
+        import torch
+        L = load_library()
+        batch, B, H = x.shape
+        c = kv._cache(k_cache, v_cache, k_scale, v_scale)
+        kv._table(table, batch)
+        kv._flat("ctx_len", ctx_len, torch.int32, batch)
+        if h_f32 is None:
+            h_f32 = torch.empty((batch, B, H), dtype=torch.float32, device=x.device)
+        if h_bf16 is None:
+            h_bf16 = torch.empty((batch, B, H), dtype=torch.bfloat16, device=x.device)
+        for t in (x, h_f32, h_bf16):
+            assert t.is_contiguous() and t.device == kv.device
+        with torch.cuda.device(kv.device):
+            st = L.xp_layer_forward_paged(self._h, kv._h, batch, B, 1 if causal else 0, window,
+                                          sinks, _ptr(x), *c, _ptr(table), table.shape[1],
+                                          _ptr(ctx_len), _ptr(h_f32), _ptr(h_bf16),
+                                          _stream(stream))
+        if st != XP_OK:
+            raise XpError(st, "xp_layer_forward_paged: " + L.xp_layer_last_error(self._h).decode())
+        return h_f32, h_bf16
+
     def close(self):
         if getattr(self, "_h", None):
             load_library().xp_layer_destroy(self._h)
+            self._h = None
+
+    def __del__(self):  # pragma: no cover
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class PagedKV:
+    """The paged context cache (xp_kv_*): pages and slots from lengths, writes of
+    new keys and values, and attention over the pages.  The caches [n_pages]
+    [n_kv][page_size][head_dim] (``cache_shape``; bf16 or torch.float8_e4m3fn)
+    and the tables belong to the caller."""
+
+    def __init__(self, n_heads: int, n_kv: int, page_size: int, n_pages: int, max_batch: int,
+                 max_tokens: int, max_len: int, head_dim: int = 128, cache_dtype=None,
+                 shared: bool = False, device="cuda"):
+        import torch
+        L = load_library()
+        self.cache_dtype = torch.bfloat16 if cache_dtype is None else cache_dtype
+        dt = {torch.bfloat16: XP_BF16, torch.float8_e4m3fn: XP_E4M3}.get(self.cache_dtype)
+        if dt is None:
+            raise ValueError(f"cache_dtype {cache_dtype}: torch.bfloat16 or torch.float8_e4m3fn")
+        self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.n_heads, self.n_kv, self.head_dim, self.page_size = n_heads, n_kv, head_dim, page_size
+        self.n_pages = n_pages
+        self.cache_shape = (n_pages, n_kv, page_size, head_dim)
+        st = _KvShape(n_heads=n_heads, n_kv=n_kv, head_dim=head_dim, page_size=page_size,
+                      n_pages=n_pages, dtype=dt)
+        h = ctypes.c_void_p(0)
+        with torch.cuda.device(self.device):
+            s = L.xp_kv_create(ctypes.byref(st), max_batch, max_tokens, max_len,
+                               1 if shared else 0, ctypes.byref(h))
+        if s != XP_OK:
+            raise XpError(s, "xp_kv_create: " + L.xp_kv_last_error(None).decode())
+        self._h = h
+        self._L = L
+
+    # ------------------------------------------------------------------
+    def _call(self, name, *args, stream=None):
+        import torch
+        with torch.cuda.device(self.device):
+            s = getattr(self._L, name)(self._h, *args, _stream(stream))
+        if s != XP_OK:
+            raise XpError(s, f"{name}: " + self._L.xp_kv_last_error(self._h).decode())
+
+    def _flat(self, name, t, dtype, n, optional=False):
+        """A contiguous device vector of n (None: any number of) elements."""
+        if t is None and optional:
+            return None
+        if (t is None or t.dtype != dtype or not t.is_contiguous() or t.device != self.device
+                or t.dim() != 1 or (n is not None and t.numel() != n)):
+            raise ValueError(f"{name}: expected a contiguous {dtype} tensor of "
+                             f"{'any number of' if n is None else n} elements on {self.device}")
+        return t
+
+    def _rows(self, name, t, heads, tokens=None):
+        """Token rows [tokens][heads][head_dim] of bf16, each contiguous."""
+        import torch
+        if (t.dtype != torch.bfloat16 or t.dim() != 3 or t.device != self.device
+                or tuple(t.shape[1:]) != (heads, self.head_dim)
+                or (tokens is not None and t.shape[0] != tokens)
+                or t.stride(2) != 1 or (heads > 1 and t.stride(1) != self.head_dim)):
+            raise ValueError(f"{name}: expected bf16 [{'tokens' if tokens is None else tokens}]"
+                             f"[{heads}][{self.head_dim}] rows on {self.device}")
+        # the row distance of a single row is free
+        return t.stride(0) if t.shape[0] > 1 else heads * self.head_dim
+
+    def _cache(self, k_cache, v_cache, k_scale, v_scale):
+        import torch
+        for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
+            if (t.dtype != self.cache_dtype or tuple(t.shape) != self.cache_shape
+                    or not t.is_contiguous() or t.device != self.device):
+                raise ValueError(f"{name}: expected a contiguous {self.cache_dtype} tensor "
+                                 f"{self.cache_shape} on {self.device}")
+        self._flat("k_scale", k_scale, torch.float32, self.n_kv, optional=True)
+        self._flat("v_scale", v_scale, torch.float32, self.n_kv, optional=True)
+        return _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale)
+
+    def _table(self, table, n):
+        import torch
+        if (table.dtype != torch.int32 or table.dim() != 2 or table.shape[0] != n
+                or table.shape[1] < 1 or not table.is_contiguous() or table.device != self.device):
+            raise ValueError(f"table: expected a contiguous int32 [{n}][pages] tensor on "
+                             f"{self.device}")
+
+    def map(self, lens, add, table, held, pool, pool_n, cu=None, kv_len=None, slots=None,
+            stream=None):
+        """Pages and slots from lengths (xp_kv_map): table, held, pool and pool_n
+        are updated, and cu, kv_len and slots written where given."""
+        import torch
+        i32 = torch.int32
+        n = lens.numel()
+        self._table(table, n)
+        for name, t, m, opt in (("lens", lens, n, False), ("add", add, n, False),
+                                ("held", held, n, False), ("pool", pool, self.n_pages, False),
+                                ("pool_n", pool_n, 1, False), ("cu", cu, n + 1, True),
+                                ("kv_len", kv_len, n, True), ("slots", slots, None, True)):
+            self._flat(name, t, i32, m, optional=opt)
+        self._call("xp_kv_map", n, _ptr(lens), _ptr(add), _ptr(table), table.shape[1],
+                   _ptr(held), _ptr(pool), _ptr(pool_n), _ptr(cu), _ptr(kv_len), _ptr(slots),
+                   0 if slots is None else slots.numel(), stream=stream)
+        return cu, kv_len, slots
+
+    def write(self, k, v, slots, k_cache, v_cache, k_scale=None, v_scale=None, stream=None):
+        """K and V rows [tokens][n_kv][head_dim] to their slots (xp_kv_write)."""
+        import torch
+        n = k.shape[0]
+        k_ld, v_ld = self._rows("k", k, self.n_kv), self._rows("v", v, self.n_kv, n)
+        self._flat("slots", slots, torch.int32, n)
+        c = self._cache(k_cache, v_cache, k_scale, v_scale)
+        if n:
+            self._call("xp_kv_write", n, _ptr(k), k_ld, _ptr(v), v_ld, _ptr(slots), *c,
+                       stream=stream)
+
+    def _attend(self, name, groups, q, k_cache, v_cache, table, kv_len, cu_q, max_q, causal,
+                window, sinks, scale, k_scale, v_scale, out, lse, stream):
+        import torch
+        n, tokens = kv_len.numel(), q.shape[0]
+        self._flat("kv_len", kv_len, torch.int32, n)
+        self._flat("cu_q", cu_q, torch.int32, n + 1, optional=True)
+        self._table(table, n)
+        if max_q is None:
+            if cu_q is not None:
+                raise ValueError("max_q is required with cu_q")
+            max_q = tokens // n if n else 0
+        if out is None:
+            out = torch.empty((tokens, self.n_heads, self.head_dim), dtype=torch.bfloat16,
+                              device=self.device)
+        q_ld = self._rows("q", q, self.n_heads)
+        out_ld = self._rows("out", out, self.n_heads, tokens)
+        if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous()
+                                or tuple(lse.shape) != (tokens, self.n_heads)
+                                or lse.device != self.device):
+            raise ValueError(f"lse: expected contiguous float32 [{tokens}][{self.n_heads}]")
+        c = self._cache(k_cache, v_cache, k_scale, v_scale)
+        if n and tokens:
+            self._call(name, n, tokens, max_q, *groups, _ptr(q), q_ld, _ptr(cu_q), _ptr(kv_len),
+                       _ptr(table), table.shape[1], *c, 1 if causal else 0, window, sinks,
+                       0.0 if scale is None else scale, _ptr(out), out_ld, _ptr(lse),
+                       stream=stream)
+        return out
+
+    def attend(self, q, k_cache, v_cache, table, kv_len, cu_q=None, max_q=None, causal=True,
+               window=0, sinks=0, scale=None, k_scale=None, v_scale=None, out=None, lse=None,
+               stream=None):
+        """Attention of the tokens q [tokens][n_heads][head_dim] over their
+        requests' pages (xp_kv_attn); without cu_q every request has the same
+        number of them.  Returns out (allocated when None)."""
+        return self._attend("xp_kv_attn", (), q, k_cache, v_cache, table, kv_len, cu_q, max_q,
+                            causal, window, sinks, scale, k_scale, v_scale, out, lse, stream)
+
+    def attend_shared(self, q, k_cache, v_cache, table, kv_len, group_start, shared_len, cu_q=None,
+                      max_q=None, causal=True, window=0, sinks=0, scale=None, k_scale=None,
+                      v_scale=None, out=None, lse=None, stream=None):
+        """attend() for groups of neighbouring requests whose first shared_len keys
+        are the same pages, read once per group (xp_kv_attn_shared)."""
+        import torch
+        groups = shared_len.numel()
+        self._flat("shared_len", shared_len, torch.int32, groups)
+        self._flat("group_start", group_start, torch.int32, groups + 1)
+        return self._attend("xp_kv_attn_shared", (groups, _ptr(group_start), _ptr(shared_len)), q,
+                            k_cache, v_cache, table, kv_len, cu_q, max_q, causal, window, sinks,
+                            scale, k_scale, v_scale, out, lse, stream)
+
+    def device_errors(self, stream=None) -> int:
+        """The XP_DEVERR_* bits set since the last read; synchronizes."""
+        v = ctypes.c_uint32(0)
+        self._call("xp_kv_device_errors", ctypes.byref(v), stream=stream)
+        return int(v.value)
+
+    def close(self):
+        if getattr(self, "_h", None):
+            self._L.xp_kv_destroy(self._h)
             self._h = None
 
     def __del__(self):  # pragma: no cover
