@@ -34,14 +34,15 @@ struct KvEntry {
 };
 constexpr int kKvEntryInts = sizeof(KvEntry) / 4;
 
-// where share s of the work begins: unit f = (entry e, KV head, tile j)
+// where share s of the work begins: unit f, at tile j of (entry e, KV head kvh), or
+// -j units before its first
 struct KvShare {
   int32_t f, e, kvh, j;
 };
 
 // Workspace of the attention (device pointers).
 struct KvAttnWs {
-  int32_t* hdr = nullptr;            // [0] units, [1] units a share, [2] entries
+  int32_t* hdr = nullptr;            // [0] units, [1] units of a share, [2] entries
   KvShare* share = nullptr;          // [shares + 1]
   KvEntry* ent = nullptr;            // [entries]
   int32_t* cum = nullptr;            // [entries + 1] units before each entry

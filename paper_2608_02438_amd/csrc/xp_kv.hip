@@ -146,11 +146,24 @@ __global__ __launch_bounds__(kMapThreads) void k_kv_map(const KvMap d) {
     free0 = free0 < 0 ? 0 : (free0 > d.n_pages ? d.n_pages : free0);
   }
   int top = free0 + R;
-  for (int i = tid; i < R; i += kMapThreads) {
-    const int b = kv_owner(rel, d.n, i);
-    int32_t* at = d.table + b * d.ld + old[b] - (rel[b + 1] - rel[b]) + (i - rel[b]);
-    if (top - 1 - i < d.n_pages) d.pool[top - 1 - i] = *at;
-    *at = -1;
+  constexpr int kBack = 8;                        // pages of a thread under way at a time
+  for (int i0 = tid; i0 < R; i0 += kBack * kMapThreads) {
+    int32_t* at[kBack];
+    int32_t page[kBack];
+#pragma unroll
+    for (int u = 0; u < kBack; ++u) {
+      const int i = i0 + u * kMapThreads < R ? i0 + u * kMapThreads : i0;
+      const int b = kv_owner(rel, d.n, i);
+      at[u] = d.table + b * d.ld + old[b] - (rel[b + 1] - rel[b]) + (i - rel[b]);
+      page[u] = *at[u];
+    }
+#pragma unroll
+    for (int u = 0; u < kBack; ++u) {
+      const int i = i0 + u * kMapThreads;
+      if (i >= R) continue;
+      if (top - 1 - i < d.n_pages) d.pool[top - 1 - i] = page[u];
+      *at[u] = -1;
+    }
   }
   top = top < d.n_pages ? top : d.n_pages;
   __syncthreads();                                // the pool holds them
@@ -216,15 +229,21 @@ __global__ __launch_bounds__(256) void k_kv_slots(const KvMap d) {
 // The write.  A thread moves VE values of one head of one token: 16 bytes of
 // the cache.  Bound by memory.
 // ---------------------------------------------------------------------------
-// x / s to e4m3, the quotient rounded once: to odd in fp32 (of the two
-// neighbours of an inexact quotient the one with an odd last bit), then to
-// nearest even in the conversion.  Saturates at 448; NaN stays.
-__device__ __forceinline__ float f8_quotient(float x, float s) {
-  float q = __fdiv_rn(x, s);
-  const float r = fmaf(-q, s, x);                 // the exact rest
-  const uint32_t u = __float_as_uint(q);
-  if (r != 0.f && q != 0.f && !(u & 1u) && fabsf(q) < 1e30f)  // up in magnitude where the rest has q's sign
-    q = __uint_as_float((r > 0.f) == (q > 0.f) == (s > 0.f) ? u + 1u : u - 1u);
+// x / s (inv = 1 / s) to e4m3, the quotient rounded once: an fp32 quotient less
+// than one step from the true one, to odd where it is not exact (an even one moves
+// one step towards the truth), so that no middle between two e4m3 values lies
+// between it and the truth; then to nearest even in the conversion.  Saturates at
+// 448; NaN stays.
+__device__ __forceinline__ float f8_quotient(float x, float s, float inv) {
+  // beyond 448 by far: no rounding to decide, and no overflow below
+  float q = x * inv;
+  if (fabsf(q) < 1024.f) {
+    q = fmaf(fmaf(-q, s, x), inv, q);             // one step of Newton's
+    const float r = fmaf(-q, s, x);               // the exact rest
+    const uint32_t u = __float_as_uint(q);
+    const uint32_t up = (u ^ __float_as_uint(r) ^ __float_as_uint(s)) >> 31 ? u - 1u : u + 1u;
+    q = (r != 0.f) & (q != 0.f) & !(u & 1u) ? __uint_as_float(up) : q;
+  }
   return q > 448.f ? 448.f : (q < -448.f ? -448.f : q);
 }
 
@@ -283,16 +302,16 @@ __global__ __launch_bounds__(256) void k_kv_write(const KvWrite d) {
   } else {
     const u32x4 b = ld16(src + 8);
     const float* sp = isv ? d.vs : d.ks;
-    const float s = sp != nullptr ? sp[g] : 1.f;
+    const float s = sp != nullptr ? sp[g] : 1.f, inv = __fdiv_rn(1.f, s);
     u32x4 y;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const uint32_t w0 = q < 2 ? a[2 * q] : b[2 * q - 4], w1 = q < 2 ? a[2 * q + 1] : b[2 * q - 3];
-      int z = __builtin_amdgcn_cvt_pk_fp8_f32(f8_quotient(__uint_as_float(w0 << 16), s),
-                                              f8_quotient(__uint_as_float(w0 & 0xffff0000u), s), 0,
+      int z = __builtin_amdgcn_cvt_pk_fp8_f32(f8_quotient(__uint_as_float(w0 << 16), s, inv),
+                                              f8_quotient(__uint_as_float(w0 & 0xffff0000u), s, inv), 0,
                                               false);
-      z = __builtin_amdgcn_cvt_pk_fp8_f32(f8_quotient(__uint_as_float(w1 << 16), s),
-                                          f8_quotient(__uint_as_float(w1 & 0xffff0000u), s), z, true);
+      z = __builtin_amdgcn_cvt_pk_fp8_f32(f8_quotient(__uint_as_float(w1 << 16), s, inv),
+                                          f8_quotient(__uint_as_float(w1 & 0xffff0000u), s, inv), z, true);
       y[q] = (uint32_t)z;
     }
     *reinterpret_cast<u32x4*>(dst) = y;
@@ -306,7 +325,7 @@ __global__ void k_kv_clear_err(uint32_t* err) {
 bool kv_units_fit(const xp_kv* kv, int64_t tokens, int64_t n, int groups, int64_t table_ld) {
   const int64_t keys = std::min<int64_t>(kv->max_pages, table_ld) * kv->P;
   const int64_t ent = (tokens * kv->grp / 32 + n) * (groups > 0 ? 2 : 1);
-  return ent * (keys / kKvTile + 2) * kv->nkv < ((int64_t)1 << 31);
+  return ent * (keys / kKvTile + 8) * kv->nkv < ((int64_t)1 << 31);
 }
 
 hipError_t launch_kv_write(const xp_kv* kv, int tokens, const uint16_t* k, const uint16_t* v,

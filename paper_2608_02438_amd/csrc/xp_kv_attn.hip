@@ -32,6 +32,7 @@ namespace xp {
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 // read-only data at wave-uniform addresses: scalar loads
 #define XP_AS4 __attribute__((address_space(4)))
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 typedef const XP_AS4 int32_t* scalar_i32;
 
 __device__ __forceinline__ scalar_i32 as_scalar(const void* p) {
@@ -75,7 +76,11 @@ struct KvDev {
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanWaves = kPlanThreads / kWave;
 constexpr int kPlanCum = 4096;       // entries whose sums stay in LDS
-constexpr int kPlanMinShare = 4;     // units a share has at least
+// Units that a segment counts beside its key tiles, for its rows' loads, its first
+// tile's latency and its results: without them the shares at the beginnings of
+// prompts, many segments of a few tiles, ran 1.65 ms where the others took 1.0.
+constexpr int kSegUnits = 3;
+constexpr int kPlanMinShare = kSegUnits + 2;   // units a share has at least
 
 // exclusive sum over the workgroup of each thread's v; *total their sum
 __device__ __forceinline__ int block_scan(int v, int* lds, int* total) {
@@ -267,7 +272,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d) {
       // no row sees a key: one tile, wholly masked, writes the zeros
       x.tiles = imax(x.n1 + imax(b1 - x.b0, 0), 1);
       d.w.ent[e] = x;
-      units = x.tiles * d.nkv;
+      units = (x.tiles + kSegUnits) * d.nkv;
     }
     int all;
     const int before = block_scan(units, red, &all);
@@ -292,10 +297,10 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d) {
     if (r.f < W) {
       r.e = T <= kPlanCum ? last_at_most((const int*)cums, T, r.f)
                           : last_at_most((const int32_t*)d.w.cum, T, r.f);
-      const int tiles = d.w.ent[r.e].tiles;
+      const int units = d.w.ent[r.e].tiles + kSegUnits;
       const int in = r.f - (T <= kPlanCum ? cums[r.e] : d.w.cum[r.e]);
-      r.kvh = in / tiles;
-      r.j = in - r.kvh * tiles;
+      r.kvh = in / units;
+      r.j = in - r.kvh * units - kSegUnits;       // negative: before the first tile
     }
     d.w.share[s] = r;
   }
@@ -341,59 +346,98 @@ __device__ __forceinline__ uint32_t lds_byte(const void* p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
 }
 
-// V operands of one 16-key step for ND blocks of 32 dims: the addresses a[] of
-// the lane's part of each (b[]: of the keys 8 further), with the wait for the
-// reads.  Written out because the compiler takes its transposing-read builtin
-// for a use of the global-to-LDS loads in flight and waits for all of them.
-template <int ND, int OFF>
-__device__ __forceinline__ void lds_v16(const uint32_t* a, const uint32_t* b, u32x4* v) {
-  uint2 r[2 * ND];
-  if constexpr (ND == 4) {
+// V operands of two 16-key steps (OFF bytes into the lane's addresses, the second
+// 16 rows of RB bytes further) for ND blocks of 32 dims, with the wait for the
+// reads: a[] the lane's part of each block, b[] (+ 8 RB) the same of the keys 8
+// further (8-bit rows: one read brings both groups of four keys).  Written out
+// because the compiler takes its transposing-read builtin for a use of the
+// global-to-LDS loads in flight and waits for all of them.
+template <int ND, bool F8, int OFF, int RB>
+__device__ __forceinline__ void lds_v(const uint32_t* a, const uint32_t* b, u32x4 (&v)[2][ND]) {
+  constexpr int ON = OFF + 16 * RB, OB = OFF + 8 * RB, ONB = OFF + 24 * RB;
+  if constexpr (!F8 && ND == 4) {
+    uint2 r[16];
     asm volatile(
-        "ds_read_b64_tr_b16 %0, %8 offset:%16\n\tds_read_b64_tr_b16 %1, %12 offset:%16\n\t"
-        "ds_read_b64_tr_b16 %2, %9 offset:%16\n\tds_read_b64_tr_b16 %3, %13 offset:%16\n\t"
-        "ds_read_b64_tr_b16 %4, %10 offset:%16\n\tds_read_b64_tr_b16 %5, %14 offset:%16\n\t"
-        "ds_read_b64_tr_b16 %6, %11 offset:%16\n\tds_read_b64_tr_b16 %7, %15 offset:%16\n\t"
+        "ds_read_b64_tr_b16 %0, %16 offset:%24\n\t"
+        "ds_read_b64_tr_b16 %1, %20 offset:%25\n\t"
+        "ds_read_b64_tr_b16 %2, %17 offset:%24\n\t"
+        "ds_read_b64_tr_b16 %3, %21 offset:%25\n\t"
+        "ds_read_b64_tr_b16 %4, %18 offset:%24\n\t"
+        "ds_read_b64_tr_b16 %5, %22 offset:%25\n\t"
+        "ds_read_b64_tr_b16 %6, %19 offset:%24\n\t"
+        "ds_read_b64_tr_b16 %7, %23 offset:%25\n\t"
+        "ds_read_b64_tr_b16 %8, %16 offset:%26\n\t"
+        "ds_read_b64_tr_b16 %9, %20 offset:%27\n\t"
+        "ds_read_b64_tr_b16 %10, %17 offset:%26\n\t"
+        "ds_read_b64_tr_b16 %11, %21 offset:%27\n\t"
+        "ds_read_b64_tr_b16 %12, %18 offset:%26\n\t"
+        "ds_read_b64_tr_b16 %13, %22 offset:%27\n\t"
+        "ds_read_b64_tr_b16 %14, %19 offset:%26\n\t"
+        "ds_read_b64_tr_b16 %15, %23 offset:%27\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]),
+          "=&v"(r[6]), "=&v"(r[7]), "=&v"(r[8]), "=&v"(r[9]), "=&v"(r[10]),
+          "=&v"(r[11]), "=&v"(r[12]), "=&v"(r[13]), "=&v"(r[14]), "=&v"(r[15])
+        : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]),
+          "n"(OFF), "n"(OB), "n"(ON), "n"(ONB)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      v[i / ND][i % ND] = u32x4{r[2 * i].x, r[2 * i].y, r[2 * i + 1].x, r[2 * i + 1].y};
+  } else if constexpr (!F8) {
+    uint2 r[8];
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %8 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %1, %10 offset:%13\n\t"
+        "ds_read_b64_tr_b16 %2, %9 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %3, %11 offset:%13\n\t"
+        "ds_read_b64_tr_b16 %4, %8 offset:%14\n\t"
+        "ds_read_b64_tr_b16 %5, %10 offset:%15\n\t"
+        "ds_read_b64_tr_b16 %6, %9 offset:%14\n\t"
+        "ds_read_b64_tr_b16 %7, %11 offset:%15\n\t"
         "s_waitcnt lgkmcnt(0)"
         : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]),
           "=&v"(r[6]), "=&v"(r[7])
-        : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]),
-          "n"(OFF)
+        : "v"(a[0]), "v"(a[1]), "v"(b[0]), "v"(b[1]),
+          "n"(OFF), "n"(OB), "n"(ON), "n"(ONB)
         : "memory");
-  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      v[i / ND][i % ND] = u32x4{r[2 * i].x, r[2 * i].y, r[2 * i + 1].x, r[2 * i + 1].y};
+  } else if constexpr (ND == 4) {
+    uint2 r[8];
     asm volatile(
-        "ds_read_b64_tr_b16 %0, %4 offset:%8\n\tds_read_b64_tr_b16 %1, %6 offset:%8\n\t"
-        "ds_read_b64_tr_b16 %2, %5 offset:%8\n\tds_read_b64_tr_b16 %3, %7 offset:%8\n\t"
+        "ds_read_b64_tr_b8 %0, %8 offset:%12\n\t"
+        "ds_read_b64_tr_b8 %1, %9 offset:%12\n\t"
+        "ds_read_b64_tr_b8 %2, %10 offset:%12\n\t"
+        "ds_read_b64_tr_b8 %3, %11 offset:%12\n\t"
+        "ds_read_b64_tr_b8 %4, %8 offset:%13\n\t"
+        "ds_read_b64_tr_b8 %5, %9 offset:%13\n\t"
+        "ds_read_b64_tr_b8 %6, %10 offset:%13\n\t"
+        "ds_read_b64_tr_b8 %7, %11 offset:%13\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]),
+          "=&v"(r[6]), "=&v"(r[7])
+        : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]),
+          "n"(OFF), "n"(ON)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i / ND][i % ND] = f8_bf16x8(r[i].x, r[i].y);
+  } else {
+    uint2 r[4];
+    asm volatile(
+        "ds_read_b64_tr_b8 %0, %4 offset:%6\n\t"
+        "ds_read_b64_tr_b8 %1, %5 offset:%6\n\t"
+        "ds_read_b64_tr_b8 %2, %4 offset:%7\n\t"
+        "ds_read_b64_tr_b8 %3, %5 offset:%7\n\t"
         "s_waitcnt lgkmcnt(0)"
         : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3])
-        : "v"(a[0]), "v"(a[1]), "v"(b[0]), "v"(b[1]), "n"(OFF)
+        : "v"(a[0]), "v"(a[1]),
+          "n"(OFF), "n"(ON)
         : "memory");
-  }
 #pragma unroll
-  for (int i = 0; i < ND; ++i) v[i] = u32x4{r[2 * i].x, r[2 * i].y, r[2 * i + 1].x, r[2 * i + 1].y};
-}
-// the same of 8-bit rows: one read brings both groups of four keys
-template <int ND, int OFF>
-__device__ __forceinline__ void lds_v8(const uint32_t* a, u32x4* v) {
-  uint2 r[ND];
-  if constexpr (ND == 4) {
-    asm volatile(
-        "ds_read_b64_tr_b8 %0, %4 offset:%8\n\tds_read_b64_tr_b8 %1, %5 offset:%8\n\t"
-        "ds_read_b64_tr_b8 %2, %6 offset:%8\n\tds_read_b64_tr_b8 %3, %7 offset:%8\n\t"
-        "s_waitcnt lgkmcnt(0)"
-        : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3])
-        : "v"(a[0]), "v"(a[1]), "v"(a[2]), "v"(a[3]), "n"(OFF)
-        : "memory");
-  } else {
-    asm volatile(
-        "ds_read_b64_tr_b8 %0, %2 offset:%4\n\tds_read_b64_tr_b8 %1, %3 offset:%4\n\t"
-        "s_waitcnt lgkmcnt(0)"
-        : "=&v"(r[0]), "=&v"(r[1])
-        : "v"(a[0]), "v"(a[1]), "n"(OFF)
-        : "memory");
+    for (int i = 0; i < 4; ++i) v[i / ND][i % ND] = f8_bf16x8(r[i].x, r[i].y);
   }
-#pragma unroll
-  for (int i = 0; i < ND; ++i) v[i] = f8_bf16x8(r[i].x, r[i].y);
 }
 
 // some 16-bit (8-bit) value of x is an infinity or NaN
@@ -410,6 +454,18 @@ __device__ __forceinline__ bool has_nonfinite(u32x4 x) {
     }
   }
   return any;
+}
+
+// ones over each bf16 of x that is an infinity or NaN
+__device__ __forceinline__ uint32_t nonfinite_mask(uint32_t x) {
+  return ((x & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u) |
+         ((x & 0x7f80u) == 0x7f80u ? 0xffffu : 0u);
+}
+
+// bf16 1 where the bf16 x is an infinity (c = 0), a negative one (1) or NaN (2)
+__device__ __forceinline__ uint32_t ones_of(int c, uint32_t x) {
+  const bool is = c == 0 ? x == 0x7f80u : (c == 1 ? x == 0xff80u : (x & 0x7fffu) > 0x7f80u);
+  return is ? 0x3f80u : 0u;
 }
 
 // A row's view of the keys: [lo, lo + n) and [floor, floor + s).
@@ -455,27 +511,20 @@ __global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
   int f = sh[0], e = sh[1], kvh = sh[2], j = sh[3];
   const int f1 = sh[4];
   if (f >= f1) return;                            // whole workgroup
-  // byte offsets of the lane's chunk in the loads of 16 rows
-  uint32_t lp[IPG];
-#pragma unroll
-  for (int i = 0; i < IPG; ++i) {
-    const int r = i * (kWave / CPR) + lane / CPR;
-    lp[i] = (uint32_t)(r * RB + 16 * ((lane % CPR) ^ SH::swz(r)));
-  }
-  // V reads: the lane's byte addresses within a stage for each block of 32 dims
-  uint32_t va[ND], vb[ND];
-#pragma unroll
-  for (int db = 0; db < ND; ++db) {
-    if constexpr (F8) {
-      const int jj = (lane & 15) >> 1, r = 4 * h + (jj & 3) + 8 * (jj >> 2);
-      va[db] = r * RB + 16 * ((2 * db + ((lane >> 4) & 1)) ^ SH::swz(r)) + 8 * (lane & 1);
-      vb[db] = 0;
-    } else {
-      const int r = 4 * h + ((lane & 15) >> 2);
-      const int c = 4 * db + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-      va[db] = r * RB + 16 * (c ^ SH::swz(r)) + 8 * (lane & 1);
-      vb[db] = (r + 8) * RB + 16 * (c ^ SH::swz(r + 8)) + 8 * (lane & 1);
-    }
+  // The lane's byte addresses within 16 rows being loaded, and within a stage's K
+  // and V: one register each.  The others follow by an exclusive or in the bits of
+  // the chunk, load i (1 KB each): 1024 i + (lp ^ kLoadX i); K's 16-byte chunk 2 ks +
+  // h: ka ^ 32 ks; block db of 32 dims of V: va ^ kVX db, its keys 8 further: ^ 32,
+  // 8 rows on.
+  constexpr int kLoadX = CPR == 16 ? 16 : 32, kVX = F8 ? 32 : 64;
+  uint32_t lp, ka, va;
+  {
+    const int r = lane / CPR;
+    lp = (uint32_t)(r * RB + 16 * ((lane % CPR) ^ SH::swz(r)));
+    ka = (uint32_t)(li * RB + 16 * (h ^ SH::swz(li)));
+    const int rv = F8 ? 4 * h + ((lane >> 1) & 3) + 8 * ((lane >> 3) & 1) : 4 * h + ((lane & 15) >> 2);
+    const int cv = F8 ? (lane >> 4) & 1 : 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    va = (uint32_t)(rv * RB + 16 * (cv ^ SH::swz(rv)) + 8 * (lane & 1));
   }
   const int P1 = (1 << d.logP) - 1;
   for (;;) {
@@ -483,8 +532,13 @@ __global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
   const int tok0 = en[0], row0 = en[1], nrows = en[2], seq = en[3], p0 = en[4], prefix = en[5];
   const int kfloor = en[6], kceil = en[7], ks_ = en[8], klo = en[9], khi = en[10], tiles = en[11];
   const int a0 = en[12], n1 = en[13], b0 = en[14];
-  const int nj = imin(tiles - j, f1 - f);         // tiles of this part (>= 1)
-  const bool whole = j == 0 && nj == tiles;
+  // the part's tiles [j, j + nj); its first kSegUnits units are none
+  const int left = f1 - f + imin(j, 0);           // units of the share from tile max(j, 0) on
+  f += tiles - j;                                 // the segment's end
+  j = imax(j, 0);
+  const int nj = imin(tiles - j, left);
+  if (nj <= 0) return;                            // whole workgroup: the share ends before a tile
+  const bool whole = nj == tiles;
   auto tile_key = [&](int t) { return kKvTile * (t < n1 ? a0 + t : b0 + t - n1); };
 
   // ---- the wave's query rows (B operand): row li of its 32 ----
@@ -553,13 +607,14 @@ __global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
       u32x4* dst = lds + slot * SH::kStage + (gi >= 4 ? SH::kHalf : 0) + rb * CPR;
       if (inner) {
 #pragma unroll
-        for (int i = 0; i < IPG; ++i) lds_dma16(base + lp[i], dst + 64 * i);
+        for (int i = 0; i < IPG; ++i) lds_dma16(base + 1024 * i + (lp ^ (kLoadX * i)), dst + 64 * i);
       } else {
 #pragma unroll
         for (int i = 0; i < IPG; ++i) {
           const int key = g0 + i * (kWave / CPR) + lane / CPR;
           const bool any = key >= kfloor && key < khi && (key >= klo || key < ks_);
-          lds_dma16(any ? base + lp[i] : d.w.zero + 16 * (lane & 15), dst + 64 * i);
+          lds_dma16(any ? base + 1024 * i + (lp ^ (kLoadX * i)) : d.w.zero + 16 * (lane & 15),
+                    dst + 64 * i);
         }
       }
     }
@@ -601,25 +656,44 @@ __global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
     // tiles that no row of the wave sees
     if (!live || k0 >= wend || (k0 + NK <= wbeg && k0 >= wsink)) continue;
     const bool full = k0 >= kfloor && k0 + NK <= whi && (k0 >= wlo || k0 + NK <= wsink);
+    // K operands are read in groups, the next group while one multiplies: left to
+    // itself the compiler reads one, waits for it and multiplies, 16 times a tile.
+    // (The opaque copies keep it from holding every address in a register.)
+    constexpr int NKL = F8 ? NKS / 2 : NKS;       // 16-byte reads of a key
+    constexpr int GK = NKL < 4 ? NKL : 4, NGK = KB * NKL / GK;
+    uint32_t kx = ka + lds_byte(Ks);
+    asm volatile("" : "+v"(kx));
+    u32x4 kf[2][GK];
+    auto k_read = [&](int g) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < GK; ++i)
+        kf[g & 1][i] = *(const lds_u32x4*)(uintptr_t)((kx ^ (32 * ((g * GK + i) % NKL))) +
+                                                      32 * RB * (g * GK / NKL));
+      __builtin_amdgcn_sched_barrier(0);
+    };
     floatx16 sc[KB];
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
-      const int kr = 32 * kb + li, sw = SH::swz(kr);
-      floatx16 acc;
+    for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) acc[i] = 0.f;
-      if constexpr (F8) {
+      for (int i = 0; i < 16; ++i) sc[kb][i] = 0.f;
+    k_read(0);
+    if constexpr (NGK > 1) k_read(1);
 #pragma unroll
-        for (int kp = 0; kp < NKS / 2; ++kp) {
-          const u32x4 x = Ks[kr * CPR + ((2 * kp + h) ^ sw)];
-          acc = mma32(f8_bf16x8(x.x, x.y), qf[2 * kp], acc);
-          acc = mma32(f8_bf16x8(x.z, x.w), qf[2 * kp + 1], acc);
+    for (int g = 0; g < NGK; ++g) {
+      const int kb = g * GK / NKL;
+#pragma unroll
+      for (int i = 0; i < GK; ++i) {
+        const u32x4 x = kf[g & 1][i];
+        const int ks = (g * GK + i) % NKL;
+        if constexpr (F8) {
+          sc[kb] = mma32(f8_bf16x8(x.x, x.y), qf[2 * ks], sc[kb]);
+          sc[kb] = mma32(f8_bf16x8(x.z, x.w), qf[2 * ks + 1], sc[kb]);
+        } else {
+          sc[kb] = mma32(x, qf[ks], sc[kb]);
         }
-      } else {
-#pragma unroll
-        for (int ks = 0; ks < NKS; ++ks) acc = mma32(Ks[kr * CPR + ((2 * ks + h) ^ sw)], qf[ks], acc);
       }
-      sc[kb] = acc;
+      __builtin_amdgcn_sched_barrier(0);
+      if (g + 2 < NGK) k_read(g + 2);
     }
     if (!full) {
 #pragma unroll
@@ -662,73 +736,66 @@ __global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
       for (int i = lane; i < NK * CPR; i += kWave) odd |= has_nonfinite<F8>(Vs[i]);
       odd = __ballot(odd) != 0;
     }
-    if (!odd) {
-      const uint32_t vs0 = lds_byte(Vs);
+    uint32_t vx = va + lds_byte(Vs);
+    asm volatile("" : "+v"(vx));
+    auto step = [&](auto u_) __attribute__((always_inline)) {
+      constexpr int u0 = decltype(u_)::value;     // steps u0, u0 + 1: one 32-key block
+      u32x4 v[2][ND], ph[2], pl[2];
       uint32_t xa[ND], xb[ND];
 #pragma unroll
       for (int db = 0; db < ND; ++db) {
-        xa[db] = va[db] + vs0;
-        xb[db] = vb[db] + vs0;
+        xa[db] = vx ^ (kVX * db);
+        xb[db] = xa[db] ^ 32;
       }
-      auto step = [&](auto u_) __attribute__((always_inline)) {
-        constexpr int u = decltype(u_)::value, kb = u / 2, i0 = 8 * (u % 2);
-        u32x4 v[ND], ph, pl;
+      lds_v<ND, F8, 16 * u0 * RB, RB>(xa, xb, v);
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float e0 = sc[kb][i0 + 2 * i], e1 = sc[kb][i0 + 2 * i + 1];
-          ph[i] = pk_bf16(e0, e1);
+          const float e0 = sc[u0 / 2][8 * u + 2 * i], e1 = sc[u0 / 2][8 * u + 2 * i + 1];
+          ph[u][i] = pk_bf16(e0, e1);
           if constexpr (PARTS == 2)
-            pl[i] = pk_bf16(e0 - __uint_as_float(ph[i] << 16),
-                            e1 - __uint_as_float(ph[i] & 0xFFFF0000u));
+            pl[u][i] = pk_bf16(e0 - __uint_as_float(ph[u][i] << 16),
+                               e1 - __uint_as_float(ph[u][i] & 0xFFFF0000u));
         }
-        if constexpr (F8) lds_v8<ND, 16 * u * RB>(xa, v);
-        else lds_v16<ND, 16 * u * RB>(xa, xb, v);
+      // Rows must not meet the infinities and NaN of keys that they do not see (0
+      // times one is no number): those values leave the operands, and the rows
+      // with a numerator for one get it from a product with ones in its places.
+      // Only tiles on the border of some row's view come here, and only if they
+      // hold such values.
+      if (__builtin_expect(odd, 0)) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int db = 0; db < ND; ++db) {
+#pragma unroll 1
+            for (int c = 0; c < 3; ++c) {         // inf, -inf, NaN
+              u32x4 one;
+#pragma unroll
+              for (int w = 0; w < 4; ++w)
+                one[w] = ones_of(c, v[u][db][w] & 0xffffu) | ones_of(c, v[u][db][w] >> 16) << 16;
+              floatx16 y;
+#pragma unroll
+              for (int i = 0; i < 16; ++i) y[i] = 0.f;
+              y = mma32(one, ph[u], y);
+              const float val = c == 0 ? INFINITY : (c == 1 ? -INFINITY : NAN);
+#pragma unroll
+              for (int i = 0; i < 16; ++i) o[db][i] += y[i] > 0.f ? val : 0.f;
+            }
+#pragma unroll
+            for (int w = 0; w < 4; ++w) v[u][db][w] &= ~nonfinite_mask(v[u][db][w]);
+          }
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int db = 0; db < ND; ++db) {
-          if constexpr (PARTS == 2) o[db] = mma32(v[db], pl, o[db]);
-          o[db] = mma32(v[db], ph, o[db]);
+          if constexpr (PARTS == 2) o[db] = mma32(v[u][db], pl[u], o[db]);
+          o[db] = mma32(v[u][db], ph[u], o[db]);
         }
-      };
-      step(std::integral_constant<int, 0>{});
-      step(std::integral_constant<int, 1>{});
-      if constexpr (KB == 2) {
-        step(std::integral_constant<int, 2>{});
-        step(std::integral_constant<int, 3>{});
-      }
-    } else {
-      // Rows must not meet the values of keys that they do not see (0 times an
-      // infinity is no number): key by key, each row its own.  Only tiles on the
-      // border of some row's view come here, and only if they hold such values.
-      const char* vbytes = reinterpret_cast<const char*>(Vs);
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
-#pragma unroll 1
-        for (int x = 0; x < 32; ++x) {
-          const int i = 4 * (x >> 3) + (x & 3), hh = (x >> 2) & 1, r = 32 * kb + x;
-          float ei = 0.f;
-#pragma unroll
-          for (int y = 0; y < 16; ++y) ei = y == i ? sc[kb][y] : ei;
-          const float pk = __shfl(ei, li + 32 * hh, kWave);
-          if (!sees(k0 + r)) continue;
-#pragma unroll
-          for (int db = 0; db < ND; ++db)
-#pragma unroll
-            for (int y = 0; y < 16; ++y) {
-              const int dim = 32 * db + 8 * (y / 4) + 4 * h + y % 4;
-              const int c = F8 ? dim >> 4 : dim >> 3;
-              const char* at = vbytes + r * RB + 16 * (c ^ SH::swz(r));
-              float v;
-              if constexpr (F8) {
-                const uint32_t b = *reinterpret_cast<const uint8_t*>(at + (dim & 15));
-                v = __builtin_amdgcn_cvt_f32_fp8(b, 0);
-              } else {
-                v = bf16_to_f32(*reinterpret_cast<const uint16_t*>(at + 2 * (dim & 7)));
-              }
-              o[db][y] = fmaf(pk, v, o[db][y]);
-            }
-        }
-      }
-    }
+    };
+    step(std::integral_constant<int, 0>{});
+    if constexpr (KB == 2) step(std::integral_constant<int, 2>{});
   }
   l_run = fsum_xor32(l_run);
   if constexpr (WK == 2) {
@@ -788,9 +855,8 @@ __global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
     }
   }
   // ---- on to the next segment of the share ----
-  f += nj;
   if (f >= f1) return;                            // whole workgroup
-  j = 0;
+  j = -kSegUnits;
   if (++kvh == d.nkv) {
     kvh = 0;
     ++e;
@@ -816,8 +882,8 @@ struct KvSum {
   }
 };
 
-// the parts of row rr of the segment of units [a, a + tiles), cut at multiples of
-// S: the first at the end of share a / S, the others at the beginning of theirs
+// the parts of row rr of the segment whose tiles are units [a, a + tiles), cut at
+// multiples of S: the first at the end of share a / S, the others at the beginning of theirs
 template <int HD>
 __device__ __forceinline__ void add_parts(const KvDev& d, int R, int a, int tiles, int S, int rr,
                                           int c, KvSum& x) {
@@ -859,8 +925,8 @@ __global__ __launch_bounds__(256) void k_kv_join(const KvDev d, int R) {
   const int s = blockIdx.x + 1;
   const scalar_i32 sh = as_scalar(d.w.share + s), hd = as_scalar(d.w.hdr);
   const int f = sh[0], e = sh[1], kvh = sh[2], j = sh[3], S = hd[1];
-  if (f >= hd[0] || j == 0) return;               // past the end, or nothing is cut here
-  const int a = f - j;
+  if (f >= hd[0] || j <= 0) return;               // past the end, or nothing is cut here
+  const int a = f - j;                            // the unit of the segment's first tile
   if (a < f - S) return;                          // cut before: an earlier workgroup's
   const scalar_i32 en = as_scalar(d.w.ent + e);
   const int tok0 = en[0], row0 = en[1], nrows = en[2], tiles = en[11];
@@ -890,7 +956,8 @@ __global__ __launch_bounds__(256) void k_kv_join_rows(const KvDev d, int R, int 
     const int lr = (tok - (k == 0 ? d.w.gtok[g] : d.w.stok[b])) * d.grp + hg;
     const int e = d.w.off[k == 0 ? n + g : b] + lr / R;
     if (e >= d.w.hdr[2]) continue;                // dropped: token ranges that overlap
-    const int tiles = d.w.ent[e].tiles, a = d.w.cum[e] + kvh * tiles;
+    const int tiles = d.w.ent[e].tiles;
+    const int a = d.w.cum[e] + kvh * (tiles + kSegUnits) + kSegUnits;
     if (a / S == (a + tiles - 1) / S) {
       const int64_t prow = d.row0 + ((int64_t)(1 - k) * d.total_q + tok) * d.nh + head;
       const float2 ml = *reinterpret_cast<const float2*>(d.w.ml + 2 * prow);

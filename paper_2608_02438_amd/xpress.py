@@ -415,8 +415,8 @@ class Layer:
         L = load_library()
         batch, B, H = x.shape
         c = kv._cache(k_cache, v_cache, k_scale, v_scale)
-        kv._table(table, batch)
-        kv._flat("ctx_len", ctx_len, torch.int32, batch)
+        tb = kv._table(table, batch)
+        ctx = kv._flat("ctx_len", ctx_len, torch.int32, batch)
         if h_f32 is None:
             h_f32 = torch.empty((batch, B, H), dtype=torch.float32, device=x.device)
         if h_bf16 is None:
@@ -425,9 +425,8 @@ class Layer:
             assert t.is_contiguous() and t.device == kv.device
         with torch.cuda.device(kv.device):
             st = L.xp_layer_forward_paged(self._h, kv._h, batch, B, 1 if causal else 0, window,
-                                          sinks, _ptr(x), *c, _ptr(table), table.shape[1],
-                                          _ptr(ctx_len), _ptr(h_f32), _ptr(h_bf16),
-                                          _stream(stream))
+                                          sinks, _ptr(x), *c, *tb, ctx, _ptr(h_f32),
+                                          _ptr(h_bf16), _stream(stream))
         if st != XP_OK:
             raise XpError(st, "xp_layer_forward_paged: " + L.xp_layer_last_error(self._h).decode())
         return h_f32, h_bf16
@@ -464,7 +463,8 @@ class PagedKV:
             self.device = torch.device("cuda", torch.cuda.current_device())
         self.n_heads, self.n_kv, self.head_dim, self.page_size = n_heads, n_kv, head_dim, page_size
         self.n_pages = n_pages
-        self.cache_shape = (n_pages, n_kv, page_size, head_dim)
+        self.cache_shape = torch.Size((n_pages, n_kv, page_size, head_dim))
+        self._torch, self._index = torch, self.device.index
         st = _KvShape(n_heads=n_heads, n_kv=n_kv, head_dim=head_dim, page_size=page_size,
                       n_pages=n_pages, dtype=dt)
         h = ctypes.c_void_p(0)
@@ -478,88 +478,90 @@ class PagedKV:
 
     # ------------------------------------------------------------------
     def _call(self, name, *args, stream=None):
-        import torch
-        with torch.cuda.device(self.device):
+        torch = self._torch
+        if torch.cuda.current_device() == self._index:
             s = getattr(self._L, name)(self._h, *args, _stream(stream))
+        else:
+            with torch.cuda.device(self._index):
+                s = getattr(self._L, name)(self._h, *args, _stream(stream))
         if s != XP_OK:
             raise XpError(s, f"{name}: " + self._L.xp_kv_last_error(self._h).decode())
 
     def _flat(self, name, t, dtype, n, optional=False):
-        """A contiguous device vector of n (None: any number of) elements."""
+        """The address of a contiguous device vector of n (None: any number of)
+        elements, None for an optional one that is not given."""
         if t is None and optional:
             return None
-        if (t is None or t.dtype != dtype or not t.is_contiguous() or t.device != self.device
-                or t.dim() != 1 or (n is not None and t.numel() != n)):
+        if (t is None or t.dtype != dtype or t.dim() != 1 or not t.is_contiguous()
+                or t.get_device() != self._index or (n is not None and t.shape[0] != n)):
             raise ValueError(f"{name}: expected a contiguous {dtype} tensor of "
                              f"{'any number of' if n is None else n} elements on {self.device}")
-        return t
+        return t.data_ptr()
 
     def _rows(self, name, t, heads, tokens=None):
-        """Token rows [tokens][heads][head_dim] of bf16, each contiguous."""
-        import torch
-        if (t.dtype != torch.bfloat16 or t.dim() != 3 or t.device != self.device
-                or tuple(t.shape[1:]) != (heads, self.head_dim)
-                or (tokens is not None and t.shape[0] != tokens)
-                or t.stride(2) != 1 or (heads > 1 and t.stride(1) != self.head_dim)):
+        """The token rows' distance of [tokens][heads][head_dim] bf16, heads contiguous."""
+        shape, hd = t.shape, self.head_dim
+        if (t.dtype != self._torch.bfloat16 or len(shape) != 3 or shape[1] != heads
+                or shape[2] != hd or (tokens is not None and shape[0] != tokens)
+                or t.get_device() != self._index):
             raise ValueError(f"{name}: expected bf16 [{'tokens' if tokens is None else tokens}]"
-                             f"[{heads}][{self.head_dim}] rows on {self.device}")
+                             f"[{heads}][{hd}] rows on {self.device}")
+        if t.is_contiguous():
+            return heads * hd
+        if t.stride(2) != 1 or (heads > 1 and t.stride(1) != hd):
+            raise ValueError(f"{name}: expected contiguous [{heads}][{hd}] rows")
         # the row distance of a single row is free
-        return t.stride(0) if t.shape[0] > 1 else heads * self.head_dim
+        return t.stride(0) if shape[0] > 1 else heads * hd
 
     def _cache(self, k_cache, v_cache, k_scale, v_scale):
-        import torch
-        for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
-            if (t.dtype != self.cache_dtype or tuple(t.shape) != self.cache_shape
-                    or not t.is_contiguous() or t.device != self.device):
-                raise ValueError(f"{name}: expected a contiguous {self.cache_dtype} tensor "
-                                 f"{self.cache_shape} on {self.device}")
-        self._flat("k_scale", k_scale, torch.float32, self.n_kv, optional=True)
-        self._flat("v_scale", v_scale, torch.float32, self.n_kv, optional=True)
-        return _ptr(k_cache), _ptr(v_cache), _ptr(k_scale), _ptr(v_scale)
+        for t in (k_cache, v_cache):
+            if (t.dtype != self.cache_dtype or t.shape != self.cache_shape
+                    or not t.is_contiguous() or t.get_device() != self._index):
+                raise ValueError(f"k_cache, v_cache: expected contiguous {self.cache_dtype} "
+                                 f"tensors {tuple(self.cache_shape)} on {self.device}")
+        f32 = self._torch.float32
+        return (k_cache.data_ptr(), v_cache.data_ptr(),
+                self._flat("k_scale", k_scale, f32, self.n_kv, optional=True),
+                self._flat("v_scale", v_scale, f32, self.n_kv, optional=True))
 
     def _table(self, table, n):
-        import torch
-        if (table.dtype != torch.int32 or table.dim() != 2 or table.shape[0] != n
-                or table.shape[1] < 1 or not table.is_contiguous() or table.device != self.device):
+        if (table.dtype != self._torch.int32 or table.dim() != 2 or table.shape[0] != n
+                or table.shape[1] < 1 or not table.is_contiguous()
+                or table.get_device() != self._index):
             raise ValueError(f"table: expected a contiguous int32 [{n}][pages] tensor on "
                              f"{self.device}")
+        return table.data_ptr(), table.shape[1]
 
     def map(self, lens, add, table, held, pool, pool_n, cu=None, kv_len=None, slots=None,
             stream=None):
         """Pages and slots from lengths (xp_kv_map): table, held, pool and pool_n
         are updated, and cu, kv_len and slots written where given."""
-        import torch
-        i32 = torch.int32
-        n = lens.numel()
-        self._table(table, n)
-        for name, t, m, opt in (("lens", lens, n, False), ("add", add, n, False),
-                                ("held", held, n, False), ("pool", pool, self.n_pages, False),
-                                ("pool_n", pool_n, 1, False), ("cu", cu, n + 1, True),
-                                ("kv_len", kv_len, n, True), ("slots", slots, None, True)):
-            self._flat(name, t, i32, m, optional=opt)
-        self._call("xp_kv_map", n, _ptr(lens), _ptr(add), _ptr(table), table.shape[1],
-                   _ptr(held), _ptr(pool), _ptr(pool_n), _ptr(cu), _ptr(kv_len), _ptr(slots),
-                   0 if slots is None else slots.numel(), stream=stream)
+        i32, flat = self._torch.int32, self._flat
+        n = lens.shape[0]
+        self._call("xp_kv_map", n, flat("lens", lens, i32, n), flat("add", add, i32, n),
+                   *self._table(table, n), flat("held", held, i32, n),
+                   flat("pool", pool, i32, self.n_pages), flat("pool_n", pool_n, i32, 1),
+                   flat("cu", cu, i32, n + 1, True), flat("kv_len", kv_len, i32, n, True),
+                   flat("slots", slots, i32, None, True), 0 if slots is None else slots.shape[0],
+                   stream=stream)
         return cu, kv_len, slots
 
     def write(self, k, v, slots, k_cache, v_cache, k_scale=None, v_scale=None, stream=None):
         """K and V rows [tokens][n_kv][head_dim] to their slots (xp_kv_write)."""
-        import torch
         n = k.shape[0]
         k_ld, v_ld = self._rows("k", k, self.n_kv), self._rows("v", v, self.n_kv, n)
-        self._flat("slots", slots, torch.int32, n)
+        sl = self._flat("slots", slots, self._torch.int32, n)
         c = self._cache(k_cache, v_cache, k_scale, v_scale)
         if n:
-            self._call("xp_kv_write", n, _ptr(k), k_ld, _ptr(v), v_ld, _ptr(slots), *c,
+            self._call("xp_kv_write", n, k.data_ptr(), k_ld, v.data_ptr(), v_ld, sl, *c,
                        stream=stream)
 
     def _attend(self, name, groups, q, k_cache, v_cache, table, kv_len, cu_q, max_q, causal,
                 window, sinks, scale, k_scale, v_scale, out, lse, stream):
-        import torch
-        n, tokens = kv_len.numel(), q.shape[0]
-        self._flat("kv_len", kv_len, torch.int32, n)
-        self._flat("cu_q", cu_q, torch.int32, n + 1, optional=True)
-        self._table(table, n)
+        torch = self._torch
+        n, tokens = kv_len.shape[0], q.shape[0]
+        lens = self._flat("kv_len", kv_len, torch.int32, n)
+        cu = self._flat("cu_q", cu_q, torch.int32, n + 1, optional=True)
         if max_q is None:
             if cu_q is not None:
                 raise ValueError("max_q is required with cu_q")
@@ -571,14 +573,14 @@ class PagedKV:
         out_ld = self._rows("out", out, self.n_heads, tokens)
         if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous()
                                 or tuple(lse.shape) != (tokens, self.n_heads)
-                                or lse.device != self.device):
+                                or lse.get_device() != self._index):
             raise ValueError(f"lse: expected contiguous float32 [{tokens}][{self.n_heads}]")
+        tb = self._table(table, n)
         c = self._cache(k_cache, v_cache, k_scale, v_scale)
         if n and tokens:
-            self._call(name, n, tokens, max_q, *groups, _ptr(q), q_ld, _ptr(cu_q), _ptr(kv_len),
-                       _ptr(table), table.shape[1], *c, 1 if causal else 0, window, sinks,
-                       0.0 if scale is None else scale, _ptr(out), out_ld, _ptr(lse),
-                       stream=stream)
+            self._call(name, n, tokens, max_q, *groups, q.data_ptr(), q_ld, cu, lens, *tb, *c,
+                       1 if causal else 0, window, sinks, 0.0 if scale is None else scale,
+                       out.data_ptr(), out_ld, _ptr(lse), stream=stream)
         return out
 
     def attend(self, q, k_cache, v_cache, table, kv_len, cu_q=None, max_q=None, causal=True,
@@ -595,11 +597,10 @@ class PagedKV:
                       v_scale=None, out=None, lse=None, stream=None):
         """attend() for groups of neighbouring requests whose first shared_len keys
         are the same pages, read once per group (xp_kv_attn_shared)."""
-        import torch
-        groups = shared_len.numel()
-        self._flat("shared_len", shared_len, torch.int32, groups)
-        self._flat("group_start", group_start, torch.int32, groups + 1)
-        return self._attend("xp_kv_attn_shared", (groups, _ptr(group_start), _ptr(shared_len)), q,
+        i32, groups = self._torch.int32, shared_len.shape[0]
+        return self._attend("xp_kv_attn_shared",
+                            (groups, self._flat("group_start", group_start, i32, groups + 1),
+                             self._flat("shared_len", shared_len, i32, groups)), q,
                             k_cache, v_cache, table, kv_len, cu_q, max_q, causal, window, sinks,
                             scale, k_scale, v_scale, out, lse, stream)
 
