@@ -55,6 +55,7 @@ struct KvAttnWs {
   int32_t* stok = nullptr;           // [batch] first token of each sequence
   int32_t* sgrp = nullptr;           // [batch] its group, or -1
   int32_t* gtok = nullptr;           // [groups] first token of each group
+  char* dump = nullptr;              // a row of 128 floats that takes what no one reads
   const char* zero = nullptr;        // 256 bytes of zeros: a key row that no one sees
 };
 

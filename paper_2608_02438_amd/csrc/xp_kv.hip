@@ -451,6 +451,7 @@ extern "C" xp_status xp_kv_create(const xp_kv_shape* s, int32_t max_batch, int32
       {(void**)&kv->take, (nb + 1) * 4},
       {(void**)&kv->old, nb * 4},
       {(void**)&acu, (nb + 1) * 4},
+      {(void**)&kv->a.dump, 512},
       {(void**)&kv->a.hdr, 256},
       {(void**)&kv->a.share, ((size_t)shares + 1) * sizeof(KvShare)},
       {(void**)&kv->a.ent, (size_t)kv->entries * sizeof(KvEntry)},

@@ -450,7 +450,7 @@ __device__ __forceinline__ bool has_nonfinite(u32x4 x) {
       const uint32_t y = ~x[i] & 0x7f7f7f7fu;     // 0 where all seven bits are ones
       any |= ((y - 0x01010101u) & ~y & 0x80808080u) != 0u;
     } else {
-      any |= (x[i] & 0x7f800000u) == 0x7f800000u || (x[i] & 0x7f80u) == 0x7f80u;
+      any |= ((x[i] & 0x7f800000u) == 0x7f800000u) | ((x[i] & 0x7f80u) == 0x7f80u);
     }
   }
   return any;
@@ -472,33 +472,35 @@ __device__ __forceinline__ uint32_t ones_of(int c, uint32_t x) {
 struct KvSees {
   int lo, floor;
   uint32_t n, s;
-  __device__ __forceinline__ bool operator()(int key) const {
-    return ((uint32_t)(key - lo) < n) | ((uint32_t)(key - floor) < s);
-  }
 };
 
-// WR x WK waves: wave (wr, wk) takes rows 32 wr .. + 31 of the tile and the
-// wk-th part of each tile's keys.  S^T = K Q^T and O^T = V^T P^T on
-// v_mfma_f32_32x32x16_bf16: a lane holds one query row (l % 32) in both, so the
-// softmax's statistics are the lane's own but for one exchange with lane l ^ 32,
-// and the numerators go from the accumulators of S straight into the B operand
+// WR x WK waves: wave (wr, wk) takes rows 32 wr .. + 31 of the tile and the wk-th
+// part of each tile's keys, in blocks of 32.  S^T = K Q^T and O^T =
+// V^T P^T on v_mfma_f32_32x32x16_bf16: a lane holds one query row (l % 32) in both,
+// so the softmax's statistics are the lane's own but for one exchange with lane l ^
+// 32, and the numerators go from the accumulators of S straight into the B operand
 // (its k order is that of the keys 16 t + 4 (l / 32) + 0..3 and + 8, which the
 // transposing reads of V follow).  Scores are kept in base 2.  A row's reference
-// maximum moves only when a score exceeds it by more than 2^8, so most tiles
-// rescale nothing.  Numerators enter P V as PARTS bf16 parts: two (16
-// significant bits) where the call is bound by memory.
+// maximum moves only when a score exceeds it by more than 2^8, so most blocks
+// rescale nothing.  Numerators enter P V as PARTS bf16 parts: two (16 significant
+// bits) where the call is bound by memory.
 // Tiles wait in an LDS ring of NST stages filled by global_load_lds; the keys
 // that no row of the tile sees are loaded as zeros, whatever lies there.
+// Matrix pipe and vector pipe work side by side only if one wave's instructions
+// alternate (two waves of a SIMD run in step, held by the tiles' barriers), and a
+// product that follows the one it adds to waits for it.  So block n's numerators
+// are formed between the products of block n + 1's scores and of block n - 1's P V,
+// in turn.
 template <int HD, bool F8, int WR, int WK, int NST, int PARTS>
 __global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
   using SH = KvRows<HD, F8>;
-  constexpr int NW = WR * WK, R = 32 * WR, KB = 2 / WK, ND = HD / 32, NKS = HD / 16;
+  constexpr int NW = WR * WK, R = 32 * WR, NB = 2 / WK, ND = HD / 32, NKS = HD / 16;
   constexpr int RB = SH::RB, CPR = SH::CPR, IPG = SH::IPG;
   constexpr int NG = 8 / NW;                      // groups of 16 rows that a wave loads
-  static_assert(NG * NW == 8 && KB * WK == 2, "waves");
+  static_assert(NG * NW == 8 && NB * WK == 2, "waves");
   constexpr int PER = NG * IPG;                   // loads of a wave for a stage
-  static_assert((NST - 2) * PER < 64, "vmcnt field");
-  constexpr int kMerge = (HD / 2 + 2) * kWave;    // floats a wave hands over
+  static_assert((NST - 1) * PER < 64, "vmcnt field");
+  constexpr int kMerge = (HD / 2 + 2) * kWave;    // floats that a wave hands over
   static_assert(WK == 1 || WR * kMerge * 4 <= NST * SH::kStage * 16, "merge in LDS");
   __shared__ __align__(256) u32x4 lds[NST * SH::kStage];
   const int lane = threadIdx.x & 63;
@@ -542,43 +544,37 @@ __global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
   auto tile_key = [&](int t) { return kKvTile * (t < n1 ? a0 + t : b0 + t - n1); };
 
   // ---- the wave's query rows (B operand): row li of its 32 ----
-  const int rr = 32 * wr + li;
   const bool live = 32 * wr < nrows;              // wave-uniform
+  const int rr = 32 * wr + li;
   const bool rv = rr < nrows;
-  const int row = row0 + (rv ? rr : 0);
-  const int tk = row / d.grp, head = kvh * d.grp + (row - tk * d.grp);
-  const int64_t tok = tok0 + tk;
   u32x4 qf[NKS];
+  KvSees sees;
+  int pmin, pmax;
   {
-    const uint16_t* qs = d.q + tok * d.q_ld + (int64_t)head * HD;
+    const int row = row0 + (rv ? rr : 0), tk = row / d.grp;
+    const int64_t tok = tok0 + tk;
+    const uint16_t* qs = d.q + tok * d.q_ld + (int64_t)(kvh * d.grp + (row - tk * d.grp)) * HD;
 #pragma unroll
-    for (int ks = 0; ks < NKS; ++ks) {
-      const int dim = F8 ? 32 * (ks >> 1) + 16 * h + 8 * (ks & 1) : 16 * ks + 8 * h;
-      qf[ks] = ld16(qs + dim);
-    }
+    for (int ks = 0; ks < NKS; ++ks)
+      qf[ks] = ld16(qs + (F8 ? 32 * (ks >> 1) + 16 * h + 8 * (ks & 1) : 16 * ks + 8 * h));
+    const int p = prefix ? d.w.pos[tok] : p0 + tk;
+    const int hi = rv ? (d.causal ? imin(p + 1, kceil) : kceil) : kfloor;
+    const int lo = d.window > 0 ? imax(p - d.window + 1, kfloor) : kfloor;
+    sees = KvSees{lo, kfloor, (uint32_t)imax(hi - lo, 0),
+                  d.window > 0 ? (uint32_t)imax(imin(d.sinks, hi) - kfloor, 0) : 0u};
+    pmin = rv ? p : 0x7fffffff;
+    pmax = rv ? p : -0x7fffffff;
   }
-  const int p = prefix ? d.w.pos[tok] : p0 + tk;
-  const int hi = rv ? (d.causal ? imin(p + 1, kceil) : kceil) : kfloor;
-  const int lo = d.window > 0 ? imax(p - d.window + 1, kfloor) : kfloor;
-  const KvSees sees{lo, kfloor, (uint32_t)imax(hi - lo, 0),
-                    d.window > 0 ? (uint32_t)imax(imin(d.sinks, hi) - kfloor, 0) : 0u};
-  // keys that every row of the wave sees: [wlo, whi), and [kfloor, wsink); and
-  // beyond wend, or between the sinks and wbeg, none sees any
-  int whi, wend, wlo, wbeg;
-  {
-    int pmin = rv ? p : 0x7fffffff, pmax = rv ? p : -0x7fffffff;
+  // keys that every row of the wave sees: [kfloor or wlo, whi), and [kfloor, wsink)
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      pmin = imin(pmin, __shfl_xor(pmin, o, kWave));
-      pmax = imax(pmax, __shfl_xor(pmax, o, kWave));
-    }
-    pmin = __builtin_amdgcn_readfirstlane(pmin);
-    pmax = __builtin_amdgcn_readfirstlane(pmax);
-    whi = d.causal ? imin(pmin < 0x7fffffff ? pmin + 1 : pmin, kceil) : kceil;
-    wend = d.causal ? imin(pmax + 1, kceil) : kceil;
-    wlo = d.window > 0 ? imax(pmax - d.window + 1, kfloor) : kfloor;
-    wbeg = d.window > 0 ? imax(pmin - d.window + 1, kfloor) : kfloor;
+  for (int o = 32; o > 0; o >>= 1) {
+    pmin = imin(pmin, __shfl_xor(pmin, o, kWave));
+    pmax = imax(pmax, __shfl_xor(pmax, o, kWave));
   }
+  pmin = __builtin_amdgcn_readfirstlane(pmin);
+  pmax = __builtin_amdgcn_readfirstlane(pmax);
+  const int whi = d.causal ? imin(pmin < 0x7fffffff ? pmin + 1 : pmin, kceil) : kceil;
+  const int wlo = d.window > 0 ? imax(pmax - d.window + 1, kfloor) : kfloor;
   const int wsink = d.window > 0 ? d.sinks : 0;
   const float scale2 = d.scale2 * (F8 && d.k_scale != nullptr ? d.k_scale[kvh] : 1.f);
 
@@ -599,7 +595,7 @@ __global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
       int page = pg[g];
       if ((uint32_t)page >= (uint32_t)d.n_pages) {
         const int from = imax(g0, kfloor), to = imin(g0 + 16, khi);
-        if (from < to && (to > klo || from < ks_) && lane == 0) atomicOr(d.err, XP_DEVERR_PAGE);
+        if (from < to && (to > klo || from < ks_)) atomicOr(d.err, XP_DEVERR_PAGE);
         page = 0;
       }
       const char* base = (gi >= 4 ? d.vc : d.kc) +
@@ -619,10 +615,19 @@ __global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
       }
     }
   };
+  // The scores of a block of keys are formed while the block before it goes through
+  // its softmax, so K is needed a block ahead of V.  With one block a tile (WK = 2)
+  // K of tile t is done with when iteration t begins, and the waves that load K run
+  // one tile ahead: before it they have brought tiles up to t + NST - 1, else, as the
+  // waves that load V, up to t + NST - 2.  Tile i lies in stage i % NST.
+  const int is_k = wave < NW / 2 ? 1 : 0, ahead = NB == 1 ? is_k : 0;
+  // loads still under way when iteration t has what it needs: K of tile t + 1, V of t
+  constexpr int kWaitV = (NST - 2) * PER, kWaitK = (NB == 1 ? NST - 2 : NST - 3) * PER;
+  static_assert(kWaitK >= 0, "stages");
   pages(j);
 #pragma unroll
-  for (int t = 0; t < NST - 1; ++t)
-    if (t < nj) {                                 // whole workgroup
+  for (int t = 0; t < NST; ++t)
+    if (t < nj && t < NST - 1 + ahead) {          // whole wave
       issue(j + t, t);
       pages(j + imin(t + 1, nj - 1));
     }
@@ -634,168 +639,247 @@ __global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
 
-  int slot = 0;
-#pragma unroll 1
-  for (int t = 0; t < nj; ++t) {
-    // tile t landed (every wave's loads), and every wave is done with t - 1,
-    // whose slot takes tile t + NST - 1
-    asm volatile("" ::: "memory");
-    if (t + NST - 2 < nj) __builtin_amdgcn_s_waitcnt(0x0070 | (((NST - 2) * PER) & 15) | ((((NST - 2) * PER) >> 4) << 14));
-    else __builtin_amdgcn_s_waitcnt(0x0070);
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    if (t + NST - 1 < nj) {
-      issue(j + t + NST - 1, slot == 0 ? NST - 1 : slot - 1);
-      pages(j + imin(t + NST, nj - 1));
-    }
-    const u32x4* Ks = lds + slot * SH::kStage + 32 * wk * CPR;
-    const u32x4* Vs = Ks + SH::kHalf;
-    slot = slot + 1 == NST ? 0 : slot + 1;
-    const int k0 = tile_key(j + t) + 32 * wk;
-    constexpr int NK = 32 * KB;                   // the wave's keys of the tile
-    // tiles that no row of the wave sees
-    if (!live || k0 >= wend || (k0 + NK <= wbeg && k0 >= wsink)) continue;
-    const bool full = k0 >= kfloor && k0 + NK <= whi && (k0 >= wlo || k0 + NK <= wsink);
-    // K operands are read in groups, the next group while one multiplies: left to
-    // itself the compiler reads one, waits for it and multiplies, 16 times a tile.
-    // (The opaque copies keep it from holding every address in a register.)
-    constexpr int NKL = F8 ? NKS / 2 : NKS;       // 16-byte reads of a key
-    constexpr int GK = NKL < 4 ? NKL : 4, NGK = KB * NKL / GK;
-    uint32_t kx = ka + lds_byte(Ks);
-    asm volatile("" : "+v"(kx));
-    u32x4 kf[2][GK];
-    auto k_read = [&](int g) __attribute__((always_inline)) {
+  // every row of the wave sees every key of the block that begins at k0
+  auto all_seen = [&](int k0) {
+    return k0 >= kfloor && k0 + 32 <= whi && (k0 >= wlo || k0 + 32 <= wsink);
+  };
+  // K operands of the block at row r of a stage
+  u32x4 kf[NKS];
+  auto k_read = [&](int stage, int r) __attribute__((always_inline)) {
+    uint32_t kx = ka + lds_byte(lds + stage * SH::kStage + r * CPR);
+    asm volatile("" : "+v"(kx));                  // opaque: no address is kept for the next block
 #pragma unroll
-      for (int i = 0; i < GK; ++i)
-        kf[g & 1][i] = *(const lds_u32x4*)(uintptr_t)((kx ^ (32 * ((g * GK + i) % NKL))) +
-                                                      32 * RB * (g * GK / NKL));
-      __builtin_amdgcn_sched_barrier(0);
-    };
-    floatx16 sc[KB];
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) sc[kb][i] = 0.f;
-    k_read(0);
-    if constexpr (NGK > 1) k_read(1);
-#pragma unroll
-    for (int g = 0; g < NGK; ++g) {
-      const int kb = g * GK / NKL;
-#pragma unroll
-      for (int i = 0; i < GK; ++i) {
-        const u32x4 x = kf[g & 1][i];
-        const int ks = (g * GK + i) % NKL;
-        if constexpr (F8) {
-          sc[kb] = mma32(f8_bf16x8(x.x, x.y), qf[2 * ks], sc[kb]);
-          sc[kb] = mma32(f8_bf16x8(x.z, x.w), qf[2 * ks + 1], sc[kb]);
-        } else {
-          sc[kb] = mma32(x, qf[ks], sc[kb]);
-        }
+    for (int i = 0; i < (F8 ? NKS / 2 : NKS); ++i)
+      kf[F8 ? 2 * i : i] = *(const lds_u32x4*)(uintptr_t)(kx ^ (32 * i));
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto k_operand = [&](int i) {                   // in order: an even i leaves i + 1 behind
+    if constexpr (F8) {
+      if (i % 2 == 0) {
+        const u32x4 x = kf[i];
+        kf[i + 1] = f8_bf16x8(x.z, x.w);
+        return f8_bf16x8(x.x, x.y);
       }
-      __builtin_amdgcn_sched_barrier(0);
-      if (g + 2 < NGK) k_read(g + 2);
     }
-    if (!full) {
+    return kf[i];
+  };
+  // V operands of a block, and the numerators (as bf16 parts) of this one and the next
+  u32x4 v[2][ND], ph[2][2], pl[2][2];
+  auto v_read = [&](int stage, int r) __attribute__((always_inline)) {
+    uint32_t vx = va + lds_byte(lds + stage * SH::kStage + SH::kHalf + r * CPR);
+    asm volatile("" : "+v"(vx));
+    uint32_t xa[ND], xb[ND];
 #pragma unroll
-      for (int kb = 0; kb < KB; ++kb)
+    for (int db = 0; db < ND; ++db) {
+      xa[db] = vx ^ (kVX * db);
+      xb[db] = xa[db] ^ 32;
+    }
+    lds_v<ND, F8, 0, RB>(xa, xb, v);
+  };
+  auto v_product = [&](int x, const u32x4 (&a)[2], const u32x4 (&b)[2])
+      __attribute__((always_inline)) {
+    const int u = x / ND, db = x % ND;
+    if constexpr (PARTS == 2) o[db] = mma32(v[u][db], b[u], o[db]);
+    o[db] = mma32(v[u][db], a[u], o[db]);
+  };
+  // infinities or NaN among the block's V
+  auto odd_values = [&](int stage, int r) __attribute__((always_inline)) {
+    const u32x4* Vs = lds + stage * SH::kStage + SH::kHalf + r * CPR;
+    bool odd = false;
+#pragma unroll 1
+    for (int i = 0; i < 32 * CPR / kWave; ++i) odd |= has_nonfinite<F8>(Vs[kWave * i + lane]);
+    return __ballot(odd) != 0;
+  };
+  // Rows must not meet the infinities and NaN of keys that they do not see (0 times
+  // one is no number): those values leave the operands, and the rows with a
+  // numerator for one get it from a product with ones in its places.  Only blocks on
+  // the border of some row's view come here, and only if they hold such values.
+  auto take_odd = [&](const u32x4 (&a)[2]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          sc[kb][i] = sees(k0 + 32 * kb + 8 * (i / 4) + 4 * h + i % 4) ? sc[kb][i] : -INFINITY;
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int db = 0; db < ND; ++db) {
+#pragma unroll 1
+        for (int c = 0; c < 3; ++c) {             // inf, -inf, NaN
+          u32x4 one;
+#pragma unroll
+          for (int w = 0; w < 4; ++w)
+            one[w] = ones_of(c, v[u][db][w] & 0xffffu) | ones_of(c, v[u][db][w] >> 16) << 16;
+          const float val = c == 0 ? INFINITY : (c == 1 ? -INFINITY : NAN);
+          floatx16 y;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) y[i] = 0.f;
+          y = mma32(one, a[u], y);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[db][i] += y[i] > 0.f ? val : 0.f;
+        }
+#pragma unroll
+        for (int w = 0; w < 4; ++w) v[u][db][w] &= ~nonfinite_mask(v[u][db][w]);
+      }
+  };
+  constexpr int EP = 16 / NKS;                    // numerators beside a product of S
+  // a pair of them, and l, which sums them in fp32
+  auto pack = [&](const floatx16& s, int x, u32x4 (&a)[2], u32x4 (&b)[2])
+      __attribute__((always_inline)) {
+    const int u = x / 8, i = x % 8 / 2;
+    const float e0 = s[x], e1 = s[x + 1];
+    l_run += e0;
+    l_run += e1;
+    uint32_t y = pk_bf16(e0, e1);
+    asm volatile("" : "+v"(y), "+v"(l_run));      // here, not where it is used
+    a[u][i] = y;
+    if constexpr (PARTS == 2) {
+      y = pk_bf16(e0 - __uint_as_float(y << 16), e1 - __uint_as_float(y & 0xFFFF0000u));
+      asm volatile("" : "+v"(y));
+      b[u][i] = y;
+    }
+  };
+  // Block n at row r of a stage (first key k0, scores in s), numerators to set PAR;
+  // nx takes the scores of block n + 1 (at row rn of stage sn; where there is none,
+  // of whatever lies there).
+  auto block = [&](auto par, int k0, int stage, int r, floatx16& s, int sn, int rn, floatx16& nx)
+      __attribute__((always_inline)) {
+    constexpr int PAR = decltype(par)::value;
+    k_read(sn, rn);
+    bool odd = false;
+    if (!all_seen(k0)) {
+      uint32_t a = (uint32_t)(k0 + 4 * h - sees.lo), b = (uint32_t)(k0 + 4 * h - sees.floor);
+      asm volatile("" : "+v"(a), "+v"(b));        // opaque: no key is kept in a register
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const uint32_t c = 8 * (i / 4) + i % 4;
+        s[i] = (a + c < sees.n) | (b + c < sees.s) ? s[i] : -INFINITY;
+      }
+      odd = odd_values(stage, r);
     }
     constexpr float kLazy = 8.f;
-    float mt = -INFINITY;
+    float mt = s[0];
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) mt = fmaxf(mt, sc[kb][i]);
+    for (int i = 1; i < 16; ++i) mt = fmaxf(mt, s[i]);
     mt = fmax_xor32(mt) * scale2;
-    if (__ballot(mt > m_run + kLazy) != 0) {      // wave-uniform
+    const bool grow = __ballot(mt > m_run + kLazy) != 0;   // wave-uniform
+    float alpha = 1.f;
+    if (grow) {
       const float mref = fmaxf(m_run, mt);
-      const float alpha = __builtin_amdgcn_exp2f(m_run - (mref == -INFINITY ? 0.f : mref));
+      alpha = __builtin_amdgcn_exp2f(m_run - (mref == -INFINITY ? 0.f : mref));
       l_run *= alpha;
+      m_run = mref;
+    }
+    // with no visible key yet (m = -inf) every exponent below is -inf: 0
+    const float ref = m_run == -INFINITY ? 0.f : m_run;
+    floatx16 c0;
+#pragma unroll
+    for (int y = 0; y < 16; ++y) c0[y] = 0.f;
+    // Beside each product of S: EP numerators, the packing of the EP before them, and
+    // the products of P V of block n - 1 (relative to the reference before it grew).
+    // The order is fixed: the compiler's own is all products, then everything else.
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < NKS; ++i) {
+#pragma unroll
+      for (int x = EP * i; x < EP * (i + 1); ++x) {
+        float y = __builtin_amdgcn_exp2f(fmaf(s[x], scale2, -ref));
+        asm volatile("" : "+v"(y));
+        s[x] = y;
+      }
+      if (i > 0) {
+#pragma unroll
+        for (int x = EP * (i - 1); x < EP * i; x += 2) pack(s, x, ph[PAR], pl[PAR]);
+      }
+      nx = mma32(k_operand(i), qf[i], i == 0 ? c0 : nx);
+#pragma unroll
+      for (int x = 2 * ND * i / NKS; x < 2 * ND * (i + 1) / NKS; ++x)
+        v_product(x, ph[1 - PAR], pl[1 - PAR]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int x = 16 - EP; x < 16; x += 2) pack(s, x, ph[PAR], pl[PAR]);
+    if (grow) {
 #pragma unroll
       for (int db = 0; db < ND; ++db)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
-      m_run = mref;
     }
-    // with no visible key yet (m = -inf) every exponent below is -inf: 0
-    const float mxs = m_run == -INFINITY ? 0.f : m_run;
-    float ls = 0.f;
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        sc[kb][i] = __builtin_amdgcn_exp2f(fmaf(sc[kb][i], scale2, -mxs));
-        ls += sc[kb][i];
-      }
-    l_run += ls;
-    bool odd = false;                             // infinities or NaN among the tile's V
-    if (!full) {
-#pragma unroll 1
-      for (int i = lane; i < NK * CPR; i += kWave) odd |= has_nonfinite<F8>(Vs[i]);
-      odd = __ballot(odd) != 0;
+    v_read(stage, r);
+    if (__builtin_expect(odd, 0)) take_odd(ph[PAR]);
+  };
+  auto after = [](int stage) { return stage + 1 == NST ? 0 : stage + 1; };
+  // The beginning of iteration t: K of tile t + 1 and V of tile t landed (every
+  // wave's loads), and every wave is done with what the next loads replace.
+  auto begin = [&](int t, int stage) __attribute__((always_inline)) {
+    asm volatile("" ::: "memory");
+    if (t + NST - 2 + ahead < nj) {
+      if (is_k) __builtin_amdgcn_s_waitcnt(0x0070 | (kWaitK & 15) | ((kWaitK >> 4) << 14));
+      else __builtin_amdgcn_s_waitcnt(0x0070 | (kWaitV & 15) | ((kWaitV >> 4) << 14));
+    } else {
+      __builtin_amdgcn_s_waitcnt(0x0070);
     }
-    uint32_t vx = va + lds_byte(Vs);
-    asm volatile("" : "+v"(vx));
-    auto step = [&](auto u_) __attribute__((always_inline)) {
-      constexpr int u0 = decltype(u_)::value;     // steps u0, u0 + 1: one 32-key block
-      u32x4 v[2][ND], ph[2], pl[2];
-      uint32_t xa[ND], xb[ND];
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    if (t + NST - 1 + ahead < nj) {
+      issue(j + t + NST - 1 + ahead, ahead ? stage : (stage == 0 ? NST - 1 : stage - 1));
+      pages(j + imin(t + NST + ahead, nj - 1));
+    }
+  };
+  // K of the first tile landed
+  asm volatile("" ::: "memory");
+  if (is_k) {
+    constexpr int kFirst = (NST - 2 + (NB == 1 ? 1 : 0)) * PER;
+    if (NST - 1 + ahead <= nj) __builtin_amdgcn_s_waitcnt(0x0070 | (kFirst & 15) | ((kFirst >> 4) << 14));
+    else __builtin_amdgcn_s_waitcnt(0x0070);
+  }
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  floatx16 sa, sb;
+  constexpr std::integral_constant<int, 0> even{};
+  constexpr std::integral_constant<int, 1> uneven{};
+  if (live) {                                     // the first block's scores
+    k_read(0, 32 * wk);
+    floatx16 c0;
 #pragma unroll
-      for (int db = 0; db < ND; ++db) {
-        xa[db] = vx ^ (kVX * db);
-        xb[db] = xa[db] ^ 32;
-      }
-      lds_v<ND, F8, 16 * u0 * RB, RB>(xa, xb, v);
+    for (int y = 0; y < 16; ++y) c0[y] = 0.f;
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+    for (int i = 0; i < NKS; ++i) sa = mma32(k_operand(i), qf[i], i == 0 ? c0 : sa);
+  }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float e0 = sc[u0 / 2][8 * u + 2 * i], e1 = sc[u0 / 2][8 * u + 2 * i + 1];
-          ph[u][i] = pk_bf16(e0, e1);
-          if constexpr (PARTS == 2)
-            pl[u][i] = pk_bf16(e0 - __uint_as_float(ph[u][i] << 16),
-                               e1 - __uint_as_float(ph[u][i] & 0xFFFF0000u));
-        }
-      // Rows must not meet the infinities and NaN of keys that they do not see (0
-      // times one is no number): those values leave the operands, and the rows
-      // with a numerator for one get it from a product with ones in its places.
-      // Only tiles on the border of some row's view come here, and only if they
-      // hold such values.
-      if (__builtin_expect(odd, 0)) {
+  for (int u = 0; u < 2; ++u) {                   // and nothing for the block before it
+    ph[1][u] = u32x4{0u, 0u, 0u, 0u};
+    if constexpr (PARTS == 2) pl[1][u] = ph[1][u];
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int db = 0; db < ND; ++db) {
+    for (int db = 0; db < ND; ++db) v[u][db] = u32x4{0u, 0u, 0u, 0u};
+  }
+  int stage = 0;
+  bool last_even = false;                         // the last block's numerators are set 0
 #pragma unroll 1
-            for (int c = 0; c < 3; ++c) {         // inf, -inf, NaN
-              u32x4 one;
-#pragma unroll
-              for (int w = 0; w < 4; ++w)
-                one[w] = ones_of(c, v[u][db][w] & 0xffffu) | ones_of(c, v[u][db][w] >> 16) << 16;
-              floatx16 y;
-#pragma unroll
-              for (int i = 0; i < 16; ++i) y[i] = 0.f;
-              y = mma32(one, ph[u], y);
-              const float val = c == 0 ? INFINITY : (c == 1 ? -INFINITY : NAN);
-#pragma unroll
-              for (int i = 0; i < 16; ++i) o[db][i] += y[i] > 0.f ? val : 0.f;
-            }
-#pragma unroll
-            for (int w = 0; w < 4; ++w) v[u][db][w] &= ~nonfinite_mask(v[u][db][w]);
-          }
+  for (int t = 0; t < nj; ++t) {
+    begin(t, stage);
+    int k0 = tile_key(j + t) + 32 * wk;
+    if constexpr (NB == 2) {
+      if (live) {
+        block(even, k0, stage, 0, sa, stage, 32, sb);
+        block(uneven, k0 + 32, stage, 32, sb, after(stage), 0, sa);
       }
+    } else {                                      // two tiles: the scores change places
+      if (live) block(even, k0, stage, 32 * wk, sa, after(stage), 32 * wk, sb);
+      stage = after(stage);
+      if (++t == nj) {                            // whole workgroup
+        last_even = true;
+        break;
+      }
+      begin(t, stage);
+      k0 = tile_key(j + t) + 32 * wk;
+      if (live) block(uneven, k0, stage, 32 * wk, sb, after(stage), 32 * wk, sa);
+    }
+    stage = after(stage);
+  }
+  if (live) {                                     // P V of the last block
+    if (NB == 1 && last_even) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int x = 0; x < 2 * ND; ++x) v_product(x, ph[0], pl[0]);
+    } else {
 #pragma unroll
-        for (int db = 0; db < ND; ++db) {
-          if constexpr (PARTS == 2) o[db] = mma32(v[u][db], pl[u], o[db]);
-          o[db] = mma32(v[u][db], ph[u], o[db]);
-        }
-    };
-    step(std::integral_constant<int, 0>{});
-    if constexpr (KB == 2) step(std::integral_constant<int, 2>{});
+      for (int x = 0; x < 2 * ND; ++x) v_product(x, ph[1], pl[1]);
+    }
   }
   l_run = fsum_xor32(l_run);
   if constexpr (WK == 2) {
@@ -825,33 +909,44 @@ __global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
     }
   }
   // ---- results: the rows themselves, or what k_kv_join(_rows) adds up ----
-  if (rv && wk == 0) {
+  // Lanes without a row write to a row that no one reads: with branches of single
+  // lanes here this compiler brought registers back under the narrower mask.
+  if (wk == 0) {
+    const int row = row0 + rr, tk = row / d.grp;
+    const int64_t tok = tok0 + tk;
+    const int head = kvh * d.grp + (row - tk * d.grp);
     if (whole && d.groups == 0) {
-      const float inv = l_run == 0.f ? 0.f
-                                     : (F8 && d.v_scale != nullptr ? d.v_scale[kvh] : 1.f) / l_run;
-      uint16_t* op = d.out + tok * d.out_ld + (int64_t)head * HD + 4 * h;
+      const float inv = l_run == 0.f
+          ? 0.f : (F8 && d.v_scale != nullptr ? d.v_scale[kvh] : 1.f) / l_run;
+      uint16_t* op = (rv ? d.out + tok * d.out_ld + (int64_t)head * HD : (uint16_t*)d.w.dump) + 4 * h;
 #pragma unroll
       for (int db = 0; db < ND; ++db)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const uint2 v{pk_bf16(o[db][4 * i] * inv, o[db][4 * i + 1] * inv),
-                        pk_bf16(o[db][4 * i + 2] * inv, o[db][4 * i + 3] * inv)};
-          *reinterpret_cast<uint2*>(op + 32 * db + 8 * i) = v;
+          const floatx16& y = o[db];
+          *reinterpret_cast<uint2*>(op + 32 * db + 8 * i) =
+              uint2{pk_bf16(y[4 * i] * inv, y[4 * i + 1] * inv),
+                    pk_bf16(y[4 * i + 2] * inv, y[4 * i + 3] * inv)};
         }
-      if (d.lse != nullptr && h == 0)
-        d.lse[tok * d.nh + head] = l_run == 0.f
+      if (d.lse != nullptr) {
+        const float y = l_run == 0.f
             ? -INFINITY : (m_run + __builtin_amdgcn_logf(l_run)) * 0.69314718055994531f;
+        *(rv ? d.lse + tok * d.nh + head : (float*)d.w.dump) = y;
+      }
     } else {
       const int64_t prow = whole ? d.row0 + ((int64_t)prefix * d.total_q + tok) * d.nh + head
                                  : (int64_t)(2 * sidx + (j == 0 ? 1 : 0)) * R + rr;
-      float* op = d.w.part + prow * HD + 4 * h;
+      float* op = (rv ? d.w.part + prow * HD : (float*)d.w.dump) + 4 * h;
 #pragma unroll
       for (int db = 0; db < ND; ++db)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 4; ++i) {
+          const floatx16& y = o[db];
           *reinterpret_cast<floatx4*>(op + 32 * db + 8 * i) =
-              floatx4{o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]};
-      if (h == 0) *reinterpret_cast<float2*>(d.w.ml + 2 * prow) = float2{m_run, l_run};
+              floatx4{y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]};
+        }
+      *reinterpret_cast<float2*>(rv ? d.w.ml + 2 * prow : (float*)d.w.dump) =
+          float2{m_run, l_run};
     }
   }
   // ---- on to the next segment of the share ----
@@ -983,7 +1078,7 @@ __global__ void k_kv_unseen(int32_t* __restrict__ tseq, int n) {
 // room for a second workgroup and its loads.
 static int kv_rows(int64_t rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
 static int kv_shares(const xp_kv* kv, int R) {
-  return std::max(8, kv->cus * (R == 256 ? 1 : 2) / 8 * 8);
+  return std::max(8, kv->cus * (R >= 128 ? 1 : 2) / 8 * 8);
 }
 
 void kv_attn_sizes(const xp_kv* kv, int64_t* rows, int* entries, int* shares) {
@@ -1064,20 +1159,20 @@ hipError_t launch_kv_attn(const xp_kv* kv, const KvAttnArgs& a, hipStream_t st) 
 #define XP_KV(HD_, F8_, WR_, WK_, NST_, PARTS_)                                                  \
   hipLaunchKernelGGL((k_kv_attn<HD_, F8_, WR_, WK_, NST_, PARTS_>), dim3(shares),                \
                      dim3((WR_) * (WK_) * kWave), 0, st, d)
-#define XP_KV_R(HD_, F8_, N2_)                                                                   \
+#define XP_KV_R(HD_, F8_, N2_, N1_)                                                              \
   do {                                                                                           \
     if (R == 32) XP_KV(HD_, F8_, 1, 2, N2_, 2);                                                  \
     else if (R == 64) XP_KV(HD_, F8_, 2, 2, N2_, 2);                                             \
-    else if (R == 128) XP_KV(HD_, F8_, 4, 1, N2_, 2);                                            \
-    else XP_KV(HD_, F8_, 8, 1, 4, 1);                                                            \
+    else if (R == 128) XP_KV(HD_, F8_, 4, 2, N1_, 1);                                            \
+    else XP_KV(HD_, F8_, 8, 1, N1_, 1);                                                          \
   } while (0)
   const bool f8 = kv->dtype == XP_E4M3;
   if (kv->hd == 128) {
-    if (f8) XP_KV_R(128, true, 4);
-    else XP_KV_R(128, false, 2);
+    if (f8) XP_KV_R(128, true, 4, 8);
+    else XP_KV_R(128, false, 2, 4);
   } else {
-    if (f8) XP_KV_R(64, true, 4);
-    else XP_KV_R(64, false, 4);
+    if (f8) XP_KV_R(64, true, 4, 8);
+    else XP_KV_R(64, false, 4, 8);
   }
 #undef XP_KV_R
 #undef XP_KV

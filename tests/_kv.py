@@ -128,4 +128,5 @@ class Call:
 
 
 def parts_of(rows):
-    return 2 if rows <= 128 else 1
+    # two bf16 parts of the numerators in calls of up to 64 rows, one above (c below)
+    return 2 if rows <= 64 else 1

@@ -238,7 +238,7 @@ def test_attend_max_q_costs_time_only(rows):
     kv = c.device(max_tokens=512)
     m = dict(causal=True, window=50, sinks=10)
     print(f"attend: tiles of {rows} rows", flush=True)
-    c.check(c.run(kv, max_q=rows // 2, **m), parts=1 if rows == 256 else 2, **m)
+    c.check(c.run(kv, max_q=rows // 2, **m), parts=parts_of(rows), **m)
     kv.close()
 
 
