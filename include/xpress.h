@@ -478,9 +478,9 @@ xp_status xp_kv_write(xp_kv* kv, int32_t tokens, const void* k, int64_t k_ld, co
  * if causal, and j > p - window or j < sinks if there is a window.  A token that
  * sees no key gives 0 (lse -inf).  Keys that a token does not see do not enter
  * its result, whatever they hold.  Scores and sums are fp32; the numerators enter
- * the product with V as two bf16 parts, as one in calls of more than 64 rows
- * (max_q times the heads of a group; with shared prefixes at least the mean tokens
- * of a group times the heads).
+ * the product with V as two bf16 parts, as one with an 8-bit cache and in calls of
+ * more than 64 rows (max_q times the heads of a group; with shared prefixes at least
+ * the mean tokens of a group times the heads).
  * Pages outside [0, n_pages) where a key is read are replaced by 0 and set
  * XP_DEVERR_PAGE; lengths outside [0, max_len] are clamped (XP_DEVERR_LENGTH).
  * The same call gives the same bits; a request's summation order follows the

@@ -242,7 +242,7 @@ __device__ __forceinline__ float f8_quotient(float x, float s, float inv) {
     const float r = fmaf(-q, s, x);               // the exact rest
     const uint32_t u = __float_as_uint(q);
     const uint32_t up = (u ^ __float_as_uint(r) ^ __float_as_uint(s)) >> 31 ? u - 1u : u + 1u;
-    q = (r != 0.f) & (q != 0.f) & !(u & 1u) ? __uint_as_float(up) : q;
+    q = ((r != 0.f) & (q != 0.f) & !(u & 1u)) ? __uint_as_float(up) : q;
   }
   return q > 448.f ? 448.f : (q < -448.f ? -448.f : q);
 }

@@ -468,6 +468,30 @@ __device__ __forceinline__ uint32_t ones_of(int c, uint32_t x) {
   return is ? 0x3f80u : 0u;
 }
 
+// n KB of a page into LDS, 1 KB a load; a load's immediate offset counts for the
+// memory and the LDS address alike.  The second with the non-temporal hint, for keys
+// that one row tile streams: 48 single tokens over 4096 keys 157 -> 139 us (5.1 ->
+// 5.8 TB/s), 32 blocks of 16 over 8192 225 -> 209; from 128 rows on no change.
+__device__ __forceinline__ void kv_dma(const char* base, uint32_t lp, uint32_t x, int n, u32x4* dst) {
+  const uint64_t b = (uint64_t)(uintptr_t)base;
+  __builtin_amdgcn_global_load_lds((const void*)(uintptr_t)(b + lp), dst, 16, 0, 0);
+  if (n > 1) __builtin_amdgcn_global_load_lds((const void*)(uintptr_t)(b + (lp ^ x)), dst, 16, 1024, 0);
+  if (n > 2) {
+    __builtin_amdgcn_global_load_lds((const void*)(uintptr_t)(b + (lp ^ (2 * x))), dst, 16, 2048, 0);
+    __builtin_amdgcn_global_load_lds((const void*)(uintptr_t)(b + (lp ^ (3 * x))), dst, 16, 3072, 0);
+  }
+}
+
+__device__ __forceinline__ void kv_dma_nt(const char* base, uint32_t lp, uint32_t x, int n, u32x4* dst) {
+  const uint64_t b = (uint64_t)(uintptr_t)base;
+  __builtin_amdgcn_global_load_lds((const void*)(uintptr_t)(b + lp), dst, 16, 0, 2);
+  if (n > 1) __builtin_amdgcn_global_load_lds((const void*)(uintptr_t)(b + (lp ^ x)), dst, 16, 1024, 2);
+  if (n > 2) {
+    __builtin_amdgcn_global_load_lds((const void*)(uintptr_t)(b + (lp ^ (2 * x))), dst, 16, 2048, 2);
+    __builtin_amdgcn_global_load_lds((const void*)(uintptr_t)(b + (lp ^ (3 * x))), dst, 16, 3072, 2);
+  }
+}
+
 // A row's view of the keys: [lo, lo + n) and [floor, floor + s).
 struct KvSees {
   int lo, floor;
@@ -580,6 +604,11 @@ __global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
 
   // ---- loads ----
   const scalar_i32 tb = as_scalar(d.table + (int64_t)seq * d.table_ld);
+  // the first page's rows of this KV head, and the bytes from page to page
+  const char* heads = (wave < NW / 2 ? d.kc : d.vc) + (((int64_t)kvh << d.logP) * RB);
+  const uint32_t page_bytes = (uint32_t)(d.nkv * RB) << d.logP;
+  const int kin = imax(klo, kfloor);              // from here to khi, or to ks_, some row sees all
+  uint32_t bad = 0;                               // a page outside the cache was asked for
   int pg[NG];
   auto pages = [&](int t) {                       // page ids of the wave's rows of tile t
 #pragma unroll
@@ -588,29 +617,36 @@ __global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
   };
   auto issue = [&](int t, int slot) __attribute__((always_inline)) {
     const int k0 = tile_key(t);
-    const bool inner = k0 >= kfloor && k0 + kKvTile <= khi && (k0 >= klo || k0 + kKvTile <= ks_);
+    const bool inner = ((k0 >= kin) & (k0 + kKvTile <= khi)) | ((k0 >= kfloor) & (k0 + kKvTile <= ks_));
+    u32x4* stage = lds + slot * SH::kStage + wave * (NG * 16 * CPR);   // its rows of K, then V
+    if (inner) {
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      const int gi = wave * NG + g, rb = 16 * (gi & 3), g0 = k0 + rb;
-      int page = pg[g];
-      if ((uint32_t)page >= (uint32_t)d.n_pages) {
-        const int from = imax(g0, kfloor), to = imin(g0 + 16, khi);
-        if (from < to && (to > klo || from < ks_)) atomicOr(d.err, XP_DEVERR_PAGE);
-        page = 0;
+      for (int g = 0; g < NG; ++g) {
+        const uint32_t page = (uint32_t)pg[g];
+        const bool ok = page < (uint32_t)d.n_pages;
+        bad |= ok ? 0u : XP_DEVERR_PAGE;
+        const char* base = heads + (uint64_t)(ok ? page : 0u) * page_bytes +
+                           ((k0 + 16 * ((wave * NG + g) & 3)) & P1) * RB;
+        // a load's offset counts for both addresses
+        if constexpr (R <= 64) kv_dma_nt(base, lp, kLoadX, IPG, stage + 16 * g * CPR);
+        else kv_dma(base, lp, kLoadX, IPG, stage + 16 * g * CPR);
       }
-      const char* base = (gi >= 4 ? d.vc : d.kc) +
-                         ((((int64_t)page * d.nkv + kvh) << d.logP) + (g0 & P1)) * RB;
-      u32x4* dst = lds + slot * SH::kStage + (gi >= 4 ? SH::kHalf : 0) + rb * CPR;
-      if (inner) {
+    } else {
 #pragma unroll
-        for (int i = 0; i < IPG; ++i) lds_dma16(base + 1024 * i + (lp ^ (kLoadX * i)), dst + 64 * i);
-      } else {
+      for (int g = 0; g < NG; ++g) {
+        const int g0 = k0 + 16 * ((wave * NG + g) & 3);
+        const uint32_t page = (uint32_t)pg[g];
+        const bool ok = page < (uint32_t)d.n_pages;
+        const int from = imax(g0, kfloor), to = imin(g0 + 16, khi);
+        bad |= (!ok & (from < to) & ((to > klo) | (from < ks_))) ? XP_DEVERR_PAGE : 0u;
+        const char* base = heads + (uint64_t)(ok ? page : 0u) * page_bytes + (g0 & P1) * RB;
 #pragma unroll
         for (int i = 0; i < IPG; ++i) {
           const int key = g0 + i * (kWave / CPR) + lane / CPR;
-          const bool any = key >= kfloor && key < khi && (key >= klo || key < ks_);
-          lds_dma16(any ? base + 1024 * i + (lp ^ (kLoadX * i)) : d.w.zero + 16 * (lane & 15),
-                    dst + 64 * i);
+          const bool any = (key >= kfloor) & (key < khi) & ((key >= klo) | (key < ks_));
+          const uint64_t at = (uint64_t)(uintptr_t)base + 1024 * i + (lp ^ (kLoadX * i));
+          const uint64_t none = (uint64_t)(uintptr_t)d.w.zero + 16 * (lane & 15);
+          lds_dma16((const void*)(uintptr_t)(any ? at : none), stage + 16 * g * CPR + 64 * i);
         }
       }
     }
@@ -748,7 +784,7 @@ __global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const uint32_t c = 8 * (i / 4) + i % 4;
-        s[i] = (a + c < sees.n) | (b + c < sees.s) ? s[i] : -INFINITY;
+        s[i] = ((a + c < sees.n) | (b + c < sees.s)) ? s[i] : -INFINITY;
       }
       odd = odd_values(stage, r);
     }
@@ -949,6 +985,7 @@ __global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
           float2{m_run, l_run};
     }
   }
+  if (bad != 0) atomicOr(d.err, bad);
   // ---- on to the next segment of the share ----
   if (f >= f1) return;                            // whole workgroup
   j = -kSegUnits;
@@ -1077,9 +1114,13 @@ __global__ void k_kv_unseen(int32_t* __restrict__ tseq, int n) {
 // sequences) brings: the fewest waves that hold them, so that short ones leave
 // room for a second workgroup and its loads.
 static int kv_rows(int64_t rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
-static int kv_shares(const xp_kv* kv, int R) {
-  return std::max(8, kv->cus * (R >= 128 ? 1 : 2) / 8 * 8);
+// Workgroups of a CU: 8 waves, or as many as the rings leave room for (a ring of two
+// 32 KB stages twice).
+static int kv_wgs(const xp_kv* kv, int R) {
+  const bool wide = kv->hd == 128 && kv->dtype == XP_BF16;
+  return R >= 128 ? 1 : (R == 64 || wide ? 2 : 4);
 }
+static int kv_shares(const xp_kv* kv, int R) { return std::max(8, kv->cus * kv_wgs(kv, R) / 8 * 8); }
 
 void kv_attn_sizes(const xp_kv* kv, int64_t* rows, int* entries, int* shares) {
   const int64_t all = (int64_t)kv->max_tokens * kv->grp;
@@ -1159,20 +1200,23 @@ hipError_t launch_kv_attn(const xp_kv* kv, const KvAttnArgs& a, hipStream_t st) 
 #define XP_KV(HD_, F8_, WR_, WK_, NST_, PARTS_)                                                  \
   hipLaunchKernelGGL((k_kv_attn<HD_, F8_, WR_, WK_, NST_, PARTS_>), dim3(shares),                \
                      dim3((WR_) * (WK_) * kWave), 0, st, d)
-#define XP_KV_R(HD_, F8_, N2_, N1_)                                                              \
+  // stages: what leaves room for kv_wgs workgroups in 160 KB (NS_ for 32 rows, N2_ for
+  // 64, N1_ above).  Two bf16 parts of the numerators where a bf16 cache is read by
+  // so few rows that memory bounds the call; an 8-bit V is coarser than one part.
+#define XP_KV_R(HD_, F8_, NS_, N2_, N1_)                                                         \
   do {                                                                                           \
-    if (R == 32) XP_KV(HD_, F8_, 1, 2, N2_, 2);                                                  \
-    else if (R == 64) XP_KV(HD_, F8_, 2, 2, N2_, 2);                                             \
+    if (R == 32) XP_KV(HD_, F8_, 1, 2, NS_, F8_ ? 1 : 2);                                        \
+    else if (R == 64) XP_KV(HD_, F8_, 2, 2, N2_, F8_ ? 1 : 2);                                   \
     else if (R == 128) XP_KV(HD_, F8_, 4, 2, N1_, 1);                                            \
     else XP_KV(HD_, F8_, 8, 1, N1_, 1);                                                          \
   } while (0)
   const bool f8 = kv->dtype == XP_E4M3;
   if (kv->hd == 128) {
-    if (f8) XP_KV_R(128, true, 4, 8);
-    else XP_KV_R(128, false, 2, 4);
+    if (f8) XP_KV_R(128, true, 2, 4, 8);
+    else XP_KV_R(128, false, 2, 2, 4);
   } else {
-    if (f8) XP_KV_R(64, true, 4, 8);
-    else XP_KV_R(64, false, 4, 8);
+    if (f8) XP_KV_R(64, true, 2, 4, 8);
+    else XP_KV_R(64, false, 2, 4, 8);
   }
 #undef XP_KV_R
 #undef XP_KV

@@ -127,6 +127,7 @@ class Call:
         print(f"    worst error {worst:.3f} of the bound", flush=True)
 
 
-def parts_of(rows):
-    # two bf16 parts of the numerators in calls of up to 64 rows, one above (c below)
-    return 2 if rows <= 64 else 1
+def parts_of(rows, cache="bf16"):
+    # the bf16 parts of the numerators: two over a bf16 cache in calls of up to 64
+    # rows, else one (its rounding is c's part of the bound above)
+    return 2 if rows <= 64 and cache == "bf16" else 1

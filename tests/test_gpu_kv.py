@@ -226,7 +226,7 @@ def test_attend(name, hd, cache, P):
         out = torch.full((c.total, c.heads, hd), float("nan"), dtype=torch.bfloat16, device="cuda")
         lse = torch.full((c.total, c.heads), float("nan"), device="cuda")
         c.run(kv, out=out, lse=lse, **m)
-        c.check(out, lse, parts=parts_of(c.rows()), **m)
+        c.check(out, lse, parts=parts_of(c.rows(), c.cache), **m)
         assert kv.device_errors() == 0
     kv.close()
 
@@ -299,7 +299,7 @@ def test_values_that_no_row_or_not_every_row_sees(cache, hd, ql):
     kv = c.device()
     print(f"masked values: {cache} hd={hd} ql={ql}", flush=True)
     out = c.run(kv, window=W, sinks=5).double().cpu().numpy()
-    want = c.oracle(causal=True, window=W, sinks=5, parts=parts_of(c.rows()))
+    want = c.oracle(causal=True, window=W, sinks=5, parts=parts_of(c.rows(), c.cache))
     for b in want:
         o, _, eb, _ = want[b]
         m = ql[b]
@@ -322,7 +322,7 @@ def test_infinite_values_of_later_tokens(cache, ql):
     kv = c.device()
     out = c.run(kv).double().cpu().numpy()
     with np.errstate(invalid="ignore"):
-        want = c.oracle(causal=True, parts=parts_of(c.rows()))
+        want = c.oracle(causal=True, parts=parts_of(c.rows(), c.cache))
     for b in want:
         o, _, eb, _ = want[b]
         got = out[c.cu[b]:c.cu[b + 1]]
@@ -346,7 +346,7 @@ def test_equal_bits_every_time_and_on_another_stream():
     b = c.run(kv, window=500, sinks=20, stream=s, out=torch.empty_like(a))
     s.synchronize()
     assert a.equal(b)
-    c.check(a, causal=True, window=500, sinks=20, parts=parts_of(c.rows()))
+    c.check(a, causal=True, window=500, sinks=20, parts=parts_of(c.rows(), c.cache))
     kv.close()
 
 
@@ -466,7 +466,7 @@ def test_attend_shared(name, hd, cache):
         lse = torch.full((c.total, c.heads), float("nan"), device="cuda")
         c.run(kv, shared=True, out=out, lse=lse, **m)
         assert kv.device_errors() == 0
-        c.check(out, lse, parts=parts_of(rows), **m)
+        c.check(out, lse, parts=parts_of(rows, cache), **m)
         again = c.run(kv, shared=True, **m)
         assert again.equal(out)
     kv.close()
@@ -611,7 +611,7 @@ def test_prompts_then_blocks_as_a_serving_loop(cache, window, sinks):
                 w = sc.astype(np.float64)[None, :, None]
                 rows = [R.to_e4m3(x[new] / w) * w for x in (k, v)]
             keys = [np.concatenate([p, r]) for p, r in zip(past[b], rows)]
-            parts = parts_of(int(add.max()) * heads // n_kv)
+            parts = parts_of(int(add.max()) * heads // n_kv, cache)
             if add[b]:
                 o, lse, spread, score = R.attend(q[new], *keys, window=window, sinks=sinks)
                 m = keys[0].shape[0]
