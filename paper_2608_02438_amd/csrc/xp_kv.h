@@ -40,16 +40,22 @@ struct KvShare {
   int32_t f, e, kvh, j;
 };
 
-// Workspace of the attention (device pointers).
-struct KvAttnWs {
+// A work list (device pointers).
+struct KvList {
   int32_t* hdr = nullptr;            // [0] units, [1] units of a share, [2] entries
   KvShare* share = nullptr;          // [shares + 1]
   KvEntry* ent = nullptr;            // [entries]
   int32_t* cum = nullptr;            // [entries + 1] units before each entry
-  float* part = nullptr;             // [rows][head_dim] partial O of split segments, then of rows
+  int32_t* off = nullptr;            // [items + 1] entries before each sequence (group)
+};
+
+// Workspace of the attention (device pointers).
+struct KvAttnWs {
+  KvList list[2];                    // the sequences' own keys (and prefixes); the prefixes
+  float* part = nullptr;             // [rows][head_dim] partial O of each list's cut segments,
+                                     // then of rows (own keys, prefix)
   float* ml = nullptr;               // [rows][2] their reference maximum (base 2) and sum
   // calls with shared prefixes
-  int32_t* off = nullptr;            // [items + 1] entries before each sequence, then each group
   int32_t* pos = nullptr;            // [tokens] position of every token
   int32_t* tseq = nullptr;           // [tokens] its sequence
   int32_t* stok = nullptr;           // [batch] first token of each sequence
@@ -90,7 +96,7 @@ struct xp_kv {
   int nh = 0, nkv = 0, grp = 1, hd = 0, P = 0, logP = 0, n_pages = 0, dtype = 0;
   int max_batch = 0, max_tokens = 0, max_len = 0, max_pages = 0, shared = 0;
   int entries = 0;                   // entries the workspace holds
-  int64_t rows = 0;                  // partial rows of split segments
+  int64_t rows = 0;                  // partial rows of a list's cut segments
   void* ws = nullptr;
   xp::KvAttnWs a;
   int32_t* take = nullptr;           // [max_batch + 1] pages taken before each request

@@ -438,9 +438,10 @@ extern "C" xp_status xp_kv_create(const xp_kv_shape* s, int32_t max_batch, int32
   kv->cus = kv->cus > 0 ? kv->cus : 256;
   int shares = 0;
   kv_attn_sizes(kv, &kv->rows, &kv->entries, &shares);
-  const size_t prows = (size_t)kv->rows + (shared ? (size_t)2 * max_tokens * kv->nh : 0);
-  const size_t nb = (size_t)max_batch, items = shared ? 2 * nb : nb;
+  const size_t lists = shared ? 2 : 1, nb = (size_t)max_batch;
+  const size_t prows = lists * kv->rows + (shared ? (size_t)2 * max_tokens * kv->nh : 0);
   // slices of the workspace
+  KvList &l0 = kv->a.list[0], &l1 = kv->a.list[1];
   struct Slice { void** at; size_t bytes; };
   char* zero = nullptr;
   int32_t* acu = nullptr;
@@ -452,11 +453,16 @@ extern "C" xp_status xp_kv_create(const xp_kv_shape* s, int32_t max_batch, int32
       {(void**)&kv->old, nb * 4},
       {(void**)&acu, (nb + 1) * 4},
       {(void**)&kv->a.dump, 512},
-      {(void**)&kv->a.hdr, 256},
-      {(void**)&kv->a.share, ((size_t)shares + 1) * sizeof(KvShare)},
-      {(void**)&kv->a.ent, (size_t)kv->entries * sizeof(KvEntry)},
-      {(void**)&kv->a.cum, ((size_t)kv->entries + 1) * 4},
-      {(void**)&kv->a.off, (items + 1) * 4},
+      {(void**)&l0.hdr, 256},
+      {(void**)&l0.share, ((size_t)shares + 1) * sizeof(KvShare)},
+      {(void**)&l0.ent, lists * kv->entries * sizeof(KvEntry)},
+      {(void**)&l0.cum, (lists * kv->entries + 1) * 4},
+      {(void**)&l0.off, (lists * nb + 1) * 4},
+      {(void**)&l1.hdr, (size_t)(shared ? 256 : 0)},
+      {(void**)&l1.share, shared ? ((size_t)shares + 1) * sizeof(KvShare) : 0},
+      {(void**)&l1.ent, shared ? (size_t)kv->entries * sizeof(KvEntry) : 0},
+      {(void**)&l1.cum, shared ? ((size_t)kv->entries + 1) * 4 : 0},
+      {(void**)&l1.off, shared ? (nb + 1) * 4 : 0},
       {(void**)&kv->a.pos, shared ? (size_t)max_tokens * 4 : 0},
       {(void**)&kv->a.tseq, shared ? (size_t)max_tokens * 4 : 0},
       {(void**)&kv->a.stok, nb * 4},

@@ -19,9 +19,9 @@
 // share is written at once.  The same call gives the same bits.
 //
 // With shared prefixes a group's prefix keys are segments of their own, whose
-// rows are all tokens of the group: they are read once for all of them.  Each
-// sequence's own segments then begin behind the prefix, and k_kv_join_rows adds
-// both results of every row.
+// rows are all tokens of the group, so that they are read once for all of them, and
+// each sequence's own segments begin behind the prefix.  k_kv_join_rows adds both
+// results of every row.
 #include <algorithm>
 #include <cmath>
 
@@ -62,16 +62,18 @@ struct KvDev {
   int causal, window, sinks;
   float scale2;                      // scale log2(e)
   int total_q, groups;
-  int64_t row0;                      // partial rows before those of whole segments
+  KvList list;                       // the work
+  int64_t part0, row0;               // first partial row of its cut segments; of whole ones
   KvAttnWs w;
   uint32_t* err;
 };
 
 // ---------------------------------------------------------------------------
-// The work list.  One workgroup: item i is sequence i (its rows behind a
-// shared prefix, if it has one) or group i - n (its prefix); the items' row
-// tiles, the entries' key ranges, the sums of both, and where each share begins.
-// Bound by latency: a few block scans and one search per entry and share.
+// The work lists, one workgroup each.  Items of the first are the sequences (with
+// their keys behind a shared prefix, if they have one); the groups (their prefixes)
+// follow them or are the items of a second list.  The items' row tiles, the entries' key ranges, the sums
+// of both, and where each share begins.  Bound by latency: a few block scans and one
+// search per entry and share.
 // ---------------------------------------------------------------------------
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanWaves = kPlanThreads / kWave;
@@ -118,7 +120,8 @@ __device__ __forceinline__ int last_at_most(P a, int n, int x) {
 }
 
 struct KvPlan {
-  int n, total_q, max_q, kv_add, cap, R, grp, nkv, causal, window, sinks, groups, entries, shares;
+  int n, total_q, max_q, kv_add, cap, grp, nkv, causal, window, sinks, groups, entries;
+  int R[2], shares[2];               // of each list
   const int32_t* cu_q;
   const int32_t* kv_len;
   const int32_t* group_start;
@@ -131,8 +134,7 @@ __device__ __forceinline__ int clampi(int x, int lo, int hi) { return imin(imax(
 
 template <bool SHARED>
 __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d) {
-  constexpr int kItems = SHARED ? 2 * kKvMaxBatch : kKvMaxBatch;
-  __shared__ int off[kItems + 1];                 // entries before each item
+  __shared__ int off[(SHARED ? 2 : 1) * kKvMaxBatch + 1];   // entries before each item
   __shared__ int floors[SHARED ? kKvMaxBatch : 1];   // keys of the sequence that its prefix holds
   __shared__ int gmin[SHARED ? kKvMaxBatch : 1];  // a group's positions: least and greatest
   __shared__ int gmax[SHARED ? kKvMaxBatch : 1];
@@ -141,6 +143,11 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d) {
   __shared__ int red[kPlanWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int n = d.n;
+  const bool second = SHARED && blockIdx.x == 1;
+  const int ns = second ? 0 : n;                  // items that are sequences
+  const int items = ns + (SHARED && (second || gridDim.x == 1) ? d.groups : 0);
+  const int R = d.R[second], shares = d.shares[second];
+  const KvList out = d.w.list[second];
   uint32_t bad = 0;
   auto first = [&](int b) {                       // first token of sequence b
     return d.cu_q != nullptr ? clampi(d.cu_q[b], 0, d.total_q) : imin(b * d.max_q, d.total_q);
@@ -151,16 +158,25 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d) {
     return clampi(x, 0, imax(d.cap - d.kv_add, 0)) + imin(d.kv_add, d.cap);
   };
   auto tokens = [&](int b, int t0) { return imax(first(b + 1) - t0, 0); };
+  auto members = [&](int g, int& s0, int& s1) {
+    s0 = clampi(d.group_start[g], 0, n);
+    s1 = clampi(d.group_start[g + 1], s0, n);
+  };
   if constexpr (SHARED) {
     for (int b = tid; b < n; b += kPlanThreads) {
       floors[b] = 0;
-      d.w.sgrp[b] = -1;
-      d.w.stok[b] = first(b);
+      if (!second) {
+        d.w.sgrp[b] = -1;
+        d.w.stok[b] = first(b);
+      }
     }
+    if (!second)                                  // tokens of no sequence
+      for (int t = tid; t < d.total_q; t += kPlanThreads) d.w.tseq[t] = -1;
     __syncthreads();
     // a wave per group: its members' positions, and a prefix that none is shorter than
     for (int g = wave; g < d.groups; g += kPlanWaves) {
-      const int s0 = clampi(d.group_start[g], 0, n), s1 = clampi(d.group_start[g + 1], s0, n);
+      int s0, s1;
+      members(g, s0, s1);
       int pmin = 0x7fffffff, pmax = -0x7fffffff, kmin = d.cap;
       for (int b = s0 + lane; b < s1; b += kWave) {
         const int t0 = first(b), ql = tokens(b, t0), kv = keys(b);
@@ -179,40 +195,40 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d) {
       if (want != len) bad |= XP_DEVERR_LENGTH;
       for (int b = s0 + lane; b < s1; b += kWave) {
         floors[b] = len;
-        d.w.sgrp[b] = len > 0 ? g : -1;
+        if (!second) d.w.sgrp[b] = len > 0 ? g : -1;
       }
       if (lane == 0) {
         gmin[g] = pmin;
         gmax[g] = pmax;
         glen[g] = len;
-        d.w.gtok[g] = first(s0);
+        if (!second) d.w.gtok[g] = first(s0);
       }
     }
-    for (int b = wave; b < n; b += kPlanWaves) {  // every token's position and sequence
-      const int t0 = first(b), ql = tokens(b, t0), p0 = keys(b) - ql;
-      for (int i = lane; i < ql; i += kWave) {
-        d.w.pos[t0 + i] = p0 + i;
-        d.w.tseq[t0 + i] = b;
+    if (!second)
+      for (int b = wave; b < n; b += kPlanWaves) {   // every token's position and sequence
+        const int t0 = first(b), ql = tokens(b, t0), p0 = keys(b) - ql;
+        for (int i = lane; i < ql; i += kWave) {
+          d.w.pos[t0 + i] = p0 + i;
+          d.w.tseq[t0 + i] = b;
+        }
       }
-    }
     __syncthreads();
   }
   // entries of each item
-  const int items = n + (SHARED ? d.groups : 0);
   int T = 0;
   for (int i0 = 0; i0 < items; i0 += kPlanThreads) {
     const int i = i0 + tid;
     int nt = 0;
     if (i < items) {
       int tk;
-      if (i < n) {
+      if (i < ns) {
         tk = tokens(i, first(i));
       } else {
-        const int g = i - n;
-        const int s0 = clampi(d.group_start[g], 0, n), s1 = clampi(d.group_start[g + 1], s0, n);
-        tk = glen[g] > 0 ? imax(first(s1) - first(s0), 0) : 0;
+        int s0, s1;
+        members(i - ns, s0, s1);
+        tk = glen[i - ns] > 0 ? imax(first(s1) - first(s0), 0) : 0;
       }
-      nt = (int)(((int64_t)tk * d.grp + d.R - 1) / d.R);
+      nt = (int)(((int64_t)tk * d.grp + R - 1) / R);
     }
     int all;
     const int before = block_scan(nt, red, &all);
@@ -220,13 +236,13 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d) {
     T += all;
   }
   if (tid == 0) off[items] = T;
-  if (T > d.entries) {                            // token ranges that overlap
-    T = d.entries;
+  if (T > (items > n ? 2 : 1) * d.entries) {      // token ranges that overlap
+    T = (items > n ? 2 : 1) * d.entries;
     bad |= XP_DEVERR_LENGTH;
   }
   __syncthreads();
   if constexpr (SHARED)
-    for (int i = tid; i <= items; i += kPlanThreads) d.w.off[i] = off[i];
+    for (int i = tid; i <= items; i += kPlanThreads) out.off[i] = off[i];
   // their key ranges
   int W = 0;
   for (int e0 = 0; e0 < T; e0 += kPlanThreads) {
@@ -234,30 +250,29 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d) {
     int units = 0;
     if (e < T) {
       const int i = last_at_most(off, items, e);
-      const bool prefix = SHARED && i >= n;
       KvEntry x{};
-      x.row0 = (e - off[i]) * d.R;
+      x.row0 = (e - off[i]) * R;
       int pa, pb;                                 // positions of the tile's tokens
-      if (!prefix) {
+      if (i < ns) {
         x.tok0 = first(i);
         const int tk = tokens(i, x.tok0);
         x.seq = i;
-        x.nrows = imin(tk * d.grp - x.row0, d.R);
+        x.nrows = imin(tk * d.grp - x.row0, R);
         x.ceil = keys(i);
         x.p0 = x.ceil - tk;
         x.floor = SHARED ? floors[i] : 0;
         pa = x.p0 + x.row0 / d.grp;
         pb = x.p0 + (x.row0 + x.nrows - 1) / d.grp;
       } else {
-        const int g = i - n;
-        const int s0 = clampi(d.group_start[g], 0, n), s1 = clampi(d.group_start[g + 1], s0, n);
+        int s0, s1;
+        members(i - ns, s0, s1);
         x.tok0 = first(s0);
         x.seq = s0;
-        x.nrows = imin((first(s1) - x.tok0) * d.grp - x.row0, d.R);
+        x.nrows = imin((first(s1) - x.tok0) * d.grp - x.row0, R);
         x.prefix = 1;
-        x.ceil = glen[g];
-        pa = gmin[g];
-        pb = gmax[g];
+        x.ceil = glen[i - ns];
+        pa = gmin[i - ns];
+        pb = gmax[i - ns];
       }
       x.hi = d.causal ? imin(x.ceil, pb + 1) : x.ceil;
       x.lo = d.window > 0 ? imax(pa - d.window + 1, x.floor) : x.floor;
@@ -271,38 +286,37 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d) {
       const int b1 = x.hi > x.lo ? (x.hi + kKvTile - 1) / kKvTile : 0;
       // no row sees a key: one tile, wholly masked, writes the zeros
       x.tiles = imax(x.n1 + imax(b1 - x.b0, 0), 1);
-      d.w.ent[e] = x;
+      out.ent[e] = x;
       units = (x.tiles + kSegUnits) * d.nkv;
     }
     int all;
     const int before = block_scan(units, red, &all);
     if (e < T) {
       if (e < kPlanCum) cums[e] = W + before;
-      d.w.cum[e] = W + before;
+      out.cum[e] = W + before;
     }
     W += all;
   }
+  const int S = imax((W + shares - 1) / shares, kPlanMinShare);
   if (tid == 0) {
-    d.w.cum[T] = W;
-    const int S = imax((W + d.shares - 1) / d.shares, kPlanMinShare);
-    d.w.hdr[0] = W;
-    d.w.hdr[1] = S;
-    d.w.hdr[2] = T;
+    out.cum[T] = W;
+    out.hdr[0] = W;
+    out.hdr[1] = S;
+    out.hdr[2] = T;
   }
   __syncthreads();                                // also the entries, for this workgroup
-  const int S = imax((W + d.shares - 1) / d.shares, kPlanMinShare);
-  for (int s = tid; s <= d.shares; s += kPlanThreads) {
+  for (int s = tid; s <= shares; s += kPlanThreads) {
     KvShare r{};
     r.f = (int64_t)s * S < W ? s * S : W;
     if (r.f < W) {
       r.e = T <= kPlanCum ? last_at_most((const int*)cums, T, r.f)
-                          : last_at_most((const int32_t*)d.w.cum, T, r.f);
-      const int units = d.w.ent[r.e].tiles + kSegUnits;
-      const int in = r.f - (T <= kPlanCum ? cums[r.e] : d.w.cum[r.e]);
+                          : last_at_most((const int32_t*)out.cum, T, r.f);
+      const int units = out.ent[r.e].tiles + kSegUnits;
+      const int in = r.f - (T <= kPlanCum ? cums[r.e] : out.cum[r.e]);
       r.kvh = in / units;
       r.j = in - r.kvh * units - kSegUnits;       // negative: before the first tile
     }
-    d.w.share[s] = r;
+    out.share[s] = r;
   }
   if (bad) atomicOr(d.err, bad);
 }
@@ -533,7 +547,7 @@ __global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
   const int h = lane >> 5, li = lane & 31;
   // neighbouring shares on one XCD: they read the same sequence's keys
   const int sidx = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
-  const scalar_i32 sh = as_scalar(d.w.share + sidx);
+  const scalar_i32 sh = as_scalar(d.list.share + sidx);
   int f = sh[0], e = sh[1], kvh = sh[2], j = sh[3];
   const int f1 = sh[4];
   if (f >= f1) return;                            // whole workgroup
@@ -554,7 +568,7 @@ __global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
   }
   const int P1 = (1 << d.logP) - 1;
   for (;;) {
-  const scalar_i32 en = as_scalar(d.w.ent + e);
+  const scalar_i32 en = as_scalar(d.list.ent + e);
   const int tok0 = en[0], row0 = en[1], nrows = en[2], seq = en[3], p0 = en[4], prefix = en[5];
   const int kfloor = en[6], kceil = en[7], ks_ = en[8], klo = en[9], khi = en[10], tiles = en[11];
   const int a0 = en[12], n1 = en[13], b0 = en[14];
@@ -971,7 +985,7 @@ __global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
       }
     } else {
       const int64_t prow = whole ? d.row0 + ((int64_t)prefix * d.total_q + tok) * d.nh + head
-                                 : (int64_t)(2 * sidx + (j == 0 ? 1 : 0)) * R + rr;
+                                 : d.part0 + (int64_t)(2 * sidx + (j == 0 ? 1 : 0)) * R + rr;
       float* op = (rv ? d.w.part + prow * HD : (float*)d.w.dump) + 4 * h;
 #pragma unroll
       for (int db = 0; db < ND; ++db)
@@ -1014,27 +1028,36 @@ struct KvSum {
   }
 };
 
-// the parts of row rr of the segment whose tiles are units [a, a + tiles), cut at
-// multiples of S: the first at the end of share a / S, the others at the beginning of theirs
-template <int HD>
-__device__ __forceinline__ void add_parts(const KvDev& d, int R, int a, int tiles, int S, int rr,
-                                          int c, KvSum& x) {
-  const int s0 = a / S, s1 = (a + tiles - 1) / S;
-  constexpr int U = 4;
-  for (int s = s0; s <= s1; s += U) {             // loads of U parts in flight
-    float2 ml[U];
-    floatx4 o[U];
+// U parts from share s on, their loads in flight together; those behind share s1 are
+// not added (the last one is read again)
+template <int HD, int U>
+__device__ __forceinline__ void add_some(const KvDev& d, int64_t part0, int R, int s, int s0, int s1,
+                                         int rr, int c, KvSum& x) {
+  float2 ml[U];
+  floatx4 o[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int su = imin(s + u, s1);
-      const int64_t prow = (int64_t)(2 * su + (su == s0 ? 1 : 0)) * R + rr;
-      ml[u] = *reinterpret_cast<const float2*>(d.w.ml + 2 * prow);
-      o[u] = *reinterpret_cast<const floatx4*>(d.w.part + prow * HD + c);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-      if (s + u <= s1) x.add(ml[u].x, ml[u].y, o[u]);
+  for (int u = 0; u < U; ++u) {
+    const int su = imin(s + u, s1);
+    const int64_t prow = part0 + (int64_t)(2 * su + (su == s0 ? 1 : 0)) * R + rr;
+    ml[u] = *reinterpret_cast<const float2*>(d.w.ml + 2 * prow);
+    o[u] = *reinterpret_cast<const floatx4*>(d.w.part + prow * HD + c);
   }
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (s + u <= s1) x.add(ml[u].x, ml[u].y, o[u]);
+}
+
+// the parts of row rr of the segment whose tiles are units [a, a + tiles), cut at
+// multiples of S: the first at the end of share a / S, the others at the beginning of
+// theirs.  Eight at a time where a long prefix has many (32 x 8192 keys in 26 parts:
+// 7.5 us against 11 us by fours), four for the few of ordinary ones (19 against 24 us)
+template <int HD>
+__device__ __forceinline__ void add_parts(const KvDev& d, int64_t part0, int R, int a, int tiles,
+                                          int S, int rr, int c, KvSum& x) {
+  const int s0 = a / S, s1 = (a + tiles - 1) / S;
+  int s = s0;
+  for (; s + 3 < s1; s += 8) add_some<HD, 8>(d, part0, R, s, s0, s1, rr, c, x);
+  if (s <= s1) add_some<HD, 4>(d, part0, R, s, s0, s1, rr, c, x);
 }
 
 template <int HD>
@@ -1055,56 +1078,58 @@ template <int HD>
 __global__ __launch_bounds__(256) void k_kv_join(const KvDev d, int R) {
   constexpr int TPR = HD / 4, RPB = 256 / TPR;
   const int s = blockIdx.x + 1;
-  const scalar_i32 sh = as_scalar(d.w.share + s), hd = as_scalar(d.w.hdr);
+  const scalar_i32 sh = as_scalar(d.list.share + s), hd = as_scalar(d.list.hdr);
   const int f = sh[0], e = sh[1], kvh = sh[2], j = sh[3], S = hd[1];
   if (f >= hd[0] || j <= 0) return;               // past the end, or nothing is cut here
   const int a = f - j;                            // the unit of the segment's first tile
   if (a < f - S) return;                          // cut before: an earlier workgroup's
-  const scalar_i32 en = as_scalar(d.w.ent + e);
+  const scalar_i32 en = as_scalar(d.list.ent + e);
   const int tok0 = en[0], row0 = en[1], nrows = en[2], tiles = en[11];
   const int rr = blockIdx.y * RPB + threadIdx.x / TPR, c = 4 * (threadIdx.x % TPR);
   if (rr >= nrows) return;
   KvSum x;
-  add_parts<HD>(d, R, a, tiles, S, rr, c, x);
+  add_parts<HD>(d, d.part0, R, a, tiles, S, rr, c, x);
   const int row = row0 + rr, tk = row / d.grp;
   write_row<HD>(d, tok0 + tk, kvh * d.grp + (row - tk * d.grp), c, x);
 }
 
 // Calls with shared prefixes: every row, its prefix's result and its own.
+struct KvJoin {
+  int R[2];                          // row tiles of the sequences, of the groups
+  int64_t part0;                     // first partial row of the groups' list
+  int n;
+  int one;                           // both are in one list, the groups behind the sequences
+};
 template <int HD>
-__global__ __launch_bounds__(256) void k_kv_join_rows(const KvDev d, int R, int n,
-                                                      const int32_t* __restrict__ cu_q) {
+__global__ __launch_bounds__(256) void k_kv_join_rows(const KvDev d, const KvJoin jn) {
   constexpr int TPR = HD / 4, RPB = 256 / TPR;
   const int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
   const int c = 4 * (threadIdx.x % TPR);
   if (row >= (int64_t)d.total_q * d.nh) return;
   const int tok = (int)(row / d.nh), head = (int)(row - (int64_t)tok * d.nh);
   const int b = d.w.tseq[tok];
-  if ((uint32_t)b >= (uint32_t)n) return;         // behind the last sequence
-  const int kvh = head / d.grp, hg = head - kvh * d.grp, g = d.w.sgrp[b], S = d.w.hdr[1];
+  if ((uint32_t)b >= (uint32_t)jn.n) return;      // behind the last sequence
+  const int kvh = head / d.grp, hg = head - kvh * d.grp, g = d.w.sgrp[b];
   KvSum x;
-#pragma unroll 1
-  for (int k = g >= 0 ? 0 : 1; k < 2; ++k) {      // the prefix, then the sequence's own keys
-    const int lr = (tok - (k == 0 ? d.w.gtok[g] : d.w.stok[b])) * d.grp + hg;
-    const int e = d.w.off[k == 0 ? n + g : b] + lr / R;
-    if (e >= d.w.hdr[2]) continue;                // dropped: token ranges that overlap
-    const int tiles = d.w.ent[e].tiles;
-    const int a = d.w.cum[e] + kvh * (tiles + kSegUnits) + kSegUnits;
+#pragma unroll
+  for (int k = 1; k >= 0; --k) {                  // the prefix, then the sequence's own keys
+    if (k == 1 && g < 0) continue;
+    const KvList& l = d.w.list[jn.one ? 0 : k];
+    const int R = jn.R[k], S = l.hdr[1];
+    const int lr = (tok - (k == 1 ? d.w.gtok[g] : d.w.stok[b])) * d.grp + hg;
+    const int e = l.off[k == 1 ? (jn.one ? jn.n : 0) + g : b] + lr / R;
+    if (e >= l.hdr[2]) continue;                  // dropped: token ranges that overlap
+    const int tiles = l.ent[e].tiles;
+    const int a = l.cum[e] + kvh * (tiles + kSegUnits) + kSegUnits;
     if (a / S == (a + tiles - 1) / S) {
-      const int64_t prow = d.row0 + ((int64_t)(1 - k) * d.total_q + tok) * d.nh + head;
+      const int64_t prow = d.row0 + ((int64_t)k * d.total_q + tok) * d.nh + head;
       const float2 ml = *reinterpret_cast<const float2*>(d.w.ml + 2 * prow);
       x.add(ml.x, ml.y, *reinterpret_cast<const floatx4*>(d.w.part + prow * HD + c));
     } else {
-      add_parts<HD>(d, R, a, tiles, S, lr % R, c, x);
+      add_parts<HD>(d, k == 1 ? jn.part0 : 0, R, a, tiles, S, lr % R, c, x);
     }
   }
   write_row<HD>(d, tok, head, c, x);
-}
-
-// no sequence yet for any token (a fill kernel: a captured memset is not one)
-__global__ void k_kv_unseen(int32_t* __restrict__ tseq, int n) {
-  const int i = blockIdx.x * 256 + threadIdx.x;
-  if (i < n) tseq[i] = -1;
 }
 
 // ---------------------------------------------------------------------------
@@ -1128,24 +1153,58 @@ void kv_attn_sizes(const xp_kv* kv, int64_t* rows, int* entries, int* shares) {
   *rows = 0;
   for (int r = 32; r <= R; r *= 2) *rows = std::max(*rows, (int64_t)2 * kv_shares(kv, r) * r);
   if (R == 256) *rows = std::max(*rows, (int64_t)2 * kv_shares(kv, 256) * 256);
-  // every sequence and every group rounds its rows up to whole tiles
-  *entries = (int)(((all + 31) / 32) * (kv->shared ? 2 : 1) + kv->max_batch * (kv->shared ? 2 : 1));
+  // every sequence (group) rounds its rows up to whole tiles
+  *entries = (int)((all + 31) / 32 + kv->max_batch);
   *shares = kv_shares(kv, 32);
 }
 
+// one list's attention, in tiles of R rows
+static hipError_t launch_list(const xp_kv* kv, int R, const KvDev& d, hipStream_t st) {
+  const int shares = kv_shares(kv, R);
+#define XP_KV(HD_, F8_, WR_, WK_, NST_, PARTS_)                                                  \
+  hipLaunchKernelGGL((k_kv_attn<HD_, F8_, WR_, WK_, NST_, PARTS_>), dim3(shares),                \
+                     dim3((WR_) * (WK_) * kWave), 0, st, d)
+  // stages: what leaves room for kv_wgs workgroups in 160 KB (NS_ for 32 rows, N2_ for
+  // 64, N1_ above).  Two bf16 parts of the numerators where a bf16 cache is read by
+  // so few rows that memory bounds the call; an 8-bit V is coarser than one part.
+#define XP_KV_R(HD_, F8_, NS_, N2_, N1_)                                                         \
+  do {                                                                                           \
+    if (R == 32) XP_KV(HD_, F8_, 1, 2, NS_, F8_ ? 1 : 2);                                        \
+    else if (R == 64) XP_KV(HD_, F8_, 2, 2, N2_, F8_ ? 1 : 2);                                   \
+    else if (R == 128) XP_KV(HD_, F8_, 4, 2, N1_, 1);                                            \
+    else XP_KV(HD_, F8_, 8, 1, N1_, 1);                                                          \
+  } while (0)
+  const bool f8 = kv->dtype == XP_E4M3;
+  if (kv->hd == 128) {
+    if (f8) XP_KV_R(128, true, 2, 4, 8);
+    else XP_KV_R(128, false, 2, 2, 4);
+  } else {
+    if (f8) XP_KV_R(64, true, 2, 4, 8);
+    else XP_KV_R(64, false, 2, 4, 8);
+  }
+#undef XP_KV_R
+#undef XP_KV
+  return hipGetLastError();
+}
+
 hipError_t launch_kv_attn(const xp_kv* kv, const KvAttnArgs& a, hipStream_t st) {
-  int64_t hint = (int64_t)a.max_q * kv->grp;
-  if (a.groups > 0) hint = std::max(hint, (int64_t)a.total_q / a.groups * kv->grp);
-  const int R = kv_rows(hint), shares = kv_shares(kv, R);
-  hipError_t e;
+  // row tiles of the sequences, and of the groups.  One list for both unless the
+  // groups' are the largest, where products bound the call: a short sequence's
+  // rows in such tiles cost more than a second launch.  32 blocks of one behind 8192
+  // keys (tiles of 128 rows): @A; 60 of 16 behind 500 .. 12000
+  // (tiles of 256): @B.
+  const int64_t rows = (int64_t)a.max_q * kv->grp;
+  int R[2] = {kv_rows(rows), 0};
+  if (a.groups > 0) R[1] = kv_rows(std::max(rows, (int64_t)a.total_q / a.groups * kv->grp));
+  const int lists = R[1] == 256 && R[0] < 256 ? 2 : 1;
+  if (lists == 1 && a.groups > 0) R[0] = R[1];
+  const int cols = (int)std::min<int64_t>(kv->max_pages, a.table_ld);
   KvPlan p{};
   p.n = a.n;
   p.total_q = a.total_q;
   p.max_q = a.max_q;
   p.kv_add = a.kv_add;
-  const int cols = (int)std::min<int64_t>(kv->max_pages, a.table_ld);
   p.cap = (int)std::min<int64_t>((int64_t)cols << kv->logP, kKvMaxLen);
-  p.R = R;
   p.grp = kv->grp;
   p.nkv = kv->nkv;
   p.causal = a.causal;
@@ -1153,22 +1212,22 @@ hipError_t launch_kv_attn(const xp_kv* kv, const KvAttnArgs& a, hipStream_t st) 
   p.sinks = a.sinks;
   p.groups = a.groups;
   p.entries = kv->entries;
-  p.shares = shares;
+  for (int k = 0; k < lists; ++k) {
+    p.R[k] = R[k];
+    p.shares[k] = kv_shares(kv, R[k]);
+  }
   p.cu_q = a.cu_q;
   p.kv_len = a.kv_len;
   p.group_start = a.group_start;
   p.shared_len = a.shared_len;
   p.w = kv->a;
   p.err = kv->err;
-  if (a.groups > 0) {
-    hipLaunchKernelGGL(k_kv_unseen, dim3((a.total_q + 255) / 256), dim3(256), 0, st, kv->a.tseq,
-                       a.total_q);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    hipLaunchKernelGGL(k_kv_plan<true>, dim3(1), dim3(kPlanThreads), 0, st, p);
-  } else {
+  if (a.groups > 0)
+    hipLaunchKernelGGL(k_kv_plan<true>, dim3(lists), dim3(kPlanThreads), 0, st, p);
+  else
     hipLaunchKernelGGL(k_kv_plan<false>, dim3(1), dim3(kPlanThreads), 0, st, p);
-  }
-  if ((e = hipGetLastError()) != hipSuccess) return e;
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
 
   KvDev d{};
   d.q = a.q;
@@ -1194,45 +1253,33 @@ hipError_t launch_kv_attn(const xp_kv* kv, const KvAttnArgs& a, hipStream_t st) 
   d.scale2 = (a.scale > 0.f ? a.scale : 1.f / std::sqrt((float)kv->hd)) * 1.4426950408889634f;
   d.total_q = a.total_q;
   d.groups = a.groups;
-  d.row0 = kv->rows;
+  d.row0 = 2 * kv->rows;
   d.w = kv->a;
   d.err = kv->err;
-#define XP_KV(HD_, F8_, WR_, WK_, NST_, PARTS_)                                                  \
-  hipLaunchKernelGGL((k_kv_attn<HD_, F8_, WR_, WK_, NST_, PARTS_>), dim3(shares),                \
-                     dim3((WR_) * (WK_) * kWave), 0, st, d)
-  // stages: what leaves room for kv_wgs workgroups in 160 KB (NS_ for 32 rows, N2_ for
-  // 64, N1_ above).  Two bf16 parts of the numerators where a bf16 cache is read by
-  // so few rows that memory bounds the call; an 8-bit V is coarser than one part.
-#define XP_KV_R(HD_, F8_, NS_, N2_, N1_)                                                         \
-  do {                                                                                           \
-    if (R == 32) XP_KV(HD_, F8_, 1, 2, NS_, F8_ ? 1 : 2);                                        \
-    else if (R == 64) XP_KV(HD_, F8_, 2, 2, N2_, F8_ ? 1 : 2);                                   \
-    else if (R == 128) XP_KV(HD_, F8_, 4, 2, N1_, 1);                                            \
-    else XP_KV(HD_, F8_, 8, 1, N1_, 1);                                                          \
-  } while (0)
-  const bool f8 = kv->dtype == XP_E4M3;
-  if (kv->hd == 128) {
-    if (f8) XP_KV_R(128, true, 2, 4, 8);
-    else XP_KV_R(128, false, 2, 2, 4);
-  } else {
-    if (f8) XP_KV_R(64, true, 2, 4, 8);
-    else XP_KV_R(64, false, 2, 4, 8);
+  const bool wide = kv->hd == 128;
+  if (a.groups == 0) {
+    d.list = kv->a.list[0];
+    if ((e = launch_list(kv, R[0], d, st)) != hipSuccess) return e;
+    const dim3 grid(kv_shares(kv, R[0]) - 1, R[0] * kv->hd / 1024);
+    if (wide) hipLaunchKernelGGL(k_kv_join<128>, grid, dim3(256), 0, st, d, R[0]);
+    else hipLaunchKernelGGL(k_kv_join<64>, grid, dim3(256), 0, st, d, R[0]);
+    return hipGetLastError();
   }
-#undef XP_KV_R
-#undef XP_KV
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  if (a.groups > 0) {
-    const int rpb = 1024 / kv->hd;
-    const dim3 grid((unsigned)(((int64_t)a.total_q * kv->nh + rpb - 1) / rpb));
-    if (kv->hd == 128)
-      hipLaunchKernelGGL(k_kv_join_rows<128>, grid, dim3(256), 0, st, d, R, a.n, a.cu_q);
-    else
-      hipLaunchKernelGGL(k_kv_join_rows<64>, grid, dim3(256), 0, st, d, R, a.n, a.cu_q);
-  } else {
-    const dim3 grid(shares - 1, R * kv->hd / 1024);
-    if (kv->hd == 128) hipLaunchKernelGGL(k_kv_join<128>, grid, dim3(256), 0, st, d, R);
-    else hipLaunchKernelGGL(k_kv_join<64>, grid, dim3(256), 0, st, d, R);
+  for (int k = lists - 1; k >= 0; --k) {          // the prefixes, then the sequences' own keys
+    d.list = kv->a.list[k];
+    d.part0 = k * kv->rows;
+    if ((e = launch_list(kv, R[k], d, st)) != hipSuccess) return e;
   }
+  KvJoin jn{};
+  jn.R[0] = R[0];
+  jn.R[1] = R[1];
+  jn.part0 = lists == 2 ? kv->rows : 0;
+  jn.n = a.n;
+  jn.one = lists == 1;
+  const int rpb = 1024 / kv->hd;
+  const dim3 grid((unsigned)(((int64_t)a.total_q * kv->nh + rpb - 1) / rpb));
+  if (wide) hipLaunchKernelGGL(k_kv_join_rows<128>, grid, dim3(256), 0, st, d, jn);
+  else hipLaunchKernelGGL(k_kv_join_rows<64>, grid, dim3(256), 0, st, d, jn);
   return hipGetLastError();
 }
 
