@@ -1190,9 +1190,9 @@ static hipError_t launch_list(const xp_kv* kv, int R, const KvDev& d, hipStream_
 hipError_t launch_kv_attn(const xp_kv* kv, const KvAttnArgs& a, hipStream_t st) {
   // row tiles of the sequences, and of the groups.  One list for both unless the
   // groups' are the largest, where products bound the call: a short sequence's
-  // rows in such tiles cost more than a second launch.  32 blocks of one behind 8192
-  // keys (tiles of 128 rows): @A; 60 of 16 behind 500 .. 12000
-  // (tiles of 256): @B.
+  // rows in such tiles cost more than a second launch.  32 single tokens behind 8192 keys
+  // (tiles of 128 rows): one list 53 us, two 61; 60 blocks of 16 behind 500 .. 12000
+  // (tiles of 256): 239 and 218.
   const int64_t rows = (int64_t)a.max_q * kv->grp;
   int R[2] = {kv_rows(rows), 0};
   if (a.groups > 0) R[1] = kv_rows(std::max(rows, (int64_t)a.total_q / a.groups * kv->grp));
