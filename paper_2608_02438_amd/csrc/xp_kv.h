@@ -26,11 +26,12 @@ constexpr int kKvMaxRows = 256;      // query rows (token, head of the group) of
 // b0 + j - n1).
 struct KvEntry {
   int32_t tok0, row0, nrows, seq;    // seq: the row of the block table
-  int32_t p0;                        // position of token tok0 (a sequence's rows)
+  int32_t p0;                        // position of token tok0; of several sequences the least
   int32_t prefix;                    // 1: rows of several sequences, positions from pos[]
   int32_t floor, ceil;
   int32_t s, lo, hi, tiles;
-  int32_t a0, n1, b0, pad;
+  int32_t a0, n1, b0;
+  int32_t p1;                        // the greatest position of several sequences
 };
 constexpr int kKvEntryInts = sizeof(KvEntry) / 4;
 

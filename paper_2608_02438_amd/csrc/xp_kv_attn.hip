@@ -271,8 +271,8 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d) {
         x.nrows = imin((first(s1) - x.tok0) * d.grp - x.row0, R);
         x.prefix = 1;
         x.ceil = glen[i - ns];
-        pa = gmin[i - ns];
-        pb = gmax[i - ns];
+        pa = x.p0 = gmin[i - ns];
+        pb = x.p1 = gmax[i - ns];
       }
       x.hi = d.causal ? imin(x.ceil, pb + 1) : x.ceil;
       x.lo = d.window > 0 ? imax(pa - d.window + 1, x.floor) : x.floor;
@@ -506,6 +506,13 @@ __device__ __forceinline__ void kv_dma_nt(const char* base, uint32_t lp, uint32_
   }
 }
 
+// the upper 32 lanes of a and the lower ones of b change places
+__device__ __forceinline__ void swap_halves(uint32_t& a, uint32_t& b) {
+  const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+  a = r[0];
+  b = r[1];
+}
+
 // A row's view of the keys: [lo, lo + n) and [floor, floor + s).
 struct KvSees {
   int lo, floor;
@@ -587,7 +594,6 @@ __global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
   const bool rv = rr < nrows;
   u32x4 qf[NKS];
   KvSees sees;
-  int pmin, pmax;
   {
     const int row = row0 + (rv ? rr : 0), tk = row / d.grp;
     const int64_t tok = tok0 + tk;
@@ -600,18 +606,12 @@ __global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
     const int lo = d.window > 0 ? imax(p - d.window + 1, kfloor) : kfloor;
     sees = KvSees{lo, kfloor, (uint32_t)imax(hi - lo, 0),
                   d.window > 0 ? (uint32_t)imax(imin(d.sinks, hi) - kfloor, 0) : 0u};
-    pmin = rv ? p : 0x7fffffff;
-    pmax = rv ? p : -0x7fffffff;
   }
-  // keys that every row of the wave sees: [kfloor or wlo, whi), and [kfloor, wsink)
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    pmin = imin(pmin, __shfl_xor(pmin, o, kWave));
-    pmax = imax(pmax, __shfl_xor(pmax, o, kWave));
-  }
-  pmin = __builtin_amdgcn_readfirstlane(pmin);
-  pmax = __builtin_amdgcn_readfirstlane(pmax);
-  const int whi = d.causal ? imin(pmin < 0x7fffffff ? pmin + 1 : pmin, kceil) : kceil;
+  // keys that every row of the wave sees: [kfloor or wlo, whi), and [kfloor, wsink);
+  // rows of several sequences: that every one of the group's does
+  const int pmin = p0 + (prefix ? 0 : (row0 + 32 * wr) / d.grp);
+  const int pmax = prefix ? en[15] : p0 + (row0 + imin(32 * wr + 31, nrows - 1)) / d.grp;
+  const int whi = d.causal ? imin(pmin + 1, kceil) : kceil;
   const int wlo = d.window > 0 ? imax(pmax - d.window + 1, kfloor) : kfloor;
   const int wsink = d.window > 0 ? d.sinks : 0;
   const float scale2 = d.scale2 * (F8 && d.k_scale != nullptr ? d.k_scale[kvh] : 1.f);
@@ -623,13 +623,12 @@ __global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
   const uint32_t page_bytes = (uint32_t)(d.nkv * RB) << d.logP;
   const int kin = imax(klo, kfloor);              // from here to khi, or to ks_, some row sees all
   uint32_t bad = 0;                               // a page outside the cache was asked for
-  int pg[NG];
-  auto pages = [&](int t) {                       // page ids of the wave's rows of tile t
+  auto pages = [&](int t, int (&pg)[NG]) {        // page ids of the wave's rows of tile t
 #pragma unroll
     for (int g = 0; g < NG; ++g)
       pg[g] = tb[imin((tile_key(t) + 16 * ((wave * NG + g) & 3)) >> d.logP, d.cols - 1)];
   };
-  auto issue = [&](int t, int slot) __attribute__((always_inline)) {
+  auto issue = [&](int t, int slot, const int (&pg)[NG]) __attribute__((always_inline)) {
     const int k0 = tile_key(t);
     const bool inner = ((k0 >= kin) & (k0 + kKvTile <= khi)) | ((k0 >= kfloor) & (k0 + kKvTile <= ks_));
     u32x4* stage = lds + slot * SH::kStage + wave * (NG * 16 * CPR);   // its rows of K, then V
@@ -674,13 +673,13 @@ __global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
   // loads still under way when iteration t has what it needs: K of tile t + 1, V of t
   constexpr int kWaitV = (NST - 2) * PER, kWaitK = (NB == 1 ? NST - 2 : NST - 3) * PER;
   static_assert(kWaitK >= 0, "stages");
-  pages(j);
+  int pg[NG], pg0[NST][NG];
+#pragma unroll
+  for (int t = 0; t < NST; ++t) pages(j + imin(t, nj - 1), pg0[t]);
+  pages(j + imin(NST - 1 + ahead, nj - 1), pg);
 #pragma unroll
   for (int t = 0; t < NST; ++t)
-    if (t < nj && t < NST - 1 + ahead) {          // whole wave
-      issue(j + t, t);
-      pages(j + imin(t + 1, nj - 1));
-    }
+    if (t < nj && t < NST - 1 + ahead) issue(j + t, t, pg0[t]);   // whole wave
 
   float m_run = -INFINITY, l_run = 0.f;           // the row's; l of this half's keys
   floatx16 o[ND];
@@ -867,8 +866,8 @@ __global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     if (t + NST - 1 + ahead < nj) {
-      issue(j + t + NST - 1 + ahead, ahead ? stage : (stage == 0 ? NST - 1 : stage - 1));
-      pages(j + imin(t + NST + ahead, nj - 1));
+      issue(j + t + NST - 1 + ahead, ahead ? stage : (stage == 0 ? NST - 1 : stage - 1), pg);
+      pages(j + imin(t + NST + ahead, nj - 1), pg);
     }
   };
   // K of the first tile landed
@@ -937,17 +936,19 @@ __global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
     // O = 2^(m0 - M) O0 + 2^(m1 - M) O1, l likewise, M = max(m0, m1)
     __syncthreads();                              // every wave's reads of the ring done
     float* mg = reinterpret_cast<float*>(lds) + wr * kMerge + lane;
+    floatx4* mo = reinterpret_cast<floatx4*>(mg - lane + 2 * kWave) + lane;
     if (wk == 1) {
 #pragma unroll
       for (int db = 0; db < ND; ++db)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) mg[(16 * db + i) * kWave] = o[db][i];
-      mg[HD / 2 * kWave] = m_run;
-      mg[(HD / 2 + 1) * kWave] = l_run;
+        for (int i = 0; i < 16; i += 4)
+          mo[(4 * db + i / 4) * kWave] = floatx4{o[db][i], o[db][i + 1], o[db][i + 2], o[db][i + 3]};
+      mg[0] = m_run;
+      mg[kWave] = l_run;
     }
     __syncthreads();
     if (wk == 0) {
-      const float m1 = mg[HD / 2 * kWave], l1 = mg[(HD / 2 + 1) * kWave];
+      const float m1 = mg[0], l1 = mg[kWave];
       const float M = fmaxf(m_run, m1), Ms = M == -INFINITY ? 0.f : M;
       const float w0 = __builtin_amdgcn_exp2f(m_run - Ms), w1 = __builtin_amdgcn_exp2f(m1 - Ms);
       m_run = M;
@@ -955,7 +956,7 @@ __global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
 #pragma unroll
       for (int db = 0; db < ND; ++db)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) o[db][i] = w0 * o[db][i] + w1 * mg[(16 * db + i) * kWave];
+        for (int i = 0; i < 16; ++i) o[db][i] = w0 * o[db][i] + w1 * mo[(4 * db + i / 4) * kWave][i % 4];
     }
   }
   // ---- results: the rows themselves, or what k_kv_join(_rows) adds up ----
@@ -968,15 +969,19 @@ __global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
     if (whole && d.groups == 0) {
       const float inv = l_run == 0.f
           ? 0.f : (F8 && d.v_scale != nullptr ? d.v_scale[kvh] : 1.f) / l_run;
-      uint16_t* op = (rv ? d.out + tok * d.out_ld + (int64_t)head * HD : (uint16_t*)d.w.dump) + 4 * h;
+      uint16_t* op = (rv ? d.out + tok * d.out_ld + (int64_t)head * HD : (uint16_t*)d.w.dump) + 8 * h;
 #pragma unroll
       for (int db = 0; db < ND; ++db)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 4; i += 2) {
           const floatx16& y = o[db];
-          *reinterpret_cast<uint2*>(op + 32 * db + 8 * i) =
-              uint2{pk_bf16(y[4 * i] * inv, y[4 * i + 1] * inv),
-                    pk_bf16(y[4 * i + 2] * inv, y[4 * i + 3] * inv)};
+          uint32_t w[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) w[k] = pk_bf16(y[4 * i + 2 * k] * inv, y[4 * i + 2 * k + 1] * inv);
+          // 16 bytes a lane: dims 8 i + 0..7 here, 8 (i + 1) + 0..7 in lane + 32
+          swap_halves(w[0], w[2]);
+          swap_halves(w[1], w[3]);
+          *reinterpret_cast<u32x4*>(op + 32 * db + 8 * i) = u32x4{w[0], w[1], w[2], w[3]};
         }
       if (d.lse != nullptr) {
         const float y = l_run == 0.f
