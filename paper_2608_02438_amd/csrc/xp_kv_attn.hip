@@ -628,9 +628,12 @@ __global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
     for (int g = 0; g < NG; ++g)
       pg[g] = tb[imin((tile_key(t) + 16 * ((wave * NG + g) & 3)) >> d.logP, d.cols - 1)];
   };
-  auto issue = [&](int t, int slot, const int (&pg)[NG]) __attribute__((always_inline)) {
+  // tile t to a slot; a segment's first tiles by the general way alone (a tile all of
+  // whose keys some row sees needs no test of its keys, but costs a copy of the code)
+  auto issue = [&](auto first, int t, int slot, const int (&pg)[NG]) __attribute__((always_inline)) {
     const int k0 = tile_key(t);
-    const bool inner = ((k0 >= kin) & (k0 + kKvTile <= khi)) | ((k0 >= kfloor) & (k0 + kKvTile <= ks_));
+    const bool inner = !decltype(first)::value &&
+        (((k0 >= kin) & (k0 + kKvTile <= khi)) | ((k0 >= kfloor) & (k0 + kKvTile <= ks_)));
     u32x4* stage = lds + slot * SH::kStage + wave * (NG * 16 * CPR);   // its rows of K, then V
     if (inner) {
 #pragma unroll
@@ -677,9 +680,13 @@ __global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
 #pragma unroll
   for (int t = 0; t < NST; ++t) pages(j + imin(t, nj - 1), pg0[t]);
   pages(j + imin(NST - 1 + ahead, nj - 1), pg);
+  // The query rows are waited for here: with loads to LDS under way the compiler waits
+  // for all of them before it uses a register that was loaded.
+#pragma unroll
+  for (int ks = 0; ks < NKS; ++ks) asm volatile("" : "+v"(qf[ks]));
 #pragma unroll
   for (int t = 0; t < NST; ++t)
-    if (t < nj && t < NST - 1 + ahead) issue(j + t, t, pg0[t]);   // whole wave
+    if (t < nj && t < NST - 1 + ahead) issue(std::true_type{}, j + t, t, pg0[t]);   // whole wave
 
   float m_run = -INFINITY, l_run = 0.f;           // the row's; l of this half's keys
   floatx16 o[ND];
@@ -866,7 +873,7 @@ __global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     if (t + NST - 1 + ahead < nj) {
-      issue(j + t + NST - 1 + ahead, ahead ? stage : (stage == 0 ? NST - 1 : stage - 1), pg);
+      issue(std::false_type{}, j + t + NST - 1 + ahead, ahead ? stage : (stage == 0 ? NST - 1 : stage - 1), pg);
       pages(j + imin(t + NST + ahead, nj - 1), pg);
     }
   };
