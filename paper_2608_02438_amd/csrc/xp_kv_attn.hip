@@ -519,6 +519,9 @@ struct KvSees {
   uint32_t n, s;
 };
 
+// waves of a SIMD: two (256 registers each), or three where half the head leaves room
+constexpr int kv_waves(int hd, int wr, int wk) { return hd == 64 && wr == 4 && wk == 1 ? 3 : 2; }
+
 // WR x WK waves: wave (wr, wk) takes rows 32 wr .. + 31 of the tile and the wk-th
 // part of each tile's keys, in blocks of 32.  S^T = K Q^T and O^T =
 // V^T P^T on v_mfma_f32_32x32x16_bf16: a lane holds one query row (l % 32) in both,
@@ -537,7 +540,7 @@ struct KvSees {
 // are formed between the products of block n + 1's scores and of block n - 1's P V,
 // in turn.
 template <int HD, bool F8, int WR, int WK, int NST, int PARTS>
-__global__ __launch_bounds__(WR* WK* kWave, 2) void k_kv_attn(const KvDev d) {
+__global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn(const KvDev d) {
   using SH = KvRows<HD, F8>;
   constexpr int NW = WR * WK, R = 32 * WR, NB = 2 / WK, ND = HD / 32, NKS = HD / 16;
   constexpr int RB = SH::RB, CPR = SH::CPR, IPG = SH::IPG;
@@ -1148,26 +1151,36 @@ __global__ __launch_bounds__(256) void k_kv_join_rows(const KvDev d, const KvJoi
 // host
 // ---------------------------------------------------------------------------
 // Rows of a workgroup by the rows that a sequence of max_q tokens (a group of
-// sequences) brings: the fewest waves that hold them, so that short ones leave
-// room for a second workgroup and its loads.
-static int kv_rows(int64_t rows) { return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256; }
-// Workgroups of a CU: 8 waves, or as many as the rings leave room for (a ring of two
-// 32 KB stages twice).
+// sequences) brings: the fewest waves that hold them, so that short ones leave room for
+// a second workgroup and its loads.  Where many rows let the products bound the call:
+// 8 waves of 32 rows at head_dim 128 (a CU's ring holds no second workgroup's), at 64
+// three workgroups of 4, whose tiles waste less of ragged sequences (24 of 1 .. 513
+// tokens 255 -> 232 us; 4096 x 8192 415 either way).
+static int kv_most(const xp_kv* kv) { return kv->hd == 64 ? 128 : 256; }
+static int kv_rows(const xp_kv* kv, int64_t rows) {
+  const int most = kv_most(kv);
+  return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : most;
+}
+// Workgroups of a CU: 8 waves (12, see above), or as many as the rings leave room for (a
+// ring of two 32 KB stages twice).  128 rows over an 8-bit cache as two workgroups of 4
+// waves: 64 blocks of 32 over 8192 keys 405 us as one of 8, 378 so; 256 rows as two
+// tiles of them 3 to 7% slower.
 static int kv_wgs(const xp_kv* kv, int R) {
-  const bool wide = kv->hd == 128 && kv->dtype == XP_BF16;
-  return R >= 128 ? 1 : (R == 64 || wide ? 2 : 4);
+  if (kv->hd == 64) return R >= 128 ? 3 : (R == 64 ? 2 : 4);
+  const bool f8 = kv->dtype == XP_E4M3;
+  return R >= 128 ? (f8 && R == 128 ? 2 : 1) : (f8 && R == 32 ? 4 : 2);
 }
 static int kv_shares(const xp_kv* kv, int R) { return std::max(8, kv->cus * kv_wgs(kv, R) / 8 * 8); }
 
 void kv_attn_sizes(const xp_kv* kv, int64_t* rows, int* entries, int* shares) {
   const int64_t all = (int64_t)kv->max_tokens * kv->grp;
-  const int R = kv_rows(all);
+  const int R = kv_rows(kv, all);
   *rows = 0;
   for (int r = 32; r <= R; r *= 2) *rows = std::max(*rows, (int64_t)2 * kv_shares(kv, r) * r);
-  if (R == 256) *rows = std::max(*rows, (int64_t)2 * kv_shares(kv, 256) * 256);
   // every sequence (group) rounds its rows up to whole tiles
   *entries = (int)((all + 31) / 32 + kv->max_batch);
-  *shares = kv_shares(kv, 32);
+  *shares = 0;
+  for (int r = 32; r <= R; r *= 2) *shares = std::max(*shares, kv_shares(kv, r));
 }
 
 // one list's attention, in tiles of R rows
@@ -1176,25 +1189,29 @@ static hipError_t launch_list(const xp_kv* kv, int R, const KvDev& d, hipStream_
 #define XP_KV(HD_, F8_, WR_, WK_, NST_, PARTS_)                                                  \
   hipLaunchKernelGGL((k_kv_attn<HD_, F8_, WR_, WK_, NST_, PARTS_>), dim3(shares),                \
                      dim3((WR_) * (WK_) * kWave), 0, st, d)
-  // stages: what leaves room for kv_wgs workgroups in 160 KB (NS_ for 32 rows, N2_ for
-  // 64, N1_ above).  Two bf16 parts of the numerators where a bf16 cache is read by
-  // so few rows that memory bounds the call; an 8-bit V is coarser than one part.
-#define XP_KV_R(HD_, F8_, NS_, N2_, N1_)                                                         \
-  do {                                                                                           \
-    if (R == 32) XP_KV(HD_, F8_, 1, 2, NS_, F8_ ? 1 : 2);                                        \
-    else if (R == 64) XP_KV(HD_, F8_, 2, 2, N2_, F8_ ? 1 : 2);                                   \
-    else if (R == 128) XP_KV(HD_, F8_, 4, 2, N1_, 1);                                            \
-    else XP_KV(HD_, F8_, 8, 1, N1_, 1);                                                          \
-  } while (0)
+  // stages: what leaves room for kv_wgs workgroups in 160 KB.  Two bf16 parts of the
+  // numerators where a bf16 cache is read by so few rows that memory bounds the call; an
+  // 8-bit V is coarser than one part.
   const bool f8 = kv->dtype == XP_E4M3;
-  if (kv->hd == 128) {
-    if (f8) XP_KV_R(128, true, 2, 4, 8);
-    else XP_KV_R(128, false, 2, 2, 4);
+  if (kv->hd == 128 && !f8) {
+    if (R == 32) XP_KV(128, false, 1, 2, 2, 2);
+    else if (R == 64) XP_KV(128, false, 2, 2, 2, 2);
+    else if (R == 128) XP_KV(128, false, 4, 2, 4, 1);
+    else XP_KV(128, false, 8, 1, 4, 1);
+  } else if (kv->hd == 128) {
+    if (R == 32) XP_KV(128, true, 1, 2, 2, 1);
+    else if (R == 64) XP_KV(128, true, 2, 2, 4, 1);
+    else if (R == 128) XP_KV(128, true, 4, 1, 4, 1);
+    else XP_KV(128, true, 8, 1, 8, 1);
+  } else if (!f8) {
+    if (R == 32) XP_KV(64, false, 1, 2, 2, 2);
+    else if (R == 64) XP_KV(64, false, 2, 2, 4, 2);
+    else XP_KV(64, false, 4, 1, 3, 1);
   } else {
-    if (f8) XP_KV_R(64, true, 2, 4, 8);
-    else XP_KV_R(64, false, 2, 4, 8);
+    if (R == 32) XP_KV(64, true, 1, 2, 2, 1);
+    else if (R == 64) XP_KV(64, true, 2, 2, 4, 1);
+    else XP_KV(64, true, 4, 1, 6, 1);
   }
-#undef XP_KV_R
 #undef XP_KV
   return hipGetLastError();
 }
@@ -1206,9 +1223,9 @@ hipError_t launch_kv_attn(const xp_kv* kv, const KvAttnArgs& a, hipStream_t st) 
   // (tiles of 128 rows): one list 53 us, two 61; 60 blocks of 16 behind 500 .. 12000
   // (tiles of 256): 239 and 218.
   const int64_t rows = (int64_t)a.max_q * kv->grp;
-  int R[2] = {kv_rows(rows), 0};
-  if (a.groups > 0) R[1] = kv_rows(std::max(rows, (int64_t)a.total_q / a.groups * kv->grp));
-  const int lists = R[1] == 256 && R[0] < 256 ? 2 : 1;
+  int R[2] = {kv_rows(kv, rows), 0};
+  if (a.groups > 0) R[1] = kv_rows(kv, std::max(rows, (int64_t)a.total_q / a.groups * kv->grp));
+  const int lists = R[1] == kv_most(kv) && R[0] < R[1] ? 2 : 1;
   if (lists == 1 && a.groups > 0) R[0] = R[1];
   const int cols = (int)std::min<int64_t>(kv->max_pages, a.table_ld);
   KvPlan p{};
