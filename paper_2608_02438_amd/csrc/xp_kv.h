@@ -15,7 +15,19 @@ namespace xp {
 constexpr int kKvTile = 64;          // keys of an attention tile
 constexpr int kKvMaxBatch = 4096;    // sequences of a call
 constexpr int kKvMaxLen = 1 << 22;   // keys of a sequence
-constexpr int kKvMaxRows = 256;      // query rows (token, head of the group) of a workgroup
+
+// the last index in [lo, hi) whose a[] is at most x (a[lo] <= x, a non-decreasing)
+template <typename P>
+__device__ __forceinline__ int kv_owner(P a, int lo, int hi, int x) {
+  while (hi - lo > 1) {
+    const int m = (lo + hi) >> 1;
+    if (a[m] <= x) lo = m;
+    else hi = m;
+  }
+  return lo;
+}
+template <typename P>
+__device__ __forceinline__ int kv_owner(P a, int n, int x) { return kv_owner(a, 0, n, x); }
 
 // One row tile of the attention's work list: up to R query rows of one
 // sequence (or of the sequences of one group, for a shared prefix), and the
@@ -68,7 +80,7 @@ struct KvAttnWs {
 
 // Arguments of the attention's kernels.
 struct KvAttnArgs {
-  int n, total_q, max_q;             // max_q: tokens of every sequence where cu_q is NULL
+  int n, total_q, max_q;             // max_q: tokens of the longest sequence; of each without cu_q
   const int32_t* cu_q;
   const int32_t* kv_len;
   int kv_add;                        // added to every kv_len (the layer's own block)

@@ -17,17 +17,6 @@
 
 namespace xp {
 
-// the last index in [lo, hi) whose a[] is at most x (a[lo] <= x, a non-decreasing)
-__device__ __forceinline__ int kv_owner(const int* a, int lo, int hi, int x) {
-  while (hi - lo > 1) {
-    const int m = (lo + hi) >> 1;
-    if (a[m] <= x) lo = m;
-    else hi = m;
-  }
-  return lo;
-}
-__device__ __forceinline__ int kv_owner(const int* a, int n, int x) { return kv_owner(a, 0, n, x); }
-
 struct KvMap {
   int n, logP, cols, n_pages, max_slots;
   const int32_t* lens;

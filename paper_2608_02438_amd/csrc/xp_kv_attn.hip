@@ -107,18 +107,6 @@ __device__ __forceinline__ int block_scan(int v, int* lds, int* total) {
   return before + x - v;
 }
 
-// the last index in [0, n) whose a[] is at most x (a[0] <= x, a non-decreasing)
-template <typename P>
-__device__ __forceinline__ int last_at_most(P a, int n, int x) {
-  int lo = 0, hi = n;
-  while (hi - lo > 1) {
-    const int m = (lo + hi) >> 1;
-    if (a[m] <= x) lo = m;
-    else hi = m;
-  }
-  return lo;
-}
-
 struct KvPlan {
   int n, total_q, max_q, kv_add, cap, grp, nkv, causal, window, sinks, groups, entries;
   int R[2], shares[2];               // of each list
@@ -214,7 +202,8 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d) {
       }
     __syncthreads();
   }
-  // entries of each item
+  // entries of each item; where token ranges overlap, as many as the tokens could have
+  const int most = (items > n ? 2 : 1) * d.entries;
   int T = 0;
   for (int i0 = 0; i0 < items; i0 += kPlanThreads) {
     const int i = i0 + tid;
@@ -233,11 +222,11 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d) {
     int all;
     const int before = block_scan(nt, red, &all);
     if (i < items) off[i] = T + before;
-    T += all;
+    T = T > most ? T : T + all;                   // stays far below 2^31
   }
   if (tid == 0) off[items] = T;
-  if (T > (items > n ? 2 : 1) * d.entries) {      // token ranges that overlap
-    T = (items > n ? 2 : 1) * d.entries;
+  if (T > most) {
+    T = most;
     bad |= XP_DEVERR_LENGTH;
   }
   __syncthreads();
@@ -249,7 +238,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d) {
     const int e = e0 + tid;
     int units = 0;
     if (e < T) {
-      const int i = last_at_most(off, items, e);
+      const int i = kv_owner((const int*)off, items, e);
       KvEntry x{};
       x.row0 = (e - off[i]) * R;
       int pa, pb;                                 // positions of the tile's tokens
@@ -309,8 +298,8 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d) {
     KvShare r{};
     r.f = (int64_t)s * S < W ? s * S : W;
     if (r.f < W) {
-      r.e = T <= kPlanCum ? last_at_most((const int*)cums, T, r.f)
-                          : last_at_most((const int32_t*)out.cum, T, r.f);
+      r.e = T <= kPlanCum ? kv_owner((const int*)cums, T, r.f)
+                          : kv_owner((const int32_t*)out.cum, T, r.f);
       const int units = out.ent[r.e].tiles + kSegUnits;
       const int in = r.f - (T <= kPlanCum ? cums[r.e] : out.cum[r.e]);
       r.kvh = in / units;
@@ -1133,7 +1122,7 @@ __global__ __launch_bounds__(256) void k_kv_join_rows(const KvDev d, const KvJoi
     const int R = jn.R[k], S = l.hdr[1];
     const int lr = (tok - (k == 1 ? d.w.gtok[g] : d.w.stok[b])) * d.grp + hg;
     const int e = l.off[k == 1 ? (jn.one ? jn.n : 0) + g : b] + lr / R;
-    if (e >= l.hdr[2]) continue;                  // dropped: token ranges that overlap
+    if (lr < 0 || e >= l.hdr[2]) continue;        // token ranges that overlap
     const int tiles = l.ent[e].tiles;
     const int a = l.cum[e] + kvh * (tiles + kSegUnits) + kSegUnits;
     if (a / S == (a + tiles - 1) / S) {
@@ -1240,7 +1229,7 @@ hipError_t launch_kv_attn(const xp_kv* kv, const KvAttnArgs& a, hipStream_t st) 
   p.window = a.window;
   p.sinks = a.sinks;
   p.groups = a.groups;
-  p.entries = kv->entries;
+  p.entries = (int)((int64_t)a.total_q * kv->grp / 32 + a.n);   // of a list: no more fit the tokens
   for (int k = 0; k < lists; ++k) {
     p.R[k] = R[k];
     p.shares[k] = kv_shares(kv, R[k]);

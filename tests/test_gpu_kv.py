@@ -495,6 +495,68 @@ def test_shared_tokens_behind_the_last_sequence_stay():
     kv.close()
 
 
+@pytest.mark.parametrize("hd,cache", [(128, "bf16"), (64, "bf16"), (128, "e4m3"), (64, "e4m3")])
+def test_shared_prefixes_of_many_rows(hd, cache):
+    """Blocks whose groups fill the largest row tiles and whose own rows do not:
+    prefixes and own keys in work lists of their own; captured, replayed with new
+    lengths, a request outside the groups."""
+    import torch
+    ql = [16, 9, 16, 16, 1, 16, 16, 0, 16, 16, 16, 16, 5]
+    own = [40, 3, 0, 700, 20, 16, 90, 0, 17, 130, 64, 5, 333]
+    pre = [900] * 7 + [640] * 5 + [0]
+    kv_len = [max(p + o, q) for p, o, q in zip(pre, own, ql)]
+    c = Call(72 + hd, kv_len, ql, heads=8, n_kv=2, hd=hd, cache=cache, P=16,
+             groups=[(0, 7, 896), (7, 12, 640)])
+    kv = c.device(shared=True)
+    rows = c.total // 2 * 4
+    assert rows > 256 and max(ql) * 4 <= 64                   # tiles of both sizes
+    out = torch.empty_like(c.dq)
+    for m in (dict(causal=True), dict(causal=False), dict(causal=True, window=100, sinks=20),
+              dict(causal=True, window=800)):
+        print(f"shared, many rows: hd={hd} {cache} {m}", flush=True)
+        c.run(kv, shared=True, out=out, **m)
+        assert kv.device_errors() == 0
+        c.check(out, parts=parts_of(rows, cache), **m)
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        c.run(kv, shared=True, out=out)
+    for cut in (0, 7, 0):
+        c.kv = [max(x - cut, 0) if p == 0 or x - cut >= p else x for x, p in zip(kv_len, pre)]
+        c.dkv.copy_(_i32(c.kv))
+        out.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        c.check(out, causal=True, parts=parts_of(rows, cache))
+        assert c.run(kv, shared=True).equal(out)
+    kv.close()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_token_ranges_that_overlap_many_times(hd):
+    """Ranges that count far more rows than there are tokens are cut to what the work
+    lists hold, reported, and leave the handle as it was."""
+    import torch
+    from paper_2608_02438_amd import xpress as X
+    n, tokens = 600, 512
+    c = Call(75 + hd, [40] * n, [1] * tokens + [0] * (n - tokens), heads=8, n_kv=1, hd=hd, P=16,
+             groups=[(0, 300, 16), (300, 600, 32)], spare=5)
+    kv = c.device(shared=True)
+    good, alone = c.run(kv, shared=True), c.run(kv)
+    assert kv.device_errors() == 0
+    back = _i32([tokens if b % 2 else 0 for b in range(n + 1)])
+    down = _i32([tokens - tokens * b // n for b in range(n + 1)])
+    for cu, max_q in ((back, 1), (back, tokens), (down, 1)):
+        for shared in (False, True):
+            print(f"overlapping ranges: hd={hd} max_q={max_q} shared={shared}", flush=True)
+            c.run(kv, shared=shared, cu_q=cu, max_q=max_q)
+            torch.cuda.synchronize()
+        assert (kv.device_errors() & X.XP_DEVERR_LENGTH) == (X.XP_DEVERR_LENGTH if cu is back else 0)
+    assert c.run(kv, shared=True).equal(good) and c.run(kv).equal(alone)
+    assert kv.device_errors() == 0
+    kv.close()
+
+
 # ---------------------------------------------------------------------------
 # refusals
 # ---------------------------------------------------------------------------
