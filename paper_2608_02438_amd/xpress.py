@@ -566,6 +566,8 @@ class PagedKV:
             if cu_q is not None:
                 raise ValueError("max_q is required with cu_q")
             max_q = tokens // n if n else 0
+        elif cu_q is not None:
+            max_q = min(max_q, tokens)                        # no request has more
         if out is None:
             out = torch.empty((tokens, self.n_heads, self.head_dim), dtype=torch.bfloat16,
                               device=self.device)
@@ -588,7 +590,7 @@ class PagedKV:
                stream=None):
         """Attention of the tokens q [tokens][n_heads][head_dim] over their
         requests' pages (xp_kv_attn); without cu_q every request has the same
-        number of them.  Returns out (allocated when None)."""
+        number of them, with it at most max_q (any upper bound).  Returns out (allocated when None)."""
         return self._attend("xp_kv_attn", (), q, k_cache, v_cache, table, kv_len, cu_q, max_q,
                             causal, window, sinks, scale, k_scale, v_scale, out, lse, stream)
 

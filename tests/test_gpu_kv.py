@@ -242,6 +242,14 @@ def test_attend_max_q_costs_time_only(rows):
     kv.close()
 
 
+def test_attend_takes_any_upper_bound_of_the_tokens():
+    """A bound above the handle's own (a configuration's longest prompt)."""
+    c = Call(43, [90, 30], [20, 7], heads=4, n_kv=2)
+    kv = c.device()
+    assert c.run(kv, max_q=100000).equal(c.run(kv, max_q=c.total))
+    kv.close()
+
+
 def test_attend_uniform_lengths_without_cu_q():
     c = Call(11, [40, 300, 71, 16], [16] * 4, heads=4, n_kv=2)
     kv = c.device()
