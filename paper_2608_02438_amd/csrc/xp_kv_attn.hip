@@ -8,7 +8,7 @@
 //   (window == 0 or j > p - window or j < sinks);
 // o = sum_j softmax_j(scale q.k_j) v_j over these, 0 if there are none.
 //
-// Work list (k_kv_plan).  The rows of a KV head's group, (token, head) pairs,
+// Work list (k_kv_plan, plan_own).  The rows of a KV head's group, (token, head) pairs,
 // are cut into tiles of up to R rows; a tile walks the 64-key tiles that any of
 // its rows sees.  (row tile, KV head, key tile) in this order is a list of units
 // that k_kv_attn cuts into equal shares, one a workgroup, whatever the lengths:
@@ -45,7 +45,20 @@ __device__ __forceinline__ float fsum_xor32(float x) {
 __device__ __forceinline__ int imin(int a, int b) { return a < b ? a : b; }
 __device__ __forceinline__ int imax(int a, int b) { return a > b ? a : b; }
 
-// What the kernels read of a call.
+__device__ __forceinline__ int clampi(int x, int lo, int hi) { return imin(imax(x, lo), hi); }
+
+// What the work lists follow from.
+struct KvPlan {
+  int n, total_q, max_q, kv_add, cap, grp, nkv, causal, window, sinks, groups;
+  int entries;                       // that a list holds at most
+  int R[2], shares[2];               // of each list
+  const int32_t* cu_q;
+  const int32_t* kv_len;
+  const int32_t* group_start;
+  const int32_t* shared_len;
+};
+
+// What the attention's kernels read of a call.
 struct KvDev {
   const uint16_t* q;
   int64_t q_ld;
@@ -62,6 +75,7 @@ struct KvDev {
   int causal, window, sinks;
   float scale2;                      // scale log2(e)
   int total_q, groups;
+  KvPlan p;
   KvList list;                       // the work
   int64_t part0, row0;               // first partial row of its cut segments; of whole ones
   KvAttnWs w;
@@ -71,9 +85,10 @@ struct KvDev {
 // ---------------------------------------------------------------------------
 // The work lists, one workgroup each.  Items of the first are the sequences (with
 // their keys behind a shared prefix, if they have one); the groups (their prefixes)
-// follow them or are the items of a second list.  The items' row tiles, the entries' key ranges, the sums
-// of both, and where each share begins.  Bound by latency: a few block scans and one
-// search per entry and share.
+// follow them or are the items of a second list.  The items' row tiles, the entries'
+// key ranges, the sums of both, and where each share begins.  Bound by latency, a few
+// block scans and one search per entry and share: 64 sequences 8 us, 60 behind five
+// prefixes 10.5.  (Small calls: plan_own.)
 // ---------------------------------------------------------------------------
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanWaves = kPlanThreads / kWave;
@@ -107,21 +122,46 @@ __device__ __forceinline__ int block_scan(int v, int* lds, int* total) {
   return before + x - v;
 }
 
-struct KvPlan {
-  int n, total_q, max_q, kv_add, cap, grp, nkv, causal, window, sinks, groups, entries;
-  int R[2], shares[2];               // of each list
-  const int32_t* cu_q;
-  const int32_t* kv_len;
-  const int32_t* group_start;
-  const int32_t* shared_len;
-  KvAttnWs w;
-  uint32_t* err;
-};
-
-__device__ __forceinline__ int clampi(int x, int lo, int hi) { return imin(imax(x, lo), hi); }
+// first token of sequence b
+__device__ __forceinline__ int plan_first(const KvPlan& d, int b) {
+  return d.cu_q != nullptr ? clampi(d.cu_q[b], 0, d.total_q) : imin(b * d.max_q, d.total_q);
+}
+// its keys
+__device__ __forceinline__ int plan_keys(const KvPlan& d, int b, uint32_t& bad) {
+  const int x = d.kv_len[b];
+  if (x < 0 || x > d.cap - d.kv_add) bad |= XP_DEVERR_LENGTH;
+  return clampi(x, 0, imax(d.cap - d.kv_add, 0)) + imin(d.kv_add, d.cap);
+}
+// the key tiles of an entry whose tokens have positions pa .. pb
+__device__ __forceinline__ void plan_tiles(const KvPlan& d, KvEntry& x, int pa, int pb) {
+  x.hi = d.causal ? imin(x.ceil, pb + 1) : x.ceil;
+  x.lo = d.window > 0 ? imax(pa - d.window + 1, x.floor) : x.floor;
+  x.s = d.window > 0 ? imax(imin(d.sinks, x.hi), x.floor) : x.floor;
+  const bool sink = x.s > x.floor;
+  const int fl = x.floor / kKvTile;
+  x.a0 = sink ? fl : x.lo / kKvTile;
+  const int a1 = sink ? (x.s + kKvTile - 1) / kKvTile : x.a0;
+  x.n1 = a1 - x.a0;
+  x.b0 = imax(x.lo / kKvTile, a1);
+  const int b1 = x.hi > x.lo ? (x.hi + kKvTile - 1) / kKvTile : 0;
+  // no row sees a key: one tile, wholly masked, writes the zeros
+  x.tiles = imax(x.n1 + imax(b1 - x.b0, 0), 1);
+}
+// the entry of the rows from x.row0 on of sequence i, its tk tokens from t0 on
+__device__ __forceinline__ void plan_rows(const KvPlan& d, KvEntry& x, int i, int t0, int tk,
+                                          int keys, int floor, int R) {
+  x.tok0 = t0;
+  x.seq = i;
+  x.nrows = imin(tk * d.grp - x.row0, R);
+  x.ceil = keys;
+  x.p0 = keys - tk;
+  x.floor = floor;
+  plan_tiles(d, x, x.p0 + x.row0 / d.grp, x.p0 + (x.row0 + x.nrows - 1) / d.grp);
+}
 
 template <bool SHARED>
-__global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d) {
+__global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d, const KvAttnWs w,
+                                                                uint32_t* __restrict__ err) {
   __shared__ int off[(SHARED ? 2 : 1) * kKvMaxBatch + 1];   // entries before each item
   __shared__ int floors[SHARED ? kKvMaxBatch : 1];   // keys of the sequence that its prefix holds
   __shared__ int gmin[SHARED ? kKvMaxBatch : 1];  // a group's positions: least and greatest
@@ -135,16 +175,10 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d) {
   const int ns = second ? 0 : n;                  // items that are sequences
   const int items = ns + (SHARED && (second || gridDim.x == 1) ? d.groups : 0);
   const int R = d.R[second], shares = d.shares[second];
-  const KvList out = d.w.list[second];
+  const KvList out = w.list[second];
   uint32_t bad = 0;
-  auto first = [&](int b) {                       // first token of sequence b
-    return d.cu_q != nullptr ? clampi(d.cu_q[b], 0, d.total_q) : imin(b * d.max_q, d.total_q);
-  };
-  auto keys = [&](int b) {                        // its keys
-    const int x = d.kv_len[b];
-    if (x < 0 || x > d.cap - d.kv_add) bad |= XP_DEVERR_LENGTH;
-    return clampi(x, 0, imax(d.cap - d.kv_add, 0)) + imin(d.kv_add, d.cap);
-  };
+  auto first = [&](int b) { return plan_first(d, b); };
+  auto keys = [&](int b) { return plan_keys(d, b, bad); };
   auto tokens = [&](int b, int t0) { return imax(first(b + 1) - t0, 0); };
   auto members = [&](int g, int& s0, int& s1) {
     s0 = clampi(d.group_start[g], 0, n);
@@ -154,12 +188,12 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d) {
     for (int b = tid; b < n; b += kPlanThreads) {
       floors[b] = 0;
       if (!second) {
-        d.w.sgrp[b] = -1;
-        d.w.stok[b] = first(b);
+        w.sgrp[b] = -1;
+        w.stok[b] = first(b);
       }
     }
     if (!second)                                  // tokens of no sequence
-      for (int t = tid; t < d.total_q; t += kPlanThreads) d.w.tseq[t] = -1;
+      for (int t = tid; t < d.total_q; t += kPlanThreads) w.tseq[t] = -1;
     __syncthreads();
     // a wave per group: its members' positions, and a prefix that none is shorter than
     for (int g = wave; g < d.groups; g += kPlanWaves) {
@@ -183,21 +217,21 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d) {
       if (want != len) bad |= XP_DEVERR_LENGTH;
       for (int b = s0 + lane; b < s1; b += kWave) {
         floors[b] = len;
-        if (!second) d.w.sgrp[b] = len > 0 ? g : -1;
+        if (!second) w.sgrp[b] = len > 0 ? g : -1;
       }
       if (lane == 0) {
         gmin[g] = pmin;
         gmax[g] = pmax;
         glen[g] = len;
-        if (!second) d.w.gtok[g] = first(s0);
+        if (!second) w.gtok[g] = first(s0);
       }
     }
     if (!second)
       for (int b = wave; b < n; b += kPlanWaves) {   // every token's position and sequence
         const int t0 = first(b), ql = tokens(b, t0), p0 = keys(b) - ql;
         for (int i = lane; i < ql; i += kWave) {
-          d.w.pos[t0 + i] = p0 + i;
-          d.w.tseq[t0 + i] = b;
+          w.pos[t0 + i] = p0 + i;
+          w.tseq[t0 + i] = b;
         }
       }
     __syncthreads();
@@ -243,15 +277,8 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d) {
       x.row0 = (e - off[i]) * R;
       int pa, pb;                                 // positions of the tile's tokens
       if (i < ns) {
-        x.tok0 = first(i);
-        const int tk = tokens(i, x.tok0);
-        x.seq = i;
-        x.nrows = imin(tk * d.grp - x.row0, R);
-        x.ceil = keys(i);
-        x.p0 = x.ceil - tk;
-        x.floor = SHARED ? floors[i] : 0;
-        pa = x.p0 + x.row0 / d.grp;
-        pb = x.p0 + (x.row0 + x.nrows - 1) / d.grp;
+        const int t0 = first(i);
+        plan_rows(d, x, i, t0, tokens(i, t0), keys(i), SHARED ? floors[i] : 0, R);
       } else {
         int s0, s1;
         members(i - ns, s0, s1);
@@ -260,21 +287,10 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d) {
         x.nrows = imin((first(s1) - x.tok0) * d.grp - x.row0, R);
         x.prefix = 1;
         x.ceil = glen[i - ns];
-        pa = x.p0 = gmin[i - ns];
-        pb = x.p1 = gmax[i - ns];
+        x.p0 = gmin[i - ns];
+        x.p1 = gmax[i - ns];
+        plan_tiles(d, x, x.p0, x.p1);
       }
-      x.hi = d.causal ? imin(x.ceil, pb + 1) : x.ceil;
-      x.lo = d.window > 0 ? imax(pa - d.window + 1, x.floor) : x.floor;
-      x.s = d.window > 0 ? imax(imin(d.sinks, x.hi), x.floor) : x.floor;
-      const bool sink = x.s > x.floor;
-      const int fl = x.floor / kKvTile;
-      x.a0 = sink ? fl : x.lo / kKvTile;
-      const int a1 = sink ? (x.s + kKvTile - 1) / kKvTile : x.a0;
-      x.n1 = a1 - x.a0;
-      x.b0 = imax(x.lo / kKvTile, a1);
-      const int b1 = x.hi > x.lo ? (x.hi + kKvTile - 1) / kKvTile : 0;
-      // no row sees a key: one tile, wholly masked, writes the zeros
-      x.tiles = imax(x.n1 + imax(b1 - x.b0, 0), 1);
       out.ent[e] = x;
       units = (x.tiles + kSegUnits) * d.nkv;
     }
@@ -307,7 +323,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d) {
     }
     out.share[s] = r;
   }
-  if (bad) atomicOr(d.err, bad);
+  if (bad) atomicOr(err, bad);
 }
 
 // ---------------------------------------------------------------------------
@@ -508,6 +524,69 @@ struct KvSees {
   uint32_t n, s;
 };
 
+// inclusive sum over the wave
+__device__ __forceinline__ int wave_scan(int v, int lane) {
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const int y = __shfl_up(v, o, kWave);
+    v += lane >= o ? y : 0;
+  }
+  return v;
+}
+
+// A work list of at most 64 entries, made by one wave of every workgroup for itself, a
+// lane per sequence and then per entry: small calls spare a launch and the way of the
+// list through memory (one token over 100 keys 17.2 -> 14.6 us, 48 in a window 72.5 -> 70.8).
+// Entries to ent, the share's beginning to sh[0..3] (and its global copy, for
+// k_kv_join) and its end to sh[4].
+constexpr int kOwnEntries = kWave;
+__device__ __forceinline__ void plan_own(const KvDev& d, int R, int shares, int sidx, KvEntry* ent,
+                                         int32_t* sh) {
+  const KvPlan& p = d.p;
+  const int lane = threadIdx.x & 63, b = imin(lane, p.n - 1);
+  uint32_t bad = 0;
+  const int t0 = plan_first(p, b), t1 = plan_first(p, b + 1), keys = plan_keys(p, b, bad);
+  const int tk = lane < p.n ? imax(t1 - t0, 0) : 0;
+  const int nt = (tk * p.grp + R - 1) / R;
+  const int upto = wave_scan(nt, lane), off = upto - nt, all = __shfl(upto, kWave - 1, kWave);
+  bad |= all > p.entries ? XP_DEVERR_LENGTH : 0u;   // token ranges that overlap
+  const int T = imin(all, p.entries);
+  const int me = imin(lane, imax(T - 1, 0));
+  int i = 0;                                      // the last sequence whose entries begin at most at me
+#pragma unroll
+  for (int o = kWave / 2; o > 0; o >>= 1) {
+    const int at = __shfl(off, imin(i + o, kWave - 1), kWave);
+    i += ((i + o < p.n) & (at <= me)) ? o : 0;
+  }
+  KvEntry x{};
+  x.row0 = (me - __shfl(off, i, kWave)) * R;
+  plan_rows(p, x, i, __shfl(t0, i, kWave), __shfl(tk, i, kWave), __shfl(keys, i, kWave), 0, R);
+  const int units = lane < T ? (x.tiles + kSegUnits) * p.nkv : 0;
+  const int sum = wave_scan(units, lane), cum = sum - units, W = __shfl(sum, kWave - 1, kWave);
+  const int S = imax((W + shares - 1) / shares, kPlanMinShare);
+  const int f = (int)(((int64_t)sidx * S) < W ? sidx * S : W);
+  const int f1 = (int)(((int64_t)sidx + 1) * S < W ? (sidx + 1) * S : W);
+  const uint64_t before = __ballot((lane < T) & (cum <= f));
+  const int e = before != 0 ? 63 - __builtin_clzll(before) : 0;
+  const int seg = __shfl(x.tiles, e, kWave) + kSegUnits, in = f - __shfl(cum, e, kWave);
+  const KvShare r{f, e, in / seg, in % seg - kSegUnits};
+  ent[lane] = x;
+  sh[0] = r.f;                                    // every lane the same
+  sh[1] = r.e;
+  sh[2] = r.kvh;
+  sh[3] = r.j;
+  sh[4] = f1;
+  d.list.share[sidx] = r;
+  if (blockIdx.x == 0) {                          // the list, for k_kv_join
+    KvEntry* to = lane < T ? d.list.ent + lane : (KvEntry*)d.w.dump;
+    *to = x;
+    d.list.hdr[0] = W;
+    d.list.hdr[1] = S;
+    d.list.hdr[2] = T;
+    if (__ballot(bad != 0) != 0) atomicOr(d.err, XP_DEVERR_LENGTH);
+  }
+}
+
 // waves of a SIMD: two (256 registers each), or three where half the head leaves room
 constexpr int kv_waves(int hd, int wr, int wk) { return hd == 64 && wr == 4 && wk == 1 ? 3 : 2; }
 
@@ -528,7 +607,7 @@ constexpr int kv_waves(int hd, int wr, int wk) { return hd == 64 && wr == 4 && w
 // product that follows the one it adds to waits for it.  So block n's numerators
 // are formed between the products of block n + 1's scores and of block n - 1's P V,
 // in turn.
-template <int HD, bool F8, int WR, int WK, int NST, int PARTS>
+template <int HD, bool F8, int WR, int WK, int NST, int PARTS, bool OWN>
 __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn(const KvDev d) {
   using SH = KvRows<HD, F8>;
   constexpr int NW = WR * WK, R = 32 * WR, NB = 2 / WK, ND = HD / 32, NKS = HD / 16;
@@ -546,9 +625,18 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
   const int h = lane >> 5, li = lane & 31;
   // neighbouring shares on one XCD: they read the same sequence's keys
   const int sidx = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
-  const scalar_i32 sh = as_scalar(d.list.share + sidx);
-  int f = sh[0], e = sh[1], kvh = sh[2], j = sh[3];
-  const int f1 = sh[4];
+  __shared__ KvEntry own_ent[OWN ? kOwnEntries : 1];
+  __shared__ int32_t own_sh[8];
+  if constexpr (OWN) {
+    if (wave == 0) plan_own(d, R, gridDim.x, sidx, own_ent, own_sh);
+    __syncthreads();
+  }
+  auto share = [&](int i) {
+    if constexpr (OWN) return __builtin_amdgcn_readfirstlane(own_sh[i]);
+    else return as_scalar(d.list.share + sidx)[i];
+  };
+  int f = share(0), e = share(1), kvh = share(2), j = share(3);
+  const int f1 = share(4);
   if (f >= f1) return;                            // whole workgroup
   // The lane's byte addresses within 16 rows being loaded, and within a stage's K
   // and V: one register each.  The others follow by an exclusive or in the bits of
@@ -567,7 +655,12 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
   }
   const int P1 = (1 << d.logP) - 1;
   for (;;) {
-  const scalar_i32 en = as_scalar(d.list.ent + e);
+  int en[kKvEntryInts];
+#pragma unroll
+  for (int i = 0; i < kKvEntryInts; ++i) {
+    if constexpr (OWN) en[i] = __builtin_amdgcn_readfirstlane(reinterpret_cast<const int32_t*>(own_ent + e)[i]);
+    else en[i] = as_scalar(d.list.ent + e)[i];
+  }
   const int tok0 = en[0], row0 = en[1], nrows = en[2], seq = en[3], p0 = en[4], prefix = en[5];
   const int kfloor = en[6], kceil = en[7], ks_ = en[8], klo = en[9], khi = en[10], tiles = en[11];
   const int a0 = en[12], n1 = en[13], b0 = en[14];
@@ -1173,34 +1266,42 @@ void kv_attn_sizes(const xp_kv* kv, int64_t* rows, int* entries, int* shares) {
 }
 
 // one list's attention, in tiles of R rows
-static hipError_t launch_list(const xp_kv* kv, int R, const KvDev& d, hipStream_t st) {
+static hipError_t launch_list(const xp_kv* kv, int R, bool own, const KvDev& d, hipStream_t st) {
   const int shares = kv_shares(kv, R);
-#define XP_KV(HD_, F8_, WR_, WK_, NST_, PARTS_)                                                  \
-  hipLaunchKernelGGL((k_kv_attn<HD_, F8_, WR_, WK_, NST_, PARTS_>), dim3(shares),                \
+#define XP_KV1(HD_, F8_, WR_, WK_, NST_, PARTS_, OWN_)                                           \
+  hipLaunchKernelGGL((k_kv_attn<HD_, F8_, WR_, WK_, NST_, PARTS_, OWN_>), dim3(shares),          \
                      dim3((WR_) * (WK_) * kWave), 0, st, d)
+#define XP_KV(HD_, F8_, WR_, WK_, NST_, PARTS_) XP_KV1(HD_, F8_, WR_, WK_, NST_, PARTS_, false)
+#define XP_KV_OWN(HD_, F8_, WR_, WK_, NST_, PARTS_)                                              \
+  do {                                                                                           \
+    if (own) XP_KV1(HD_, F8_, WR_, WK_, NST_, PARTS_, true);                                     \
+    else XP_KV1(HD_, F8_, WR_, WK_, NST_, PARTS_, false);                                        \
+  } while (0)
   // stages: what leaves room for kv_wgs workgroups in 160 KB.  Two bf16 parts of the
   // numerators where a bf16 cache is read by so few rows that memory bounds the call; an
   // 8-bit V is coarser than one part.
   const bool f8 = kv->dtype == XP_E4M3;
   if (kv->hd == 128 && !f8) {
-    if (R == 32) XP_KV(128, false, 1, 2, 2, 2);
-    else if (R == 64) XP_KV(128, false, 2, 2, 2, 2);
+    if (R == 32) XP_KV_OWN(128, false, 1, 2, 2, 2);
+    else if (R == 64) XP_KV_OWN(128, false, 2, 2, 2, 2);
     else if (R == 128) XP_KV(128, false, 4, 2, 4, 1);
     else XP_KV(128, false, 8, 1, 4, 1);
   } else if (kv->hd == 128) {
-    if (R == 32) XP_KV(128, true, 1, 2, 2, 1);
-    else if (R == 64) XP_KV(128, true, 2, 2, 4, 1);
+    if (R == 32) XP_KV_OWN(128, true, 1, 2, 2, 1);
+    else if (R == 64) XP_KV_OWN(128, true, 2, 2, 4, 1);
     else if (R == 128) XP_KV(128, true, 4, 1, 4, 1);
     else XP_KV(128, true, 8, 1, 8, 1);
   } else if (!f8) {
-    if (R == 32) XP_KV(64, false, 1, 2, 2, 2);
-    else if (R == 64) XP_KV(64, false, 2, 2, 4, 2);
+    if (R == 32) XP_KV_OWN(64, false, 1, 2, 2, 2);
+    else if (R == 64) XP_KV_OWN(64, false, 2, 2, 4, 2);
     else XP_KV(64, false, 4, 1, 3, 1);
   } else {
-    if (R == 32) XP_KV(64, true, 1, 2, 2, 1);
-    else if (R == 64) XP_KV(64, true, 2, 2, 4, 1);
+    if (R == 32) XP_KV_OWN(64, true, 1, 2, 2, 1);
+    else if (R == 64) XP_KV_OWN(64, true, 2, 2, 4, 1);
     else XP_KV(64, true, 4, 1, 6, 1);
   }
+#undef XP_KV1
+#undef XP_KV_OWN
 #undef XP_KV
   return hipGetLastError();
 }
@@ -1238,14 +1339,17 @@ hipError_t launch_kv_attn(const xp_kv* kv, const KvAttnArgs& a, hipStream_t st) 
   p.kv_len = a.kv_len;
   p.group_start = a.group_start;
   p.shared_len = a.shared_len;
-  p.w = kv->a;
-  p.err = kv->err;
-  if (a.groups > 0)
-    hipLaunchKernelGGL(k_kv_plan<true>, dim3(lists), dim3(kPlanThreads), 0, st, p);
-  else
-    hipLaunchKernelGGL(k_kv_plan<false>, dim3(1), dim3(kPlanThreads), 0, st, p);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  const int64_t most = (int64_t)a.total_q * kv->grp / R[0] + a.n;
+  const bool own = a.groups == 0 && R[0] <= 64 && most <= kOwnEntries;
+  if (own) p.entries = (int)most;
+  hipError_t e;
+  if (!own) {
+    if (a.groups > 0)
+      hipLaunchKernelGGL(k_kv_plan<true>, dim3(lists), dim3(kPlanThreads), 0, st, p, kv->a, kv->err);
+    else
+      hipLaunchKernelGGL(k_kv_plan<false>, dim3(1), dim3(kPlanThreads), 0, st, p, kv->a, kv->err);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
 
   KvDev d{};
   d.q = a.q;
@@ -1272,12 +1376,13 @@ hipError_t launch_kv_attn(const xp_kv* kv, const KvAttnArgs& a, hipStream_t st) 
   d.total_q = a.total_q;
   d.groups = a.groups;
   d.row0 = 2 * kv->rows;
+  d.p = p;
   d.w = kv->a;
   d.err = kv->err;
   const bool wide = kv->hd == 128;
   if (a.groups == 0) {
     d.list = kv->a.list[0];
-    if ((e = launch_list(kv, R[0], d, st)) != hipSuccess) return e;
+    if ((e = launch_list(kv, R[0], own, d, st)) != hipSuccess) return e;
     const dim3 grid(kv_shares(kv, R[0]) - 1, R[0] * kv->hd / 1024);
     if (wide) hipLaunchKernelGGL(k_kv_join<128>, grid, dim3(256), 0, st, d, R[0]);
     else hipLaunchKernelGGL(k_kv_join<64>, grid, dim3(256), 0, st, d, R[0]);
@@ -1286,7 +1391,7 @@ hipError_t launch_kv_attn(const xp_kv* kv, const KvAttnArgs& a, hipStream_t st) 
   for (int k = lists - 1; k >= 0; --k) {          // the prefixes, then the sequences' own keys
     d.list = kv->a.list[k];
     d.part0 = k * kv->rows;
-    if ((e = launch_list(kv, R[k], d, st)) != hipSuccess) return e;
+    if ((e = launch_list(kv, R[k], false, d, st)) != hipSuccess) return e;
   }
   KvJoin jn{};
   jn.R[0] = R[0];

@@ -242,6 +242,29 @@ def test_attend_max_q_costs_time_only(rows):
     kv.close()
 
 
+@pytest.mark.parametrize("hd,cache", [(128, "bf16"), (64, "e4m3")])
+def test_attend_more_sequences_than_lanes(hd, cache):
+    """Prompts, blocks and single tokens of more sequences than a wave's lanes, and
+    the same ones in calls of few."""
+    ql = [(150, 1, 16, 33, 0, 2)[i % 6] for i in range(70)]
+    kv_len = [x + (0, 200, 90, 7, 30, 1)[i % 5] for i, x in enumerate(ql)]
+    c = Call(44, kv_len, ql, heads=4, n_kv=2, hd=hd, cache=cache)
+    kv = c.device()
+    for m in (dict(causal=True), dict(causal=False, window=70, sinks=5)):
+        print(f"many sequences: hd={hd} {cache} {m}", flush=True)
+        out = c.run(kv, **m)
+        assert kv.device_errors() == 0
+        c.check(out, parts=1, **m)
+        few = c.run(kv, **m).fill_(7)
+        for b in range(0, 70, 14):
+            t = slice(c.cu[b], c.cu[b + 14])
+            kv.attend(c.dq[t], c.dk, c.dv, c.dtable[b:b + 14], c.dkv[b:b + 14],
+                      cu_q=(c.dcu[b:b + 15] - c.dcu[b]).contiguous(), max_q=150, k_scale=c.dks,
+                      v_scale=c.dvs, out=few[t], **m)
+        c.check(few, parts=1, **m)
+    kv.close()
+
+
 def test_attend_takes_any_upper_bound_of_the_tokens():
     """A bound above the handle's own (a configuration's longest prompt)."""
     c = Call(43, [90, 30], [20, 7], heads=4, n_kv=2)
