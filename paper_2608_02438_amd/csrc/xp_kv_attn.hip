@@ -459,21 +459,30 @@ __device__ __forceinline__ void lds_v(const uint32_t* a, const uint32_t* b, u32x
   }
 }
 
-// some 16-bit (8-bit) value of x is an infinity or NaN
+// Infinities and NaN among 16-bit (8-bit) values: the largest magnitudes so far (the
+// bytes all of whose low bits were ones).
+typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
 template <bool F8>
-__device__ __forceinline__ bool has_nonfinite(u32x4 x) {
-  bool any = false;
+struct KvOdd {
+  uint32_t acc = 0;
+  __device__ __forceinline__ void add(u32x4 x) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (F8) {
-      const uint32_t y = ~x[i] & 0x7f7f7f7fu;     // 0 where all seven bits are ones
-      any |= ((y - 0x01010101u) & ~y & 0x80808080u) != 0u;
-    } else {
-      any |= ((x[i] & 0x7f800000u) == 0x7f800000u) | ((x[i] & 0x7f80u) == 0x7f80u);
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (F8) {
+        const uint32_t y = ~x[i] & 0x7f7f7f7fu;   // a byte 0: all seven bits are ones
+        acc |= (y - 0x01010101u) & ~y;
+      } else {
+        const ushort2v m = __builtin_elementwise_max(
+            __builtin_bit_cast(ushort2v, acc), __builtin_bit_cast(ushort2v, x[i] & 0x7fff7fffu));
+        acc = __builtin_bit_cast(uint32_t, m);
+      }
     }
   }
-  return any;
-}
+  __device__ __forceinline__ bool any() const {
+    if constexpr (F8) return (acc & 0x80808080u) != 0u;
+    else return (acc >= 0x7f800000u) | ((acc & 0xffffu) >= 0x7f80u);
+  }
+};
 
 // ones over each bf16 of x that is an infinity or NaN
 __device__ __forceinline__ uint32_t nonfinite_mask(uint32_t x) {
@@ -826,10 +835,17 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
   // infinities or NaN among the block's V
   auto odd_values = [&](int stage, int r) __attribute__((always_inline)) {
     const u32x4* Vs = lds + stage * SH::kStage + SH::kHalf + r * CPR;
-    bool odd = false;
+    constexpr int N = 32 * CPR / kWave, U = N < 4 ? N : 4;   // reads of a lane, at a time
+    KvOdd<F8> odd;
 #pragma unroll 1
-    for (int i = 0; i < 32 * CPR / kWave; ++i) odd |= has_nonfinite<F8>(Vs[kWave * i + lane]);
-    return __ballot(odd) != 0;
+    for (int i = 0; i < N; i += U) {
+      u32x4 x[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) x[u] = Vs[kWave * (i + u) + lane];
+#pragma unroll
+      for (int u = 0; u < U; ++u) odd.add(x[u]);
+    }
+    return __ballot(odd.any()) != 0;
   };
   // Rows must not meet the infinities and NaN of keys that they do not see (0 times
   // one is no number): those values leave the operands, and the rows with a
