@@ -616,6 +616,12 @@ constexpr int kv_waves(int hd, int wr, int wk) { return hd == 64 && wr == 4 && w
 // product that follows the one it adds to waits for it.  So block n's numerators
 // are formed between the products of block n + 1's scores and of block n - 1's P V,
 // in turn.
+// Bound by memory up to 128 rows (48 single tokens over 4096 keys 138 us, 5.8 TB/s; 32
+// blocks of 16 over 8192 182 us, 5.9; 64 of 32 445 us, 4.9 TB/s and 620 TFLOP/s), by
+// the loop's vector instructions beside the products above (4096 tokens x 8192 keys:
+// 560 us, 980 TFLOP/s; head_dim 64, with as many exponentials to half the products,
+// 410 us, 670).  A segment's beginning and end take about 10000 cycles, 2 to 3 tiles:
+// four causal prompts of 4096 668 us, 822 TFLOP/s.
 template <int HD, bool F8, int WR, int WK, int NST, int PARTS, bool OWN>
 __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn(const KvDev d) {
   using SH = KvRows<HD, F8>;
@@ -1126,7 +1132,9 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
 
 // ---------------------------------------------------------------------------
 // Joining.  Part (m_i, l_i, O_i) of a row: O = sum 2^(m_i - M) O_i, l likewise,
-// M = max m_i, parts in order.
+// M = max m_i, parts in order.  A workgroup per share and 1024 / head_dim rows, most of
+// which find nothing cut: 4 us, 12 to 17 with a tile of 128 or 256 rows for every
+// share; every row of 960 tokens with a prefix 21 us (reads of the parts from memory).
 // ---------------------------------------------------------------------------
 struct KvSum {
   float m = -INFINITY, l = 0.f;
@@ -1284,40 +1292,35 @@ void kv_attn_sizes(const xp_kv* kv, int64_t* rows, int* entries, int* shares) {
 // one list's attention, in tiles of R rows
 static hipError_t launch_list(const xp_kv* kv, int R, bool own, const KvDev& d, hipStream_t st) {
   const int shares = kv_shares(kv, R);
-#define XP_KV1(HD_, F8_, WR_, WK_, NST_, PARTS_, OWN_)                                           \
-  hipLaunchKernelGGL((k_kv_attn<HD_, F8_, WR_, WK_, NST_, PARTS_, OWN_>), dim3(shares),          \
-                     dim3((WR_) * (WK_) * kWave), 0, st, d)
-#define XP_KV(HD_, F8_, WR_, WK_, NST_, PARTS_) XP_KV1(HD_, F8_, WR_, WK_, NST_, PARTS_, false)
-#define XP_KV_OWN(HD_, F8_, WR_, WK_, NST_, PARTS_)                                              \
+#define XP_KV(HD_, F8_, WR_, WK_, NST_, PARTS_)                                                  \
   do {                                                                                           \
-    if (own) XP_KV1(HD_, F8_, WR_, WK_, NST_, PARTS_, true);                                     \
-    else XP_KV1(HD_, F8_, WR_, WK_, NST_, PARTS_, false);                                        \
+    if (own)                                                                                     \
+      hipLaunchKernelGGL((k_kv_attn<HD_, F8_, WR_, WK_, NST_, PARTS_, true>), dim3(shares),      \
+                         dim3((WR_) * (WK_) * kWave), 0, st, d);                                 \
+    else                                                                                         \
+      hipLaunchKernelGGL((k_kv_attn<HD_, F8_, WR_, WK_, NST_, PARTS_, false>), dim3(shares),     \
+                         dim3((WR_) * (WK_) * kWave), 0, st, d);                                 \
   } while (0)
-  // stages: what leaves room for kv_wgs workgroups in 160 KB.  Two bf16 parts of the
-  // numerators where a bf16 cache is read by so few rows that memory bounds the call; an
-  // 8-bit V is coarser than one part.
   const bool f8 = kv->dtype == XP_E4M3;
   if (kv->hd == 128 && !f8) {
-    if (R == 32) XP_KV_OWN(128, false, 1, 2, 2, 2);
-    else if (R == 64) XP_KV_OWN(128, false, 2, 2, 2, 2);
+    if (R == 32) XP_KV(128, false, 1, 2, 2, 2);
+    else if (R == 64) XP_KV(128, false, 2, 2, 2, 2);
     else if (R == 128) XP_KV(128, false, 4, 2, 4, 1);
     else XP_KV(128, false, 8, 1, 4, 1);
   } else if (kv->hd == 128) {
-    if (R == 32) XP_KV_OWN(128, true, 1, 2, 2, 1);
-    else if (R == 64) XP_KV_OWN(128, true, 2, 2, 4, 1);
+    if (R == 32) XP_KV(128, true, 1, 2, 2, 1);
+    else if (R == 64) XP_KV(128, true, 2, 2, 4, 1);
     else if (R == 128) XP_KV(128, true, 4, 1, 4, 1);
     else XP_KV(128, true, 8, 1, 8, 1);
   } else if (!f8) {
-    if (R == 32) XP_KV_OWN(64, false, 1, 2, 2, 2);
-    else if (R == 64) XP_KV_OWN(64, false, 2, 2, 4, 2);
+    if (R == 32) XP_KV(64, false, 1, 2, 2, 2);
+    else if (R == 64) XP_KV(64, false, 2, 2, 4, 2);
     else XP_KV(64, false, 4, 1, 3, 1);
   } else {
-    if (R == 32) XP_KV_OWN(64, true, 1, 2, 2, 1);
-    else if (R == 64) XP_KV_OWN(64, true, 2, 2, 4, 1);
+    if (R == 32) XP_KV(64, true, 1, 2, 2, 1);
+    else if (R == 64) XP_KV(64, true, 2, 2, 4, 1);
     else XP_KV(64, true, 4, 1, 6, 1);
   }
-#undef XP_KV1
-#undef XP_KV_OWN
 #undef XP_KV
   return hipGetLastError();
 }
@@ -1356,7 +1359,7 @@ hipError_t launch_kv_attn(const xp_kv* kv, const KvAttnArgs& a, hipStream_t st) 
   p.group_start = a.group_start;
   p.shared_len = a.shared_len;
   const int64_t most = (int64_t)a.total_q * kv->grp / R[0] + a.n;
-  const bool own = a.groups == 0 && R[0] <= 64 && most <= kOwnEntries;
+  const bool own = a.groups == 0 && most <= kOwnEntries;
   if (own) p.entries = (int)most;
   hipError_t e;
   if (!own) {
