@@ -65,7 +65,9 @@ __device__ __forceinline__ void take_page(const KvMap& d, int k, const int* take
 // block scans over the requests, then one search per page and slot (8 requests with
 // blocks of 17: 7 us; 512 without slots 6.6).
 constexpr int kMapThreads = 1024;
-constexpr int kMapOneLaunch = 8192;  // slots up to which one launch does all
+// Slots up to which one launch does all: 4096 of 64 requests 9.2 us in one, 11.2 in two;
+// 8192 12.3 and 11.2, 32768 31.6 and 11.2.
+constexpr int kMapOneLaunch = 6144;
 template <bool ALL>
 __global__ __launch_bounds__(kMapThreads) void k_kv_map(const KvMap d) {
   __shared__ int rel[kKvMaxBatch + 1], take[kKvMaxBatch + 1], acu[kKvMaxBatch + 1];
