@@ -59,7 +59,6 @@ struct KvList {
   KvShare* share = nullptr;          // [shares + 1]
   KvEntry* ent = nullptr;            // [entries]
   int32_t* cum = nullptr;            // [entries + 1] units before each entry
-  int32_t* off = nullptr;            // [items + 1] entries before each sequence (group)
 };
 
 // Workspace of the attention (device pointers).
@@ -70,10 +69,8 @@ struct KvAttnWs {
   float* ml = nullptr;               // [rows][2] their reference maximum (base 2) and sum
   // calls with shared prefixes
   int32_t* pos = nullptr;            // [tokens] position of every token
-  int32_t* tseq = nullptr;           // [tokens] its sequence
-  int32_t* stok = nullptr;           // [batch] first token of each sequence
-  int32_t* sgrp = nullptr;           // [batch] its group, or -1
-  int32_t* gtok = nullptr;           // [groups] first token of each group
+  int2* row[2] = {};                 // [tokens] first row among its sequence's (group's; -1:
+                                     // none), and their first entry
   char* dump = nullptr;              // a row of 128 floats that takes what no one reads
   const char* zero = nullptr;        // 256 bytes of zeros: a key row that no one sees
 };

@@ -39,10 +39,11 @@ __device__ __forceinline__ int pool_page(const int32_t* pool, int top, int k) { 
 // Slot of token t: request b = owner(t), its position's page from the table or,
 // where this call takes it, from the pool.
 __device__ __forceinline__ int slot_of(const KvMap& d, int t, const int* acu, const int* take,
-                                       const int32_t* old, int top, uint32_t& bad) {
+                                       const int32_t* old, const int32_t* len, int top,
+                                       uint32_t& bad) {
   if (t >= acu[d.n]) return -1;
   const int b = kv_owner(acu, d.n, t);
-  const int pos = d.lens[b] + t - acu[b], col = pos >> d.logP, h = old[b];
+  const int pos = len[b] + t - acu[b], col = pos >> d.logP, h = old[b];
   if (take[b + 1] > take[b] && take[b + 1] > top) return -1;     // not served
   const int page = col < h ? d.table[b * d.ld + col] : pool_page(d.pool, top, take[b] + col - h);
   if ((uint32_t)page >= (uint32_t)d.n_pages) {
@@ -71,12 +72,13 @@ constexpr int kMapOneLaunch = 6144;
 template <bool ALL>
 __global__ __launch_bounds__(kMapThreads) void k_kv_map(const KvMap d) {
   __shared__ int rel[kKvMaxBatch + 1], take[kKvMaxBatch + 1], acu[kKvMaxBatch + 1];
-  __shared__ int old[kKvMaxBatch];
+  __shared__ int old[kKvMaxBatch], len[kKvMaxBatch];   // len: -1 where it was left alone
   __shared__ int64_t red[3][kMapThreads / kWave];
   __shared__ int taken;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   uint32_t bad = 0;
   int64_t sum[3] = {0, 0, 0};
+  int free0 = d.pool_n[0];
   auto sat = [](int64_t x) { return (int)(x < 0x7fffffff ? x : 0x7fffffff); };
   if (tid == 0) taken = 0;
   for (int b0 = 0; b0 < d.n; b0 += kMapThreads) {
@@ -85,10 +87,12 @@ __global__ __launch_bounds__(kMapThreads) void k_kv_map(const KvMap d) {
     if (b < d.n) {
       const int x = d.lens[b], a = d.add[b], h = d.held[b];
       old[b] = h;
+      len[b] = x;
       const int64_t total = (int64_t)x + a;
       if (x < 0 || a < 0 || h < 0 || h > d.cols || total > (int64_t)d.cols << d.logP) {
         bad |= XP_DEVERR_LENGTH;                  // left as it is
         old[b] = h < 0 ? 0 : (h > d.cols ? d.cols : h);
+        len[b] = -1;
       } else {
         const int need = (int)((total + (1 << d.logP) - 1) >> d.logP);
         v[0] = need < h ? h - need : 0;
@@ -96,22 +100,27 @@ __global__ __launch_bounds__(kMapThreads) void k_kv_map(const KvMap d) {
         v[2] = a;
       }
     }
-    int64_t in[3];
+    // only the waves that have requests: with all sixteen at it their exchanges, one
+    // LDS for all, were most of a small call's time
+    const int left = d.n - b0, waves = left < kMapThreads ? (left + kWave - 1) / kWave : kMapThreads / kWave;
+    int64_t in[3] = {0, 0, 0};
+    if (wave < waves) {
 #pragma unroll
-    for (int q = 0; q < 3; ++q) {
-      in[q] = v[q];
+      for (int q = 0; q < 3; ++q) {
+        in[q] = v[q];
 #pragma unroll
-      for (int o = 1; o < kWave; o <<= 1) {
-        const int64_t y = __shfl_up((long long)in[q], o, kWave);
-        if (lane >= o) in[q] += y;
+        for (int o = 1; o < kWave; o <<= 1) {
+          const int64_t y = __shfl_up((long long)in[q], o, kWave);
+          if (lane >= o) in[q] += y;
+        }
+        if (lane == kWave - 1) red[q][wave] = in[q];
       }
-      if (lane == kWave - 1) red[q][wave] = in[q];
     }
     __syncthreads();
 #pragma unroll
     for (int q = 0; q < 3; ++q) {
       int64_t before = sum[q];
-      for (int w = 0; w < kMapThreads / kWave; ++w) {
+      for (int w = 0; w < waves; ++w) {
         const int64_t t = red[q][w];
         before += w < wave ? t : 0;
         sum[q] += t;
@@ -132,7 +141,6 @@ __global__ __launch_bounds__(kMapThreads) void k_kv_map(const KvMap d) {
   }
   __syncthreads();
   const int R = (int)sum[0];
-  int free0 = d.pool_n[0];
   if (free0 < 0 || free0 > d.n_pages - R) {  // more pages than there are
     bad |= XP_DEVERR_POOL;
     free0 = free0 < 0 ? 0 : (free0 > d.n_pages ? d.n_pages : free0);
@@ -173,10 +181,8 @@ __global__ __launch_bounds__(kMapThreads) void k_kv_map(const KvMap d) {
     if (ok && tk + rl > 0) d.held[b] = old[b] + tk - rl;
     if (d.cu) d.cu[b] = acu[b];
     // a request that was left as it is has no keys to speak of
-    const int x = d.lens[b], a = d.add[b], h = d.held[b];
-    const bool valid = x >= 0 && a >= 0 && h >= 0 && h <= d.cols &&
-                       (int64_t)x + a <= (int64_t)d.cols << d.logP;
-    if (d.kv_len) d.kv_len[b] = valid ? (ok ? x + a : x) : 0;
+    const int x = len[b];
+    if (d.kv_len) d.kv_len[b] = x < 0 ? 0 : (ok ? x + d.add[b] : x);
     if (!ALL) {
       d.take[b] = take[b];
       d.old[b] = old[b];
@@ -200,7 +206,7 @@ __global__ __launch_bounds__(kMapThreads) void k_kv_map(const KvMap d) {
     for (int k = tid; k < T; k += kMapThreads) take_page(d, k, take, old, top);
     if (d.slots)
       for (int t = tid; t < d.max_slots; t += kMapThreads)
-        d.slots[t] = slot_of(d, t, acu, take, old, top, bad);
+        d.slots[t] = slot_of(d, t, acu, take, old, len, top, bad);
   }
   if (bad) atomicOr(d.err, bad);
 }
@@ -219,7 +225,7 @@ __global__ __launch_bounds__(256) void k_kv_slots(const KvMap d) {
   uint32_t bad = 0;
   for (int k = blockIdx.x * 256 + threadIdx.x; k < T; k += step) take_page(d, k, take, d.old, top);
   for (int64_t t = blockIdx.x * 256 + threadIdx.x; t < d.max_slots; t += step)
-    d.slots[t] = slot_of(d, (int)t, acu, take, d.old, top, bad);
+    d.slots[t] = slot_of(d, (int)t, acu, take, d.old, d.lens, top, bad);
   if (bad) atomicOr(d.err, bad);
 }
 
@@ -457,17 +463,13 @@ extern "C" xp_status xp_kv_create(const xp_kv_shape* s, int32_t max_batch, int32
       {(void**)&l0.share, ((size_t)shares + 1) * sizeof(KvShare)},
       {(void**)&l0.ent, lists * kv->entries * sizeof(KvEntry)},
       {(void**)&l0.cum, (lists * kv->entries + 1) * 4},
-      {(void**)&l0.off, (lists * nb + 1) * 4},
       {(void**)&l1.hdr, (size_t)(shared ? 256 : 0)},
       {(void**)&l1.share, shared ? ((size_t)shares + 1) * sizeof(KvShare) : 0},
       {(void**)&l1.ent, shared ? (size_t)kv->entries * sizeof(KvEntry) : 0},
       {(void**)&l1.cum, shared ? ((size_t)kv->entries + 1) * 4 : 0},
-      {(void**)&l1.off, shared ? (nb + 1) * 4 : 0},
       {(void**)&kv->a.pos, shared ? (size_t)max_tokens * 4 : 0},
-      {(void**)&kv->a.tseq, shared ? (size_t)max_tokens * 4 : 0},
-      {(void**)&kv->a.stok, nb * 4},
-      {(void**)&kv->a.sgrp, nb * 4},
-      {(void**)&kv->a.gtok, nb * 4},
+      {(void**)&kv->a.row[0], shared ? (size_t)max_tokens * 8 : 0},
+      {(void**)&kv->a.row[1], shared ? (size_t)max_tokens * 8 : 0},
       {(void**)&kv->a.ml, prows * 8},
       {(void**)&kv->a.part, prows * hd * 4},
   };

@@ -99,21 +99,24 @@ constexpr int kPlanCum = 4096;       // entries whose sums stay in LDS
 constexpr int kSegUnits = 3;
 constexpr int kPlanMinShare = kSegUnits + 2;   // units a share has at least
 
-// exclusive sum over the workgroup of each thread's v; *total their sum
-__device__ __forceinline__ int block_scan(int v, int* lds, int* total) {
+// exclusive sum over the workgroup of each thread's v, 0 from thread `count` on (whose
+// waves stay out of it); *total their sum
+__device__ __forceinline__ int block_scan(int v, int count, int* lds, int* total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int waves = imin((count + kWave - 1) / kWave, kPlanWaves);
   int x = v;
+  if (wave < waves) {
 #pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const int y = __shfl_up(x, o, kWave);
-    if (lane >= o) x += y;
+    for (int o = 1; o < kWave; o <<= 1) {
+      const int y = __shfl_up(x, o, kWave);
+      if (lane >= o) x += y;
+    }
   }
   __syncthreads();
-  if (lane == kWave - 1) lds[wave] = x;
+  if (wave < waves && lane == kWave - 1) lds[wave] = x;
   __syncthreads();
   int before = 0, all = 0;
-#pragma unroll
-  for (int w = 0; w < kPlanWaves; ++w) {
+  for (int w = 0; w < waves; ++w) {
     const int t = lds[w];
     before += w < wave ? t : 0;
     all += t;
@@ -185,15 +188,11 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d, const 
     s1 = clampi(d.group_start[g + 1], s0, n);
   };
   if constexpr (SHARED) {
-    for (int b = tid; b < n; b += kPlanThreads) {
-      floors[b] = 0;
-      if (!second) {
-        w.sgrp[b] = -1;
-        w.stok[b] = first(b);
-      }
+    for (int b = tid; b < n; b += kPlanThreads) floors[b] = 0;
+    for (int t = tid; t < d.total_q; t += kPlanThreads) {   // tokens of no sequence, of no group
+      if (!second) w.row[0][t] = int2{-1, 0};
+      if (items > ns) w.row[1][t] = int2{-1, 0};
     }
-    if (!second)                                  // tokens of no sequence
-      for (int t = tid; t < d.total_q; t += kPlanThreads) w.tseq[t] = -1;
     __syncthreads();
     // a wave per group: its members' positions, and a prefix that none is shorter than
     for (int g = wave; g < d.groups; g += kPlanWaves) {
@@ -215,25 +214,13 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d, const 
       }
       const int want = d.shared_len[g], len = clampi(want, 0, kmin);
       if (want != len) bad |= XP_DEVERR_LENGTH;
-      for (int b = s0 + lane; b < s1; b += kWave) {
-        floors[b] = len;
-        if (!second) w.sgrp[b] = len > 0 ? g : -1;
-      }
+      for (int b = s0 + lane; b < s1; b += kWave) floors[b] = len;
       if (lane == 0) {
         gmin[g] = pmin;
         gmax[g] = pmax;
         glen[g] = len;
-        if (!second) w.gtok[g] = first(s0);
       }
     }
-    if (!second)
-      for (int b = wave; b < n; b += kPlanWaves) {   // every token's position and sequence
-        const int t0 = first(b), ql = tokens(b, t0), p0 = keys(b) - ql;
-        for (int i = lane; i < ql; i += kWave) {
-          w.pos[t0 + i] = p0 + i;
-          w.tseq[t0 + i] = b;
-        }
-      }
     __syncthreads();
   }
   // entries of each item; where token ranges overlap, as many as the tokens could have
@@ -254,7 +241,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d, const 
       nt = (int)(((int64_t)tk * d.grp + R - 1) / R);
     }
     int all;
-    const int before = block_scan(nt, red, &all);
+    const int before = block_scan(nt, items - i0, red, &all);
     if (i < items) off[i] = T + before;
     T = T > most ? T : T + all;                   // stays far below 2^31
   }
@@ -264,8 +251,22 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d, const 
     bad |= XP_DEVERR_LENGTH;
   }
   __syncthreads();
-  if constexpr (SHARED)
-    for (int i = tid; i <= items; i += kPlanThreads) out.off[i] = off[i];
+  if constexpr (SHARED) {                         // a wave per item: where its tokens' rows are
+    if (!second)
+      for (int b = wave; b < n; b += kPlanWaves) {
+        const int t0 = first(b), ql = tokens(b, t0), p0 = keys(b) - ql;
+        for (int i = lane; i < ql; i += kWave) {
+          w.pos[t0 + i] = p0 + i;
+          w.row[0][t0 + i] = int2{i * d.grp, off[b]};
+        }
+      }
+    for (int g = wave; g < items - ns; g += kPlanWaves) {
+      int s0, s1;
+      members(g, s0, s1);
+      const int t0 = first(s0), ql = glen[g] > 0 ? first(s1) - t0 : 0;
+      for (int i = lane; i < ql; i += kWave) w.row[1][t0 + i] = int2{i * d.grp, off[ns + g]};
+    }
+  }
   // their key ranges
   int W = 0;
   for (int e0 = 0; e0 < T; e0 += kPlanThreads) {
@@ -295,7 +296,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d, const 
       units = (x.tiles + kSegUnits) * d.nkv;
     }
     int all;
-    const int before = block_scan(units, red, &all);
+    const int before = block_scan(units, T - e0, red, &all);
     if (e < T) {
       if (e < kPlanCum) cums[e] = W + before;
       out.cum[e] = W + before;
@@ -1218,7 +1219,6 @@ __global__ __launch_bounds__(256) void k_kv_join(const KvDev d, int R) {
 struct KvJoin {
   int R[2];                          // row tiles of the sequences, of the groups
   int64_t part0;                     // first partial row of the groups' list
-  int n;
   int one;                           // both are in one list, the groups behind the sequences
 };
 template <int HD>
@@ -1228,26 +1228,32 @@ __global__ __launch_bounds__(256) void k_kv_join_rows(const KvDev d, const KvJoi
   const int c = 4 * (threadIdx.x % TPR);
   if (row >= (int64_t)d.total_q * d.nh) return;
   const int tok = (int)(row / d.nh), head = (int)(row - (int64_t)tok * d.nh);
-  const int b = d.w.tseq[tok];
-  if ((uint32_t)b >= (uint32_t)jn.n) return;      // behind the last sequence
-  const int kvh = head / d.grp, hg = head - kvh * d.grp, g = d.w.sgrp[b];
+  const int kvh = head / d.grp, hg = head - kvh * d.grp;
+  const int2 at[2] = {d.w.row[0][tok], d.w.row[1][tok]};
+  if (at[0].x < 0) return;                        // behind the last sequence
+  int lr[2], c0[2], c1[2], S[2];                  // row, units before and behind its entry
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const KvList& l = d.w.list[jn.one ? 0 : k];
+    lr[k] = at[k].x + hg;
+    const int e = at[k].y + lr[k] / jn.R[k];
+    const bool has = (at[k].x >= 0) & (e < l.hdr[2]);   // past it: token ranges that overlap
+    S[k] = l.hdr[1];
+    c0[k] = l.cum[has ? e : 0];
+    c1[k] = has ? l.cum[e + 1] : 0;
+  }
   KvSum x;
 #pragma unroll
   for (int k = 1; k >= 0; --k) {                  // the prefix, then the sequence's own keys
-    if (k == 1 && g < 0) continue;
-    const KvList& l = d.w.list[jn.one ? 0 : k];
-    const int R = jn.R[k], S = l.hdr[1];
-    const int lr = (tok - (k == 1 ? d.w.gtok[g] : d.w.stok[b])) * d.grp + hg;
-    const int e = l.off[k == 1 ? (jn.one ? jn.n : 0) + g : b] + lr / R;
-    if (lr < 0 || e >= l.hdr[2]) continue;        // token ranges that overlap
-    const int tiles = l.ent[e].tiles;
-    const int a = l.cum[e] + kvh * (tiles + kSegUnits) + kSegUnits;
-    if (a / S == (a + tiles - 1) / S) {
+    if (c1[k] == 0) continue;
+    const int seg = (c1[k] - c0[k]) / d.nkv, tiles = seg - kSegUnits;
+    const int a = c0[k] + kvh * seg + kSegUnits;
+    if (a / S[k] == (a + tiles - 1) / S[k]) {
       const int64_t prow = d.row0 + ((int64_t)k * d.total_q + tok) * d.nh + head;
       const float2 ml = *reinterpret_cast<const float2*>(d.w.ml + 2 * prow);
       x.add(ml.x, ml.y, *reinterpret_cast<const floatx4*>(d.w.part + prow * HD + c));
     } else {
-      add_parts<HD>(d, k == 1 ? jn.part0 : 0, R, a, tiles, S, lr % R, c, x);
+      add_parts<HD>(d, k == 1 ? jn.part0 : 0, jn.R[k], a, tiles, S[k], lr[k] % jn.R[k], c, x);
     }
   }
   write_row<HD>(d, tok, head, c, x);
@@ -1416,7 +1422,6 @@ hipError_t launch_kv_attn(const xp_kv* kv, const KvAttnArgs& a, hipStream_t st) 
   jn.R[0] = R[0];
   jn.R[1] = R[1];
   jn.part0 = lists == 2 ? kv->rows : 0;
-  jn.n = a.n;
   jn.one = lists == 1;
   const int rpb = 1024 / kv->hd;
   const dim3 grid((unsigned)(((int64_t)a.total_q * kv->nh + rpb - 1) / rpb));
