@@ -64,10 +64,10 @@ __device__ __forceinline__ void take_page(const KvMap& d, int k, const int* take
 // over the requests before it; the releases, the tables' new lengths and the
 // pool's; with ALL also the pages taken and the slots.  Bound by latency: three
 // block scans over the requests, then one search per page and slot (8 requests with
-// blocks of 17: 7 us; 512 without slots 6.6).
+// blocks of 17: 4.6 us; 512 without slots 5.2).
 constexpr int kMapThreads = 1024;
-// Slots up to which one launch does all: 4096 of 64 requests 9.2 us in one, 11.2 in two;
-// 8192 12.3 and 11.2, 32768 31.6 and 11.2.
+// Slots up to which one launch does all: 4096 of 64 requests 6.6 us in one, 8.9 in two;
+// 8192 9.6 and 8.8, 32768 27.7 and 8.8.
 constexpr int kMapOneLaunch = 6144;
 template <bool ALL>
 __global__ __launch_bounds__(kMapThreads) void k_kv_map(const KvMap d) {
@@ -148,7 +148,7 @@ __global__ __launch_bounds__(kMapThreads) void k_kv_map(const KvMap d) {
   int top = free0 + R;
   // A wave returns kBack * 64 neighbouring pages at a time: one search finds the
   // requests of every 64th, and each page's lies between those of its 64 (a search
-  // per page kept one workgroup's shared memory busy: 32000 pages 35 us, now 18).
+  // per page kept one workgroup's shared memory busy: 32000 pages 35 us, now 16).
   constexpr int kBack = 8;
   for (int i0 = wave * kBack * kWave; i0 < R; i0 += kBack * kMapThreads) {
     const int mark = i0 + lane * kWave;

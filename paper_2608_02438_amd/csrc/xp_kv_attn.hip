@@ -87,8 +87,8 @@ struct KvDev {
 // their keys behind a shared prefix, if they have one); the groups (their prefixes)
 // follow them or are the items of a second list.  The items' row tiles, the entries'
 // key ranges, the sums of both, and where each share begins.  Bound by latency, a few
-// block scans and one search per entry and share: 64 sequences 8 us, 60 behind five
-// prefixes 10.5.  (Small calls: plan_own.)
+// block scans and one search per entry and share: 64 sequences 7 us, 60 behind five
+// prefixes 9.4.  (Small calls: plan_own.)
 // ---------------------------------------------------------------------------
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanWaves = kPlanThreads / kWave;
@@ -97,7 +97,10 @@ constexpr int kPlanCum = 4096;       // entries whose sums stay in LDS
 // tile's latency and its results: without them the shares at the beginnings of
 // prompts, many segments of a few tiles, ran 1.65 ms where the others took 1.0.
 constexpr int kSegUnits = 3;
-constexpr int kPlanMinShare = kSegUnits + 2;   // units a share has at least
+// A share has one unit at least: small calls spread over all workgroups, a tile each,
+// and leave the parts to the join (one token over 180 .. 500 keys: 14.3 .. 14.8 us,
+// with shares of two units 16.3 .. 16.5, of five 18.6 .. 20.5).
+constexpr int kPlanMinShare = 1;
 
 // exclusive sum over the workgroup of each thread's v, 0 from thread `count` on (whose
 // waves stay out of it); *total their sum
