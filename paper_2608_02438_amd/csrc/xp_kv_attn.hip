@@ -507,20 +507,20 @@ __device__ __forceinline__ uint32_t ones_of(int c, uint32_t x) {
 __device__ __forceinline__ void kv_dma(const char* base, uint32_t lp, uint32_t x, int n, u32x4* dst) {
   const uint64_t b = (uint64_t)(uintptr_t)base;
   __builtin_amdgcn_global_load_lds((const void*)(uintptr_t)(b + lp), dst, 16, 0, 0);
-  if (n > 1) __builtin_amdgcn_global_load_lds((const void*)(uintptr_t)(b + (lp ^ x)), dst, 16, 1024, 0);
+  if (n > 1) __builtin_amdgcn_global_load_lds((const void*)(uintptr_t)(b + (lp ^ x)), dst, 16, 1 * 1024, 0);
   if (n > 2) {
-    __builtin_amdgcn_global_load_lds((const void*)(uintptr_t)(b + (lp ^ (2 * x))), dst, 16, 2048, 0);
-    __builtin_amdgcn_global_load_lds((const void*)(uintptr_t)(b + (lp ^ (3 * x))), dst, 16, 3072, 0);
+    __builtin_amdgcn_global_load_lds((const void*)(uintptr_t)(b + (lp ^ (2 * x))), dst, 16, 2 * 1024, 0);
+    __builtin_amdgcn_global_load_lds((const void*)(uintptr_t)(b + (lp ^ (3 * x))), dst, 16, 3 * 1024, 0);
   }
 }
 
 __device__ __forceinline__ void kv_dma_nt(const char* base, uint32_t lp, uint32_t x, int n, u32x4* dst) {
   const uint64_t b = (uint64_t)(uintptr_t)base;
   __builtin_amdgcn_global_load_lds((const void*)(uintptr_t)(b + lp), dst, 16, 0, 2);
-  if (n > 1) __builtin_amdgcn_global_load_lds((const void*)(uintptr_t)(b + (lp ^ x)), dst, 16, 1024, 2);
+  if (n > 1) __builtin_amdgcn_global_load_lds((const void*)(uintptr_t)(b + (lp ^ x)), dst, 16, 1 * 1024, 2);
   if (n > 2) {
-    __builtin_amdgcn_global_load_lds((const void*)(uintptr_t)(b + (lp ^ (2 * x))), dst, 16, 2048, 2);
-    __builtin_amdgcn_global_load_lds((const void*)(uintptr_t)(b + (lp ^ (3 * x))), dst, 16, 3072, 2);
+    __builtin_amdgcn_global_load_lds((const void*)(uintptr_t)(b + (lp ^ (2 * x))), dst, 16, 2 * 1024, 2);
+    __builtin_amdgcn_global_load_lds((const void*)(uintptr_t)(b + (lp ^ (3 * x))), dst, 16, 3 * 1024, 2);
   }
 }
 

@@ -381,6 +381,41 @@ def test_equal_bits_every_time_and_on_another_stream():
     kv.close()
 
 
+def test_two_handles_at_once():
+    """Calls of two handles on two streams, and two captured graphs of one handle
+    replayed in turn."""
+    import torch
+    calls = [Call(45, [700, 90, 300], [3, 16, 40], heads=8, n_kv=2),
+             Call(46, [1, 2500], [1, 2], heads=4, n_kv=2, cache="e4m3", P=64)]
+    handles = [c.device() for c in calls]
+    alone = [c.run(kv) for c, kv in zip(calls, handles)]
+    streams = [torch.cuda.Stream() for _ in calls]
+    torch.cuda.synchronize()
+    outs = [[], []]
+    for _ in range(10):
+        for i, (c, kv) in enumerate(zip(calls, handles)):
+            with torch.cuda.stream(streams[i]):
+                outs[i].append(c.run(kv))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(o.equal(alone[i]) for o in outs[i])
+    c, kv = calls[0], handles[0]
+    masks = [dict(causal=True), dict(causal=False, window=50)]
+    eager = [c.run(kv, **m) for m in masks]
+    graphs, res = [torch.cuda.CUDAGraph() for _ in masks], [torch.empty_like(c.dq) for _ in masks]
+    for g, m, o in zip(graphs, masks, res):
+        torch.cuda.synchronize()
+        with torch.cuda.graph(g):
+            c.run(kv, out=o, **m)
+    for k in (0, 1, 1, 0, 1):
+        res[k].zero_()
+        graphs[k].replay()
+        torch.cuda.synchronize()
+        assert res[k].equal(eager[k])
+    for kv in handles:
+        kv.close()
+
+
 @pytest.mark.parametrize("shared", [False, True])
 def test_captured_calls_replay_with_new_lengths(shared):
     import torch
@@ -818,6 +853,34 @@ def test_layer_over_windowed_and_8bit_pages():
             assert np.abs(h[b].cpu().numpy() - ref).max() <= bar
         layer.close()
         kv.close()
+
+
+def test_layer_over_pages_captured():
+    """Replayed with shorter contexts, eager calls in between."""
+    import torch
+    layer, kv, d = _paged_layer(2, 4, 16, [150, 0, 65], "bf16", seed=12)
+    h = torch.empty(3, 16, 256, device="cuda")
+    hb = torch.empty(3, 16, 256, dtype=torch.bfloat16, device="cuda")
+
+    def call():
+        return layer.forward_paged(d["x"], kv, d["pk"], d["pv"], d["table"], d["cl"], window=90,
+                                   sinks=3, h_f32=h, h_bf16=hb)
+    call()
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        call()
+    for ctx in ([150, 0, 65], [140, 0, 50], [131, 0, 49], [150, 0, 65]):
+        d["cl"].copy_(_i32(ctx))
+        h.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        got, bits = h.clone(), hb.clone()
+        call()
+        assert got.equal(h) and bits.equal(hb) and got.abs().max() > 0
+    assert kv.device_errors() == 0
+    layer.close()
+    kv.close()
 
 
 def test_layer_over_pages_rejects_bad_calls():
