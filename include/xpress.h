@@ -470,7 +470,8 @@ xp_status xp_kv_write(xp_kv* kv, int32_t tokens, const void* k, int64_t k_ld, co
  *   window      0: none; W: a token at position p sees keys j > p - W only
  *   sinks       with a window, keys j < sinks stay visible
  *   scale       of q.k; 0: 1 / sqrt(head_dim)
- *   out         [tokens][n_heads][head_dim] bf16, token rows out_ld apart
+ *   out         [tokens][n_heads][head_dim] bf16, token rows out_ld apart; apart
+ *               from q
  *   lse         [tokens][n_heads] float or NULL: log sum exp of the scaled scores
  *
  * Query head h reads KV head h / (n_heads / n_kv).  Token i of request b has
@@ -480,7 +481,8 @@ xp_status xp_kv_write(xp_kv* kv, int32_t tokens, const void* k, int64_t k_ld, co
  * its result, whatever they hold.  Scores and sums are fp32; the numerators enter
  * the product with V as two bf16 parts, as one with an 8-bit cache and in calls of
  * more than 64 rows (max_q times the heads of a group; with shared prefixes at least
- * the mean tokens of a group times the heads).
+ * the mean tokens of a group times the heads, or, for the keys behind prefixes that
+ * fill the largest row tiles, max_q alone).
  * Pages outside [0, n_pages) where a key is read are replaced by 0 and set
  * XP_DEVERR_PAGE; lengths outside [0, max_len] are clamped (XP_DEVERR_LENGTH).
  * The same call gives the same bits; a request's summation order follows the
