@@ -464,7 +464,8 @@ xp_status xp_kv_write(xp_kv* kv, int32_t tokens, const void* k, int64_t k_ld, co
  *               - 1; NULL: max_q each (tokens = n max_q).  Tokens from cu_q[n]
  *               on are left as they are.
  *   max_q       the most tokens of a request, up to max_tokens (it sizes the row
- *               tiles; a wrong one costs time only)
+ *               tiles and chooses the numerators' parts, below; a wrong one costs
+ *               time only)
  *   kv_len      [n] int32: keys of request b, the new tokens' own among them
  *   causal      1 or 0 (the drafter's bidirectional block)
  *   window      0: none; W: a token at position p sees keys j > p - W only

@@ -36,13 +36,13 @@ struct KvMap {
 // The pool's page number k from its top, given `top` free pages.
 __device__ __forceinline__ int pool_page(const int32_t* pool, int top, int k) { return pool[top - 1 - k]; }
 
-// Slot of token t: request b = owner(t), its position's page from the table or,
-// where this call takes it, from the pool.
+// Slot of token t: its request b (from lo, before hi), its position's page from the
+// table or, where this call takes it, from the pool.
 __device__ __forceinline__ int slot_of(const KvMap& d, int t, const int* acu, const int* take,
                                        const int32_t* old, const int32_t* len, int top,
-                                       uint32_t& bad) {
+                                       uint32_t& bad, int lo, int hi) {
   if (t >= acu[d.n]) return -1;
-  const int b = kv_owner(acu, d.n, t);
+  const int b = kv_owner(acu, lo, hi, t);
   const int pos = len[b] + t - acu[b], col = pos >> d.logP, h = old[b];
   if (take[b + 1] > take[b] && take[b + 1] > top) return -1;     // not served
   const int page = col < h ? d.table[b * d.ld + col] : pool_page(d.pool, top, take[b] + col - h);
@@ -66,9 +66,9 @@ __device__ __forceinline__ void take_page(const KvMap& d, int k, const int* take
 // block scans over the requests, then one search per page and slot (8 requests with
 // blocks of 17: 4.6 us; 512 without slots 5.2).
 constexpr int kMapThreads = 1024;
-// Slots up to which one launch does all: 4096 of 64 requests 6.6 us in one, 8.9 in two;
-// 8192 9.6 and 8.8, 32768 27.7 and 8.8.
-constexpr int kMapOneLaunch = 6144;
+// Slots up to which one launch does all: 4096 of 64 requests 6.6 us in one, 7.5 in two;
+// 8192 9.6 and 7.6, 32768 27.7 and 7.6.
+constexpr int kMapOneLaunch = 5120;
 template <bool ALL>
 __global__ __launch_bounds__(kMapThreads) void k_kv_map(const KvMap d) {
   __shared__ int rel[kKvMaxBatch + 1], take[kKvMaxBatch + 1], acu[kKvMaxBatch + 1];
@@ -206,14 +206,14 @@ __global__ __launch_bounds__(kMapThreads) void k_kv_map(const KvMap d) {
     for (int k = tid; k < T; k += kMapThreads) take_page(d, k, take, old, top);
     if (d.slots)
       for (int t = tid; t < d.max_slots; t += kMapThreads)
-        d.slots[t] = slot_of(d, t, acu, take, old, len, top, bad);
+        d.slots[t] = slot_of(d, t, acu, take, old, len, top, bad, 0, d.n);
   }
   if (bad) atomicOr(d.err, bad);
 }
 
 // The pages taken and the slots of a large call, over many workgroups (a slot's
 // page comes from the pool where this call takes it, so that no workgroup waits
-// for another's table entries).  524000 slots: 8.9 us.
+// for another's table entries).  524000 slots: 6.5 us.
 __global__ __launch_bounds__(256) void k_kv_slots(const KvMap d) {
   __shared__ int take[kKvMaxBatch + 1], acu[kKvMaxBatch + 1];
   for (int b = threadIdx.x; b <= d.n; b += 256) {
@@ -224,8 +224,26 @@ __global__ __launch_bounds__(256) void k_kv_slots(const KvMap d) {
   const int top = d.top[0], T = d.top[1], step = gridDim.x * 256;
   uint32_t bad = 0;
   for (int k = blockIdx.x * 256 + threadIdx.x; k < T; k += step) take_page(d, k, take, d.old, top);
-  for (int64_t t = blockIdx.x * 256 + threadIdx.x; t < d.max_slots; t += step)
-    d.slots[t] = slot_of(d, (int)t, acu, take, d.old, d.lens, top, bad);
+  // a wave takes 256 neighbouring slots: one search for the requests of every 64th
+  constexpr int kU = 4;
+  const int lane = threadIdx.x & 63, last = acu[d.n] - 1;
+  for (int64_t i0 = ((int64_t)blockIdx.x * 256 + (threadIdx.x & ~63)) * kU; i0 < d.max_slots;
+       i0 += (int64_t)step * kU) {
+    const int64_t mark = i0 + lane * kWave;
+    const int own = last < 0 ? 0 : kv_owner(acu, d.n, (int)(mark < last ? mark : last));
+    int slot[kU];
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const int64_t t = i0 + u * kWave + lane;
+      slot[u] = t < d.max_slots
+          ? slot_of(d, (int)t, acu, take, d.old, d.lens, top, bad,
+                    __builtin_amdgcn_readlane(own, u), __builtin_amdgcn_readlane(own, u + 1) + 1)
+          : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < kU; ++u)
+      if (i0 + u * kWave + lane < d.max_slots) d.slots[i0 + u * kWave + lane] = slot[u];
+  }
   if (bad) atomicOr(d.err, bad);
 }
 
