@@ -148,8 +148,8 @@ __global__ __launch_bounds__(kMapThreads) void k_kv_map(const KvMap d) {
   int top = free0 + R;
   // A wave returns kBack * 64 neighbouring pages at a time: one search finds the
   // requests of every 64th, and each page's lies between those of its 64 (a search
-  // per page kept one workgroup's shared memory busy: 32000 pages 35 us, now 16).
-  constexpr int kBack = 8;
+  // per page kept one workgroup's shared memory busy: 32000 pages 35 us, now 15).
+  constexpr int kBack = 16;
   for (int i0 = wave * kBack * kWave; i0 < R; i0 += kBack * kMapThreads) {
     const int mark = i0 + lane * kWave;
     const int own = kv_owner(rel, d.n, mark < R ? mark : R - 1);   // lanes 0 .. kBack
