@@ -418,7 +418,7 @@ const char* xp_kv_last_error(const xp_kv* kv);
  *   pool [n_pages] in/out, pool_n [1] in/out   the free pages, a stack whose top
  *       is pool[pool_n - 1]
  *   cu [n + 1] or NULL        exclusive sums of add
- *   kv_len [n] or NULL        lens + add
+ *   kv_len [n] or NULL        lens + add; may be the array of lens or of add
  *   slots [max_slots] or NULL slot of new token i of request b at cu[b] + i; -1
  *       from cu[n] on
  *

@@ -112,6 +112,7 @@ struct xp_kv {
   int32_t* take = nullptr;           // [max_batch + 1] pages taken before each request
   int32_t* old = nullptr;            // [max_batch] pages held before the call
   int32_t* acu = nullptr;            // [max_batch + 1] new tokens before each request
+  int32_t* len = nullptr;            // [max_batch] tokens before the call (-1: left alone)
   int32_t* top = nullptr;            // [2] free pages after the releases, pages taken
   uint32_t* err = nullptr;
   std::string msg;

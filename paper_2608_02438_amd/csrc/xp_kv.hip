@@ -29,7 +29,7 @@ struct KvMap {
   int32_t* cu;
   int32_t* kv_len;
   int32_t* slots;
-  int32_t *take, *old, *acu, *top;   // for k_kv_slots
+  int32_t *take, *old, *acu, *len, *top;   // for k_kv_slots, which may run with kv_len in lens's place
   uint32_t* err;
 };
 
@@ -187,6 +187,7 @@ __global__ __launch_bounds__(kMapThreads) void k_kv_map(const KvMap d) {
       d.take[b] = take[b];
       d.old[b] = old[b];
       d.acu[b] = acu[b];
+      d.len[b] = len[b];
     }
   }
   __syncthreads();
@@ -236,7 +237,7 @@ __global__ __launch_bounds__(256) void k_kv_slots(const KvMap d) {
     for (int u = 0; u < kU; ++u) {
       const int64_t t = i0 + u * kWave + lane;
       slot[u] = t < d.max_slots
-          ? slot_of(d, (int)t, acu, take, d.old, d.lens, top, bad,
+          ? slot_of(d, (int)t, acu, take, d.old, d.len, top, bad,
                     __builtin_amdgcn_readlane(own, u), __builtin_amdgcn_readlane(own, u + 1) + 1)
           : 0;
     }
@@ -468,7 +469,7 @@ extern "C" xp_status xp_kv_create(const xp_kv_shape* s, int32_t max_batch, int32
   KvList &l0 = kv->a.list[0], &l1 = kv->a.list[1];
   struct Slice { void** at; size_t bytes; };
   char* zero = nullptr;
-  int32_t* acu = nullptr;
+  int32_t *acu = nullptr, *len = nullptr;
   const Slice slices[] = {
       {(void**)&zero, 256},
       {(void**)&kv->err, 256},
@@ -476,6 +477,7 @@ extern "C" xp_status xp_kv_create(const xp_kv_shape* s, int32_t max_batch, int32
       {(void**)&kv->take, (nb + 1) * 4},
       {(void**)&kv->old, nb * 4},
       {(void**)&acu, (nb + 1) * 4},
+      {(void**)&len, nb * 4},
       {(void**)&kv->a.dump, 512},
       {(void**)&l0.hdr, 256},
       {(void**)&l0.share, ((size_t)shares + 1) * sizeof(KvShare)},
@@ -506,6 +508,7 @@ extern "C" xp_status xp_kv_create(const xp_kv_shape* s, int32_t max_batch, int32
   }
   kv->a.zero = zero;
   kv->acu = acu;
+  kv->len = len;
   // the zero row and the device error word; done before the call returns
   e = hipMemset(kv->ws, 0, 512);
   if (e == hipSuccess) e = hipDeviceSynchronize();
@@ -572,6 +575,7 @@ extern "C" xp_status xp_kv_map(xp_kv* kv, int32_t n, const int32_t* lens, const 
   d.take = kv->take;
   d.old = kv->old;
   d.acu = kv->acu;
+  d.len = kv->len;
   d.top = kv->top;
   d.err = kv->err;
   hipStream_t st = (hipStream_t)stream;
