@@ -501,9 +501,10 @@ xp_status xp_kv_attn(xp_kv* kv, int32_t n, int32_t tokens, int32_t max_q, const 
  * The same for requests that begin with common prefixes: group g is requests
  * group_start[g] .. group_start[g + 1] - 1 (neighbours; [groups + 1] int32), whose
  * first shared_len[g] ([groups] int32) keys are the same pages.  They are read
- * once for the whole group, through its first request's table.  shared_len may
- * end inside a page and reach into the new tokens; it is clamped to the shortest
- * member (XP_DEVERR_LENGTH).  Requests outside every group, and groups of length
+ * once for the whole group, through the table of its first request that has new
+ * tokens (requests without any need no keys or pages).  shared_len may end inside a
+ * page and reach into the new tokens; it is clamped to the shortest member that has
+ * tokens (XP_DEVERR_LENGTH).  Requests outside every group, and groups of length
  * 0, are attended as in xp_kv_attn.  The result differs from xp_kv_attn's in
  * summation order only.
  */

@@ -173,6 +173,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d, const 
   __shared__ int gmin[SHARED ? kKvMaxBatch : 1];  // a group's positions: least and greatest
   __shared__ int gmax[SHARED ? kKvMaxBatch : 1];
   __shared__ int glen[SHARED ? kKvMaxBatch : 1];  // and its prefix keys
+  __shared__ int gseq[SHARED ? kKvMaxBatch : 1];  // its first request that has tokens
   __shared__ int cums[kPlanCum];
   __shared__ int red[kPlanWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -201,19 +202,21 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d, const 
     for (int g = wave; g < d.groups; g += kPlanWaves) {
       int s0, s1;
       members(g, s0, s1);
-      int pmin = 0x7fffffff, pmax = -0x7fffffff, kmin = d.cap;
+      int pmin = 0x7fffffff, pmax = -0x7fffffff, kmin = d.cap, smin = n;
       for (int b = s0 + lane; b < s1; b += kWave) {
         const int t0 = first(b), ql = tokens(b, t0), kv = keys(b);
         if (ql == 0) continue;
         pmin = imin(pmin, kv - ql);
         pmax = imax(pmax, kv - 1);
         kmin = imin(kmin, kv);
+        smin = imin(smin, b);
       }
 #pragma unroll
       for (int o = 32; o > 0; o >>= 1) {
         pmin = imin(pmin, __shfl_xor(pmin, o, kWave));
         pmax = imax(pmax, __shfl_xor(pmax, o, kWave));
         kmin = imin(kmin, __shfl_xor(kmin, o, kWave));
+        smin = imin(smin, __shfl_xor(smin, o, kWave));
       }
       const int want = d.shared_len[g], len = clampi(want, 0, kmin);
       if (want != len) bad |= XP_DEVERR_LENGTH;
@@ -222,6 +225,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d, const 
         gmin[g] = pmin;
         gmax[g] = pmax;
         glen[g] = len;
+        gseq[g] = smin;
       }
     }
     __syncthreads();
@@ -287,7 +291,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d, const 
         int s0, s1;
         members(i - ns, s0, s1);
         x.tok0 = first(s0);
-        x.seq = s0;
+        x.seq = imin(gseq[i - ns], n - 1);
         x.nrows = imin((first(s1) - x.tok0) * d.grp - x.row0, R);
         x.prefix = 1;
         x.ceil = glen[i - ns];

@@ -54,3 +54,28 @@ def test_map_of_two_launches_returns_and_takes():
         lens[0] = 100
         lens[rng.integers(1, n)] = 0
     s.kv.close()
+
+
+@pytest.mark.parametrize("ql,kv_len", [([0, 2, 1, 3], [0, 130, 140, 200]),
+                                       ([0, 0, 1, 1], [0, 40, 128, 129]),
+                                       ([0, 16, 16, 16, 16, 16, 16, 16], [0] + [300] * 7)])
+@pytest.mark.parametrize("hd,cache", [(128, "bf16"), (64, "e4m3")])
+def test_shared_prefix_of_a_group_whose_first_requests_have_no_tokens(ql, kv_len, hd, cache):
+    """The first request has ended: no keys, no pages in its row of the table."""
+    import torch
+    n = len(ql)
+    # the pages come from a call in which every member holds them
+    c = Call(140 + n, [max(x, 128) for x in kv_len], ql, heads=8, n_kv=2, hd=hd, cache=cache, P=16,
+             groups=[(0, n, 128)])
+    kv = c.device(shared=True)
+    c.kv = kv_len
+    for b, x in enumerate(kv_len):
+        c.dtable[b, R.pages_of(x, 16):] = -1
+    c.dkv = _i32(kv_len)
+    rows = max(max(ql), c.total) * 4
+    for m in (dict(causal=True), dict(causal=False), dict(causal=True, window=40, sinks=20)):
+        print(f"first member empty: {ql} hd={hd} {cache} {m}", flush=True)
+        out = c.run(kv, shared=True, **m)
+        assert kv.device_errors() == 0
+        c.check(out, parts=parts_of(rows, cache), **m)
+    kv.close()
