@@ -504,9 +504,10 @@ xp_status xp_kv_attn(xp_kv* kv, int32_t n, int32_t tokens, int32_t max_q, const 
  * once for the whole group, through the table of its first request that has new
  * tokens (requests without any need no keys or pages).  shared_len may end inside a
  * page and reach into the new tokens; it is clamped to the shortest member that has
- * tokens (XP_DEVERR_LENGTH).  Requests outside every group, and groups of length
- * 0, are attended as in xp_kv_attn.  The result differs from xp_kv_attn's in
- * summation order only.
+ * tokens (XP_DEVERR_LENGTH).  group_start does not run backwards: where it does, no
+ * prefix is shared, and outside 0 .. n it is clamped (XP_DEVERR_LENGTH both).  Requests
+ * outside every group, and groups of length 0, are attended as in xp_kv_attn.  The
+ * result differs from xp_kv_attn's in summation order only.
  */
 xp_status xp_kv_attn_shared(xp_kv* kv, int32_t n, int32_t tokens, int32_t max_q, int32_t groups,
                             const int32_t* group_start, const int32_t* shared_len, const void* q,

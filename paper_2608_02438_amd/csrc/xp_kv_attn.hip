@@ -197,7 +197,15 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d, const 
       if (!second) w.row[0][t] = int2{-1, 0};
       if (items > ns) w.row[1][t] = int2{-1, 0};
     }
-    __syncthreads();
+    // Groups that run backwards could hold a request twice: then none is shared.
+    bool back = false;
+    for (int g = tid; g < d.groups; g += kPlanThreads) {
+      const int s0 = d.group_start[g], s1 = d.group_start[g + 1];
+      back |= s1 < s0;
+      if ((s0 < 0) | (s1 > n)) bad |= XP_DEVERR_LENGTH;
+    }
+    const bool apart = __syncthreads_or(back);
+    if (apart) bad |= XP_DEVERR_LENGTH;
     // a wave per group: its members' positions, and a prefix that none is shorter than
     for (int g = wave; g < d.groups; g += kPlanWaves) {
       int s0, s1;
@@ -218,7 +226,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d, const 
         kmin = imin(kmin, __shfl_xor(kmin, o, kWave));
         smin = imin(smin, __shfl_xor(smin, o, kWave));
       }
-      const int want = d.shared_len[g], len = clampi(want, 0, kmin);
+      const int want = d.shared_len[g], len = apart ? 0 : clampi(want, 0, kmin);
       if (want != len) bad |= XP_DEVERR_LENGTH;
       for (int b = s0 + lane; b < s1; b += kWave) floors[b] = len;
       if (lane == 0) {

@@ -79,3 +79,19 @@ def test_shared_prefix_of_a_group_whose_first_requests_have_no_tokens(ql, kv_len
         assert kv.device_errors() == 0
         c.check(out, parts=parts_of(rows, cache), **m)
     kv.close()
+
+
+@pytest.mark.parametrize("starts,lens", [([0, 3, 2, 5], [64, 0, 128]), ([5, 0], [128]),
+                                         ([0, 2, 9], [64, 128]), ([-3, 2, 5], [64, 128])])
+def test_groups_out_of_order_are_reported_and_attended_alone(starts, lens):
+    from paper_2608_02438_amd import xpress as X
+    c = Call(150, [200, 210, 195, 260, 300], [1, 2, 3, 1, 2], heads=4, n_kv=2,
+             groups=[(0, 2, 128), (2, 5, 128)])
+    kv = c.device(shared=True)
+    for m in (dict(causal=True), dict(causal=True, window=100, sinks=20)):
+        print(f"groups {starts} {m}", flush=True)
+        c.dgs, c.dgl = _i32(starts), _i32(lens)
+        out = c.run(kv, shared=True, **m)
+        assert kv.device_errors() == X.XP_DEVERR_LENGTH
+        c.check(out, parts=2, **m)
+    kv.close()
