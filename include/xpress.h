@@ -478,10 +478,10 @@ xp_status xp_kv_write(xp_kv* kv, int32_t tokens, const void* k, int64_t k_ld, co
  * Query head h reads KV head h / (n_heads / n_kv).  Token i of request b has
  * position p = kv_len[b] - q_len[b] + i and sees key j iff j < kv_len[b], j <= p
  * if causal, and j > p - window or j < sinks if there is a window.  A token that
- * sees no key gives 0 (lse -inf).  Keys that a token does not see do not enter
- * its result, whatever they hold.  Scores and sums are fp32; the numerators enter
- * the product with V as two bf16 parts, as one with an 8-bit cache and in calls of
- * more than 64 rows (max_q times the heads of a group; with shared prefixes at least
+ * sees no key gives 0 (lse -inf), one whose scores are all -inf NaN (lse -inf).
+ * Keys that a token does not see do not enter its result, whatever they hold.
+ * Scores and sums are fp32; the numerators enter the product with V as two bf16
+ * parts, as one with an 8-bit cache and in calls of more than 64 rows (max_q times the heads of a group; with shared prefixes at least
  * the mean tokens of a group times the heads, or, for the keys behind prefixes that
  * fill the largest row tiles, max_q alone).
  * Pages outside [0, n_pages) where a key is read are replaced by 0 and set

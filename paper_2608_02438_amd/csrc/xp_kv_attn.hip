@@ -6,7 +6,8 @@
 // and sees key j iff
 //   j < kv_len[b]  and  (not causal or j <= p)  and
 //   (window == 0 or j > p - window or j < sinks);
-// o = sum_j softmax_j(scale q.k_j) v_j over these, 0 if there are none.
+// o = sum_j softmax_j(scale q.k_j) v_j over these, 0 if there are none (and 0 / 0 if
+// every score is -inf).
 //
 // Work list (k_kv_plan, plan_own).  The rows of a KV head's group, (token, head) pairs,
 // are cut into tiles of up to R rows; a tile walks the 64-key tiles that any of
@@ -548,6 +549,12 @@ struct KvSees {
   int lo, floor;
   uint32_t n, s;
 };
+
+// a token at position p of a sequence of `keys` keys sees one of them
+__device__ __forceinline__ bool sees_some(const KvDev& d, int p, int keys) {
+  const int hi = d.causal ? imin(p + 1, keys) : keys;
+  return (hi > 0) & ((d.window == 0) | (hi > p - d.window + 1) | (d.sinks > 0));
+}
 
 // inclusive sum over the wave
 __device__ __forceinline__ int wave_scan(int v, int lane) {
@@ -1098,7 +1105,8 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
     const int head = kvh * d.grp + (row - tk * d.grp);
     if (whole && d.groups == 0) {
       const float inv = l_run == 0.f
-          ? 0.f : (F8 && d.v_scale != nullptr ? d.v_scale[kvh] : 1.f) / l_run;
+          ? (sees_some(d, p0 + tk, kceil) ? NAN : 0.f)
+          : (F8 && d.v_scale != nullptr ? d.v_scale[kvh] : 1.f) / l_run;
       uint16_t* op = (rv ? d.out + tok * d.out_ld + (int64_t)head * HD : (uint16_t*)d.w.dump) + 8 * h;
 #pragma unroll
       for (int db = 0; db < ND; ++db)
@@ -1197,11 +1205,13 @@ __device__ __forceinline__ void add_parts(const KvDev& d, int64_t part0, int R, 
   if (s <= s1) add_some<HD, 4>(d, part0, R, s, s0, s1, rr, c, x);
 }
 
+// p: the token's position, keys: its sequence's
 template <int HD>
 __device__ __forceinline__ void write_row(const KvDev& d, int64_t tok, int head, int c,
-                                          const KvSum& x) {
+                                          const KvSum& x, int p, int keys) {
   const int kvh = head / d.grp;
-  const float inv = x.l == 0.f ? 0.f : (d.v_scale != nullptr ? d.v_scale[kvh] : 1.f) / x.l;
+  const float inv = x.l == 0.f ? (sees_some(d, p, keys) ? NAN : 0.f)
+                               : (d.v_scale != nullptr ? d.v_scale[kvh] : 1.f) / x.l;
   *reinterpret_cast<uint2*>(d.out + tok * d.out_ld + (int64_t)head * HD + c) =
       uint2{pk_bf16(x.o[0] * inv, x.o[1] * inv), pk_bf16(x.o[2] * inv, x.o[3] * inv)};
   if (d.lse != nullptr && c == 0)
@@ -1221,13 +1231,13 @@ __global__ __launch_bounds__(256) void k_kv_join(const KvDev d, int R) {
   const int a = f - j;                            // the unit of the segment's first tile
   if (a < f - S) return;                          // cut before: an earlier workgroup's
   const scalar_i32 en = as_scalar(d.list.ent + e);
-  const int tok0 = en[0], row0 = en[1], nrows = en[2], tiles = en[11];
+  const int tok0 = en[0], row0 = en[1], nrows = en[2], p0 = en[4], keys = en[7], tiles = en[11];
   const int rr = blockIdx.y * RPB + threadIdx.x / TPR, c = 4 * (threadIdx.x % TPR);
   if (rr >= nrows) return;
   KvSum x;
   add_parts<HD>(d, d.part0, R, a, tiles, S, rr, c, x);
   const int row = row0 + rr, tk = row / d.grp;
-  write_row<HD>(d, tok0 + tk, kvh * d.grp + (row - tk * d.grp), c, x);
+  write_row<HD>(d, tok0 + tk, kvh * d.grp + (row - tk * d.grp), c, x, p0 + tk, keys);
 }
 
 // Calls with shared prefixes: every row, its prefix's result and its own.
@@ -1247,6 +1257,7 @@ __global__ __launch_bounds__(256) void k_kv_join_rows(const KvDev d, const KvJoi
   const int2 at[2] = {d.w.row[0][tok], d.w.row[1][tok]};
   if (at[0].x < 0) return;                        // behind the last sequence
   int lr[2], c0[2], c1[2], S[2];                  // row, units before and behind its entry
+  const KvEntry* own = nullptr;
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const KvList& l = d.w.list[jn.one ? 0 : k];
@@ -1256,6 +1267,7 @@ __global__ __launch_bounds__(256) void k_kv_join_rows(const KvDev d, const KvJoi
     S[k] = l.hdr[1];
     c0[k] = l.cum[has ? e : 0];
     c1[k] = has ? l.cum[e + 1] : 0;
+    if (k == 0) own = l.ent + (has ? e : 0);
   }
   KvSum x;
 #pragma unroll
@@ -1271,7 +1283,7 @@ __global__ __launch_bounds__(256) void k_kv_join_rows(const KvDev d, const KvJoi
       add_parts<HD>(d, k == 1 ? jn.part0 : 0, jn.R[k], a, tiles, S[k], lr[k] % jn.R[k], c, x);
     }
   }
-  write_row<HD>(d, tok, head, c, x);
+  write_row<HD>(d, tok, head, c, x, d.w.pos[tok], own->ceil);
 }
 
 // ---------------------------------------------------------------------------

@@ -95,3 +95,38 @@ def test_groups_out_of_order_are_reported_and_attended_alone(starts, lens):
         assert kv.device_errors() == X.XP_DEVERR_LENGTH
         c.check(out, parts=2, **m)
     kv.close()
+
+
+@pytest.mark.parametrize("shared", [False, True])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("ql", [[1, 2], [40, 70]])
+def test_rows_whose_every_score_is_minus_infinity(shared, hd, ql):
+    """0 / 0 by the formula: NaN, with a log sum of -inf; not the zeros of a row that
+    sees no key.  Rows that see one finite score are not touched by the others."""
+    import torch
+    c = Call(160 + hd, [ql[0] + 700, ql[1] - 1], ql, heads=4, n_kv=2, hd=hd, P=16,
+             groups=[(0, 1, 64), (1, 2, 0)] if shared else ())
+    first = 3                                                 # key 3 of request 0 is finite
+    c.q[:, :, 0] = np.abs(c.q[:, :, 0]) + 1
+    for b in range(2):
+        for j in range(c.kv[b]):
+            if (b, j) != (0, first):
+                c.k[c.table[b, j // 16], :, j % 16, 0] = -np.inf
+    kv = c.device(shared=shared)
+    lse = torch.empty((c.total, 4), device="cuda")
+    for m, some in ((dict(causal=True), True), (dict(causal=True, window=90), False),
+                    (dict(causal=True, window=90, sinks=2), False)):
+        print(f"infinite scores: hd={hd} ql={ql} shared={shared} {m}", flush=True)
+        out = c.run(kv, shared=shared, lse=lse, **m).double().cpu().numpy()
+        sums = lse.cpu().numpy()
+        a, b = out[:ql[0]], out[ql[0]:]
+        if some:                                              # key 3 alone has a weight
+            want = c.v[c.table[0, 0], :, first][np.repeat(np.arange(2), 2)]
+            np.testing.assert_array_equal(a, np.broadcast_to(want, a.shape))
+            assert np.isfinite(sums[:ql[0]]).all()
+        else:
+            assert np.isnan(a).all() and (sums[:ql[0]] == -np.inf).all()
+        # request 1 has a token more than keys: its first one sees none
+        assert (b[0] == 0).all() and np.isnan(b[1:]).all()
+        assert (sums[ql[0]:] == -np.inf).all()
+    kv.close()
