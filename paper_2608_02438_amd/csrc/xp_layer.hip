@@ -1493,12 +1493,12 @@ extern "C" xp_status xp_layer_forward_paged(xp_layer* L, xp_kv* kv, int32_t batc
   if (L == nullptr) return XP_EINVAL;
   if (kv == nullptr || table == nullptr || table_ld < 1)
     return layer_fail(L, XP_EINVAL, "kv, table and table_ld >= 1 are required");
-  // the most context keys that leave room for the block
-  const int64_t cap = std::min<int64_t>(kv->max_pages, table_ld) << kv->logP;
-  const int C_max = (int)std::min<int64_t>(cap, 1 << 20) - B;
-  const xp_status cs = check_call(L, batch, B, causal, x, k_cache, v_cache, std::max(C_max, 1),
-                                  ctx_len, h_f32, h_bf16);
+  const xp_status cs =
+      check_call(L, batch, B, causal, x, k_cache, v_cache, 1, ctx_len, h_f32, h_bf16);
   if (cs != XP_OK) return cs;
+  // the most context keys that leave room for the block, as the attention clamps them
+  const int64_t cap = std::min<int64_t>(kv->max_pages, table_ld) << kv->logP;
+  const int C_max = (int)std::min<int64_t>(cap, kKvMaxLen) - B;
   if (C_max < 0)
     return layer_fail(L, XP_EINVAL, "a table of %lld pages has no room for a block of %d",
                       (long long)table_ld, B);

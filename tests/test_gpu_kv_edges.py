@@ -130,3 +130,52 @@ def test_rows_whose_every_score_is_minus_infinity(shared, hd, ql):
         assert (b[0] == 0).all() and np.isnan(b[1:]).all()
         assert (sums[ql[0]:] == -np.inf).all()
     kv.close()
+
+
+@pytest.mark.parametrize("ctx", [[(1 << 20) - 17, 20], [(1 << 20) - 16, 1 << 20], [(1 << 20) + 5, 0],
+                                 [(1 << 21) - 16, (1 << 21) - 40]])
+def test_layer_over_pages_past_2_to_the_20_keys(ctx):
+    """The block's keys are rotated for their own positions.  Pages are used many
+    times over, so that a long context takes little memory; the window keeps the
+    attention to the last of them."""
+    import torch
+    import synth
+    from paper_2608_02438_amd.xpress import LAYER_WEIGHT_NAMES, Layer, PagedKV, device_tensor
+    B, nkv, nh, H, P, batch, width = 16, 2, 4, 256, 256, 2, 1 << 13
+    w = synth.scaled(synth.configs.QWEN_B1, index=971, H=H, B=B, batch=batch, n_heads=nh,
+                     n_kv_heads=nkv, ffn=256, ctx_len=None, ctx_len_range=None)
+    weights, inp = synth.make_layer_weights(w), synth.make_layer_inputs(w, c_max=64)
+    layer = Layer({k: device_tensor(weights[k]) for k in LAYER_WEIGHT_NAMES}, H, nh, nkv, 256,
+                  max_batch=batch, max_B=B, max_ctx=64)
+    x = device_tensor(inp.x)
+    kv = PagedKV(nh, nkv, P, 8, batch, batch * B, width * P)
+    table = torch.zeros((batch, width), dtype=torch.int32, device="cuda")
+    for b in range(batch):                                    # the block's pages: their own
+        for j in (ctx[b] // P, (ctx[b] + B - 1) // P):
+            table[b, j] = 1 + 3 * b + j % 3
+    kc, vc = (torch.randn(kv.cache_shape, device="cuda").to(torch.bfloat16) for _ in range(2))
+    print(f"layer: contexts {ctx}", flush=True)
+    h, _ = layer.forward_paged(x, kv, kc, vc, table, _i32(ctx), window=64)
+    assert kv.device_errors() == 0
+    LP = O.layer_ref.LayerParams.from_arrays(weights, nh, nkv, 128)
+    r16, rms = O.xpress_ref.round_bf16, O.layer_ref.rmsnorm
+    for b in range(batch):
+        xb = O.xpress_ref.to_f64(inp.x[b])
+        u = r16(rms(xb, LP.g_attn, LP.eps))
+        pos = ctx[b] + np.arange(B)
+        k = O.layer_ref.rope(rms((u @ LP.Wk.T).reshape(B, nkv, 128), LP.g_k, LP.eps), pos, LP.theta)
+        n, lo = ctx[b] + B, max(ctx[b] - 64, 0)
+        j = np.arange(lo, n)
+        rows = table[b].cpu().numpy()[j // P]
+        gk, gv = (a.double().cpu().numpy()[rows, :, j % P] for a in (kc, vc))
+        # half a bf16 step and what a differently rounded u moves
+        assert np.abs(gk[-B:] - k).max() <= 2.0 ** -7 * np.abs(k).max()
+        q = r16(O.layer_ref.rope(rms((u @ LP.Wq.T).reshape(B, nh, 128), LP.g_q, LP.eps), pos, LP.theta))
+        a = R.attend(q, gk, gv, True, 64, 0)[0]
+        x1 = xb + r16(a.reshape(B, -1)) @ LP.Wo.T
+        u2 = r16(rms(x1, LP.g_mlp, LP.eps))
+        ref = x1 + r16(O.xpress_ref.silu(u2 @ LP.Wg.T) * (u2 @ LP.Wu.T)) @ LP.Wd.T
+        bar = max(2e-2, 2.0 ** -8 * np.abs(ref).max())
+        assert np.abs(h[b].cpu().numpy() - ref).max() <= bar
+    layer.close()
+    kv.close()
