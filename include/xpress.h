@@ -370,7 +370,7 @@ xp_status xp_layer_forward_noalloc(const xp_layer_weights* w, int32_t batch, int
  *
  *   k_cache, v_cache [n_pages][n_kv][page_size][head_dim]   caller-owned
  *       XP_BF16, or XP_E4M3 with a scale per KV head (k_scale, v_scale [n_kv]
- *       float, > 0; NULL: 1): the value of an entry is e4m3 times the scale
+ *       float, 2^-60 .. 2^60; NULL: 1): the value of an entry is e4m3 times the scale
  *   table [..][table_ld] int32   the pages of each request, in order; key j of
  *       request b is row j % page_size of page table[b][j / page_size]
  *   a slot is page * page_size + row
@@ -470,7 +470,7 @@ xp_status xp_kv_write(xp_kv* kv, int32_t tokens, const void* k, int64_t k_ld, co
  *   causal      1 or 0 (the drafter's bidirectional block)
  *   window      0: none; W: a token at position p sees keys j > p - W only
  *   sinks       with a window, keys j < sinks stay visible
- *   scale       of q.k; 0: 1 / sqrt(head_dim)
+ *   scale       of q.k, 2^-60 .. 2^60; 0: 1 / sqrt(head_dim)
  *   out         [tokens][n_heads][head_dim] bf16, token rows out_ld apart; apart
  *               from q
  *   lse         [tokens][n_heads] float or NULL: log sum exp of the scaled scores

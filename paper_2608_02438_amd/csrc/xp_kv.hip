@@ -9,7 +9,6 @@
 #include <stdio.h>
 
 #include <algorithm>
-#include <cmath>
 #include <new>
 #include <string>
 
@@ -649,9 +648,9 @@ static xp_status kv_attn(xp_kv* kv, const KvAttnArgs& a, void* stream) {
                    "of 8, table_ld=%lld at least 1", (long long)a.q_ld, (long long)a.out_ld,
                    (long long)row, (long long)a.table_ld);
   if ((a.causal != 0 && a.causal != 1) || a.window < 0 || a.window > kKvMaxLen || a.sinks < 0 ||
-      a.sinks > kKvMaxLen || !(a.scale >= 0.f) || !std::isfinite(a.scale))
+      a.sinks > kKvMaxLen || !(a.scale == 0.f || (a.scale >= 0x1p-60f && a.scale <= 0x1p60f)))
     return kv_fail(kv, XP_EINVAL,
-                   "causal=%d (0, 1), window=%d, sinks=%d (0..2^22) or scale=%g (finite, >= 0) out "
+                   "causal=%d (0, 1), window=%d, sinks=%d (0..2^22) or scale=%g (0, 2^-60..2^60) out "
                    "of range", a.causal, a.window, a.sinks, (double)a.scale);
   const xp_status s = kv_cache_args(kv, a.kc, a.vc, a.k_scale, a.v_scale);
   if (s != XP_OK) return s;

@@ -562,6 +562,8 @@ class PagedKV:
     def _attend(self, name, groups, q, k_cache, v_cache, table, kv_len, cu_q, max_q, causal,
                 window, sinks, scale, k_scale, v_scale, out, lse, stream):
         torch = self._torch
+        if scale == 0:
+            raise ValueError("scale: 2^-60 .. 2^60, or None for 1 / sqrt(head_dim)")
         n, tokens = kv_len.shape[0], q.shape[0]
         lens = self._flat("kv_len", kv_len, torch.int32, n)
         cu = self._flat("cu_q", cu_q, torch.int32, n + 1, optional=True)

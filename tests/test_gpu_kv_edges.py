@@ -179,3 +179,63 @@ def test_layer_over_pages_past_2_to_the_20_keys(ctx):
         assert np.abs(h[b].cpu().numpy() - ref).max() <= bar
     layer.close()
     kv.close()
+
+
+def test_scales_out_of_range_are_refused():
+    """scale=0 is the C ABI's default, not a scale; others beyond 2^-60 .. 2^60 would
+    leave fp32's normal range."""
+    import torch
+    from paper_2608_02438_amd import xpress as X
+    c = Call(170, [40, 50], [1, 1], heads=4, n_kv=2)
+    kv = c.device(max_tokens=8)
+    out = torch.full_like(c.dq, 7)
+    for bad in (0.0, 0, -0.0):
+        with pytest.raises(ValueError):
+            c.run(kv, scale=bad, out=out)
+    for bad in (2.0 ** -61, 2.0 ** 61, 1e-45, 3e38, -1.0, float("nan")):
+        with pytest.raises((X.XpError, OverflowError)):
+            c.run(kv, scale=bad, out=out)
+    torch.cuda.synchronize()
+    assert (out == 7).all()
+    # scores of next to nothing: the mean of V
+    got = c.run(kv, scale=2.0 ** -60).double().cpu().numpy()
+    for b, n in enumerate(c.kv):
+        v = R.gather(c.v, c.table[b], n)
+        mean, spread = (np.repeat(x.mean(0), 2, axis=0) for x in (v, np.abs(v)))
+        # the numerators' and the sums' roundings, then half a bf16 step
+        assert (np.abs(got[b] - mean) <= 2.0 ** -8 * np.abs(mean) + 2.0 ** -15 * spread).all()
+    kv.close()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_scales_of_8_bit_caches_at_the_ends_of_their_range(hd):
+    """2^-60 and 2^60 for each of K and V: writes bit for bit, and attention."""
+    import torch
+    from paper_2608_02438_amd import xpress as X
+    rng = np.random.default_rng(hd)
+    ends = np.array([2.0 ** -60, 2.0 ** 60, 1.1 * 2.0 ** -59, 0.9 * 2.0 ** 59], dtype=np.float32)
+    kv = X.PagedKV(8, 4, 16, 4, 1, 32, 64, head_dim=hd, cache_dtype=torch.float8_e4m3fn)
+    s = ends.astype(np.float64)[None, :, None]
+    x = rng.normal(size=(32, 4, hd)) * 100 * s
+    x[0, :, :6] = [0.0, -0.0, 3e38, -3e38, 1e-38, np.nan]
+    d = torch.tensor(x).to(torch.bfloat16).cuda()
+    x = d.double().cpu().numpy()
+    c = [torch.zeros(kv.cache_shape, device="cuda").to(torch.float8_e4m3fn) for _ in range(2)]
+    sc = torch.tensor(ends).cuda()
+    kv.write(d, d, _i32(np.arange(32)), *c, k_scale=sc, v_scale=sc)
+    want = R.to_e4m3(x / s)
+    for a in c:
+        got = a[:2].double().cpu().numpy().transpose(0, 2, 1, 3).reshape(32, 4, hd)
+        np.testing.assert_array_equal(got, want)
+    # scores by the small scales are next to nothing; V by the large ones far from it
+    q = torch.tensor(rng.normal(size=(1, 8, hd))).to(torch.bfloat16).cuda()
+    for ks, vs in ((ends[0], ends[1]), (ends[0], ends[0])):
+        t = [torch.full((4,), float(e), device="cuda") for e in (ks, vs)]
+        out = kv.attend(q, *c, _i32([[0, 1]]), _i32([31]), k_scale=t[0], v_scale=t[1],
+                        window=20).double().cpu().numpy()
+        v = want[11:31] * np.float64(vs)
+        mean, spread = (np.repeat(y.mean(0), 2, axis=0) for y in (v, np.abs(v)))
+        # one bf16 part of the numerators, the sums, half a bf16 step
+        assert (np.abs(out[0] - mean) <= 2.0 ** -8 * np.abs(mean) + 1.01 * 2.0 ** -8 * spread).all()
+    assert kv.device_errors() == 0
+    kv.close()
