@@ -421,8 +421,12 @@ class Layer:
             h_f32 = torch.empty((batch, B, H), dtype=torch.float32, device=x.device)
         if h_bf16 is None:
             h_bf16 = torch.empty((batch, B, H), dtype=torch.bfloat16, device=x.device)
-        for t in (x, h_f32, h_bf16):
-            assert t.is_contiguous() and t.device == kv.device
+        for name, t, dt in (("x", x, torch.bfloat16), ("h_f32", h_f32, torch.float32),
+                            ("h_bf16", h_bf16, torch.bfloat16)):
+            if (t.dtype != dt or t.shape != (batch, B, self.H) or not t.is_contiguous()
+                    or t.get_device() != kv._index):
+                raise ValueError(f"{name}: expected a contiguous {dt} tensor "
+                                 f"{(batch, B, self.H)} on {kv.device}")
         with torch.cuda.device(kv.device):
             st = L.xp_layer_forward_paged(self._h, kv._h, batch, B, 1 if causal else 0, window,
                                           sinks, _ptr(x), *c, *tb, ctx, _ptr(h_f32),

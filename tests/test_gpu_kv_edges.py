@@ -239,3 +239,22 @@ def test_scales_of_8_bit_caches_at_the_ends_of_their_range(hd):
         assert (np.abs(out[0] - mean) <= 2.0 ** -8 * np.abs(mean) + 1.01 * 2.0 ** -8 * spread).all()
     assert kv.device_errors() == 0
     kv.close()
+
+
+def test_layer_over_pages_rejects_tensors_of_other_types_and_sizes():
+    """Before any launch: the kernels read and write as many bytes as the layer's."""
+    import torch
+    layer, kv, d = _paged_layer(2, 2, 8, [20, 5], "bf16", seed=13)
+    new = lambda *shape, t=torch.float32: torch.zeros(shape, dtype=t, device="cuda")  # noqa: E731
+    for kw in (dict(x=d["x"].float()), dict(x=d["x"][:, :, :128].contiguous()),
+               dict(x=d["x"].transpose(0, 1).contiguous().transpose(0, 1)), dict(x=d["x"].cpu()),
+               dict(h_f32=new(2, 8, 256, t=torch.bfloat16)), dict(h_f32=new(1, 8, 256)),
+               dict(h_f32=new(2, 8, 512)[:, :, :256]), dict(h_bf16=new(2, 8, 256)),
+               dict(h_bf16=new(2, 4, 256, t=torch.bfloat16)), dict(ctx_len=d["cl"].long()),
+               dict(ctx_len=d["cl"][:1])):
+        a = dict(dict(x=d["x"], kv=kv, k_cache=d["pk"], v_cache=d["pv"], table=d["table"],
+                      ctx_len=d["cl"]), **kw)
+        with pytest.raises(ValueError):
+            layer.forward_paged(**a)
+    layer.close()
+    kv.close()
