@@ -155,6 +155,16 @@ def _stream(stream) -> Optional[int]:
     return int(s.cuda_stream)
 
 
+def _empty_on(stream, shape, dtype, device):
+    """An output that work on `stream` (None: the current one) fills: memory of that
+    stream's, so that no earlier work on another one still uses it."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def bf16_tensor(bits: np.ndarray, device="cuda"):
     """Device bf16 tensor from bf16 bit patterns (uint16)."""
     import torch
@@ -418,9 +428,9 @@ class Layer:
         tb = kv._table(table, batch)
         ctx = kv._flat("ctx_len", ctx_len, torch.int32, batch)
         if h_f32 is None:
-            h_f32 = torch.empty((batch, B, H), dtype=torch.float32, device=x.device)
+            h_f32 = _empty_on(stream, (batch, B, H), torch.float32, x.device)
         if h_bf16 is None:
-            h_bf16 = torch.empty((batch, B, H), dtype=torch.bfloat16, device=x.device)
+            h_bf16 = _empty_on(stream, (batch, B, H), torch.bfloat16, x.device)
         for name, t, dt in (("x", x, torch.bfloat16), ("h_f32", h_f32, torch.float32),
                             ("h_bf16", h_bf16, torch.bfloat16)):
             if (t.dtype != dt or t.shape != (batch, B, self.H) or not t.is_contiguous()
@@ -578,8 +588,8 @@ class PagedKV:
         elif cu_q is not None:
             max_q = min(max_q, tokens)                        # no request has more
         if out is None:
-            out = torch.empty((tokens, self.n_heads, self.head_dim), dtype=torch.bfloat16,
-                              device=self.device)
+            out = _empty_on(stream, (tokens, self.n_heads, self.head_dim), torch.bfloat16,
+                            self.device)
         q_ld = self._rows("q", q, self.n_heads)
         out_ld = self._rows("out", out, self.n_heads, tokens)
         if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous()

@@ -258,3 +258,31 @@ def test_layer_over_pages_rejects_tensors_of_other_types_and_sizes():
             layer.forward_paged(**a)
     layer.close()
     kv.close()
+
+
+def test_outputs_allocated_for_another_stream_are_that_streams():
+    """Memory that was just freed on the current stream may still be in use there: a
+    call on another stream does not get it for its results."""
+    import torch
+    c = Call(171, [900, 300], [16, 16], heads=8, n_kv=2)
+    kv = c.device()
+    layer, lkv, d = _paged_layer(2, 2, 8, [20, 5], "bf16", seed=14)
+    want = c.run(kv)
+    h32, h16 = layer.forward_paged(d["x"], lkv, d["pk"], d["pv"], d["table"], d["cl"])
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for like, call in ((want, lambda: c.run(kv, stream=s)),
+                       (h32, lambda: layer.forward_paged(d["x"], lkv, d["pk"], d["pv"], d["table"],
+                                                         d["cl"], stream=s))):
+        freed = [torch.empty_like(t) for t in (like, h16) for _ in range(20)]
+        here = {t.data_ptr() for t in freed}
+        del freed
+        got = call()
+        got = got if isinstance(got, tuple) else (got,)
+        assert not here & {t.data_ptr() for t in got}
+        s.synchronize()
+        for a, b in zip(got, (like, h16)):
+            assert a.equal(b)
+    layer.close()
+    for k in (kv, lkv):
+        k.close()
