@@ -432,6 +432,16 @@ const char* xp_kv_last_error(const xp_kv* kv);
  * kv_len is lens, its slots are -1, and XP_DEVERR_POOL is set.  A request whose
  * numbers are out of range (negative, beyond max_len or table_ld pages) is left
  * alone with kv_len 0 and no tokens in cu (XP_DEVERR_LENGTH).
+ *
+ * Shared pages.  The map takes every page of a table for its request's own, and a
+ * page that two requests return is in the pool twice.  So the pages of a shared prefix
+ * (whole ones, f of them) belong to one request, which holds them until the last
+ * sharer has ended; a request of their own, without new tokens in the attention, does.
+ * Another request shares them when the caller writes them to the front of its table and
+ * sets held = f; from then on its lens counts the f * page_size keys.  It never gets
+ * lens + add below them.  To end it: map with lens = f * page_size, add = 0, which
+ * returns what lies behind, then set held = 0.
+ *
  * Asynchronous on `stream`; no allocation; the same call gives the same pages.
  * Errors: XP_EINVAL before any launch, XP_EHIP.
  */

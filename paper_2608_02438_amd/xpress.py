@@ -552,7 +552,10 @@ class PagedKV:
     def map(self, lens, add, table, held, pool, pool_n, cu=None, kv_len=None, slots=None,
             stream=None):
         """Pages and slots from lengths (xp_kv_map): table, held, pool and pool_n
-        are updated, and cu, kv_len and slots written where given."""
+        are updated, and cu, kv_len and slots written where given.  Every page of a
+        table counts as its request's own: one that shares a prefix's f pages has them
+        in front with held = f, and ends by lens = f * page_size, add = 0 and then
+        held = 0; the pages go back with the request that holds them for all."""
         i32, flat = self._torch.int32, self._flat
         n = lens.shape[0]
         self._call("xp_kv_map", n, flat("lens", lens, i32, n), flat("add", add, i32, n),

@@ -286,3 +286,98 @@ def test_outputs_allocated_for_another_stream_are_that_streams():
     layer.close()
     for k in (kv, lkv):
         k.close()
+
+
+@pytest.mark.parametrize("cache,prefix,window", [("bf16", 80, 0), ("e4m3", 16, 0), ("bf16", 144, 60)])
+def test_requests_share_a_prefix_end_and_leave_its_pages_to_the_others(cache, prefix, window):
+    """A prefix held by a request of its own; requests that share it take and return
+    pages of their own, one ends and an unrelated one takes its pages, a new one joins,
+    all end: no page is ever in the pool and in a table, or twice in the pool."""
+    import torch
+    from paper_2608_02438_amd.xpress import PagedKV
+    rng = np.random.default_rng(180 + prefix)
+    n, heads, n_kv, hd, P, n_pages, f = 6, 8, 2, 64, 16, 40, prefix // 16
+    dt = torch.bfloat16 if cache == "bf16" else torch.float8_e4m3fn
+    kv = PagedKV(heads, n_kv, P, n_pages, n, 256, 320, head_dim=hd, cache_dtype=dt, shared=True)
+    kc, vc = (torch.full(kv.cache_shape, float("nan"), device="cuda").to(dt) for _ in range(2))
+    sc = None if cache == "bf16" else np.array([0.011, 0.009], dtype=np.float32)
+    dsc = None if sc is None else torch.tensor(sc).cuda()
+    table = torch.full((n, 20), -1, dtype=torch.int32, device="cuda")
+    held, pool, pool_n = _i32([0] * n), _i32(rng.permutation(n_pages)), _i32([n_pages])
+    lens = torch.zeros(n, dtype=torch.int32, device="cuda")
+    past = [[np.zeros((0, n_kv, hd))] * 2 for _ in range(n)]
+
+    def pages_are_whole():
+        t, h = table.cpu().numpy(), held.cpu().numpy()
+        free = pool[:pool_n.item()].tolist()
+        own = [p for b in range(n) for p in t[b, (f if b in sharers else 0):h[b]]]
+        assert sorted(free + own) == list(range(n_pages))
+        assert all((t[b, :f] == t[0, :f]).all() for b in sharers)
+
+    def step(add, groups):
+        T = sum(add)
+        cu, kvl, slots = (torch.empty(m, dtype=torch.int32, device="cuda") for m in (n + 1, n, T))
+        kv.map(lens, _i32(add), table, held, pool, pool_n, cu=cu, kv_len=kvl, slots=slots)
+        q, k, v = (bf16(rng.normal(size=(T, h, hd)) * s) for h, s in
+                   ((heads, 2), (n_kv, 1), (n_kv, 1)))
+        dq, dk, dv = (torch.tensor(x).to(torch.bfloat16).cuda() for x in (q, k, v))
+        kv.write(dk, dv, slots, kc, vc, k_scale=dsc, v_scale=dsc)
+        starts, lengths = groups
+        out = kv.attend_shared(dq, kc, vc, table, kvl, _i32(starts), _i32(lengths), cu_q=cu,
+                               max_q=max(add), window=window, k_scale=dsc, v_scale=dsc)
+        assert kv.device_errors() == 0
+        pages_are_whole()
+        got, at = out.double().cpu().numpy(), 0
+        for b in range(n):
+            new = slice(at, at + add[b])
+            at += add[b]
+            w = 1.0 if sc is None else sc.astype(np.float64)[None, :, None]
+            past[b] = [np.concatenate([p, x[new] if sc is None else R.to_e4m3(x[new] / w) * w])
+                       for p, x in zip(past[b], (k, v))]
+            if add[b]:
+                o, _, spread, score = R.attend(q[new], *past[b], window=window)
+                m = past[b][0].shape[0]
+                d = 2 * ((hd + 12) * 2.0 ** -23 * score + 2.0 ** -22) + m * 2.0 ** -23 + 2.0 ** -20
+                c = d[..., None] + 2.0 ** -8                  # at most one part's rounding
+                assert (np.abs(got[new] - o) <= 2.0 ** -8 * (np.abs(o) + c * spread) + c * spread).all()
+        lens.add_(_i32(add))
+
+    sharers = []
+
+    def share(b):
+        table[b, :f] = table[0, :f]
+        held[b], lens[b] = f, prefix
+        past[b] = past[0]
+        sharers.append(b)
+
+    def end(bs):
+        """All of them at once: their own pages through the map, then held."""
+        for b in bs:
+            lens[b] = prefix if b in sharers else 0
+        kv.map(lens, torch.zeros_like(lens), table, held, pool, pool_n)
+        for b in bs:
+            if b in sharers:
+                held[b] = 0
+                sharers.remove(b)
+            lens[b] = 0
+            past[b] = [x[:0] for x in past[b]]
+        pages_are_whole()
+
+    print(f"shared pages: {cache} prefix={prefix} window={window}", flush=True)
+    none = ([0, n], [0])
+    step([prefix, 0, 0, 0, 0, 33], none)
+    for b in (1, 2, 3):
+        share(b)
+    group = ([0, 4, n], [prefix, 0])
+    step([0, 20, 1, 7, 0, 1], group)
+    step([0, 1, 16, 7, 0, 1], group)
+    end([2])
+    step([0, 3, 0, 1, 40, 1], group)                          # request 4 takes its pages
+    share(2)
+    step([0, 1, 50, 1, 1, 0], group)
+    end([1, 2, 5])
+    step([0, 0, 0, 5, 1, 0], group)
+    end([3])
+    end([0, 4])
+    assert pool_n.item() == n_pages
+    kv.close()
