@@ -388,8 +388,8 @@ typedef struct xp_kv xp_kv;
 
 /*
  * Create a handle for calls of up to max_batch (<= 4096) requests, max_tokens
- * (<= 2^20) new tokens and requests of up to max_len (<= 2^22) keys on the
- * current device; allocates the workspace (freed by xp_kv_destroy; with
+ * (<= 2^20) new tokens and requests of up to max_len (<= 2^22) keys, which below
+ * stands for the whole pages that hold so many, on the current device; allocates the workspace (freed by xp_kv_destroy; with
  * shared = 1 also 8 * (head_dim + 2) bytes a token and query head for
  * xp_kv_attn_shared).  Synchronous.  Calls on one handle share its workspace:
  * issue them in stream order, and replay captured graphs of them in that order
@@ -455,8 +455,8 @@ xp_status xp_kv_map(xp_kv* kv, int32_t n, const int32_t* lens, const int32_t* ad
  *   k, v   [tokens][n_kv][head_dim] bf16, token rows k_ld, v_ld elements apart
  *          (slices of a fused projection's rows; multiples of 8, 16-byte aligned)
  *   slots  [tokens] int32   -1: the token has no place; another one outside the
- *          cache is skipped and sets XP_DEVERR_SLOT.  Slots given twice: each KV
- *          head's row is that of either token.
+ *          cache is skipped and sets XP_DEVERR_SLOT.  Slots given twice: each 16
+ *          bytes of the row are those of either token.
  * An 8-bit cache stores the e4m3 value nearest to k / k_scale (ties to even, one
  * rounding), at most 448 in magnitude; NaN stays.
  * Errors: XP_EINVAL before any launch, XP_EHIP.
@@ -471,11 +471,11 @@ xp_status xp_kv_write(xp_kv* kv, int32_t tokens, const void* k, int64_t k_ld, co
  *
  *   tokens, q   q [tokens][n_heads][head_dim] bf16, token rows q_ld elements apart
  *   cu_q        [n + 1] int32: the tokens of request b are cu_q[b] .. cu_q[b + 1]
- *               - 1; NULL: max_q each (tokens = n max_q).  Tokens from cu_q[n]
- *               on are left as they are.
- *   max_q       the most tokens of a request, up to max_tokens (it sizes the row
- *               tiles and chooses the numerators' parts, below; a wrong one costs
- *               time only)
+ *               - 1; NULL: max_q each (tokens = n max_q).  The out and lse rows of
+ *               tokens from cu_q[n] on are left as they are.
+ *   max_q       the most tokens of a request, up to max_tokens.  It sizes the row
+ *               tiles and chooses the numerators' parts (below): a wrong one costs
+ *               time, one that is too large may cost the second part
  *   kv_len      [n] int32: keys of request b, the new tokens' own among them
  *   causal      1 or 0 (the drafter's bidirectional block)
  *   window      0: none; W: a token at position p sees keys j > p - W only
@@ -491,14 +491,19 @@ xp_status xp_kv_write(xp_kv* kv, int32_t tokens, const void* k, int64_t k_ld, co
  * sees no key gives 0 (lse -inf), one whose scores are all -inf NaN (lse -inf).
  * Keys that a token does not see do not enter its result, whatever they hold.
  * Scores and sums are fp32; the numerators enter the product with V as two bf16
- * parts, as one with an 8-bit cache and in calls of more than 64 rows (max_q times the heads of a group; with shared prefixes at least
- * the mean tokens of a group times the heads, or, for the keys behind prefixes that
- * fill the largest row tiles, max_q alone).
+ * parts, as one (2^-8 of sum p |v| at most) with an 8-bit cache and in calls of more
+ * than 64 rows (max_q times the heads of a group; with shared prefixes at least the
+ * mean tokens of a group times the heads, or, for the keys behind prefixes that fill
+ * the largest row tiles, max_q alone).  So a single token's result has the fewer bits
+ * in a call beside a prompt; two calls keep them.
  * Pages outside [0, n_pages) where a key is read are replaced by 0 and set
  * XP_DEVERR_PAGE; lengths outside [0, max_len] are clamped (XP_DEVERR_LENGTH).
  * The same call gives the same bits; a request's summation order follows the
  * lengths of all requests of the call.
- * Errors: XP_EINVAL before any launch (null or misaligned pointers, sizes), XP_EHIP.
+ * Errors: XP_EINVAL before any launch (null or misaligned pointers, sizes; also
+ * where (tokens n_heads / n_kv / 32 + n) (keys / 64 + 8) n_kv reaches 2^31, keys the
+ * lesser of max_len and the table's, twice that with shared prefixes: such a call is
+ * split, or made with a handle of a smaller max_len), XP_EHIP.
  */
 xp_status xp_kv_attn(xp_kv* kv, int32_t n, int32_t tokens, int32_t max_q, const void* q,
                      int64_t q_ld, const int32_t* cu_q, const int32_t* kv_len,
@@ -517,7 +522,8 @@ xp_status xp_kv_attn(xp_kv* kv, int32_t n, int32_t tokens, int32_t max_q, const 
  * tokens (XP_DEVERR_LENGTH).  group_start does not run backwards: where it does, no
  * prefix is shared, and outside 0 .. n it is clamped (XP_DEVERR_LENGTH both).  Requests
  * outside every group, and groups of length 0, are attended as in xp_kv_attn.  The
- * result differs from xp_kv_attn's in summation order only.
+ * result differs from xp_kv_attn's in summation order and, where the two choose
+ * differently, in the numerators' parts.
  */
 xp_status xp_kv_attn_shared(xp_kv* kv, int32_t n, int32_t tokens, int32_t max_q, int32_t groups,
                             const int32_t* group_start, const int32_t* shared_len, const void* q,

@@ -381,3 +381,20 @@ def test_requests_share_a_prefix_end_and_leave_its_pages_to_the_others(cache, pr
     end([0, 4])
     assert pool_n.item() == n_pages
     kv.close()
+
+
+def test_lengths_up_to_whole_pages_are_allowed():
+    """max_len stands for its whole pages: in the map, the write and the attention."""
+    import torch
+    from paper_2608_02438_amd import xpress as X
+    c = Call(190, [112, 101], [12, 3], heads=4, n_kv=2, P=16)
+    kv = c.device(max_len=100)
+    out = c.run(kv)
+    assert kv.device_errors() == 0
+    c.check(out, causal=True, parts=2)
+    wide = torch.cat([c.dtable, c.dtable], dim=1).contiguous()
+    c.dkv[1] = 113                                            # the eighth page is past them
+    got = kv.attend(c.dq, c.dk, c.dv, wide, c.dkv, cu_q=c.dcu, max_q=12)
+    assert kv.device_errors() == X.XP_DEVERR_LENGTH
+    assert got[:12].equal(out[:12])
+    kv.close()
