@@ -398,3 +398,35 @@ def test_lengths_up_to_whole_pages_are_allowed():
     assert kv.device_errors() == X.XP_DEVERR_LENGTH
     assert got[:12].equal(out[:12])
     kv.close()
+
+
+def test_write_quotients_that_fp32_moves_onto_a_middle():
+    """Scales next to x / middle for all bf16 significands x and all middles between two
+    neighbouring e4m3 values, subnormal ones among them: an fp32 quotient lies on the
+    middle where the true one does not, and goes to the even neighbour."""
+    import torch
+    from paper_2608_02438_amd import xpress as X
+    heads, hd, P = 1024, 64, 16
+    grid = R.e4m3_values()[:127]
+    mid = (grid[1:] + grid[:-1]) / 2
+    x, m = (a.ravel() for a in np.meshgrid(np.arange(128, 256) * 2.0 ** -7, mid))
+    near = (x / m).astype(np.float32)
+    s = np.concatenate([near, np.nextafter(near, np.float32(0)), np.nextafter(near, np.float32(1e9))])
+    x, s = np.concatenate([x] * 3), s
+    pad = -len(s) % heads
+    x, s = (np.concatenate([a, a[:pad]]).reshape(-1, heads) for a in (x, s))
+    want = R.to_e4m3(x / s.astype(np.float64))
+    once = R.to_e4m3((x.astype(np.float32) / s).astype(np.float64))
+    assert (once != want).mean() > 0.1                        # what rounding twice would give
+    kv = X.PagedKV(heads, heads, P, 1, 1, 1, P, head_dim=hd, cache_dtype=torch.float8_e4m3fn)
+    c = [torch.zeros(kv.cache_shape, device="cuda").to(torch.float8_e4m3fn) for _ in range(2)]
+    sign = torch.tensor([1.0, -1.0], device="cuda").repeat(hd // 2)
+    for i in range(len(s)):
+        d = (torch.tensor(x[i]).cuda()[None, :, None] * sign).to(torch.bfloat16)
+        sc = torch.tensor(s[i]).cuda()
+        kv.write(d, d, _i32([i % P]), *c, k_scale=sc, v_scale=sc)
+        got = [a[0, :, i % P].double().cpu().numpy() for a in c]
+        for g in got:
+            np.testing.assert_array_equal(g[:, 0::2], np.repeat(want[i][:, None], hd // 2, 1))
+            np.testing.assert_array_equal(g[:, 1::2], -g[:, 0::2])
+    kv.close()
