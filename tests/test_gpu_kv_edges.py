@@ -430,3 +430,70 @@ def test_write_quotients_that_fp32_moves_onto_a_middle():
             np.testing.assert_array_equal(g[:, 0::2], np.repeat(want[i][:, None], hd // 2, 1))
             np.testing.assert_array_equal(g[:, 1::2], -g[:, 0::2])
     kv.close()
+
+
+@pytest.mark.parametrize("cap,cache,shared", [(24, "bf16", False), (24, "e4m3", True), (5200, "bf16", False)])
+def test_captured_step_of_all_calls(cap, cache, shared):
+    """Map with lengths advanced in place, write, attention: one graph replayed step by
+    step beside the same calls made eagerly on buffers of their own, with accepted
+    lengths in between; a padded batch."""
+    import torch
+    from paper_2608_02438_amd.xpress import PagedKV
+    n, heads, n_kv, hd, P, n_pages, width = 3, 8, 2, 128, 16, 80, 24
+    dt = torch.bfloat16 if cache == "bf16" else torch.float8_e4m3fn
+    g = torch.Generator(device="cuda").manual_seed(cap)
+    sc = None if cache == "bf16" else torch.full((n_kv,), 0.02, device="cuda")
+    q, k, v = (torch.empty(cap, h, hd, dtype=torch.bfloat16, device="cuda")
+               for h in (heads, n_kv, n_kv))
+    lens0, add, back = _i32([0, 0, 0]), _i32([0, 0, 0]), _i32([0, 0, 0])
+
+    class Side:
+        def __init__(self):
+            self.kv = PagedKV(heads, n_kv, P, n_pages, n, cap, width * P, head_dim=hd,
+                              cache_dtype=dt, shared=shared)
+            self.c = [torch.zeros(self.kv.cache_shape, device="cuda").to(dt) for _ in range(2)]
+            self.table = torch.full((n, width), -1, dtype=torch.int32, device="cuda")
+            self.held, self.pool, self.pool_n = _i32([0] * n), _i32(range(n_pages)), _i32([n_pages])
+            self.lens, self.cu = lens0.clone(), _i32([0] * (n + 1))
+            self.slots = torch.zeros(cap, dtype=torch.int32, device="cuda")
+            self.out = torch.zeros_like(q)
+            self.starts, self.common = _i32([0, n]), _i32([0])
+
+        def step(self):
+            self.lens.sub_(back)                              # what verification rejected
+            self.kv.map(self.lens, add, self.table, self.held, self.pool, self.pool_n, cu=self.cu,
+                        kv_len=self.lens, slots=self.slots)
+            self.kv.write(k, v, self.slots, *self.c, k_scale=sc, v_scale=sc)
+            a = (q, *self.c, self.table, self.lens)
+            kw = dict(cu_q=self.cu, max_q=8, k_scale=sc, v_scale=sc, out=self.out)
+            if shared:
+                self.kv.attend_shared(*a, self.starts, self.common, **kw)
+            else:
+                self.kv.attend(*a, **kw)
+
+    a, b = Side(), Side()
+    warm = Side()
+    warm.step()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        b.step()
+    for new, less in (([8, 1, 5], [0, 0, 0]), ([8, 8, 8], [0, 0, 5]), ([1, 8, 0], [7, 1, 3]),
+                      ([8, 0, 8], [0, 4, 0]), ([8, 8, 8], [8, 0, 2])):
+        print(f"captured step: cap={cap} {cache} add={new}", flush=True)
+        for t in (q, k, v):
+            t.normal_(generator=g)
+        add.copy_(_i32(new))
+        back.copy_(_i32(less))
+        a.step()
+        graph.replay()
+        torch.cuda.synchronize()
+        used = sum(new)
+        for x, y in ((a.lens, b.lens), (a.cu, b.cu), (a.slots, b.slots), (a.table, b.table),
+                     (a.held, b.held), (a.pool_n, b.pool_n), (a.out[:used], b.out[:used])):
+            assert x.equal(y)
+        assert all(x.view(torch.uint8).equal(y.view(torch.uint8)) for x, y in zip(a.c, b.c))
+        assert (a.slots[used:] == -1).all() and a.out[:used].abs().max() > 0
+        assert a.kv.device_errors() == 0 and b.kv.device_errors() == 0
+    for s in (a, b, warm):
+        s.kv.close()
