@@ -198,15 +198,16 @@ __global__ __launch_bounds__(kPlanThreads) void k_kv_plan(const KvPlan d, const 
       if (!second) w.row[0][t] = int2{-1, 0};
       if (items > ns) w.row[1][t] = int2{-1, 0};
     }
-    // Groups that run backwards could hold a request twice: then none is shared.
+    // Groups that run backwards could hold a request twice: then none is shared.  Every
+    // wave looks through all of them (an or over the workgroup took 0.3 us longer).
     bool back = false;
-    for (int g = tid; g < d.groups; g += kPlanThreads) {
+    for (int g = lane; g < d.groups; g += kWave) {
       const int s0 = d.group_start[g], s1 = d.group_start[g + 1];
       back |= s1 < s0;
-      if ((s0 < 0) | (s1 > n)) bad |= XP_DEVERR_LENGTH;
+      bad |= (s1 < s0) | (s0 < 0) | (s1 > n) ? XP_DEVERR_LENGTH : 0u;
     }
-    const bool apart = __syncthreads_or(back);
-    if (apart) bad |= XP_DEVERR_LENGTH;
+    const bool apart = __ballot(back) != 0;
+    __syncthreads();
     // a wave per group: its members' positions, and a prefix that none is shorter than
     for (int g = wave; g < d.groups; g += kPlanWaves) {
       int s0, s1;
