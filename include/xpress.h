@@ -491,11 +491,12 @@ xp_status xp_kv_write(xp_kv* kv, int32_t tokens, const void* k, int64_t k_ld, co
  * sees no key gives 0 (lse -inf), one whose scores are all -inf NaN (lse -inf).
  * Keys that a token does not see do not enter its result, whatever they hold.
  * Scores and sums are fp32; the numerators enter the product with V as two bf16
- * parts, as one (2^-8 of sum p |v| at most) with an 8-bit cache and in calls of more
- * than 64 rows (max_q times the heads of a group; with shared prefixes at least the
- * mean tokens of a group times the heads, or, for the keys behind prefixes that fill
- * the largest row tiles, max_q alone).  So a single token's result has the fewer bits
- * in a call beside a prompt; two calls keep them.
+ * parts, as one fp16 part (2^-11 of sum p |v| at most) with an 8-bit cache, and as one
+ * bf16 part (2^-8) in calls of more than 64 rows over a bf16 one (max_q times the heads
+ * of a group; with shared prefixes at least the mean tokens of a group times the heads,
+ * or, for the keys behind prefixes that fill the largest row tiles, max_q alone).  So a
+ * single token's result over a bf16 cache has the fewer bits in a call beside a prompt;
+ * two calls keep them.
  * Pages outside [0, n_pages) where a key is read are replaced by 0 and set
  * XP_DEVERR_PAGE; lengths outside [0, max_len] are clamped (XP_DEVERR_LENGTH).
  * The same call gives the same bits; a request's summation order follows the

@@ -371,6 +371,30 @@ __device__ __forceinline__ floatx16 mma32(u32x4 a, u32x4 b, floatx16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
                                                  __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
+// the same of P and V: fp16 over an 8-bit cache
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+template <bool F8>
+__device__ __forceinline__ floatx16 mma32_pv(u32x4 a, u32x4 b, floatx16 c) {
+  if constexpr (F8)
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8, a),
+                                                  __builtin_bit_cast(half8, b), c, 0, 0, 0);
+  else return mma32(a, b, c);
+}
+template <bool F8>
+__device__ __forceinline__ uint32_t pk_p(float a, float b) {
+  if constexpr (F8)
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(xp_f32x2{a, b}, half2v));
+  else return pk_bf16(a, b);
+}
+// 8 e4m3 values to fp16 (exact)
+__device__ __forceinline__ u32x4 f8_f16x8(uint32_t a, uint32_t b) {
+  return u32x4{
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, false)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.f, true)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, false)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.f, true))};
+}
 // 8 e4m3 values to bf16 (exact)
 __device__ __forceinline__ u32x4 f8_bf16x8(uint32_t a, uint32_t b) {
   return u32x4{
@@ -459,7 +483,7 @@ __device__ __forceinline__ void lds_v(const uint32_t* a, const uint32_t* b, u32x
           "n"(OFF), "n"(ON)
         : "memory");
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i / ND][i % ND] = f8_bf16x8(r[i].x, r[i].y);
+    for (int i = 0; i < 8; ++i) v[i / ND][i % ND] = f8_f16x8(r[i].x, r[i].y);
   } else {
     uint2 r[4];
     asm volatile(
@@ -473,7 +497,7 @@ __device__ __forceinline__ void lds_v(const uint32_t* a, const uint32_t* b, u32x
           "n"(OFF), "n"(ON)
         : "memory");
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i / ND][i % ND] = f8_bf16x8(r[i].x, r[i].y);
+    for (int i = 0; i < 4; ++i) v[i / ND][i % ND] = f8_f16x8(r[i].x, r[i].y);
   }
 }
 
@@ -502,16 +526,22 @@ struct KvOdd {
   }
 };
 
-// ones over each bf16 of x that is an infinity or NaN
+// the exponent's bits of V's operand: bf16, fp16 over an 8-bit cache
+template <bool F8>
+constexpr uint32_t kOddExp = F8 ? 0x7c00u : 0x7f80u;
+// ones over each of the two values of x that is an infinity or NaN
+template <bool F8>
 __device__ __forceinline__ uint32_t nonfinite_mask(uint32_t x) {
-  return ((x & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u) |
-         ((x & 0x7f80u) == 0x7f80u ? 0xffffu : 0u);
+  constexpr uint32_t E = kOddExp<F8>;
+  return ((x & (E << 16)) == E << 16 ? 0xffff0000u : 0u) | ((x & E) == E ? 0xffffu : 0u);
 }
 
-// bf16 1 where the bf16 x is an infinity (c = 0), a negative one (1) or NaN (2)
+// 1 where the value x is an infinity (c = 0), a negative one (1) or NaN (2)
+template <bool F8>
 __device__ __forceinline__ uint32_t ones_of(int c, uint32_t x) {
-  const bool is = c == 0 ? x == 0x7f80u : (c == 1 ? x == 0xff80u : (x & 0x7fffu) > 0x7f80u);
-  return is ? 0x3f80u : 0u;
+  constexpr uint32_t E = kOddExp<F8>;
+  const bool is = c == 0 ? x == E : (c == 1 ? x == (E | 0x8000u) : (x & 0x7fffu) > E);
+  return is ? (F8 ? 0x3c00u : 0x3f80u) : 0u;
 }
 
 // n KB of a page into LDS, 1 KB a load; a load's immediate offset counts for the
@@ -633,11 +663,15 @@ constexpr int kv_waves(int hd, int wr, int wk) { return hd == 64 && wr == 4 && w
 // maximum moves only when a score exceeds it by more than 2^8, so most blocks
 // rescale nothing.
 // Numerators enter P V as PARTS bf16 parts, two (16 significant bits) or one (8).  One
-// where more than 64 rows or an 8-bit cache, whose values have 4 bits anyway, make the
-// second part's products cost time: 64 blocks of 32 over 512 .. 16384 keys 487 us with
-// one, 574 with two; prompts of 1 .. 8191 995 and 1252; a shared prefix of 8192 48 and
-// 55; 48 single tokens over 8 bits 72 and 77, 64 blocks 375 and 467.  The results' error
-// is then 2.2e-3 of their rms in place of 1.65e-3, the bf16 output's own rounding.
+// where more than 64 rows make the second part's products cost time: 64 blocks of 32 over
+// 512 .. 16384 keys 487 us with one, 574 with two; prompts of 1 .. 8191 995 and 1252; a
+// shared prefix of 8192 48 and 55.  The results' error is then 2.2e-3 of their rms in
+// place of 1.65e-3, the bf16 output's own rounding.
+// Over an 8-bit cache, whose values are exact in fp16, as one fp16 part of 11 bits: the
+// row's reference lies 2^7 below its maximum, so that numerators reach 2^15 (with the
+// 2^8 above), and those of 2^-21 of the greatest still have all 11 bits; the smaller
+// ones are off by at most 2^-25, where the sum is 2^7 at least.  Error 1.67e-3, where one
+// bf16 part had 2.2e-3 in 0 to 2% less time, two 1.66e-3 in 5 to 30% more.
 // Tiles wait in an LDS ring of NST stages filled by global_load_lds; the keys
 // that no row of the tile sees are loaded as zeros, whatever lies there.
 // Matrix pipe and vector pipe work side by side only if one wave's instructions
@@ -656,6 +690,10 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
   using SH = KvRows<HD, F8>;
   constexpr int NW = WR * WK, R = 32 * WR, NB = 2 / WK, ND = HD / 32, NKS = HD / 16;
   constexpr int RB = SH::RB, CPR = SH::CPR, IPG = SH::IPG;
+  static_assert(!F8 || PARTS == 1, "one fp16 part");
+  // fp16 numerators reach up to 2^15 (see below), so that those of far smaller scores
+  // keep their bits
+  constexpr float kAbove = F8 ? 7.f : 0.f;
   constexpr int NG = 8 / NW;                      // groups of 16 rows that a wave loads
   static_assert(NG * NW == 8 && NB * WK == 2, "waves");
   constexpr int PER = NG * IPG;                   // loads of a wave for a stage
@@ -865,7 +903,7 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
       __attribute__((always_inline)) {
     const int u = x / ND, db = x % ND;
     if constexpr (PARTS == 2) o[db] = mma32(v[u][db], b[u], o[db]);
-    o[db] = mma32(v[u][db], a[u], o[db]);
+    o[db] = mma32_pv<F8>(v[u][db], a[u], o[db]);
   };
   // infinities or NaN among the block's V
   auto odd_values = [&](int stage, int r) __attribute__((always_inline)) {
@@ -896,17 +934,17 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
           u32x4 one;
 #pragma unroll
           for (int w = 0; w < 4; ++w)
-            one[w] = ones_of(c, v[u][db][w] & 0xffffu) | ones_of(c, v[u][db][w] >> 16) << 16;
+            one[w] = ones_of<F8>(c, v[u][db][w] & 0xffffu) | ones_of<F8>(c, v[u][db][w] >> 16) << 16;
           const float val = c == 0 ? INFINITY : (c == 1 ? -INFINITY : NAN);
           floatx16 y;
 #pragma unroll
           for (int i = 0; i < 16; ++i) y[i] = 0.f;
-          y = mma32(one, a[u], y);
+          y = mma32_pv<F8>(one, a[u], y);
 #pragma unroll
           for (int i = 0; i < 16; ++i) o[db][i] += y[i] > 0.f ? val : 0.f;
         }
 #pragma unroll
-        for (int w = 0; w < 4; ++w) v[u][db][w] &= ~nonfinite_mask(v[u][db][w]);
+        for (int w = 0; w < 4; ++w) v[u][db][w] &= ~nonfinite_mask<F8>(v[u][db][w]);
       }
   };
   constexpr int EP = 16 / NKS;                    // numerators beside a product of S
@@ -917,7 +955,7 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
     const float e0 = s[x], e1 = s[x + 1];
     l_run += e0;
     l_run += e1;
-    uint32_t y = pk_bf16(e0, e1);
+    uint32_t y = pk_p<F8>(e0, e1);
     asm volatile("" : "+v"(y), "+v"(l_run));      // here, not where it is used
     a[u][i] = y;
     if constexpr (PARTS == 2) {
@@ -948,7 +986,7 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
     float mt = s[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) mt = fmaxf(mt, s[i]);
-    mt = fmax_xor32(mt) * scale2;
+    mt = fmax_xor32(mt) * scale2 - kAbove;
     const bool grow = __ballot(mt > m_run + kLazy) != 0;   // wave-uniform
     float alpha = 1.f;
     if (grow) {
@@ -992,8 +1030,25 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
     }
+    uint32_t some = 0;                            // numerators above 0; fp16 rounds small ones to it
+    if constexpr (F8) {
+      if (__builtin_expect(odd, 0)) {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) some |= s[x] > 0.f ? 1u << x : 0u;
+      }
+    }
     v_read(stage, r);
-    if (__builtin_expect(odd, 0)) take_odd(ph[PAR]);
+    if (__builtin_expect(odd, 0)) {
+      if constexpr (F8) {
+        u32x4 a[2];
+#pragma unroll
+        for (int x = 0; x < 16; x += 2)
+          a[x / 8][x % 8 / 2] = ((some >> x) & 1u) * 0x3c00u | ((some >> (x + 1)) & 1u) * 0x3c000000u;
+        take_odd(a);
+      } else {
+        take_odd(ph[PAR]);
+      }
+    }
   };
   auto after = [](int stage) { return stage + 1 == NST ? 0 : stage + 1; };
   // The beginning of iteration t: K of tile t + 1 and V of tile t landed (every

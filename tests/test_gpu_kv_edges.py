@@ -497,3 +497,73 @@ def test_captured_step_of_all_calls(cap, cache, shared):
         assert a.kv.device_errors() == 0 and b.kv.device_errors() == 0
     for s in (a, b, warm):
         s.kv.close()
+
+
+def _check_fp16_parts(c, out, **m):
+    """The bound of tests/_kv.py with numerators of one fp16 part: 2^-11 of each (half
+    a step) and, below 2^-21 of the row's greatest, 2^-25 beside a sum of 2^7 at least."""
+    got = out.double().cpu().numpy()
+    for b, (o, _, eb, _) in c.oracle(parts=2, **m).items():
+        k, v = (R.gather(x, c.table[b], c.kv[b]) for x in (c.k, c.v))
+        k, v = (x * s.astype(np.float64)[None, :, None] for x, s in ((k, c.ks), (v, c.vs)))
+        q = c.q[c.cu[b]:c.cu[b + 1]]
+        spread = R.attend(q, k, v, **m)[2]
+        small = 2.0 ** -32 * np.repeat(np.abs(v).sum(0), c.heads // c.n_kv, axis=0)
+        more = (2.0 ** -11 * spread + small) * (1 + 2.0 ** -8)
+        r = (np.abs(got[c.cu[b]:c.cu[b + 1]] - o) / (eb + more)).max()
+        print(f"    request {b}: {r:.3f} of the bound", flush=True)
+        assert r <= 1
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("ql", [[1, 1, 1], [16, 9, 16], [40, 32, 1], [90, 16, 100]])
+def test_numerators_over_8_bit_caches_keep_eleven_bits(hd, ql):
+    c = Call(200 + hd + sum(ql), [300, 700, 130], ql, heads=4, n_kv=1, hd=hd, cache="e4m3", P=32)
+    kv = c.device()
+    for m in (dict(causal=True), dict(causal=False, window=200, sinks=5)):
+        print(f"fp16 numerators: hd={hd} ql={ql} {m}", flush=True)
+        _check_fp16_parts(c, c.run(kv, **m), **m)
+    kv.close()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("gap", [4, 11, 14, 17])
+@pytest.mark.parametrize("late", [False, True])
+def test_many_small_numerators_beside_a_great_one(hd, gap, late):
+    """One key's score stands gap (in base 2) above 20000 equal ones, which together
+    weigh as much or more: in the first tile, or in the last."""
+    n = 20000
+    c = Call(210 + gap, [n, n], [1, 16], heads=4, n_kv=1, hd=hd, cache="e4m3", P=256)
+    c.q[:] = 0.0
+    c.q[..., 0] = bf16(gap / 1.4426950408889634 * hd ** 0.5)
+    c.ks[:] = 1.0
+    c.k[:, :, :, 0] = 0.0
+    for b in range(2):
+        j = n - 20 if late else 3
+        c.k[c.table[b, j // 256], :, j % 256, 0] = 1.0
+    # what the small ones bring does not cancel
+    c.v = np.abs(c.v)
+    kv = c.device()
+    print(f"small numerators: hd={hd} gap={gap} late={late}", flush=True)
+    _check_fp16_parts(c, c.run(kv, causal=True), causal=True)
+    kv.close()
+
+
+def test_nan_with_a_weight_too_small_for_fp16():
+    """A later token's key with NaN in V and a weight of 2^-40: NaN by the formula, for
+    whoever sees it."""
+    c = Call(220, [90, 64], [4, 64], heads=4, n_kv=1, hd=64, cache="e4m3", P=64)
+    c.q[:] = 0.0
+    c.q[..., 0] = 8.0
+    c.ks[:] = 1.0
+    c.k[:, :, :, 0] = 0.0
+    for b, n in enumerate((90, 64)):
+        c.k[c.table[b, (n - 2) // 64], :, (n - 2) % 64, 0] = -28.0   # 8 * -28 / 8 = -40 in base 2
+        c.v[c.table[b, (n - 2) // 64], :, (n - 2) % 64, 5] = np.nan
+    kv = c.device()
+    out = c.run(kv).double().cpu().numpy()
+    for b in range(2):
+        got = out[c.cu[b]:c.cu[b + 1]]
+        assert np.isfinite(got[:-2]).all() and np.isnan(got[-2:, :, 5]).all()
+        assert np.isfinite(np.delete(got[-2:], 5, axis=2)).all()
+    kv.close()
