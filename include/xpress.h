@@ -60,7 +60,7 @@ typedef enum { XP_F32 = 0, XP_BF16 = 1, XP_E4M3 = 2 /* 8-bit caches only */ } xp
 #define XP_DEVERR_PAGE 8u     /* a page id outside [0, n_pages) where a key is; page 0 was read, or no slot given */
 #define XP_DEVERR_SLOT 16u    /* a slot outside the cache, not written; or more new tokens than slots */
 #define XP_DEVERR_POOL 32u    /* too few free pages (requests not served), or a pool count out of range */
-#define XP_DEVERR_LENGTH 64u  /* a length, token range or page count out of range; clamped or left alone */
+#define XP_DEVERR_LENGTH 64u  /* a length, token or group range or page count out of range; clamped or left alone */
 
 typedef struct xp_handle xp_handle;
 

@@ -63,7 +63,7 @@ __device__ __forceinline__ void take_page(const KvMap& d, int k, const int* take
 // over the requests before it; the releases, the tables' new lengths and the
 // pool's; with ALL also the pages taken and the slots.  Bound by latency: three
 // block scans over the requests, then one search per page and slot (8 requests with
-// blocks of 17: 4.6 us; 512 without slots 5.2).
+// blocks of 17: 5.2 us, 4.5 at best; 512 without slots 5.4).
 constexpr int kMapThreads = 1024;
 // Slots up to which one launch does all: 4096 of 64 requests 6.6 us in one, 7.5 in two;
 // 8192 9.6 and 7.6, 32768 27.7 and 7.6.
@@ -213,7 +213,7 @@ __global__ __launch_bounds__(kMapThreads) void k_kv_map(const KvMap d) {
 
 // The pages taken and the slots of a large call, over many workgroups (a slot's
 // page comes from the pool where this call takes it, so that no workgroup waits
-// for another's table entries).  524000 slots: 6.5 us.
+// for another's table entries).  524000 slots: 6.8 us.
 __global__ __launch_bounds__(256) void k_kv_slots(const KvMap d) {
   __shared__ int take[kKvMaxBatch + 1], acu[kKvMaxBatch + 1];
   for (int b = threadIdx.x; b <= d.n; b += 256) {

@@ -88,8 +88,8 @@ struct KvDev {
 // their keys behind a shared prefix, if they have one); the groups (their prefixes)
 // follow them or are the items of a second list.  The items' row tiles, the entries'
 // key ranges, the sums of both, and where each share begins.  Bound by latency, a few
-// block scans and one search per entry and share: 64 sequences 7 us, 60 behind five
-// prefixes 9.4.  (Small calls: plan_own.)
+// block scans and one search per entry and share: 64 sequences 7.2 us, 60 behind
+// five prefixes 9.7.  (Small calls: plan_own.)
 // ---------------------------------------------------------------------------
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanWaves = kPlanThreads / kWave;
