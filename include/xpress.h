@@ -47,7 +47,11 @@ typedef enum {
   XP_ENOMEM = -4         /* device allocation of the workspace failed              */
 } xp_status;
 
-typedef enum { XP_F32 = 0, XP_BF16 = 1, XP_E4M3 = 2 /* 8-bit caches only */ } xp_dtype;
+typedef enum {
+  XP_F32 = 0, XP_BF16 = 1,
+  XP_E4M3 = 2,   /* 8-bit caches only */
+  XP_MXFP4 = 3   /* 4-bit caches only: e2m1 codes with a power of two per 32 */
+} xp_dtype;
 
 /* flags of xp_refine_block */
 #define XP_EARLY_EXIT   1u  /* skip the remaining passes once every sequence is at its fixed point */
@@ -370,7 +374,14 @@ xp_status xp_layer_forward_noalloc(const xp_layer_weights* w, int32_t batch, int
  *
  *   k_cache, v_cache [n_pages][n_kv][page_size][head_dim]   caller-owned
  *       XP_BF16, or XP_E4M3 with a scale per KV head (k_scale, v_scale [n_kv]
- *       float, 2^-60 .. 2^60; NULL: 1): the value of an entry is e4m3 times the scale
+ *       float, 2^-60 .. 2^60; NULL: 1): the value of an entry is e4m3 times the scale;
+ *       or XP_MXFP4, [n_pages][n_kv][page_size * (head_dim / 2 + head_dim / 32)] bytes:
+ *       of a page's KV head first the rows' e2m1 codes (head_dim / 2 bytes a row, dim 2 i
+ *       in the low half of byte i), then the rows' exponents (head_dim / 32 bytes a row,
+ *       byte i of dims 32 i .. 32 i + 31).  The value of an entry is its code's, 0, 0.5,
+ *       1, 1.5, 2, 3, 4, 6 (codes 0 .. 7; 8 .. 15 the negatives), times 2^(exponent - 127),
+ *       in bf16 (an infinity beyond its range, which only the exponents 253 and 254 reach);
+ *       NaN where the exponent is 255
  *   table [..][table_ld] int32   the pages of each request, in order; key j of
  *       request b is row j % page_size of page table[b][j / page_size]
  *   a slot is page * page_size + row
@@ -381,7 +392,7 @@ xp_status xp_layer_forward_noalloc(const xp_layer_weights* w, int32_t batch, int
 typedef struct {
   int32_t n_heads, n_kv, head_dim;
   int32_t page_size, n_pages;
-  int32_t dtype;                     /* xp_dtype of the caches: XP_BF16 or XP_E4M3 */
+  int32_t dtype;                     /* xp_dtype of the caches: XP_BF16, XP_E4M3, XP_MXFP4 */
 } xp_kv_shape;
 
 typedef struct xp_kv xp_kv;
@@ -459,11 +470,32 @@ xp_status xp_kv_map(xp_kv* kv, int32_t n, const int32_t* lens, const int32_t* ad
  *          bytes of the row are those of either token.
  * An 8-bit cache stores the e4m3 value nearest to k / k_scale (ties to even, one
  * rounding), at most 448 in magnitude; NaN stays.
+ * A 4-bit cache stores, for 32 consecutive values x of a row, the smallest power of two
+ * s of 2^-125 .. 2^125 with max |x| <= 7 s, and the code nearest to each x / s (ties to
+ * the even code; 6 where it lies above): with it no value is off by more than half a step
+ * of its block's greatest ones, unless 7 * 2^125 is too small.  A block that holds an
+ * infinity or NaN becomes NaN.  A slot given twice may get one token's codes with the
+ * other's exponents: its row is then neither's.
  * Errors: XP_EINVAL before any launch, XP_EHIP.
  */
 xp_status xp_kv_write(xp_kv* kv, int32_t tokens, const void* k, int64_t k_ld, const void* v,
                       int64_t v_ld, const int32_t* slots, void* k_cache, void* v_cache,
                       const float* k_scale, const float* v_scale, void* stream);
+
+/*
+ * Rows of the cache as bf16, of any type of cache: to rotate keys anew, to hand a
+ * context on, to move it to another cache.
+ *
+ *   slots  [tokens] int32   -1: the token has no place and its row becomes 0; so does
+ *          that of another one outside the cache, which sets XP_DEVERR_SLOT
+ *   k, v   [tokens][n_kv][head_dim] bf16, token rows k_ld, v_ld elements apart
+ *          (multiples of 8, 16-byte aligned); one of them may be NULL
+ * An 8-bit cache gives e4m3 times the scale, rounded once; the others' values are exact.
+ * Errors: XP_EINVAL before any launch, XP_EHIP.
+ */
+xp_status xp_kv_read(xp_kv* kv, int32_t tokens, const int32_t* slots, const void* k_cache,
+                     const void* v_cache, const float* k_scale, const float* v_scale, void* k,
+                     int64_t k_ld, void* v, int64_t v_ld, void* stream);
 
 /*
  * Attention of new tokens over the pages of their requests: single tokens,

@@ -9,6 +9,9 @@ gives no formula for the cache, so each definition is stated here:
   then requests take pages from its top, first come first served;
 * a slot is page * P + row, key j of a request is row j % P of its page j // P;
 * an 8-bit cache holds the nearest e4m3 value of x / scale, ties to even;
+* a 4-bit cache holds, for 32 values x of a row, the smallest power of two s of 2^-125
+  .. 2^125 with max |x| <= 7 s, and the nearest e2m1 value of each x / s, ties to the
+  even code, at most 6; NaN for a block with an infinity or NaN;
 * token i of a request with m tokens and n keys has position p = n - m + i and sees
   key j iff j < n, j <= p (causal) and j > p - window or j < sinks (window > 0);
   o = sum_j softmax_j(scale q.k_j) v_j, 0 where it sees none.
@@ -80,6 +83,47 @@ def to_e4m3(x):
     far, near = grid[up] - mag, mag - grid[down]
     pick = (far < near) | ((far == near) & (up % 2 == 0))
     return np.where(np.isnan(x), np.nan, np.copysign(np.where(pick, grid[up], grid[down]), x))
+
+
+E2M1 = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6], dtype=F64)
+
+
+def to_mxfp4(x):
+    """Codes [.., hd] and exponent bytes [.., hd / 32] of x [.., hd]."""
+    x = np.asarray(x, dtype=F64)
+    blocks = x.reshape(*x.shape[:-1], -1, 32)
+    top = np.abs(blocks).max(-1)
+    odd = ~np.isfinite(top)
+    s = 2.0 ** np.arange(-125, 126)
+    at = np.minimum(np.searchsorted(7 * s, np.where(odd, 0, top)), 250)   # first with top <= 7 s
+    y = np.where(odd[..., None], 0, blocks) / s[at][..., None]
+    mag = np.abs(y)
+    up = np.clip(np.searchsorted(E2M1, mag), 0, 7)
+    down = np.maximum(up - 1, 0)
+    far, near = E2M1[up] - mag, mag - E2M1[down]
+    code = np.where((far < near) | ((far == near) & (up % 2 == 0)), up, down)
+    code = np.where(odd[..., None], 0, code + 8 * np.signbit(y))
+    return code.reshape(x.shape).astype(np.uint8), np.where(odd, 255, at + 2).astype(np.uint8)
+
+
+def mxfp4_values(codes, exps):
+    v = E2M1[codes & 7] * np.where(codes & 8, -1.0, 1.0)
+    s = np.where(exps == 255, np.nan, 2.0 ** (exps.astype(F64) - 127))
+    return v * np.repeat(s, 32, axis=-1)
+
+
+def pack_mxfp4(codes, exps):
+    """Pages [n_pages][n_kv][P * (hd / 2 + hd / 32)] of codes [n_pages][n_kv][P][hd]."""
+    n, g = codes.shape[:2]
+    return np.concatenate([(codes[..., 0::2] | codes[..., 1::2] << 4).reshape(n, g, -1),
+                           exps.reshape(n, g, -1)], axis=-1)
+
+
+def unpack_mxfp4(pages, P, hd):
+    n, g = pages.shape[:2]
+    b = pages[..., :P * hd // 2].reshape(n, g, P, hd // 2)
+    codes = np.stack([b & 15, b >> 4], axis=-1).reshape(n, g, P, hd)
+    return codes, pages[..., P * hd // 2:].reshape(n, g, P, hd // 32)
 
 
 def visible(n_keys, m, causal, window, sinks):

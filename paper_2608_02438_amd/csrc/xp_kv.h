@@ -16,6 +16,12 @@ constexpr int kKvTile = 64;          // keys of an attention tile
 constexpr int kKvMaxBatch = 4096;    // sequences of a call
 constexpr int kKvMaxLen = 1 << 22;   // keys of a sequence
 
+// Bytes of a cache row of hd values.  A 4-bit cache's rows lie in two parts, the page's
+// codes (hd / 2 a row) and behind them its exponents (hd / 32 a row).
+__host__ __device__ constexpr int kv_row_bytes(int dtype, int hd) {
+  return dtype == XP_BF16 ? 2 * hd : (dtype == XP_E4M3 ? hd : hd / 2 + hd / 32);
+}
+
 // the last index in [lo, hi) whose a[] is at most x (a[lo] <= x, a non-decreasing)
 template <typename P>
 __device__ __forceinline__ int kv_owner(P a, int lo, int hi, int x) {
@@ -128,6 +134,10 @@ hipError_t launch_kv_write(const xp_kv* kv, int tokens, const uint16_t* k, const
                            int64_t k_ld, int64_t v_ld, const int32_t* slots, const int32_t* table,
                            int64_t table_ld, const int32_t* len, int B, void* kc, void* vc,
                            const float* k_scale, const float* v_scale, hipStream_t st);
+// rows of the cache back as bf16; k or v may be NULL
+hipError_t launch_kv_read(const xp_kv* kv, int tokens, const int32_t* slots, const void* kc,
+                          const void* vc, const float* k_scale, const float* v_scale, uint16_t* k,
+                          uint16_t* v, int64_t k_ld, int64_t v_ld, hipStream_t st);
 // the units of the attention's work list, counted in 32 bits, for n sequences of
 // `tokens` tokens and tables of table_ld pages
 bool kv_units_fit(const xp_kv* kv, int64_t tokens, int64_t n, int groups, int64_t table_ld);

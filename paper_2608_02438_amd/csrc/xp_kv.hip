@@ -287,8 +287,31 @@ struct KvWrite {
   uint32_t* err;
 };
 
-template <int HD, bool F8>
+// by value: a cast of a vector's element itself reads the first one
+__device__ __forceinline__ xp_bf16x2 as_bf16x2(uint32_t x) { return __builtin_bit_cast(xp_bf16x2, x); }
+// the greatest of a quad's four
+__device__ __forceinline__ uint32_t quad_max(uint32_t x) {
+  const uint32_t y = max(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xB1, 0xF, 0xF, true));
+  return max(y, (uint32_t)__builtin_amdgcn_mov_dpp((int)y, 0x4E, 0xF, 0xF, true));
+}
+// where row `slot` of KV head g begins; of a 4-bit cache its codes
+template <int HD, int FMT>
+__device__ __forceinline__ int64_t kv_row_at(int64_t slot, int g, int nkv, int logP) {
+  const int64_t head = (slot >> logP) * nkv + g;
+  const int r = (int)slot & ((1 << logP) - 1);
+  if constexpr (FMT == XP_MXFP4) return (head << logP) * kv_row_bytes(FMT, HD) + r * (HD / 2);
+  else return ((head << logP) + r) * kv_row_bytes(FMT, HD);
+}
+// from a 4-bit row's codes to its exponents
+template <int HD>
+__device__ __forceinline__ int64_t kv_exp_at(int64_t slot, int logP) {
+  const int r = (int)slot & ((1 << logP) - 1);
+  return ((int64_t)(HD / 2) << logP) - r * (HD / 2) + r * (HD / 32);
+}
+
+template <int HD, int FMT>
 __global__ __launch_bounds__(256) void k_kv_write(const KvWrite d) {
+  constexpr bool F8 = FMT == XP_E4M3, F4 = FMT == XP_MXFP4;
   constexpr int VE = F8 ? 16 : 8, CH = HD / VE;   // values, chunks of a row
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= d.items) return;
@@ -317,11 +340,31 @@ __global__ __launch_bounds__(256) void k_kv_write(const KvWrite d) {
     slot = (page << d.logP) + (int)(pos & ((1 << d.logP) - 1));
   }
   const uint16_t* src = (isv ? d.v + t * d.v_ld : d.k + t * d.k_ld) + g * HD + c * VE;
-  char* dst = (isv ? d.vc : d.kc) +
-              ((((int64_t)(slot >> d.logP) * d.nkv + g) << d.logP) + (slot & ((1 << d.logP) - 1))) *
-                  (HD * (F8 ? 1 : 2)) + 16 * c;
+  char* dst = (isv ? d.vc : d.kc) + kv_row_at<HD, FMT>(slot, g, d.nkv, d.logP) + (F4 ? 4 : 16) * c;
   const u32x4 a = ld16(src);
-  if constexpr (!F8) {
+  if constexpr (F4) {
+    // A quad of lanes has a block.  With its greatest magnitude m 2^k (1 <= m < 2) the
+    // exponent is k - 2 where m <= 1.75 and k - 1 above: 31 units of the last place more
+    // carry into the bf16 exponent exactly then.
+    typedef unsigned short us2 __attribute__((ext_vector_type(2)));
+    us2 m = __builtin_bit_cast(us2, a[0] & 0x7fff7fffu);
+#pragma unroll
+    for (int q = 1; q < 4; ++q)
+      m = __builtin_elementwise_max(m, __builtin_bit_cast(us2, a[q] & 0x7fff7fffu));
+    const uint32_t top = quad_max(m[0] > m[1] ? m[0] : m[1]);
+    const bool num = top < 0x7f80u;
+    const int e = min(max((int)((top + 31) >> 7) - 2, 2), 252);
+    const float s = __uint_as_float((uint32_t)e << 23);
+    uint32_t y = 0;
+    y = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(y, as_bf16x2(a[0]), s, 0);
+    y = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(y, as_bf16x2(a[1]), s, 1);
+    y = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(y, as_bf16x2(a[2]), s, 2);
+    y = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(y, as_bf16x2(a[3]), s, 3);
+    *reinterpret_cast<uint32_t*>(dst) = num ? y : 0u;
+    if ((c & 3) == 0)
+      *reinterpret_cast<uint8_t*>(dst - 4 * c + kv_exp_at<HD>(slot, d.logP) + c / 4) =
+          (uint8_t)(num ? e : 255);
+  } else if constexpr (!F8) {
     *reinterpret_cast<u32x4*>(dst) = a;
   } else {
     const u32x4 b = ld16(src + 8);
@@ -342,6 +385,70 @@ __global__ __launch_bounds__(256) void k_kv_write(const KvWrite d) {
   }
 }
 
+struct KvRead {
+  const int32_t* slots;
+  int64_t items;                     // tokens * n_kv * chunks of 8 values
+  int nkv, logP, n_pages;
+  const char *kc, *vc;
+  const float *ks, *vs;
+  uint16_t *k, *v;
+  int64_t k_ld, v_ld;
+  uint32_t* err;
+};
+
+// x s rounded once to bf16: the fp32 product moves off the middle between two bf16
+// values where its own rounding put it there
+__device__ __forceinline__ float product_for_bf16(float x, float s) {
+  const float p = x * s, e = fmaf(x, s, -p);
+  uint32_t u = __float_as_uint(p);
+  if ((u & 0xffffu) == 0x8000u && e != 0.f) u += (e > 0.f) == (p > 0.f) ? 1u : -1u;
+  return __uint_as_float(u);
+}
+
+// 8 values (16 bytes of the result) a thread
+template <int HD, int FMT>
+__global__ __launch_bounds__(256) void k_kv_read(const KvRead d) {
+  constexpr int CH = HD / 8;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= d.items) return;
+  const bool isv = blockIdx.y == 1 || d.k == nullptr;
+  const int c = (int)(i % CH);
+  const int64_t row = i / CH;
+  const int64_t t = row / d.nkv;
+  const int g = (int)(row - t * d.nkv);
+  const int slot = d.slots[t];
+  const bool in = (uint32_t)slot < (uint32_t)d.n_pages << d.logP;
+  if (!in && slot != -1 && g == 0 && c == 0) atomicOr(d.err, XP_DEVERR_SLOT);
+  u32x4 y{0u, 0u, 0u, 0u};
+  if (in) {
+    const char* src = (isv ? d.vc : d.kc) + kv_row_at<HD, FMT>(slot, g, d.nkv, d.logP) +
+                      c * (FMT == XP_BF16 ? 16 : (FMT == XP_E4M3 ? 8 : 4));
+    if constexpr (FMT == XP_BF16) {
+      y = ld16(src);
+    } else if constexpr (FMT == XP_E4M3) {
+      const uint2 x = *reinterpret_cast<const uint2*>(src);
+      const float* sp = isv ? d.vs : d.ks;
+      const float s = sp != nullptr ? sp[g] : 1.f;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const xp_f32x2 f = q % 2 == 0 ? __builtin_amdgcn_cvt_pk_f32_fp8((int)(q < 2 ? x.x : x.y), false)
+                                      : __builtin_amdgcn_cvt_pk_f32_fp8((int)(q < 2 ? x.x : x.y), true);
+        y[q] = pk_bf16(product_for_bf16(f[0], s), product_for_bf16(f[1], s));
+      }
+    } else {
+      const uint32_t x = *reinterpret_cast<const uint32_t*>(src);
+      const uint8_t e =
+          *reinterpret_cast<const uint8_t*>(src - 4 * c + kv_exp_at<HD>(slot, d.logP) + c / 4);
+      const float s = __uint_as_float((uint32_t)e << 23);
+      y[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, s, 0));
+      y[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, s, 1));
+      y[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, s, 2));
+      y[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, s, 3));
+    }
+  }
+  *reinterpret_cast<u32x4*>((isv ? d.v + t * d.v_ld : d.k + t * d.k_ld) + g * HD + 8 * c) = y;
+}
+
 __global__ void k_kv_clear_err(uint32_t* err) {
   if (threadIdx.x == 0) *err = 0u;
 }
@@ -356,14 +463,13 @@ hipError_t launch_kv_write(const xp_kv* kv, int tokens, const uint16_t* k, const
                            int64_t k_ld, int64_t v_ld, const int32_t* slots, const int32_t* table,
                            int64_t table_ld, const int32_t* len, int B, void* kc, void* vc,
                            const float* k_scale, const float* v_scale, hipStream_t st) {
-  const bool f8 = kv->dtype == XP_E4M3;
   KvWrite d{};
   d.k = k;
   d.v = v;
   d.k_ld = k_ld;
   d.v_ld = v_ld;
   d.nkv = kv->nkv;
-  d.items = (int64_t)tokens * kv->nkv * (kv->hd / (f8 ? 16 : 8));
+  d.items = (int64_t)tokens * kv->nkv * (kv->hd / (kv->dtype == XP_E4M3 ? 16 : 8));
   d.logP = kv->logP;
   d.n_pages = kv->n_pages;
   d.slots = slots;
@@ -378,13 +484,50 @@ hipError_t launch_kv_write(const xp_kv* kv, int tokens, const uint16_t* k, const
   d.vs = v_scale;
   d.err = kv->err;
   const dim3 grid((unsigned)((d.items + 255) / 256), 2);
+#define XP_KV(HD_, FMT_) hipLaunchKernelGGL((k_kv_write<HD_, FMT_>), grid, dim3(256), 0, st, d)
   if (kv->hd == 128) {
-    if (f8) hipLaunchKernelGGL((k_kv_write<128, true>), grid, dim3(256), 0, st, d);
-    else hipLaunchKernelGGL((k_kv_write<128, false>), grid, dim3(256), 0, st, d);
+    if (kv->dtype == XP_BF16) XP_KV(128, XP_BF16);
+    else if (kv->dtype == XP_E4M3) XP_KV(128, XP_E4M3);
+    else XP_KV(128, XP_MXFP4);
   } else {
-    if (f8) hipLaunchKernelGGL((k_kv_write<64, true>), grid, dim3(256), 0, st, d);
-    else hipLaunchKernelGGL((k_kv_write<64, false>), grid, dim3(256), 0, st, d);
+    if (kv->dtype == XP_BF16) XP_KV(64, XP_BF16);
+    else if (kv->dtype == XP_E4M3) XP_KV(64, XP_E4M3);
+    else XP_KV(64, XP_MXFP4);
   }
+#undef XP_KV
+  return hipGetLastError();
+}
+
+hipError_t launch_kv_read(const xp_kv* kv, int tokens, const int32_t* slots, const void* kc,
+                          const void* vc, const float* k_scale, const float* v_scale, uint16_t* k,
+                          uint16_t* v, int64_t k_ld, int64_t v_ld, hipStream_t st) {
+  KvRead d{};
+  d.slots = slots;
+  d.items = (int64_t)tokens * kv->nkv * (kv->hd / 8);
+  d.nkv = kv->nkv;
+  d.logP = kv->logP;
+  d.n_pages = kv->n_pages;
+  d.kc = (const char*)kc;
+  d.vc = (const char*)vc;
+  d.ks = k_scale;
+  d.vs = v_scale;
+  d.k = k;
+  d.v = v;
+  d.k_ld = k_ld;
+  d.v_ld = v_ld;
+  d.err = kv->err;
+  const dim3 grid((unsigned)((d.items + 255) / 256), k != nullptr && v != nullptr ? 2 : 1);
+#define XP_KV(HD_, FMT_) hipLaunchKernelGGL((k_kv_read<HD_, FMT_>), grid, dim3(256), 0, st, d)
+  if (kv->hd == 128) {
+    if (kv->dtype == XP_BF16) XP_KV(128, XP_BF16);
+    else if (kv->dtype == XP_E4M3) XP_KV(128, XP_E4M3);
+    else XP_KV(128, XP_MXFP4);
+  } else {
+    if (kv->dtype == XP_BF16) XP_KV(64, XP_BF16);
+    else if (kv->dtype == XP_E4M3) XP_KV(64, XP_E4M3);
+    else XP_KV(64, XP_MXFP4);
+  }
+#undef XP_KV
   return hipGetLastError();
 }
 
@@ -421,8 +564,8 @@ extern "C" xp_status xp_kv_create(const xp_kv_shape* s, int32_t max_batch, int32
     return kv_fail(nullptr, XP_EINVAL,
                    "sizes must be positive (heads=%d kv=%d head_dim=%d page_size=%d n_pages=%d)",
                    s->n_heads, s->n_kv, s->head_dim, s->page_size, s->n_pages);
-  if (s->dtype != XP_BF16 && s->dtype != XP_E4M3)
-    return kv_fail(nullptr, XP_EINVAL, "dtype %d is not XP_BF16 or XP_E4M3", s->dtype);
+  if (s->dtype != XP_BF16 && s->dtype != XP_E4M3 && s->dtype != XP_MXFP4)
+    return kv_fail(nullptr, XP_EINVAL, "dtype %d is not XP_BF16, XP_E4M3 or XP_MXFP4", s->dtype);
   if (max_batch < 1 || max_batch > kKvMaxBatch || max_tokens < 1 || max_tokens > (1 << 20) ||
       max_len < 1 || max_len > kKvMaxLen || (shared != 0 && shared != 1))
     return kv_fail(nullptr, XP_EINVAL,
@@ -599,8 +742,8 @@ static xp_status kv_cache_args(xp_kv* kv, const void* kc, const void* vc, const 
                                const float* vs) {
   if (kc == nullptr || vc == nullptr || misaligned(kc) || misaligned(vc))
     return kv_fail(kv, XP_EINVAL, "k_cache or v_cache is NULL or not 16-byte aligned");
-  if (kv->dtype == XP_BF16 && (ks != nullptr || vs != nullptr))
-    return kv_fail(kv, XP_EINVAL, "a bf16 cache has no scales");
+  if (kv->dtype != XP_E4M3 && (ks != nullptr || vs != nullptr))
+    return kv_fail(kv, XP_EINVAL, "only an 8-bit cache has scales of the caller's");
   return XP_OK;
 }
 
@@ -625,6 +768,30 @@ extern "C" xp_status xp_kv_write(xp_kv* kv, int32_t tokens, const void* k, int64
                                        v_ld, slots, nullptr, 0, nullptr, 0, k_cache, v_cache,
                                        k_scale, v_scale, (hipStream_t)stream);
   if (e != hipSuccess) return kv_fail(kv, XP_EHIP, "write launch failed: %s", hipGetErrorString(e));
+  return XP_OK;
+}
+
+extern "C" xp_status xp_kv_read(xp_kv* kv, int32_t tokens, const int32_t* slots,
+                                const void* k_cache, const void* v_cache, const float* k_scale,
+                                const float* v_scale, void* k, int64_t k_ld, void* v, int64_t v_ld,
+                                void* stream) {
+  if (kv == nullptr) return XP_EINVAL;
+  if (tokens < 0 || tokens > kv->max_tokens)
+    return kv_fail(kv, XP_EINVAL, "tokens=%d out of range 0..%d", tokens, kv->max_tokens);
+  const int64_t row = (int64_t)kv->nkv * kv->hd;
+  if ((k == nullptr && v == nullptr) || slots == nullptr || misaligned(k) || misaligned(v) ||
+      (k != nullptr && (k_ld < row || k_ld % 8 != 0)) ||
+      (v != nullptr && (v_ld < row || v_ld % 8 != 0)))
+    return kv_fail(kv, XP_EINVAL,
+                   "slots and one of k and v (16-byte aligned) are required, k_ld=%lld and v_ld=%lld "
+                   "at least n_kv*head_dim=%lld and multiples of 8", (long long)k_ld,
+                   (long long)v_ld, (long long)row);
+  xp_status s = kv_cache_args(kv, k_cache, v_cache, k_scale, v_scale);
+  if (s == XP_OK) s = kv_device(kv);
+  if (s != XP_OK || tokens == 0) return s;
+  const hipError_t e = launch_kv_read(kv, tokens, slots, k_cache, v_cache, k_scale, v_scale,
+                                      (uint16_t*)k, (uint16_t*)v, k_ld, v_ld, (hipStream_t)stream);
+  if (e != hipSuccess) return kv_fail(kv, XP_EHIP, "read launch failed: %s", hipGetErrorString(e));
   return XP_OK;
 }
 

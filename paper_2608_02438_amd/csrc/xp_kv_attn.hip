@@ -403,6 +403,14 @@ __device__ __forceinline__ u32x4 f8_bf16x8(uint32_t a, uint32_t b) {
       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, false)),
       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.f, true))};
 }
+// 8 e2m1 codes times a power of two to bf16 (exact; NaN for the exponent 255)
+__device__ __forceinline__ u32x4 f4_bf16x8(uint32_t a, float s) {
+  return u32x4{
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a, s, 0)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a, s, 1)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a, s, 2)),
+      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(a, s, 3))};
+}
 __device__ __forceinline__ uint32_t lds_byte(const void* p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
 }
@@ -685,8 +693,9 @@ constexpr int kv_waves(int hd, int wr, int wk) { return hd == 64 && wr == 4 && w
 // 560 us, 980 TFLOP/s; head_dim 64, with as many exponentials to half the products,
 // 410 us, 670).  A segment's beginning and end take about 10000 cycles, 2 to 3 tiles:
 // four causal prompts of 4096 668 us, 822 TFLOP/s.
-template <int HD, bool F8, int WR, int WK, int NST, int PARTS, bool OWN>
+template <int HD, int FMT, int WR, int WK, int NST, int PARTS, bool OWN>
 __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn(const KvDev d) {
+  constexpr bool F8 = FMT == XP_E4M3, F4 = FMT == XP_MXFP4;
   using SH = KvRows<HD, F8>;
   constexpr int NW = WR * WK, R = 32 * WR, NB = 2 / WK, ND = HD / 32, NKS = HD / 16;
   constexpr int RB = SH::RB, CPR = SH::CPR, IPG = SH::IPG;
@@ -697,7 +706,8 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
   constexpr int NG = 8 / NW;                      // groups of 16 rows that a wave loads
   static_assert(NG * NW == 8 && NB * WK == 2, "waves");
   constexpr int PER = NG * IPG;                   // loads of a wave for a stage
-  static_assert((NST - 1) * PER < 64, "vmcnt field");
+  static_assert(F4 || (NST - 1) * PER < 64, "vmcnt field");
+  static_assert(!F4 || NST >= (WK == 2 ? 2 : 3), "4-bit: K of two (three) tiles");
   constexpr int kMerge = (HD / 2 + 2) * kWave;    // floats that a wave hands over
   static_assert(WK == 1 || WR * kMerge * 4 <= NST * SH::kStage * 16, "merge in LDS");
   __shared__ __align__(256) u32x4 lds[NST * SH::kStage];
@@ -786,8 +796,9 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
   // ---- loads ----
   const scalar_i32 tb = as_scalar(d.table + (int64_t)seq * d.table_ld);
   // the first page's rows of this KV head, and the bytes from page to page
-  const char* heads = (wave < NW / 2 ? d.kc : d.vc) + (((int64_t)kvh << d.logP) * RB);
-  const uint32_t page_bytes = (uint32_t)(d.nkv * RB) << d.logP;
+  constexpr int RBM = kv_row_bytes(FMT, HD);      // bytes of a row in memory
+  const char* heads = (wave < NW / 2 ? d.kc : d.vc) + (((int64_t)kvh << d.logP) * RBM);
+  const uint32_t page_bytes = (uint32_t)(d.nkv * RBM) << d.logP;
   const int kin = imax(klo, kfloor);              // from here to khi, or to ks_, some row sees all
   uint32_t bad = 0;                               // a page outside the cache was asked for
   auto pages = [&](int t, int (&pg)[NG]) {        // page ids of the wave's rows of tile t
@@ -842,18 +853,77 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
   const int is_k = wave < NW / 2 ? 1 : 0, ahead = NB == 1 ? is_k : 0;
   // loads still under way when iteration t has what it needs: K of tile t + 1, V of t
   constexpr int kWaitV = (NST - 2) * PER, kWaitK = (NB == 1 ? NST - 2 : NST - 3) * PER;
-  static_assert(kWaitK >= 0, "stages");
-  int pg[NG], pg0[NST][NG];
+  static_assert(F4 || kWaitK >= 0, "stages");
+  // A 4-bit cache's tiles come through registers and are expanded to bf16 (exactly) on
+  // their way into the ring, so that everything behind it is a bf16 cache's.  A lane
+  // takes HD / 4 values of row lane / 4 of each 16 and their exponent.  The waves that
+  // load V store tile t + 1 in iteration t, those that load K tile t + 2, and have the
+  // tile after it under way meanwhile.
+  struct Held {
+    u32x4 x[NG];
+    uint32_t e[NG];
+  };
+  auto fetch = [&](int t, const int (&pg)[NG], Held& to) __attribute__((always_inline)) {
+    const int k0 = tile_key(t);
 #pragma unroll
-  for (int t = 0; t < NST; ++t) pages(j + imin(t, nj - 1), pg0[t]);
-  pages(j + imin(NST - 1 + ahead, nj - 1), pg);
+    for (int g = 0; g < NG; ++g) {
+      const int g0 = k0 + 16 * ((wave * NG + g) & 3), key = g0 + lane / 4, r = key & P1;
+      const uint32_t page = (uint32_t)pg[g];
+      const bool ok = page < (uint32_t)d.n_pages;
+      const int from = imax(g0, kfloor), to_ = imin(g0 + 16, khi);
+      bad |= (!ok & (from < to_) & ((to_ > klo) | (from < ks_))) ? XP_DEVERR_PAGE : 0u;
+      const char* base = heads + (uint64_t)(ok ? page : 0u) * page_bytes;
+      const bool any = (key >= kfloor) & (key < khi) & ((key >= klo) | (key < ks_));
+      const char* x = any ? base + r * (HD / 2) + (HD / 8) * (lane & 3) : d.w.zero;
+      const char* e = any ? base + ((HD / 2) << d.logP) + r * (HD / 32) + (lane & 3) * HD / 128
+                          : d.w.zero;
+      if constexpr (HD == 128) {
+        to.x[g] = ld16(x);
+      } else {
+        const uint2 y = *reinterpret_cast<const uint2*>(x);
+        to.x[g] = u32x4{y.x, y.y, 0u, 0u};
+      }
+      to.e[g] = *reinterpret_cast<const uint8_t*>(e);
+    }
+  };
+  auto put = [&](int slot, const Held& from) __attribute__((always_inline)) {
+    u32x4* stage = lds + slot * SH::kStage + wave * (NG * 16 * CPR);   // its rows of K, then V
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      const float s = __uint_as_float(from.e[g] << 23);
+      const int r = lane / 4;
+      u32x4* row = stage + (16 * g + r) * CPR;
+#pragma unroll
+      for (int i = 0; i < HD / 32; ++i)
+        row[(HD / 32 * (lane & 3) + i) ^ SH::swz(r)] = f4_bf16x8(from.x[g][i], s);
+    }
+  };
+  const int lead = F4 ? is_k : ahead;             // tiles that the wave's loads run ahead
+  constexpr int NPG = F4 ? 2 : NST;
+  Held held;
+  int pg[NG], pg0[NPG][NG];
+#pragma unroll
+  for (int t = 0; t < NPG; ++t) pages(j + imin(t, nj - 1), pg0[t]);
+  pages(j + imin(F4 ? 2 : NST - 1 + ahead, nj - 1), pg);
   // The query rows are waited for here: with loads to LDS under way the compiler waits
   // for all of them before it uses a register that was loaded.
 #pragma unroll
   for (int ks = 0; ks < NKS; ++ks) asm volatile("" : "+v"(qf[ks]));
+  if constexpr (F4) {
+    Held first;
+    fetch(j, pg0[0], first);
+    fetch(j + imin(1, nj - 1), pg0[1], held);
+    put(0, first);
+    if (is_k) {                                   // whole wave
+      put(1, held);
+      fetch(j + imin(2, nj - 1), pg, held);
+      pages(j + imin(3, nj - 1), pg);
+    }
+  } else {
 #pragma unroll
-  for (int t = 0; t < NST; ++t)
-    if (t < nj && t < NST - 1 + ahead) issue(std::true_type{}, j + t, t, pg0[t]);   // whole wave
+    for (int t = 0; t < NST; ++t)
+      if (t < nj && t < NST - 1 + ahead) issue(std::true_type{}, j + t, t, pg0[t]);   // whole wave
+  }
 
   float m_run = -INFINITY, l_run = 0.f;           // the row's; l of this half's keys
   floatx16 o[ND];
@@ -1054,6 +1124,15 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
   // The beginning of iteration t: K of tile t + 1 and V of tile t landed (every
   // wave's loads), and every wave is done with what the next loads replace.
   auto begin = [&](int t, int stage) __attribute__((always_inline)) {
+    if constexpr (F4) {
+      lds_barrier();
+      if (t + 1 + lead < nj) put((stage + 1 + lead) % NST, held);
+      if (t + 2 + lead < nj) {
+        fetch(j + t + 2 + lead, pg, held);
+        pages(j + imin(t + 3 + lead, nj - 1), pg);
+      }
+      return;
+    }
     asm volatile("" ::: "memory");
     if (t + NST - 2 + ahead < nj) {
       if (is_k) __builtin_amdgcn_s_waitcnt(0x0070 | (kWaitK & 15) | ((kWaitK >> 4) << 14));
@@ -1069,14 +1148,18 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
     }
   };
   // K of the first tile landed
-  asm volatile("" ::: "memory");
-  if (is_k) {
-    constexpr int kFirst = (NST - 2 + (NB == 1 ? 1 : 0)) * PER;
-    if (NST - 1 + ahead <= nj) __builtin_amdgcn_s_waitcnt(0x0070 | (kFirst & 15) | ((kFirst >> 4) << 14));
-    else __builtin_amdgcn_s_waitcnt(0x0070);
+  if constexpr (F4) {
+    lds_barrier();
+  } else {
+    asm volatile("" ::: "memory");
+    if (is_k) {
+      constexpr int kFirst = (NST - 2 + (NB == 1 ? 1 : 0)) * PER;
+      if (NST - 1 + ahead <= nj) __builtin_amdgcn_s_waitcnt(0x0070 | (kFirst & 15) | ((kFirst >> 4) << 14));
+      else __builtin_amdgcn_s_waitcnt(0x0070);
+    }
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
   }
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
   floatx16 sa, sb;
   constexpr std::integral_constant<int, 0> even{};
   constexpr std::integral_constant<int, 1> uneven{};
@@ -1386,34 +1469,43 @@ void kv_attn_sizes(const xp_kv* kv, int64_t* rows, int* entries, int* shares) {
 // one list's attention, in tiles of R rows
 static hipError_t launch_list(const xp_kv* kv, int R, bool own, const KvDev& d, hipStream_t st) {
   const int shares = kv_shares(kv, R);
-#define XP_KV(HD_, F8_, WR_, WK_, NST_, PARTS_)                                                  \
+#define XP_KV(HD_, FMT_, WR_, WK_, NST_, PARTS_)                                                 \
   do {                                                                                           \
     if (own)                                                                                     \
-      hipLaunchKernelGGL((k_kv_attn<HD_, F8_, WR_, WK_, NST_, PARTS_, true>), dim3(shares),      \
+      hipLaunchKernelGGL((k_kv_attn<HD_, FMT_, WR_, WK_, NST_, PARTS_, true>), dim3(shares),     \
                          dim3((WR_) * (WK_) * kWave), 0, st, d);                                 \
     else                                                                                         \
-      hipLaunchKernelGGL((k_kv_attn<HD_, F8_, WR_, WK_, NST_, PARTS_, false>), dim3(shares),     \
+      hipLaunchKernelGGL((k_kv_attn<HD_, FMT_, WR_, WK_, NST_, PARTS_, false>), dim3(shares),    \
                          dim3((WR_) * (WK_) * kWave), 0, st, d);                                 \
   } while (0)
-  const bool f8 = kv->dtype == XP_E4M3;
-  if (kv->hd == 128 && !f8) {
-    if (R == 32) XP_KV(128, false, 1, 2, 2, 2);
-    else if (R == 64) XP_KV(128, false, 2, 2, 2, 2);
-    else if (R == 128) XP_KV(128, false, 4, 2, 4, 1);
-    else XP_KV(128, false, 8, 1, 4, 1);
+  const int fmt = kv->dtype;
+  if (kv->hd == 128 && fmt == XP_BF16) {
+    if (R == 32) XP_KV(128, XP_BF16, 1, 2, 2, 2);
+    else if (R == 64) XP_KV(128, XP_BF16, 2, 2, 2, 2);
+    else if (R == 128) XP_KV(128, XP_BF16, 4, 2, 4, 1);
+    else XP_KV(128, XP_BF16, 8, 1, 4, 1);
+  } else if (kv->hd == 128 && fmt == XP_E4M3) {
+    if (R == 32) XP_KV(128, XP_E4M3, 1, 2, 2, 1);
+    else if (R == 64) XP_KV(128, XP_E4M3, 2, 2, 4, 1);
+    else if (R == 128) XP_KV(128, XP_E4M3, 4, 1, 4, 1);
+    else XP_KV(128, XP_E4M3, 8, 1, 8, 1);
   } else if (kv->hd == 128) {
-    if (R == 32) XP_KV(128, true, 1, 2, 2, 1);
-    else if (R == 64) XP_KV(128, true, 2, 2, 4, 1);
-    else if (R == 128) XP_KV(128, true, 4, 1, 4, 1);
-    else XP_KV(128, true, 8, 1, 8, 1);
-  } else if (!f8) {
-    if (R == 32) XP_KV(64, false, 1, 2, 2, 2);
-    else if (R == 64) XP_KV(64, false, 2, 2, 4, 2);
-    else XP_KV(64, false, 4, 1, 3, 1);
+    if (R == 32) XP_KV(128, XP_MXFP4, 1, 2, 2, 2);
+    else if (R == 64) XP_KV(128, XP_MXFP4, 2, 2, 2, 2);
+    else if (R == 128) XP_KV(128, XP_MXFP4, 4, 2, 3, 1);
+    else XP_KV(128, XP_MXFP4, 8, 1, 3, 1);
+  } else if (fmt == XP_BF16) {
+    if (R == 32) XP_KV(64, XP_BF16, 1, 2, 2, 2);
+    else if (R == 64) XP_KV(64, XP_BF16, 2, 2, 4, 2);
+    else XP_KV(64, XP_BF16, 4, 1, 3, 1);
+  } else if (fmt == XP_E4M3) {
+    if (R == 32) XP_KV(64, XP_E4M3, 1, 2, 2, 1);
+    else if (R == 64) XP_KV(64, XP_E4M3, 2, 2, 4, 1);
+    else XP_KV(64, XP_E4M3, 4, 1, 6, 1);
   } else {
-    if (R == 32) XP_KV(64, true, 1, 2, 2, 1);
-    else if (R == 64) XP_KV(64, true, 2, 2, 4, 1);
-    else XP_KV(64, true, 4, 1, 6, 1);
+    if (R == 32) XP_KV(64, XP_MXFP4, 1, 2, 2, 2);
+    else if (R == 64) XP_KV(64, XP_MXFP4, 2, 2, 2, 2);
+    else XP_KV(64, XP_MXFP4, 4, 1, 3, 1);
   }
 #undef XP_KV
   return hipGetLastError();

@@ -1515,8 +1515,8 @@ extern "C" xp_status xp_layer_forward_paged(xp_layer* L, xp_kv* kv, int32_t batc
     return layer_fail(L, XP_EINVAL, "the call's tokens and the tables' pages reach 2^31 key tiles");
   if (window < 0 || window > kKvMaxLen || sinks < 0 || sinks > kKvMaxLen)
     return layer_fail(L, XP_EINVAL, "window=%d or sinks=%d out of range 0..2^22", window, sinks);
-  if (kv->dtype == XP_BF16 && (k_scale != nullptr || v_scale != nullptr))
-    return layer_fail(L, XP_EINVAL, "a bf16 cache has no scales");
+  if (kv->dtype != XP_E4M3 && (k_scale != nullptr || v_scale != nullptr))
+    return layer_fail(L, XP_EINVAL, "only an 8-bit cache has scales of the caller's");
   int dev = -1;
   const hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return layer_fail(L, XP_EHIP, "device query failed: %s", hipGetErrorString(e));

@@ -20,7 +20,7 @@ LIB_PATH = os.environ.get("XPRESS_LIB") or os.path.join(
     os.path.dirname(os.path.abspath(__file__)), "libxpress.so")
 
 XP_OK, XP_EINVAL, XP_EUNSUPPORTED, XP_EHIP, XP_ENOMEM = 0, -1, -2, -3, -4
-XP_F32, XP_BF16, XP_E4M3 = 0, 1, 2
+XP_F32, XP_BF16, XP_E4M3, XP_MXFP4 = 0, 1, 2, 3
 XP_EARLY_EXIT, XP_WRITE_LOGITS = 1, 2
 XP_DEVERR_TOKEN, XP_DEVERR_TEMPERATURE, XP_DEVERR_FILTER = 1, 2, 4
 XP_DEVERR_PAGE, XP_DEVERR_SLOT, XP_DEVERR_POOL, XP_DEVERR_LENGTH = 8, 16, 32, 64
@@ -30,8 +30,8 @@ EXPORTS = ("xp_create", "xp_destroy", "xp_last_error", "xp_status_string",
            "xp_timing_read", "xp_probe_hbm_read", "xp_probe_mfma_bf16", "xp_toeplitz_mixer",
            "xp_layer_create", "xp_layer_forward", "xp_layer_destroy", "xp_layer_last_error",
            "xp_layer_forward_noalloc", "xp_kv_create", "xp_kv_destroy", "xp_kv_last_error",
-           "xp_kv_map", "xp_kv_write", "xp_kv_attn", "xp_kv_attn_shared", "xp_kv_device_errors",
-           "xp_layer_forward_paged")
+           "xp_kv_map", "xp_kv_write", "xp_kv_read", "xp_kv_attn", "xp_kv_attn_shared",
+           "xp_kv_device_errors", "xp_layer_forward_paged")
 LAYER_WEIGHT_NAMES = ("g_attn", "Wq", "Wk", "Wv", "g_q", "g_k", "Wo", "g_mlp", "Wg", "Wu", "Wd")
 STAGES = ("prep", "lmhead", "select", "rspace", "read", "verify")
 
@@ -121,6 +121,8 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     L.xp_kv_map.restype = i32
     L.xp_kv_write.argtypes = [vp, i32, vp, i64, vp, i64, vp, vp, vp, vp, vp, vp]
     L.xp_kv_write.restype = i32
+    L.xp_kv_read.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, i64, vp, i64, vp]
+    L.xp_kv_read.restype = i32
     attn = [vp, i64, vp, vp, vp, i64, vp, vp, vp, vp, i32, i32, i32, ctypes.c_float, vp, i64, vp,
             vp]
     L.xp_kv_attn.argtypes = [vp, i32, i32, i32] + attn
@@ -459,9 +461,11 @@ class Layer:
 
 class PagedKV:
     """The paged context cache (xp_kv_*): pages and slots from lengths, writes of
-    new keys and values, and attention over the pages.  The caches [n_pages]
-    [n_kv][page_size][head_dim] (``cache_shape``; bf16 or torch.float8_e4m3fn)
-    and the tables belong to the caller."""
+    new keys and values, their rows back, and attention over the pages.  The caches
+    [n_pages][n_kv][page_size][head_dim] (``cache_shape``; bf16 or torch.float8_e4m3fn)
+    and the tables belong to the caller.  With cache_dtype="mxfp4" the caches are
+    torch.uint8 [n_pages][n_kv][page_size (head_dim / 2 + head_dim / 32)]: e2m1 codes
+    and a power of two per 32 values (xp_kv_shape)."""
 
     def __init__(self, n_heads: int, n_kv: int, page_size: int, n_pages: int, max_batch: int,
                  max_tokens: int, max_len: int, head_dim: int = 128, cache_dtype=None,
@@ -469,15 +473,21 @@ class PagedKV:
         import torch
         L = load_library()
         self.cache_dtype = torch.bfloat16 if cache_dtype is None else cache_dtype
-        dt = {torch.bfloat16: XP_BF16, torch.float8_e4m3fn: XP_E4M3}.get(self.cache_dtype)
+        dt = {torch.bfloat16: XP_BF16, torch.float8_e4m3fn: XP_E4M3,
+              "mxfp4": XP_MXFP4}.get(self.cache_dtype)
         if dt is None:
-            raise ValueError(f"cache_dtype {cache_dtype}: torch.bfloat16 or torch.float8_e4m3fn")
+            raise ValueError(f"cache_dtype {cache_dtype}: torch.bfloat16, torch.float8_e4m3fn or "
+                             "'mxfp4'")
         self.device = torch.device(device)
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
         self.n_heads, self.n_kv, self.head_dim, self.page_size = n_heads, n_kv, head_dim, page_size
         self.n_pages = n_pages
         self.cache_shape = torch.Size((n_pages, n_kv, page_size, head_dim))
+        if dt == XP_MXFP4:
+            self.cache_dtype = torch.uint8
+            self.cache_shape = torch.Size((n_pages, n_kv,
+                                           page_size * (head_dim // 2 + head_dim // 32)))
         self._torch, self._index = torch, self.device.index
         self._raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         st = _KvShape(n_heads=n_heads, n_kv=n_kv, head_dim=head_dim, page_size=page_size,
@@ -575,6 +585,31 @@ class PagedKV:
         if n:
             self._call("xp_kv_write", n, k.data_ptr(), k_ld, v.data_ptr(), v_ld, sl, *c,
                        stream=stream)
+
+    def read(self, slots, k_cache, v_cache, k_scale=None, v_scale=None, k=None, v=None,
+             stream=None):
+        """The rows of `slots` as bf16 [tokens][n_kv][head_dim] (xp_kv_read), 0 where a
+        slot is -1.  Returns (k, v), allocated where None; with False in the place of one
+        of them that side is not read, and None returned for it."""
+        n = slots.shape[0]
+        sl = self._flat("slots", slots, self._torch.int32, n)
+        c = self._cache(k_cache, v_cache, k_scale, v_scale)
+        if k is False and v is False:
+            raise ValueError("k, v: one of them is read at least")
+        out, args = [], []
+        for name, t in (("k", k), ("v", v)):
+            if t is False:
+                out.append(None)
+                args += [None, 0]
+                continue
+            if t is None:
+                t = _empty_on(stream, (n, self.n_kv, self.head_dim), self._torch.bfloat16,
+                              self.device)
+            args += [t.data_ptr(), self._rows(name, t, self.n_kv, n)]
+            out.append(t)
+        if n:
+            self._call("xp_kv_read", n, sl, *c, args[0], args[1], args[2], args[3], stream=stream)
+        return tuple(out)
 
     def _attend(self, name, groups, q, k_cache, v_cache, table, kv_len, cu_q, max_q, causal,
                 window, sinks, scale, k_scale, v_scale, out, lse, stream):
