@@ -60,11 +60,12 @@ typedef enum {
 /* bits of the device error word */
 #define XP_DEVERR_TOKEN 1u  /* a token id outside [0, V) was read and replaced by 0 */
 #define XP_DEVERR_TEMPERATURE 2u  /* a sampled row's temperature was not finite and > 0; 1 was used */
-#define XP_DEVERR_FILTER 4u       /* a sampled row's top_k < 0 or top_p <= 0 (or NaN); not applied */
+#define XP_DEVERR_FILTER 4u       /* a sampled row's top_k < 0, top_p <= 0 or min_p outside 0..1 (or NaN); not applied */
 #define XP_DEVERR_PAGE 8u     /* a page id outside [0, n_pages) where a key is; page 0 was read, or no slot given */
 #define XP_DEVERR_SLOT 16u    /* a slot outside the cache, not written; or more new tokens than slots */
 #define XP_DEVERR_POOL 32u    /* too few free pages (requests not served), or a pool count out of range */
 #define XP_DEVERR_LENGTH 64u  /* a length, token or group range or page count out of range; clamped or left alone */
+#define XP_DEVERR_EMPTY 128u  /* a row of logits, all of them -inf or NaN; its id is -1 */
 
 typedef struct xp_handle xp_handle;
 
@@ -570,6 +571,44 @@ xp_status xp_kv_attn_shared(xp_kv* kv, int32_t n, int32_t tokens, int32_t max_q,
 xp_status xp_kv_device_errors(xp_kv* kv, uint32_t* out, void* stream);
 
 /*
+ * Rotary positions of one or several axes for the rows of queries and keys, with the
+ * RMSNorm over each head in front of them, as the context layer applies them to its own:
+ * what rows go through before xp_kv_write and xp_kv_attn.
+ *
+ *   y = x / sqrt(mean(x^2) + eps) * g over the head's dims, where g is given
+ *   pair j < rot_dim / 2 of a head is (y[j], y[j + rot_dim / 2]), rotated by the angle
+ *       pos[axis of j][token] * theta^(-2 j / rot_dim); dims from rot_dim on stay y
+ *   sections[a] pairs belong to axis a; their sum is rot_dim / 2.  One after the other,
+ *       or interleaved: pair j is of axis j % axes where j / axes < sections[j % axes],
+ *       else of axis 0 (an axis a > 0 then needs a + axes (sections[a] - 1) < rot_dim / 2)
+ *
+ * Built: head_dim 64, 128 or 256; rot_dim a multiple of 16; axes 1 .. 4; XP_BF16 or
+ * XP_F32; theta 1 .. 2^60; eps 0 .. 2^60.
+ */
+typedef struct {
+  int32_t head_dim, rot_dim;
+  int32_t axes, sections[4], interleaved;
+  int32_t dtype;                     /* of q, k, the gains and the results */
+  float theta, eps;
+} xp_rope_shape;
+
+/*
+ *   pos    [axes][pos_ld] int32, tokens of each row; negative ones rotate back (a key
+ *          that was rotated for p is one for p + d after another rotation by d)
+ *   q, k   [tokens][heads][head_dim], token rows q_ld, k_ld elements apart, 16-byte
+ *          aligned as their distances; no heads: NULL
+ *   g_q, g_k [head_dim] or NULL: no norm
+ *   q_out, k_out   may be q and k themselves (with the same row distances), else apart
+ * Norm, products and sums in fp32, one rounding to the result's type; angles in fp64.
+ * Asynchronous on `stream`; no handle, no allocation.
+ * Errors: XP_EINVAL, XP_EUNSUPPORTED (head_dim), before any HIP call; XP_EHIP.
+ */
+xp_status xp_rope(const xp_rope_shape* shape, int32_t tokens, const int32_t* pos, int64_t pos_ld,
+                  const void* q, int64_t q_ld, int32_t n_heads, const void* g_q, void* q_out,
+                  int64_t q_out_ld, const void* k, int64_t k_ld, int32_t n_kv, const void* g_k,
+                  void* k_out, int64_t k_out_ld, void* stream);
+
+/*
  * xp_layer_forward over the paged context cache: the block's own keys and values
  * are written to the pages of positions ctx_len[b] .. ctx_len[b] + B - 1, then
  * every query attends to its request's pages, with xp_kv_attn's causal, window
@@ -591,6 +630,52 @@ xp_status xp_layer_forward_paged(xp_layer* L, xp_kv* kv, int32_t batch, int32_t 
                                  void* v_cache, const float* k_scale, const float* v_scale,
                                  const int32_t* table, int64_t table_ld, const int32_t* ctx_len,
                                  float* h_f32, void* h_bf16, void* stream);
+
+/*
+ * Tokens from logits: the token behind a prompt (a block's anchor x_0), greedy targets
+ * for xp_verify_block, plain decoding, beside the selections inside refine and verify.
+ *
+ * A sampler serves calls of up to max_rows (<= 65536) rows of V (<= 2^18) logits on the
+ * current device.  Calls on one sampler share its workspace: issue them in stream order,
+ * and replay captured graphs of them in that order too.
+ * Errors: XP_EINVAL (sizes), XP_EUNSUPPORTED (V), XP_ENOMEM, XP_EHIP.  *out is NULL on
+ * error; xp_sampler_last_error(NULL) names the problem.
+ */
+typedef struct xp_sampler xp_sampler;
+xp_status xp_sampler_create(int32_t V, int32_t max_rows, xp_sampler** out);
+
+/* Free the sampler and its workspace (waits for the device first).  NULL is a no-op. */
+void xp_sampler_destroy(xp_sampler* s);
+
+/* Message of the last failed call on `s` (NULL: of this thread's last failed create). */
+const char* xp_sampler_last_error(const xp_sampler* s);
+
+/*
+ *   logits [rows][V] float or bf16 (dtype), rows ld elements apart (any distance >= V)
+ *   temp, temperature, top_k, top_p   [rows], as for xp_refine_block, and with the same
+ *          replacements: temp NULL = all greedy (argmax, ties to the lowest index)
+ *   min_p  [rows] float or NULL: of the tokens that top-k and top-p keep, those whose
+ *          probability under softmax(l / T) is at least min_p times the greatest one's
+ *          stay; 0 .. 1, 0: all (others set XP_DEVERR_FILTER and mean none)
+ *   u      [rows] float in [0, 1), iff temp != NULL: a sampled row takes the first token
+ *          in index order at which the sum of the kept weights exceeds u times their
+ *          sum, the last one with a weight if none does
+ *   out_ids [rows] int32; out_logprob [rows] float or NULL: the log of the token's
+ *          probability among the kept ones, 0 for greedy rows
+ * Logits of -inf (masked tokens) and NaN are never taken; a row that holds nothing else
+ * gives id -1, log probability -inf, and sets XP_DEVERR_EMPTY.  Tokens at +inf share all
+ * of the weight.  Weights e^{(l - max) / T} are formed in 64 bits and summed exactly in
+ * units of 2^-45; tokens below 2^-46 of the greatest weight have none.  The same call
+ * gives the same tokens.
+ * Errors: XP_EINVAL before any launch, XP_EHIP.
+ */
+xp_status xp_sample(xp_sampler* s, int32_t rows, int32_t dtype, const void* logits, int64_t ld,
+                    const uint8_t* temp, const float* temperature, const int32_t* top_k,
+                    const float* top_p, const float* min_p, const float* u, int32_t* out_ids,
+                    float* out_logprob, void* stream);
+
+/* Read and clear the sampler's device error word into *out (host).  Synchronizes `stream`. */
+xp_status xp_sampler_device_errors(xp_sampler* s, uint32_t* out, void* stream);
 
 /*
  * Measurement probes (not part of the method).  They give the measured peaks

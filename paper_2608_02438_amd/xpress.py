@@ -24,6 +24,7 @@ XP_F32, XP_BF16, XP_E4M3, XP_MXFP4 = 0, 1, 2, 3
 XP_EARLY_EXIT, XP_WRITE_LOGITS = 1, 2
 XP_DEVERR_TOKEN, XP_DEVERR_TEMPERATURE, XP_DEVERR_FILTER = 1, 2, 4
 XP_DEVERR_PAGE, XP_DEVERR_SLOT, XP_DEVERR_POOL, XP_DEVERR_LENGTH = 8, 16, 32, 64
+XP_DEVERR_EMPTY = 128
 
 EXPORTS = ("xp_create", "xp_destroy", "xp_last_error", "xp_status_string",
            "xp_refine_block", "xp_verify_block", "xp_device_errors", "xp_timing_enable",
@@ -31,7 +32,8 @@ EXPORTS = ("xp_create", "xp_destroy", "xp_last_error", "xp_status_string",
            "xp_layer_create", "xp_layer_forward", "xp_layer_destroy", "xp_layer_last_error",
            "xp_layer_forward_noalloc", "xp_kv_create", "xp_kv_destroy", "xp_kv_last_error",
            "xp_kv_map", "xp_kv_write", "xp_kv_read", "xp_kv_attn", "xp_kv_attn_shared",
-           "xp_kv_device_errors", "xp_layer_forward_paged")
+           "xp_kv_device_errors", "xp_layer_forward_paged", "xp_rope", "xp_sampler_create",
+           "xp_sampler_destroy", "xp_sampler_last_error", "xp_sample", "xp_sampler_device_errors")
 LAYER_WEIGHT_NAMES = ("g_attn", "Wq", "Wk", "Wv", "g_q", "g_k", "Wo", "g_mlp", "Wg", "Wu", "Wd")
 STAGES = ("prep", "lmhead", "select", "rspace", "read", "verify")
 
@@ -60,6 +62,12 @@ class _LayerWeights(ctypes.Structure):
 class _KvShape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("n_heads", "n_kv", "head_dim", "page_size",
                                               "n_pages", "dtype")]
+
+
+class _RopeShape(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("axes", ctypes.c_int32),
+                ("sections", ctypes.c_int32 * 4), ("interleaved", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("theta", ctypes.c_float), ("eps", ctypes.c_float)]
 
 
 _lib = None
@@ -132,6 +140,19 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     L.xp_layer_forward_paged.argtypes = [vp, vp, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp,
                                          i64, vp, vp, vp, vp]
     L.xp_layer_forward_paged.restype = i32
+    L.xp_rope.argtypes = [ctypes.POINTER(_RopeShape), i32, vp, i64, vp, i64, i32, vp, vp, i64, vp,
+                          i64, i32, vp, vp, i64, vp]
+    L.xp_rope.restype = i32
+    L.xp_sampler_create.argtypes = [i32, i32, ctypes.POINTER(vp)]
+    L.xp_sampler_create.restype = i32
+    L.xp_sampler_destroy.argtypes = [vp]
+    L.xp_sampler_destroy.restype = None
+    L.xp_sampler_last_error.argtypes = [vp]
+    L.xp_sampler_last_error.restype = ctypes.c_char_p
+    L.xp_sample.argtypes = [vp, i32, i32, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+    L.xp_sample.restype = i32
+    L.xp_sampler_device_errors.argtypes = [vp, ctypes.POINTER(u32), vp]
+    L.xp_sampler_device_errors.restype = i32
     L.xp_kv_device_errors.argtypes = [vp, ctypes.POINTER(u32), vp]
     L.xp_kv_device_errors.restype = i32
     _lib = L
@@ -348,6 +369,71 @@ def toeplitz_mixer(kappa, out=None, stream=None):
     _check(L.xp_toeplitz_mixer(_ptr(kappa), r, B, dt, _ptr(out), _stream(stream)),
            "xp_toeplitz_mixer")
     return out
+
+
+def rope(q, pos, sections, theta, k=None, g_q=None, g_k=None, eps=1e-6, rot_dim=None,
+         interleaved=False, q_out=None, k_out=None, stream=None):
+    """Queries and keys [tokens][heads][head_dim] (bf16 or float32, heads contiguous),
+    normed per head where a gain [head_dim] is given, and rotated by the positions pos
+    [axes][tokens] int32 (xp_rope): sections[a] pairs on axis a, rot_dim twice their sum.
+    Results go to q_out and k_out (allocated when None; q and k themselves are fine).
+    Returns (q_out, k_out)."""
+    import torch
+    L = load_library()
+    hd, dev, dt = q.shape[-1], q.device, q.dtype
+    code = {torch.float32: XP_F32, torch.bfloat16: XP_BF16}.get(dt)
+    if code is None or q.dim() != 3 or not q.is_cuda:
+        raise ValueError("q: expected a bf16 or float32 device tensor [tokens][heads][head_dim]")
+    tokens = q.shape[0]
+    sections = [int(x) for x in sections]
+    if not 1 <= len(sections) <= 4 or min(sections) < 0:
+        raise ValueError("sections: pairs of 1 to 4 axes")
+    if rot_dim is not None and rot_dim != 2 * sum(sections):
+        raise ValueError(f"rot_dim={rot_dim} is not twice the sum of sections={sections}")
+    if (pos.dtype != torch.int32 or pos.device != dev or pos.dim() != 2
+            or tuple(pos.shape) != (len(sections), tokens)
+            or (tokens > 1 and pos.stride(1) != 1)
+            or (len(sections) > 1 and pos.stride(0) < tokens)):
+        raise ValueError(f"pos: expected int32 [{len(sections)}][{tokens}] with contiguous rows "
+                         f"on {dev}")
+
+    def rows(name, t, like):
+        if (t.dtype != dt or t.device != dev or t.dim() != 3 or t.shape[0] != tokens
+                or t.shape[2] != hd or (like is not None and t.shape != like.shape)):
+            raise ValueError(f"{name}: expected {dt} [{tokens}][heads][{hd}] rows on {dev}")
+        heads = t.shape[1]
+        if t.is_contiguous():
+            return t.data_ptr(), heads * hd
+        if t.stride(2) != 1 or (heads > 1 and t.stride(1) != hd):
+            raise ValueError(f"{name}: expected contiguous [{heads}][{hd}] rows")
+        return t.data_ptr(), t.stride(0) if tokens > 1 else heads * hd
+
+    args, out = [], []
+    for name, x, g, y in (("q", q, g_q, q_out), ("k", k, g_k, k_out)):
+        if x is None:
+            if g is not None or y is not None:
+                raise ValueError(f"g_{name}, {name}_out need {name}")
+            args += [None, 0, 0, None, None, 0]
+            out.append(None)
+            continue
+        if g is not None and (g.dtype != dt or g.device != dev or tuple(g.shape) != (hd,)
+                              or not g.is_contiguous()):
+            raise ValueError(f"g_{name}: expected a contiguous {dt} [{hd}] tensor on {dev}")
+        if y is None:
+            y = _empty_on(stream, x.shape, dt, dev)
+        args += [*rows(name, x, None), x.shape[1], _ptr(g), *rows(name + "_out", y, x)]
+        out.append(y)
+    s = _RopeShape(head_dim=hd, rot_dim=2 * sum(sections), axes=len(sections),
+                   sections=(ctypes.c_int32 * 4)(*sections), interleaved=1 if interleaved else 0,
+                   dtype=code, theta=theta, eps=eps)
+    if tokens == 0:
+        return tuple(out)
+    with torch.cuda.device(dev):
+        _check(L.xp_rope(ctypes.byref(s), tokens, pos.data_ptr(),
+                         pos.stride(0) if len(sections) > 1 else tokens, *args, _stream(stream)),
+               f"xp_rope: head_dim={hd} (64, 128, 256), sections={sections} (their sum a multiple of "
+               f"8 up to {hd // 2}), theta={theta}, eps={eps}, 16-byte aligned rows")
+    return tuple(out)
 
 
 def layer_weights_struct(weights: Dict[str, object], H: int, n_heads: int, n_kv: int, ffn: int,
@@ -672,6 +758,82 @@ class PagedKV:
     def close(self):
         if getattr(self, "_h", None):
             self._L.xp_kv_destroy(self._h)
+            self._h = None
+
+    def __del__(self):  # pragma: no cover
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class Sampler:
+    """Tokens from logits (xp_sample): greedy, or sampled at a temperature with top-k,
+    top-p and min-p from given uniforms, for calls of up to max_rows rows of V logits."""
+
+    def __init__(self, V: int, max_rows: int, device="cuda"):
+        import torch
+        L = load_library()
+        self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.V, self.max_rows, self._index = V, max_rows, self.device.index
+        h = ctypes.c_void_p(0)
+        with torch.cuda.device(self.device):
+            s = L.xp_sampler_create(V, max_rows, ctypes.byref(h))
+        if s != XP_OK:
+            raise XpError(s, "xp_sampler_create: " + L.xp_sampler_last_error(None).decode())
+        self._h, self._L, self._torch = h, L, torch
+
+    def _check(self, name, s):
+        if s != XP_OK:
+            raise XpError(s, f"{name}: " + self._L.xp_sampler_last_error(self._h).decode())
+
+    def sample(self, logits, temp=None, temperature=None, top_k=None, top_p=None, min_p=None,
+               u=None, out=None, logprob=None, stream=None):
+        """The token of every row of logits [rows][V] (float32 or bf16, rows contiguous):
+        int32 `out` (allocated when None), which is returned; their log probabilities to
+        `logprob` (float32) where given.  temp (uint8): 0 = greedy; None = all greedy."""
+        torch = self._torch
+        code = {torch.float32: XP_F32, torch.bfloat16: XP_BF16}.get(logits.dtype)
+        n = logits.shape[0]
+        if (code is None or logits.dim() != 2 or logits.shape[1] != self.V
+                or logits.get_device() != self._index or (self.V > 1 and logits.stride(1) != 1)):
+            raise ValueError(f"logits: expected float32 or bf16 [rows][{self.V}], rows contiguous, "
+                             f"on {self.device}")
+        if out is None:
+            out = _empty_on(stream, (n,), torch.int32, self.device)
+        ptr = []
+        for name, t, dt in (("temp", temp, torch.uint8), ("temperature", temperature, torch.float32),
+                            ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32),
+                            ("min_p", min_p, torch.float32), ("u", u, torch.float32),
+                            ("out", out, torch.int32), ("logprob", logprob, torch.float32)):
+            if t is None:
+                ptr.append(None)
+                continue
+            if (t.dtype != dt or tuple(t.shape) != (n,) or not t.is_contiguous()
+                    or t.get_device() != self._index):
+                raise ValueError(f"{name}: expected a contiguous {dt} tensor of {n} elements on "
+                                 f"{self.device}")
+            ptr.append(t.data_ptr())
+        if n:
+            with torch.cuda.device(self._index):
+                self._check("xp_sample", self._L.xp_sample(
+                    self._h, n, code, logits.data_ptr(), logits.stride(0) if n > 1 else self.V,
+                    *ptr, _stream(stream)))
+        return out
+
+    def device_errors(self, stream=None) -> int:
+        """The XP_DEVERR_* bits set since the last read; synchronizes."""
+        v = ctypes.c_uint32(0)
+        with self._torch.cuda.device(self._index):
+            self._check("xp_sampler_device_errors", self._L.xp_sampler_device_errors(
+                self._h, ctypes.byref(v), _stream(stream)))
+        return int(v.value)
+
+    def close(self):
+        if getattr(self, "_h", None):
+            self._L.xp_sampler_destroy(self._h)
             self._h = None
 
     def __del__(self):  # pragma: no cover
