@@ -659,7 +659,7 @@ const char* xp_sampler_last_error(const xp_sampler* s);
  *          stay; 0 .. 1, 0: all (others set XP_DEVERR_FILTER and mean none)
  *   u      [rows] float in [0, 1), iff temp != NULL: a sampled row takes the first token
  *          in index order at which the sum of the kept weights exceeds u times their
- *          sum, the last one with a weight if none does
+ *          sum, the last one with a weight if none does (u below 0 counts as 0)
  *   out_ids [rows] int32; out_logprob [rows] float or NULL: the log of the token's
  *          probability among the kept ones, 0 for greedy rows
  * Logits of -inf (masked tokens) and NaN are never taken; a row that holds nothing else

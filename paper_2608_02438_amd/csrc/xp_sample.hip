@@ -13,6 +13,7 @@
 #include <stdarg.h>
 #include <stdio.h>
 
+#include <algorithm>
 #include <new>
 #include <string>
 
@@ -21,11 +22,32 @@
 namespace xp {
 
 constexpr int kSmpMaxV = 1 << 18;
-constexpr int kSmpThreads = 1024;
-constexpr int kSmpWaves = kSmpThreads / kWave;
-constexpr int kSmpSeg = kSmpThreads * 4;           // tokens of a segment, 4 a thread
-constexpr int kSmpSegs = kSmpMaxV / kSmpSeg;
-constexpr int kSmpBins = 2048;
+constexpr int kSmpChunk = 4096;                    // tokens of a chunk
+constexpr int kSmpChunks = kSmpMaxV / kSmpChunk;
+constexpr int kSmpBatch = 512;                     // rows that go through the launches together
+// passes over the vocabulary: a workgroup has some chunks of a row, a thread 16 tokens of each
+constexpr int kSmpThreads = 256;
+constexpr int kSmpPer = kSmpChunk / kSmpThreads;
+constexpr int kSmpHist = 512;                      // bins of 1 / 16 in (m - l) / T
+constexpr int kSmpCap = 16384;                     // candidates of a row
+// the last launch: a workgroup a row
+constexpr int kRowThreads = 1024;
+constexpr int kRowWaves = kRowThreads / kWave;
+constexpr int kRowBins = 2048;
+static_assert(kSmpChunk == 4 * kRowThreads, "a thread of the row has 4 tokens of a chunk");
+
+// What a row's launches leave for each other.
+struct SmpRec {
+  int32_t mode, edge;                // SmpMode; the last bin that counts
+  uint32_t n, above;                 // candidates; tokens of the bins before the edge
+  uint64_t mass_above, mass;         // the weight of those, of all tokens
+};
+enum SmpMode {
+  kSmpPlain = 0,                     // no threshold of l: the chunks' sums are final
+  kSmpList = 1,                      // the candidates are all tokens that can stay
+  kSmpEdge = 2,                      // tokens before the edge's bin stay, those of it are candidates
+  kSmpSlow = 3                       // too many candidates: the row by radix selection
+};
 
 struct Smp {
   const void* logits;
@@ -37,6 +59,15 @@ struct Smp {
   int32_t* ids;
   float* logprob;
   uint32_t* err;
+  // of the batch's rows
+  int64_t row0;
+  int chunks, per_wg;                // of a row, of a workgroup
+  uint64_t* best;                    // [rows][kSmpChunks] the largest key, lowest index
+  uint64_t* sums;                    // [rows][kSmpChunks] kept weights
+  uint64_t* mass;                    // [rows][kSmpHist]
+  uint32_t* count;                   // [rows][kSmpHist]
+  SmpRec* rec;                       // [rows]
+  uint64_t* list;                    // [rows][kSmpCap] key, index
 };
 
 // order-preserving image of a logit; 0 for NaN and -inf, which no one draws
@@ -56,16 +87,80 @@ struct SmpRow {
   __device__ __forceinline__ double x(uint32_t key) const {
     return key == top_key ? 0.0 : ((double)smp_value(key) - top) * inv_t;
   }
-  __device__ __forceinline__ uint64_t weight(uint32_t key) const {
-    if (key == 0u) return 0u;
-    const double y = x(key);
-    return y > -32.0 ? (uint64_t)rint(exp(y) * 0x1p45) : 0u;
+  // e^x 2^45 to the nearest integer: 2^k e^f with |f| <= ln 2 / 2, e^f by its series up
+  // to f^11 (2^-47 off), the integer from the sum with 2^52
+  __device__ __forceinline__ uint64_t weight_at(double y) const {
+    const double k = rint(y * 1.4426950408889634);
+    const double f = fma(-k, 0.69314718055994531, y);
+    double e = 1.0 / 39916800;
+    e = fma(e, f, 1.0 / 3628800);
+    e = fma(e, f, 1.0 / 362880);
+    e = fma(e, f, 1.0 / 40320);
+    e = fma(e, f, 1.0 / 5040);
+    e = fma(e, f, 1.0 / 720);
+    e = fma(e, f, 1.0 / 120);
+    e = fma(e, f, 1.0 / 24);
+    e = fma(e, f, 1.0 / 6);
+    e = fma(e, f, 0.5);
+    e = fma(e, f, 1.0);
+    e = fma(e, f, 1.0);
+    const int up = (int)k + 45;
+    const double v = __hiloint2double(__double2hiint(e) + (up << 20), __double2loint(e));
+    const uint64_t w = (uint64_t)__double_as_longlong(v + 0x1p52) & 0xfffffffffffffull;
+    return y > -32.0 ? w : 0u;
   }
+  __device__ __forceinline__ uint64_t weight(uint32_t key) const {
+    return key != 0u ? weight_at(x(key)) : 0u;
+  }
+  // bins of l from the largest down; kSmpHist and more have no weight
+  __device__ __forceinline__ int bin_at(double y) const {
+    const double b = y * -16.0;
+    return b < (double)kSmpHist ? (int)b : kSmpHist;
+  }
+};
+
+// What the sum of the kept weights is to exceed: u Z, not below 0 (else it would before
+// the first token); NaN is never exceeded.
+__device__ __forceinline__ double smp_goal(const Smp& d, int64_t r, uint64_t Z) {
+  const float u = d.u[r];
+  return u < 0.f ? 0.0 : (double)u * (double)Z;
+}
+
+// A sampled row's settings, replaced where they are out of range.
+struct SmpSet {
+  float t, p, mp;
+  int k;
+  uint32_t bad;
+  __device__ __forceinline__ SmpSet(const Smp& d, int64_t r) {
+    bad = 0;
+    t = d.temperature ? d.temperature[r] : 1.f;
+    if (!(t > 0.f && t < INFINITY)) {
+      bad |= XP_DEVERR_TEMPERATURE;
+      t = 1.f;
+    }
+    k = d.top_k ? d.top_k[r] : 0;
+    p = d.top_p ? d.top_p[r] : 1.f;
+    mp = d.min_p ? d.min_p[r] : 0.f;
+    if (k < 0 || !(p > 0.f) || !(mp >= 0.f && mp <= 1.f)) {
+      bad |= XP_DEVERR_FILTER;
+      k = max(k, 0);
+      p = p > 0.f ? p : 1.f;
+      mp = mp >= 0.f && mp <= 1.f ? mp : 0.f;
+    }
+    k = k < d.V ? k : 0;
+  }
+  __device__ __forceinline__ bool cuts() const { return k > 0 || p < 1.f; }
+  __device__ __forceinline__ double log_min() const { return mp > 0.f ? log((double)mp) : -INFINITY; }
 };
 
 __device__ __forceinline__ uint64_t wave_sum_u64(uint64_t v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += shfl_xor_u64(v, o);
+  return v;
+}
+__device__ __forceinline__ uint64_t wave_max_u64(uint64_t v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = umax64(v, shfl_xor_u64(v, o));
   return v;
 }
 // sums of this and lower lanes
@@ -103,78 +198,497 @@ __device__ __forceinline__ void smp_load(const Smp& d, const T* row, bool wide, 
   for (int q = 0; q < 4; ++q) key[q] = smp_key(l[q]);
 }
 
-struct SmpShared {
-  uint64_t mass[kSmpBins];
-  uint32_t count[kSmpBins];
-  uint64_t part[kSmpSegs * kSmpWaves];
-  uint64_t red[kSmpWaves + 1];
+// the row's token and its log probability, Z the sum of the kept weights
+template <typename T>
+__device__ __forceinline__ void smp_out(const Smp& d, int64_t r, const T* row, const SmpRow& w, int id,
+                                        uint64_t Z) {
+  id = min(max(id, 0), d.V - 1);                   // an index of the row, whatever was found
+  d.ids[r] = id;
+  if (d.logprob)
+    d.logprob[r] = (float)(w.x(smp_key(to_f32<T>(row[id]))) -
+                           (log((double)Z) - 45.0 * 0.69314718055994531));
+}
+
+// ---------------------------------------------------------------------------
+// The passes over the vocabulary.
+// ---------------------------------------------------------------------------
+struct SmpPlace {
+  int64_t r, row;                    // the row in the batch, in the call
+  int c0, c1;                        // its chunks
+};
+__device__ __forceinline__ SmpPlace smp_place(const Smp& d) {
+  const int groups = (d.chunks + d.per_wg - 1) / d.per_wg;
+  const int64_t r = blockIdx.x / groups;
+  const int g = (int)(blockIdx.x - r * groups);
+  return SmpPlace{r, d.row0 + r, g * d.per_wg, min((g + 1) * d.per_wg, d.chunks)};
+}
+// index of token q of the thread's i-th four in a chunk
+__device__ __forceinline__ int smp_index(int chunk, int i) {
+  return chunk * kSmpChunk + i * 4 * kSmpThreads + 4 * (int)threadIdx.x;
+}
+template <typename T>
+__device__ __forceinline__ void smp_chunk(const Smp& d, const T* row, bool wide, int chunk,
+                                          uint32_t (&key)[kSmpPer]) {
+#pragma unroll
+  for (int i = 0; i < kSmpPer / 4; ++i) {
+    uint32_t x[4];
+    smp_load(d, row, wide, smp_index(chunk, i), x);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) key[4 * i + q] = x[q];
+  }
+}
+// the row's largest key and its lowest index, from the chunks' (every wave for itself)
+__device__ __forceinline__ uint64_t smp_best(const Smp& d, int64_t r) {
+  const int lane = threadIdx.x & 63;
+  return wave_max_u64(lane < d.chunks ? d.best[r * kSmpChunks + lane] : 0u);
+}
+
+// The largest logit of every chunk; clears the row's histogram for the next launch.
+template <typename T>
+__global__ __launch_bounds__(kSmpThreads) void k_smp_max(const Smp d) {
+  __shared__ uint64_t red[kSmpThreads / kWave];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const SmpPlace at = smp_place(d);
+  const T* row = static_cast<const T*>(d.logits) + at.row * d.ld;
+  const bool wide = reinterpret_cast<uintptr_t>(row) % (4 * sizeof(T)) == 0;
+  if (at.c0 == 0 && d.temp != nullptr) {
+    for (int b = tid; b < kSmpHist; b += kSmpThreads) {
+      d.mass[at.r * kSmpHist + b] = 0;
+      d.count[at.r * kSmpHist + b] = 0;
+    }
+    if (tid == 0) d.rec[at.r] = SmpRec{};
+  }
+  for (int c = at.c0; c < at.c1; ++c) {
+    uint32_t key[kSmpPer];
+    smp_chunk(d, row, wide, c, key);
+    uint32_t top = 0;
+    int idx = 0;
+#pragma unroll
+    for (int i = 0; i < kSmpPer; ++i) {            // indices ascend
+      const bool more = key[i] > top;
+      top = more ? key[i] : top;
+      idx = more ? smp_index(c, i / 4) + i % 4 : idx;
+    }
+    const uint64_t best = wave_max_u64(((uint64_t)top << 32) | (uint32_t)~idx);
+    if (lane == 0) red[wave] = best;
+    __syncthreads();
+    if (tid == 0) {
+      uint64_t x = red[0];
+      for (int w = 1; w < kSmpThreads / kWave; ++w) x = umax64(x, red[w]);
+      d.best[at.r * kSmpChunks + c] = x;
+    }
+    __syncthreads();
+  }
+}
+
+// The weights: every chunk's sum where no threshold of l is to be found, else the row's
+// histogram of tokens and weights.
+template <typename T>
+__global__ __launch_bounds__(kSmpThreads) void k_smp_mass(const Smp d) {
+  __shared__ uint64_t mass[kSmpHist];
+  __shared__ uint32_t count[kSmpHist];
+  __shared__ uint64_t red[kSmpThreads / kWave];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const SmpPlace at = smp_place(d);
+  if (d.temp[at.row] == 0) return;
+  const T* row = static_cast<const T*>(d.logits) + at.row * d.ld;
+  const bool wide = reinterpret_cast<uintptr_t>(row) % (4 * sizeof(T)) == 0;
+  const SmpSet set(d, at.row);
+  const uint32_t top_key = (uint32_t)(smp_best(d, at.r) >> 32);
+  if (top_key == 0u) return;
+  const SmpRow w{1.0 / (double)set.t, (double)smp_value(top_key), top_key};
+  const double log_mp = set.log_min();
+  const bool cuts = set.cuts();
+  if (cuts) {
+    for (int b = tid; b < kSmpHist; b += kSmpThreads) {
+      mass[b] = 0;
+      count[b] = 0;
+    }
+    __syncthreads();
+  }
+  for (int c = at.c0; c < at.c1; ++c) {
+    uint32_t key[kSmpPer];
+    smp_chunk(d, row, wide, c, key);
+    uint64_t sum = 0;
+#pragma unroll
+    for (int i = 0; i < kSmpPer; ++i) {
+      const double y = w.x(key[i]);
+      const uint64_t e = key[i] != 0u ? w.weight_at(y) : 0u;
+      if (cuts) {
+        const int b = w.bin_at(y);
+        if (key[i] != 0u && b < kSmpHist) {
+          atomicAdd((unsigned long long*)&mass[b], (unsigned long long)e);
+          atomicAdd(&count[b], 1u);
+        }
+      } else {
+        sum += y >= log_mp ? e : 0u;
+      }
+    }
+    if (!cuts) {
+      sum = wave_sum_u64(sum);
+      if (lane == 0) red[wave] = sum;
+      __syncthreads();
+      if (tid == 0) {
+        for (int x = 1; x < kSmpThreads / kWave; ++x) sum += red[x];
+        d.sums[at.r * kSmpChunks + c] = sum;
+      }
+      __syncthreads();
+    }
+  }
+  if (cuts) {
+    __syncthreads();
+    for (int b = tid; b < kSmpHist; b += kSmpThreads)
+      if (count[b] != 0u) {
+        atomicAdd((unsigned long long*)&d.mass[at.r * kSmpHist + b], (unsigned long long)mass[b]);
+        atomicAdd(&d.count[at.r * kSmpHist + b], count[b]);
+      }
+  }
+}
+
+// What the histogram says: the bin in which the threshold lies.
+__device__ __forceinline__ SmpRec smp_decide(const Smp& d, int64_t r, const SmpSet& set) {
+  constexpr int N = kSmpHist / kWave;
+  const int lane = threadIdx.x & 63;
+  uint64_t m[N], mt = 0;
+  uint32_t n[N];
+  uint64_t nt = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    m[i] = d.mass[r * kSmpHist + N * lane + i];
+    n[i] = d.count[r * kSmpHist + N * lane + i];
+    mt += m[i];
+    nt += n[i];
+  }
+  uint64_t mb = wave_scan_u64(mt, lane), nb = wave_scan_u64(nt, lane);
+  const uint64_t mass = ((uint64_t)(uint32_t)__shfl((int)(mb >> 32), 63, kWave) << 32) |
+                        (uint32_t)__shfl((int)mb, 63, kWave);
+  const uint32_t all = (uint32_t)__shfl((int)nb, 63, kWave);
+  mb -= mt;
+  nb -= nt;
+  const bool by_k = set.k > 0 && all >= (uint32_t)set.k;   // fewer: all tokens with a weight stay
+  const double want = (double)set.p * (double)mass;
+  SmpRec x{};
+  x.mass = mass;
+  bool mine = false;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const bool hit = by_k ? nb < (uint32_t)set.k && nb + n[i] >= (uint32_t)set.k
+                          : set.p < 1.f && (double)mb < want && (double)(mb + m[i]) >= want;
+    if (hit && !mine) {
+      mine = true;
+      x.edge = N * lane + i;
+      x.above = (uint32_t)nb;
+      x.mass_above = mb;
+      const bool list = nb + n[i] <= (uint64_t)kSmpCap;
+      const bool edge = n[i] <= (uint32_t)kSmpCap && !(by_k && set.p < 1.f);
+      x.mode = list ? kSmpList : (edge ? kSmpEdge : kSmpSlow);
+    }
+    mb += m[i];
+    nb += n[i];
+  }
+  const uint64_t who = __ballot(mine);
+  if (who == 0) {                                  // nothing is cut: every token of the bins stays
+    x.mode = kSmpEdge;
+    x.edge = kSmpHist;
+    return x;
+  }
+  const int src = __builtin_ctzll(who);
+  x.mode = __shfl(x.mode, src, kWave);
+  x.edge = __shfl(x.edge, src, kWave);
+  x.above = (uint32_t)__shfl((int)x.above, src, kWave);
+  x.mass_above = ((uint64_t)(uint32_t)__shfl((int)(x.mass_above >> 32), src, kWave) << 32) |
+                 (uint32_t)__shfl((int)x.mass_above, src, kWave);
+  return x;
+}
+
+// Rows with a threshold of l: the candidates, and the sums of what stays before them.
+template <typename T>
+__global__ __launch_bounds__(kSmpThreads) void k_smp_list(const Smp d) {
+  __shared__ uint64_t red[kSmpThreads / kWave];
+  __shared__ uint32_t num[kSmpThreads / kWave], base;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const SmpPlace at = smp_place(d);
+  if (d.temp[at.row] == 0) return;
+  const SmpSet set(d, at.row);
+  if (!set.cuts()) return;
+  const uint32_t top_key = (uint32_t)(smp_best(d, at.r) >> 32);
+  if (top_key == 0u) return;
+  const SmpRec rec = smp_decide(d, at.r, set);     // every wave the same
+  if (at.c0 == 0 && tid == 0) {
+    SmpRec* to = d.rec + at.r;                     // rec.n counts meanwhile
+    to->mode = rec.mode;
+    to->edge = rec.edge;
+    to->above = rec.above;
+    to->mass_above = rec.mass_above;
+    to->mass = rec.mass;
+  }
+  if (rec.mode == kSmpSlow) return;
+  const T* row = static_cast<const T*>(d.logits) + at.row * d.ld;
+  const bool wide = reinterpret_cast<uintptr_t>(row) % (4 * sizeof(T)) == 0;
+  const SmpRow w{1.0 / (double)set.t, (double)smp_value(top_key), top_key};
+  const double log_mp = set.log_min();
+  for (int c = at.c0; c < at.c1; ++c) {
+    uint32_t key[kSmpPer];
+    smp_chunk(d, row, wide, c, key);
+    uint64_t sum = 0;
+    uint32_t pick = 0;                             // a bit a candidate
+#pragma unroll
+    for (int i = 0; i < kSmpPer; ++i) {
+      const double y = w.x(key[i]);
+      const int b = key[i] != 0u ? w.bin_at(y) : kSmpHist;
+      const bool cand = rec.mode == kSmpList ? b <= rec.edge : b == rec.edge;
+      pick |= cand && b < kSmpHist ? 1u << i : 0u;
+      if (rec.mode == kSmpEdge && b < rec.edge && y >= log_mp) sum += w.weight_at(y);
+    }
+    const uint32_t n = __popc(pick);
+    uint32_t upto = n;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+      const uint32_t x = __shfl_up(upto, o, kWave);
+      upto += lane >= o ? x : 0u;
+    }
+    sum = wave_sum_u64(sum);
+    if (lane == 63) num[wave] = upto;
+    if (lane == 0) red[wave] = sum;
+    __syncthreads();
+    if (tid == 0) {
+      uint32_t all = 0;
+      for (int x = 0; x < kSmpThreads / kWave; ++x) all += num[x];
+      base = all != 0u ? atomicAdd(&d.rec[at.r].n, all) : 0u;
+      for (int x = 1; x < kSmpThreads / kWave; ++x) sum += red[x];
+      d.sums[at.r * kSmpChunks + c] = sum;
+    }
+    __syncthreads();
+    uint32_t to = base + upto - n;
+    for (int x = 0; x < wave; ++x) to += num[x];
+#pragma unroll
+    for (int i = 0; i < kSmpPer; ++i)
+      if (((pick >> i) & 1u) && to < (uint32_t)kSmpCap)
+        d.list[at.r * kSmpCap + to++] =
+            ((uint64_t)key[i] << 32) | (uint32_t)(smp_index(c, i / 4) + i % 4);
+    __syncthreads();
+  }
+}
+
+// ---------------------------------------------------------------------------
+// The last launch: thresholds and the draw, a workgroup a row.
+// ---------------------------------------------------------------------------
+struct RowShared {
+  uint64_t bins[kRowBins];
+  uint64_t part[kSmpChunks * kRowWaves];
+  uint64_t red[kRowWaves];
   uint64_t out[4];
 };
 
-// What a radix round finds, counted from the largest key down: the bin in which
-// `before + bin` reaches the target, and what lies before it.
-struct SmpBin {
-  int bin;
-  uint64_t before;
-};
-// the first bin from the top at which the sum passes: reach(before, upto)
-template <typename F>
-__device__ __forceinline__ SmpBin smp_find(SmpShared& s, const uint64_t* val64, const uint32_t* val32,
-                                           F reach) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int b0 = kSmpBins - 1 - 2 * tid, b1 = b0 - 1;
-  const uint64_t v0 = val64 ? val64[b0] : val32[b0], v1 = val64 ? val64[b1] : val32[b1];
-  const uint64_t inc = wave_scan_u64(v0 + v1, lane);
-  if (lane == 63) s.red[wave] = inc;
-  if (tid == 0) {
-    s.out[0] = ~0ull;
-    s.out[1] = 0;
-  }
+__device__ __forceinline__ uint64_t row_sum(RowShared& s, uint64_t v) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  v = wave_sum_u64(v);
+  __syncthreads();                                 // the last sum's reads
+  if (lane == 0) s.red[wave] = v;
   __syncthreads();
-  uint64_t before = inc - v0 - v1;
-  for (int w = 0; w < wave; ++w) before += s.red[w];
-  const bool at0 = v0 > 0 && !reach(before) && reach(before + v0);
-  const bool at1 = v1 > 0 && !reach(before + v0) && reach(before + v0 + v1);
-  if (at0) {
-    s.out[0] = b0;
-    s.out[1] = before;
-  } else if (at1) {
-    s.out[0] = b1;
-    s.out[1] = before + v0;
-  }
-  __syncthreads();
-  const SmpBin r{(int)s.out[0], s.out[1]};
-  __syncthreads();
-  return r;
+  v = 0;
+#pragma unroll
+  for (int w = 0; w < kRowWaves; ++w) v += s.red[w];
+  return v;
 }
 
-// A row by one workgroup.  Thresholds by radix selection on the keys, 11 bits a round.
-template <typename T>
-__global__ __launch_bounds__(kSmpThreads) void k_sample_row(const Smp d) {
-  __shared__ SmpShared s;
+// The first of the bins, from the top one down, at which the sum passes.
+template <typename F>
+__device__ __forceinline__ int row_find(RowShared& s, F reach, uint64_t& before) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t r = blockIdx.x;
-  const T* row = static_cast<const T*>(d.logits) + r * d.ld;
-  const bool wide = reinterpret_cast<uintptr_t>(row) % (4 * sizeof(T)) == 0;
-  const int segs = (d.V + kSmpSeg - 1) / kSmpSeg;
-  // ---- the largest logit, lowest index first ----
-  uint64_t best = 0;
-  for (int g = 0; g < segs; ++g) {
-    const int i0 = g * kSmpSeg + 4 * tid;
-    uint32_t key[4];
-    smp_load(d, row, wide, i0, key);
+  const int b0 = kRowBins - 1 - 2 * tid, b1 = b0 - 1;
+  const uint64_t v0 = s.bins[b0], v1 = s.bins[b1];
+  const uint64_t inc = wave_scan_u64(v0 + v1, lane);
+  if (lane == 63) s.red[wave] = inc;
+  if (tid == 0) s.out[0] = ~0ull;
+  __syncthreads();
+  uint64_t x = inc - v0 - v1;
+  for (int w = 0; w < wave; ++w) x += s.red[w];
+  if (v0 > 0 && !reach(x) && reach(x + v0)) {
+    s.out[0] = b0;
+    s.out[1] = x;
+  } else if (v1 > 0 && !reach(x + v0) && reach(x + v0 + v1)) {
+    s.out[0] = b1;
+    s.out[1] = x + v0;
+  }
+  __syncthreads();
+  const int bin = (int)s.out[0];
+  before = s.out[1];
+  return bin;
+}
+
+// Radix selection among 32-bit keys >= lo, 11 bits a round: the key at which the sum of
+// values, from the largest key down, passes; what lies before it, and at it alone.  0
+// where it never does.  each(f) calls f(key, value) for the thread's elements.
+template <typename E, typename F>
+__device__ __forceinline__ uint32_t row_select(RowShared& s, int bits, E each, F reach,
+                                               uint64_t& before, uint64_t& at) {
+  uint32_t prefix = 0, mask = 0;
+  before = 0;
+  at = 0;
+  for (int shift = bits > 11 ? bits - 11 : 0;; shift = shift > 11 ? shift - 11 : 0) {
+    // the round's bits: those below the ones that are known
+    const uint32_t field = ~mask & ((bits < 32 ? 1u << bits : 0u) - 1u) & ~((1u << shift) - 1u);
+    __syncthreads();
+    for (int b = threadIdx.x; b < kRowBins; b += kRowThreads) s.bins[b] = 0;
+    __syncthreads();
+    each([&](uint32_t key, uint64_t v) {
+      if ((key & mask) == prefix && v != 0u)
+        atomicAdd((unsigned long long*)&s.bins[(key & field) >> shift], (unsigned long long)v);
+    });
+    __syncthreads();
+    uint64_t in;
+    const uint64_t base = before;
+    const int bin = row_find(s, [&](uint64_t x) { return reach(base + x); }, in);
+    if (bin < 0) return 0u;                        // whole workgroup
+    before = base + in;
+    at = s.bins[bin];
+    prefix |= (uint32_t)bin << shift;
+    mask |= field;
+    if (shift == 0) return prefix;
+  }
+}
+
+// How many of n equal weights stay where the sum reaches `want` among them: those before
+// which less lies.
+__device__ __forceinline__ uint64_t row_ties(double want, uint64_t before, uint64_t each, uint64_t n) {
+  uint64_t c = (uint64_t)fmax((want - (double)before) / (double)each, 0.0);
+  c = c < n ? c : n;
+  while (c > 0 && (double)(before + (c - 1) * each) >= want) --c;
+  while (c < n && (double)(before + c * each) < want) ++c;
+  return c;
+}
+
+constexpr uint32_t kIndexTop = kSmpMaxV - 1;        // indices in falling order: kIndexTop - i
+
+// The draw from the chunks' sums: the chunk in which they pass u times their sum, and
+// the token within it; kept(key, index) is a token's weight.  The last token with a
+// weight where none passes.
+template <typename T, typename K>
+__device__ __forceinline__ void row_draw(const Smp& d, RowShared& s, int64_t r, const T* row, bool wide,
+                                         const SmpRow& w, const uint64_t* sums, K kept) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const uint64_t mine = lane < d.chunks ? sums[lane] : 0u;
+  const uint64_t upto = wave_scan_u64(mine, lane);
+  const uint64_t Z = ((uint64_t)(uint32_t)__shfl((int)(upto >> 32), 63, kWave) << 32) |
+                     (uint32_t)__shfl((int)upto, 63, kWave);
+  const double goal = smp_goal(d, r, Z);
+  auto over = [&](uint64_t x) { return (double)x > goal; };
+  const uint64_t hit = __ballot(mine > 0 && over(upto)), some = __ballot(mine > 0);
+  const bool none = hit == 0;                      // u is no number below 1
+  const int c = none ? 63 - __builtin_clzll(some | 1u) : __builtin_ctzll(hit);
+  const uint64_t b = upto - mine;
+  const uint64_t before = ((uint64_t)(uint32_t)__shfl((int)(b >> 32), c, kWave) << 32) |
+                          (uint32_t)__shfl((int)b, c, kWave);
+  const int i0 = c * kSmpChunk + 4 * tid;
+  uint32_t key[4];
+  uint64_t wt[4], n = 0;
+  smp_load(d, row, wide, i0, key);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) best = umax64(best, ((uint64_t)key[q] << 32) | (uint32_t)~(i0 + q));
+  for (int q = 0; q < 4; ++q) n += wt[q] = kept(key[q], i0 + q);
+  const uint64_t inc = wave_scan_u64(n, lane);
+  __syncthreads();
+  if (lane == 63) s.red[wave] = inc;
+  __syncthreads();
+  uint64_t x = before + inc - n;
+  for (int v = 0; v < wave; ++v) x += s.red[v];
+  int pick = -1;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const bool was = over(x);
+    x += wt[q];
+    // the one token at which the sum passes; else the last of this thread's
+    if (wt[q] > 0 && (none || (!was && over(x)))) pick = i0 + q;
   }
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) best = umax64(best, shfl_xor_u64(best, o));
-  if (lane == 0) s.red[wave] = best;
+  for (int o = 32; o > 0; o >>= 1) pick = max(pick, __shfl_xor(pick, o, kWave));
   __syncthreads();
-  for (int w = 0; w < kSmpWaves; ++w) best = umax64(best, s.red[w]);
+  if (lane == 0) s.red[wave] = (uint32_t)pick;
   __syncthreads();
+  if (tid == 0) {
+    for (int v = 0; v < kRowWaves; ++v) pick = max(pick, (int)(uint32_t)s.red[v]);
+    smp_out(d, r, row, w, pick, Z);
+  }
+}
+
+// Rows with more candidates than the list holds (many equal logits, or top-k of tens of
+// thousands with top-p): radix selection over the row itself.
+template <typename T>
+__device__ __forceinline__ void row_slow(const Smp& d, RowShared& s, int64_t r, const T* row, bool wide,
+                                      const SmpRow& w, const SmpSet& set) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  auto walk = [&](auto f) {
+    for (int c = 0; c < d.chunks; ++c) {
+      uint32_t key[4];
+      smp_load(d, row, wide, c * kSmpChunk + 4 * tid, key);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) f(c, c * kSmpChunk + 4 * tid + q, key[q]);
+    }
+  };
+  uint32_t cut = 1u;                               // keys from here on stay
+  uint32_t tie_end = ~0u;                          // of those at the cut, indices before this one
+  uint64_t before, at;
+  if (set.k > 0)
+    cut = max(cut, row_select(s, 32, [&](auto f) {
+            walk([&](int, int, uint32_t key) { f(key, key != 0u ? 1u : 0u); });
+          }, [&](uint64_t x) { return x >= (uint64_t)set.k; }, before, at));
+  if (set.p < 1.f) {
+    uint64_t sum = 0;                              // of what top-k left
+    walk([&](int, int, uint32_t key) { sum += key >= cut ? w.weight(key) : 0u; });
+    sum = row_sum(s, sum);
+    const double want = (double)set.p * (double)sum;
+    const uint32_t key = row_select(s, 32, [&](auto f) {
+      walk([&](int, int, uint32_t key) {
+        if (key >= cut) f(key, w.weight(key));
+      });
+    }, [&](uint64_t x) { return (double)x >= want; }, before, at);
+    if (key != 0u) {
+      cut = key;
+      const uint64_t one = w.weight(key), n = at / one, stay = row_ties(want, before, one, n);
+      if (stay < n)
+        tie_end = kIndexTop + 1 - row_select(s, 18, [&](auto f) {
+          walk([&](int, int i, uint32_t key) {
+            if (key == cut) f(kIndexTop - (uint32_t)i, 1u);
+          });
+        }, [&](uint64_t x) { return x >= stay; }, before, at);
+    }
+  }
+  const double log_mp = set.log_min();
+  auto kept = [&](uint32_t key, int i) -> uint64_t {
+    if (key < cut || (key == cut && (uint32_t)i >= tie_end)) return 0u;
+    return w.x(key) >= log_mp ? w.weight(key) : 0u;
+  };
+  for (int c = 0; c < d.chunks; ++c) {
+    uint32_t key[4];
+    const int i0 = c * kSmpChunk + 4 * tid;
+    smp_load(d, row, wide, i0, key);
+    uint64_t sum = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) sum += kept(key[q], i0 + q);
+    sum = wave_sum_u64(sum);
+    if (lane == 0) s.part[c * kRowWaves + wave] = sum;
+  }
+  __syncthreads();
+  if (wave == 0) {
+    uint64_t sum = 0;
+    if (lane < d.chunks)
+      for (int v = 0; v < kRowWaves; ++v) sum += s.part[lane * kRowWaves + v];
+    s.bins[lane] = sum;
+  }
+  __syncthreads();
+  row_draw(d, s, r, row, wide, w, s.bins, kept);
+}
+
+template <typename T>
+__global__ __launch_bounds__(kRowThreads) void k_smp_row(const Smp d) {
+  __shared__ RowShared s;
+  __shared__ uint64_t cand[kSmpCap];               // key, index; 0: none
+  const int tid = threadIdx.x;
+  const int64_t rb = blockIdx.x, r = d.row0 + rb;
+  const uint64_t best = smp_best(d, rb);
   const uint32_t top_key = (uint32_t)(best >> 32);
   const bool sampled = d.temp != nullptr && d.temp[r] != 0;
-  if (top_key == 0u || !sampled) {
+  if (top_key == 0u || !sampled) {                 // whole workgroup
     if (tid == 0) {
       d.ids[r] = top_key == 0u ? -1 : (int)~(uint32_t)best;
       if (d.logprob) d.logprob[r] = top_key == 0u ? -INFINITY : 0.f;
@@ -182,202 +696,125 @@ __global__ __launch_bounds__(kSmpThreads) void k_sample_row(const Smp d) {
     }
     return;
   }
-  // ---- the row's settings ----
-  uint32_t bad = 0;
-  float t = d.temperature ? d.temperature[r] : 1.f;
-  if (!(t > 0.f && t < INFINITY)) {
-    bad |= XP_DEVERR_TEMPERATURE;
-    t = 1.f;
+  const T* row = static_cast<const T*>(d.logits) + r * d.ld;
+  const bool wide = reinterpret_cast<uintptr_t>(row) % (4 * sizeof(T)) == 0;
+  const SmpSet set(d, r);
+  if (set.bad && tid == 0) atomicOr(d.err, set.bad);
+  const SmpRow w{1.0 / (double)set.t, (double)smp_value(top_key), top_key};
+  const double log_mp = set.log_min();
+  const uint64_t* sums = d.sums + rb * kSmpChunks;
+  auto heavy = [&](uint32_t key) -> uint64_t { return w.x(key) >= log_mp ? w.weight(key) : 0u; };
+  if (!set.cuts()) {
+    row_draw(d, s, r, row, wide, w, sums,
+             [&](uint32_t key, int) -> uint64_t { return key != 0u ? heavy(key) : 0u; });
+    return;
   }
-  int k = d.top_k ? d.top_k[r] : 0;
-  float p = d.top_p ? d.top_p[r] : 1.f, mp = d.min_p ? d.min_p[r] : 0.f;
-  if (k < 0) {
-    bad |= XP_DEVERR_FILTER;
-    k = 0;
+  const SmpRec rec = d.rec[rb];
+  if (rec.mode == kSmpSlow) {
+    row_slow(d, s, r, row, wide, w, set);
+    return;
   }
-  if (!(p > 0.f)) {
-    bad |= XP_DEVERR_FILTER;
-    p = 1.f;
-  }
-  if (!(mp >= 0.f && mp <= 1.f)) {
-    bad |= XP_DEVERR_FILTER;
-    mp = 0.f;
-  }
-  if (bad && tid == 0) atomicOr(d.err, bad);
-  const SmpRow w{1.0 / (double)t, (double)smp_value(top_key), top_key};
-  const double log_mp = mp > 0.f ? log((double)mp) : -INFINITY;
-  // one radix selection; lo: keys below do not count.  Returns the key at which the sum
-  // passes, what lies before it, and the sum at that key alone.
-  auto select = [&](bool by_mass, uint32_t lo, auto reach, uint64_t& before, uint64_t& at) {
-    uint32_t prefix = 0, mask = 0;
-    before = 0;
-    for (int shift = 21; shift >= 0; shift = shift == 21 ? 10 : (shift == 10 ? 0 : -1)) {
-      const uint32_t field = shift == 0 ? 1023u : 2047u;
-      for (int b = tid; b < kSmpBins; b += kSmpThreads) {
-        s.mass[b] = 0;
-        s.count[b] = 0;
-      }
-      __syncthreads();
-      for (int g = 0; g < segs; ++g) {
-        uint32_t key[4];
-        smp_load(d, row, wide, g * kSmpSeg + 4 * tid, key);
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          if (key[q] != 0u && key[q] >= lo && (key[q] & mask) == prefix) {
-            const uint32_t b = (key[q] >> shift) & field;
-            if (by_mass) atomicAdd((unsigned long long*)&s.mass[b], (unsigned long long)w.weight(key[q]));
-            else atomicAdd(&s.count[b], 1u);
-          }
-      }
-      __syncthreads();
-      const uint64_t base = before;
-      const SmpBin f = smp_find(s, by_mass ? s.mass : nullptr, s.count,
-                                [&](uint64_t x) { return reach(base + x); });
-      if (f.bin < 0) return 0u;                    // the sum never passes: all keys count
-      before = base + f.before;
-      at = by_mass ? s.mass[f.bin] : s.count[f.bin];
-      prefix |= (uint32_t)f.bin << shift;
-      mask |= field << shift;
-      __syncthreads();
-    }
-    return prefix;
+  // ---- the candidates ----
+  const int n = (int)min(rec.n, (uint32_t)kSmpCap);
+  for (int i = tid; i < n; i += kRowThreads) cand[i] = d.list[rb * kSmpCap + i];   // its own ones
+  auto each = [&](auto f) {
+    for (int i = tid; i < n; i += kRowThreads) f((uint32_t)(cand[i] >> 32), (uint32_t)cand[i]);
   };
-  // ---- thresholds ----
-  uint32_t cut = 1u;                               // keys from here on stay
-  uint64_t ties = ~0ull;                           // of those at the cut, the first so many
-  if (k > 0 && k < d.V) {
-    uint64_t before, at;
-    const uint32_t key = select(false, 1u, [&](uint64_t x) { return x >= (uint64_t)k; }, before, at);
-    if (key > cut) cut = key;
-  }
-  if (p < 1.f) {
-    // the mass of what top-k left
-    uint64_t sum = 0;
-    for (int g = 0; g < segs; ++g) {
-      uint32_t key[4];
-      smp_load(d, row, wide, g * kSmpSeg + 4 * tid, key);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) sum += key[q] >= cut ? w.weight(key[q]) : 0u;
-    }
-    sum = wave_sum_u64(sum);
-    if (lane == 0) s.red[wave] = sum;
-    __syncthreads();
-    sum = 0;
-    for (int x = 0; x < kSmpWaves; ++x) sum += s.red[x];
-    __syncthreads();
-    const double want = (double)p * (double)sum;
-    uint64_t before, at = 0;
-    const uint32_t key = select(true, cut, [&](uint64_t x) { return (double)x >= want; }, before, at);
-    if (key != 0u) {
-      cut = key;
-      const uint64_t each = w.weight(key);
-      const uint64_t n = at / each;                // ties; of them those with before + i each < want
-      uint64_t c = (uint64_t)((want - (double)before) / (double)each);
-      while (c > 0 && (double)(before + (c - 1) * each) >= want) --c;
-      while (c < n && (double)(before + c * each) < want) ++c;
-      ties = c < n ? c : ~0ull;
+  // the edge's bin lies behind `above` tokens, which stay; a list begins at the top
+  const uint64_t above = rec.mode == kSmpEdge ? rec.above : 0u;
+  const uint64_t mass_above = rec.mode == kSmpEdge ? rec.mass_above : 0u;
+  uint32_t cut = 1u, tie_end = ~0u;
+  uint64_t before, at;
+  uint64_t sum = rec.mass;                         // of what top-k leaves
+  if (set.k > 0 && n > 0) {
+    const uint32_t x = row_select(s, 32, [&](auto f) {
+      each([&](uint32_t k, uint32_t) { f(k, 1u); });
+    }, [&](uint64_t x) { return above + x >= (uint64_t)set.k; }, before, at);
+    if (x != 0u) {                                 // else it leaves all that have a weight
+      cut = x;
+      sum = 0;
+      each([&](uint32_t k, uint32_t) { sum += k >= cut ? w.weight(k) : 0u; });
+      sum = row_sum(s, sum) + mass_above;
     }
   }
-  // ---- where the ties end ----
-  int tie_end = d.V;                               // tokens at the cut stay before this index
-  if (ties != ~0ull) {
-    for (int g = 0; g < segs; ++g) {
-      uint32_t key[4];
-      smp_load(d, row, wide, g * kSmpSeg + 4 * tid, key);
-      uint64_t n = 0;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) n += key[q] == cut ? 1u : 0u;
-      n = wave_sum_u64(n);
-      if (lane == 0) s.part[g * kSmpWaves + wave] = n;
+  if (set.p < 1.f && n > 0) {
+    const double want = (double)set.p * (double)sum;
+    const uint32_t x = row_select(s, 32, [&](auto f) {
+      each([&](uint32_t k, uint32_t) {
+        if (k >= cut) f(k, w.weight(k));
+      });
+    }, [&](uint64_t x) { return (double)(mass_above + x) >= want; }, before, at);
+    if (x != 0u) {
+      cut = x;
+      const uint64_t one = w.weight(x), m = at / one;
+      const uint64_t stay = row_ties(want, mass_above + before, one, m);
+      if (stay < m)
+        tie_end = kIndexTop + 1 - row_select(s, 18, [&](auto f) {
+          each([&](uint32_t k, uint32_t i) {
+            if (k == cut) f(kIndexTop - i, 1u);
+          });
+        }, [&](uint64_t x) { return x >= stay; }, before, at);
     }
-    __syncthreads();
-    uint64_t before = 0;
-    int at = 0;
-    while (before + s.part[at] < ties) before += s.part[at++];   // ties is below their number
-    uint32_t key[4];
-    const int i0 = (at / kSmpWaves) * kSmpSeg + (at % kSmpWaves) * 256 + 4 * lane;
-    smp_load(d, row, wide, i0, key);
-    uint64_t n = 0;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) n += key[q] == cut ? 1u : 0u;
-    uint64_t x = before + wave_scan_u64(n, lane) - n;
-    int end = -1;
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      if (key[q] == cut && ++x == ties) end = i0 + q + 1;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) end = max(end, __shfl_xor(end, o, kWave));
-    tie_end = end;
-    __syncthreads();
   }
-  auto kept = [&](uint32_t key, int i) -> uint64_t {
-    if (key < cut || (key == cut && i >= tie_end)) return 0u;
-    if (mp > 0.f && !(w.x(key) >= log_mp)) return 0u;
-    return w.weight(key);
-  };
-  // ---- the kept weights of each 256 tokens, their sum, and where u falls ----
-  for (int g = 0; g < segs; ++g) {
-    const int i0 = g * kSmpSeg + 4 * tid;
-    uint32_t key[4];
-    smp_load(d, row, wide, i0, key);
-    uint64_t sum = 0;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) sum += kept(key[q], i0 + q);
-    sum = wave_sum_u64(sum);
-    if (lane == 0) s.part[g * kSmpWaves + wave] = sum;
+  auto kept = [&](uint32_t k, uint32_t i) { return !(k < cut || (k == cut && i >= tie_end)); };
+  auto stays = [&](uint32_t k, uint32_t i) -> uint64_t { return kept(k, i) ? heavy(k) : 0u; };
+  if (rec.mode == kSmpList) {
+    // the draw among the candidates: by index, the lowest first
+    uint64_t Z = 0;
+    each([&](uint32_t k, uint32_t i) { Z += stays(k, i); });
+    Z = row_sum(s, Z);
+    const double goal = smp_goal(d, r, Z);
+    auto by_index = [&](auto f) {
+      each([&](uint32_t k, uint32_t i) { f(kIndexTop - i, stays(k, i)); });
+    };
+    // a sum that is to exceed the goal, or, where none does, to be whole
+    const bool none = !((double)Z > goal);
+    const uint32_t x = row_select(s, 18, by_index, [&](uint64_t x) {
+      return none ? x >= Z : (double)x > goal;
+    }, before, at);
+    if (tid == 0) smp_out(d, r, row, w, (int)(kIndexTop - x), Z);
+    return;
   }
+  // the chunks' sums with the candidates that stay
   __syncthreads();
-  if (wave != 0) return;
-  uint64_t Z = 0;
-  for (int i = lane; i < segs * kSmpWaves; i += kWave) Z += s.part[i];
-  Z = wave_sum_u64(Z);
-  const double goal = (double)d.u[r] * (double)Z;
-  auto over = [&](uint64_t x) { return (double)x > goal; };
-  // the first 256 tokens whose sum passes, or the last with any weight
-  int at = -1, last = 0;
-  uint64_t before = 0, run = 0;
-  for (int i = 0; i < segs * kSmpWaves; ++i) {
-    const uint64_t x = s.part[i];
-    if (x > 0) last = i;
-    if (over(run + x) && x > 0) {
-      at = i;
-      before = run;
-      break;
-    }
-    run += x;
-  }
-  const bool none = at < 0;                        // u is no number below 1
-  if (none) at = last;
-  const int i0 = (at / kSmpWaves) * kSmpSeg + (at % kSmpWaves) * 256 + 4 * lane;
-  uint32_t key[4];
-  uint64_t wt[4], n = 0;
-  smp_load(d, row, wide, i0, key);
-#pragma unroll
-  for (int q = 0; q < 4; ++q) n += wt[q] = kept(key[q], i0 + q);
-  uint64_t x = before + wave_scan_u64(n, lane) - n;
-  int pick = none ? -1 : 0x7fffffff;
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    x += wt[q];
-    if (wt[q] > 0) {
-      if (none) pick = i0 + q;
-      else if (over(x) && pick == 0x7fffffff) pick = i0 + q;
-    }
-  }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    const int y = __shfl_xor(pick, o, kWave);
-    pick = none ? max(pick, y) : min(pick, y);
-  }
-  if (lane == 0) {
-    d.ids[r] = pick;
-    if (d.logprob)
-      d.logprob[r] = (float)(w.x(smp_key(to_f32<T>(row[pick]))) - (log((double)Z) - 45.0 * 0.69314718055994531));
-  }
+  if (tid < kSmpChunks) s.bins[tid] = tid < d.chunks ? sums[tid] : 0u;
+  __syncthreads();
+  each([&](uint32_t k, uint32_t i) {
+    const uint64_t v = stays(k, i);
+    if (v != 0u) atomicAdd((unsigned long long*)&s.bins[i / kSmpChunk], (unsigned long long)v);
+  });
+  __syncthreads();
+  row_draw(d, s, r, row, wide, w, s.bins, [&](uint32_t k, int i) -> uint64_t {
+    if (k == 0u) return 0u;
+    const double y = w.x(k);
+    const int b = w.bin_at(y);
+    const bool in = b < rec.edge || (b == rec.edge && kept(k, (uint32_t)i));
+    return in && y >= log_mp ? w.weight_at(y) : 0u;
+  });
 }
 
 __global__ void k_smp_clear_err(uint32_t* err) {
   if (threadIdx.x == 0) *err = 0u;
+}
+
+template <typename T>
+static hipError_t launch_sample(Smp d, int rows, int cus, hipStream_t st) {
+  // as many chunks a workgroup as leave four workgroups a CU
+  d.per_wg = std::max(1, std::min(d.chunks, rows * d.chunks / (4 * cus)));
+  const dim3 grid(rows * ((d.chunks + d.per_wg - 1) / d.per_wg)), block(kSmpThreads);
+  hipError_t e;
+  hipLaunchKernelGGL(k_smp_max<T>, grid, block, 0, st, d);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  if (d.temp != nullptr) {
+    hipLaunchKernelGGL(k_smp_mass<T>, grid, block, 0, st, d);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (d.top_k != nullptr || d.top_p != nullptr) {
+      hipLaunchKernelGGL(k_smp_list<T>, grid, block, 0, st, d);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+  }
+  hipLaunchKernelGGL(k_smp_row<T>, dim3(rows), dim3(kRowThreads), 0, st, d);
+  return hipGetLastError();
 }
 
 }  // namespace xp
@@ -385,9 +822,9 @@ __global__ void k_smp_clear_err(uint32_t* err) {
 using namespace xp;
 
 struct xp_sampler {
-  int device = 0, V = 0, max_rows = 0;
+  int device = 0, cus = 0, V = 0, max_rows = 0;
   void* ws = nullptr;
-  uint32_t* err = nullptr;
+  Smp d{};                           // the workspace's slices
   std::string msg;
 };
 
@@ -422,22 +859,43 @@ extern "C" xp_status xp_sampler_create(int32_t V, int32_t max_rows, xp_sampler**
   s->V = V;
   s->max_rows = max_rows;
   hipError_t e = hipGetDevice(&s->device);
-  if (e == hipSuccess) {
-    const size_t total = 256;
-    e = hipMalloc(&s->ws, total);
-    if (e != hipSuccess) {
-      (void)hipGetLastError();
-      delete s;
-      return smp_fail(nullptr, XP_ENOMEM, "workspace of %zu bytes: %s", total, hipGetErrorString(e));
-    }
-    s->err = static_cast<uint32_t*>(s->ws);
-    e = hipMemset(s->ws, 0, 256);
-    if (e == hipSuccess) e = hipDeviceSynchronize();
-  }
+  if (e == hipSuccess)
+    e = hipDeviceGetAttribute(&s->cus, hipDeviceAttributeMultiprocessorCount, s->device);
   if (e != hipSuccess) {
-    if (s->ws) (void)hipFree(s->ws);
     delete s;
-    return smp_fail(nullptr, XP_EHIP, "sampler: %s", hipGetErrorString(e));
+    return smp_fail(nullptr, XP_EHIP, "device query failed: %s", hipGetErrorString(e));
+  }
+  s->cus = s->cus > 0 ? s->cus : 256;
+  const size_t nb = (size_t)std::min(max_rows, kSmpBatch);
+  struct Slice { void** at; size_t bytes; };
+  const Slice slices[] = {
+      {(void**)&s->d.err, 256},
+      {(void**)&s->d.best, nb * kSmpChunks * 8},
+      {(void**)&s->d.sums, nb * kSmpChunks * 8},
+      {(void**)&s->d.mass, nb * kSmpHist * 8},
+      {(void**)&s->d.count, nb * kSmpHist * 4},
+      {(void**)&s->d.rec, nb * sizeof(SmpRec)},
+      {(void**)&s->d.list, nb * kSmpCap * 8},
+  };
+  size_t total = 0;
+  for (const Slice& sl : slices) total += (sl.bytes + 255) / 256 * 256;
+  e = hipMalloc(&s->ws, total);
+  if (e != hipSuccess) {
+    (void)hipGetLastError();
+    delete s;
+    return smp_fail(nullptr, XP_ENOMEM, "workspace of %zu bytes: %s", total, hipGetErrorString(e));
+  }
+  char* at = static_cast<char*>(s->ws);
+  for (const Slice& sl : slices) {
+    *sl.at = at;
+    at += (sl.bytes + 255) / 256 * 256;
+  }
+  e = hipMemset(s->ws, 0, 256);                    // the device error word
+  if (e == hipSuccess) e = hipDeviceSynchronize();
+  if (e != hipSuccess) {
+    (void)hipFree(s->ws);
+    delete s;
+    return smp_fail(nullptr, XP_EHIP, "workspace: %s", hipGetErrorString(e));
   }
   *out = s;
   return XP_OK;
@@ -480,7 +938,7 @@ extern "C" xp_status xp_sample(xp_sampler* s, int32_t rows, int32_t dtype, const
     return smp_fail(s, XP_EINVAL, "u is required with temp, and only with it");
   const xp_status ds = smp_device(s);
   if (ds != XP_OK || rows == 0) return ds;
-  Smp d{};
+  Smp d = s->d;
   d.logits = logits;
   d.ld = ld;
   d.V = s->V;
@@ -492,11 +950,14 @@ extern "C" xp_status xp_sample(xp_sampler* s, int32_t rows, int32_t dtype, const
   d.u = u;
   d.ids = out_ids;
   d.logprob = out_logprob;
-  d.err = s->err;
-  hipStream_t st = (hipStream_t)stream;
-  if (dtype == XP_F32) hipLaunchKernelGGL(k_sample_row<float>, dim3(rows), dim3(kSmpThreads), 0, st, d);
-  else hipLaunchKernelGGL(k_sample_row<uint16_t>, dim3(rows), dim3(kSmpThreads), 0, st, d);
-  const hipError_t e = hipGetLastError();
+  d.chunks = (s->V + kSmpChunk - 1) / kSmpChunk;
+  hipError_t e = hipSuccess;
+  for (int32_t r0 = 0; r0 < rows && e == hipSuccess; r0 += kSmpBatch) {
+    d.row0 = r0;
+    const int n = std::min(rows - r0, (int32_t)kSmpBatch);
+    e = dtype == XP_F32 ? launch_sample<float>(d, n, s->cus, (hipStream_t)stream)
+                        : launch_sample<uint16_t>(d, n, s->cus, (hipStream_t)stream);
+  }
   if (e != hipSuccess) return smp_fail(s, XP_EHIP, "launch failed: %s", hipGetErrorString(e));
   return XP_OK;
 }
@@ -507,9 +968,9 @@ extern "C" xp_status xp_sampler_device_errors(xp_sampler* s, uint32_t* out, void
   const xp_status ds = smp_device(s);
   if (ds != XP_OK) return ds;
   hipStream_t st = (hipStream_t)stream;
-  hipError_t e = hipMemcpyAsync(out, s->err, sizeof(uint32_t), hipMemcpyDeviceToHost, st);
+  hipError_t e = hipMemcpyAsync(out, s->d.err, sizeof(uint32_t), hipMemcpyDeviceToHost, st);
   if (e == hipSuccess) {
-    hipLaunchKernelGGL(k_smp_clear_err, dim3(1), dim3(64), 0, st, s->err);
+    hipLaunchKernelGGL(k_smp_clear_err, dim3(1), dim3(64), 0, st, s->d.err);
     e = hipGetLastError();
   }
   if (e == hipSuccess) e = hipStreamSynchronize(st);
