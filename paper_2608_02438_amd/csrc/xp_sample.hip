@@ -39,8 +39,9 @@ static_assert(kSmpChunk == 4 * kRowThreads, "a thread of the row has 4 tokens of
 // What a row's launches leave for each other.
 struct SmpRec {
   int32_t mode, edge;                // SmpMode; the last bin that counts
-  uint32_t n, above;                 // candidates; tokens of the bins before the edge
-  uint64_t mass_above, mass;         // the weight of those, of all tokens
+  uint32_t n, pad;                   // candidates
+  uint64_t above, all;               // of the bins before the edge, of all: tokens where
+                                     // top-k decides, else weight
 };
 enum SmpMode {
   kSmpPlain = 0,                     // no threshold of l: the chunks' sums are final
@@ -64,8 +65,7 @@ struct Smp {
   int chunks, per_wg;                // of a row, of a workgroup
   uint64_t* best;                    // [rows][kSmpChunks] the largest key, lowest index
   uint64_t* sums;                    // [rows][kSmpChunks] kept weights
-  uint64_t* mass;                    // [rows][kSmpHist]
-  uint32_t* count;                   // [rows][kSmpHist]
+  uint64_t* hist;                    // [rows][kSmpHist] tokens (top-k) or weights of a bin
   SmpRec* rec;                       // [rows]
   uint64_t* list;                    // [rows][kSmpCap] key, index
 };
@@ -157,6 +157,10 @@ __device__ __forceinline__ uint64_t wave_sum_u64(uint64_t v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += shfl_xor_u64(v, o);
   return v;
+}
+__device__ __forceinline__ uint64_t shfl_u64(uint64_t v, int lane) {
+  return ((uint64_t)(uint32_t)__shfl((int)(v >> 32), lane, kWave) << 32) |
+         (uint32_t)__shfl((int)v, lane, kWave);
 }
 __device__ __forceinline__ uint64_t wave_max_u64(uint64_t v) {
 #pragma unroll
@@ -252,10 +256,7 @@ __global__ __launch_bounds__(kSmpThreads) void k_smp_max(const Smp d) {
   const T* row = static_cast<const T*>(d.logits) + at.row * d.ld;
   const bool wide = reinterpret_cast<uintptr_t>(row) % (4 * sizeof(T)) == 0;
   if (at.c0 == 0 && d.temp != nullptr) {
-    for (int b = tid; b < kSmpHist; b += kSmpThreads) {
-      d.mass[at.r * kSmpHist + b] = 0;
-      d.count[at.r * kSmpHist + b] = 0;
-    }
+    for (int b = tid; b < kSmpHist; b += kSmpThreads) d.hist[at.r * kSmpHist + b] = 0;
     if (tid == 0) d.rec[at.r] = SmpRec{};
   }
   for (int c = at.c0; c < at.c1; ++c) {
@@ -281,12 +282,11 @@ __global__ __launch_bounds__(kSmpThreads) void k_smp_max(const Smp d) {
   }
 }
 
-// The weights: every chunk's sum where no threshold of l is to be found, else the row's
-// histogram of tokens and weights.
+// The weights: every chunk's sum where no threshold of l is to be found; else the row's
+// histogram, of tokens where top-k decides and of weights for top-p alone.
 template <typename T>
 __global__ __launch_bounds__(kSmpThreads) void k_smp_mass(const Smp d) {
-  __shared__ uint64_t mass[kSmpHist];
-  __shared__ uint32_t count[kSmpHist];
+  __shared__ uint64_t hist[kSmpHist];
   __shared__ uint64_t red[kSmpThreads / kWave];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const SmpPlace at = smp_place(d);
@@ -297,34 +297,17 @@ __global__ __launch_bounds__(kSmpThreads) void k_smp_mass(const Smp d) {
   const uint32_t top_key = (uint32_t)(smp_best(d, at.r) >> 32);
   if (top_key == 0u) return;
   const SmpRow w{1.0 / (double)set.t, (double)smp_value(top_key), top_key};
-  const double log_mp = set.log_min();
-  const bool cuts = set.cuts();
-  if (cuts) {
-    for (int b = tid; b < kSmpHist; b += kSmpThreads) {
-      mass[b] = 0;
-      count[b] = 0;
-    }
-    __syncthreads();
-  }
-  for (int c = at.c0; c < at.c1; ++c) {
-    uint32_t key[kSmpPer];
-    smp_chunk(d, row, wide, c, key);
-    uint64_t sum = 0;
+  if (!set.cuts()) {
+    const double log_mp = set.log_min();
+    for (int c = at.c0; c < at.c1; ++c) {
+      uint32_t key[kSmpPer];
+      smp_chunk(d, row, wide, c, key);
+      uint64_t sum = 0;
 #pragma unroll
-    for (int i = 0; i < kSmpPer; ++i) {
-      const double y = w.x(key[i]);
-      const uint64_t e = key[i] != 0u ? w.weight_at(y) : 0u;
-      if (cuts) {
-        const int b = w.bin_at(y);
-        if (key[i] != 0u && b < kSmpHist) {
-          atomicAdd((unsigned long long*)&mass[b], (unsigned long long)e);
-          atomicAdd(&count[b], 1u);
-        }
-      } else {
-        sum += y >= log_mp ? e : 0u;
+      for (int i = 0; i < kSmpPer; ++i) {
+        const double y = w.x(key[i]);
+        sum += key[i] != 0u && y >= log_mp ? w.weight_at(y) : 0u;
       }
-    }
-    if (!cuts) {
       sum = wave_sum_u64(sum);
       if (lane == 0) red[wave] = sum;
       __syncthreads();
@@ -334,70 +317,74 @@ __global__ __launch_bounds__(kSmpThreads) void k_smp_mass(const Smp d) {
       }
       __syncthreads();
     }
+    return;
   }
-  if (cuts) {
-    __syncthreads();
-    for (int b = tid; b < kSmpHist; b += kSmpThreads)
-      if (count[b] != 0u) {
-        atomicAdd((unsigned long long*)&d.mass[at.r * kSmpHist + b], (unsigned long long)mass[b]);
-        atomicAdd(&d.count[at.r * kSmpHist + b], count[b]);
+  for (int b = tid; b < kSmpHist; b += kSmpThreads) hist[b] = 0;
+  __syncthreads();
+  const bool tokens = set.k > 0;
+  for (int c = at.c0; c < at.c1; ++c) {
+    uint32_t key[kSmpPer];
+    smp_chunk(d, row, wide, c, key);
+#pragma unroll
+    for (int i = 0; i < kSmpPer; ++i) {
+      const double y = w.x(key[i]);
+      const int b = w.bin_at(y);
+      if (key[i] != 0u && b < kSmpHist) {
+        const uint64_t v = tokens ? 1u : w.weight_at(y);
+        atomicAdd((unsigned long long*)&hist[b], (unsigned long long)v);
       }
+    }
   }
+  __syncthreads();
+  for (int b = tid; b < kSmpHist; b += kSmpThreads)
+    if (hist[b] != 0u)
+      atomicAdd((unsigned long long*)&d.hist[at.r * kSmpHist + b], (unsigned long long)hist[b]);
 }
 
 // What the histogram says: the bin in which the threshold lies.
 __device__ __forceinline__ SmpRec smp_decide(const Smp& d, int64_t r, const SmpSet& set) {
   constexpr int N = kSmpHist / kWave;
   const int lane = threadIdx.x & 63;
-  uint64_t m[N], mt = 0;
-  uint32_t n[N];
-  uint64_t nt = 0;
+  uint64_t v[N], sum = 0;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    m[i] = d.mass[r * kSmpHist + N * lane + i];
-    n[i] = d.count[r * kSmpHist + N * lane + i];
-    mt += m[i];
-    nt += n[i];
+    v[i] = d.hist[r * kSmpHist + N * lane + i];
+    sum += v[i];
   }
-  uint64_t mb = wave_scan_u64(mt, lane), nb = wave_scan_u64(nt, lane);
-  const uint64_t mass = ((uint64_t)(uint32_t)__shfl((int)(mb >> 32), 63, kWave) << 32) |
-                        (uint32_t)__shfl((int)mb, 63, kWave);
-  const uint32_t all = (uint32_t)__shfl((int)nb, 63, kWave);
-  mb -= mt;
-  nb -= nt;
-  const bool by_k = set.k > 0 && all >= (uint32_t)set.k;   // fewer: all tokens with a weight stay
-  const double want = (double)set.p * (double)mass;
+  uint64_t before = wave_scan_u64(sum, lane);
   SmpRec x{};
-  x.mass = mass;
+  x.all = shfl_u64(before, 63);
+  before -= sum;
+  const bool by_k = set.k > 0;
+  const double want = (double)set.p * (double)x.all;
   bool mine = false;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const bool hit = by_k ? nb < (uint32_t)set.k && nb + n[i] >= (uint32_t)set.k
-                          : set.p < 1.f && (double)mb < want && (double)(mb + m[i]) >= want;
+    const uint64_t upto = before + v[i];
+    const bool hit = by_k ? before < (uint64_t)set.k && upto >= (uint64_t)set.k
+                          : (double)before < want && (double)upto >= want;
     if (hit && !mine) {
       mine = true;
       x.edge = N * lane + i;
-      x.above = (uint32_t)nb;
-      x.mass_above = mb;
-      const bool list = nb + n[i] <= (uint64_t)kSmpCap;
-      const bool edge = n[i] <= (uint32_t)kSmpCap && !(by_k && set.p < 1.f);
-      x.mode = list ? kSmpList : (edge ? kSmpEdge : kSmpSlow);
+      x.above = before;
+      // top-p alone: whether the candidates are too many shows when they are counted
+      x.mode = !by_k ? kSmpEdge
+                     : (upto <= (uint64_t)kSmpCap ? kSmpList
+                        : (v[i] <= (uint64_t)kSmpCap && set.p >= 1.f ? kSmpEdge : kSmpSlow));
     }
-    mb += m[i];
-    nb += n[i];
+    before = upto;
   }
   const uint64_t who = __ballot(mine);
-  if (who == 0) {                                  // nothing is cut: every token of the bins stays
-    x.mode = kSmpEdge;
+  if (who == 0) {
+    // top-k leaves every token that has a weight: the bins' all, or what top-p cuts of them
+    x.mode = set.p >= 1.f ? kSmpEdge : kSmpSlow;
     x.edge = kSmpHist;
     return x;
   }
   const int src = __builtin_ctzll(who);
   x.mode = __shfl(x.mode, src, kWave);
   x.edge = __shfl(x.edge, src, kWave);
-  x.above = (uint32_t)__shfl((int)x.above, src, kWave);
-  x.mass_above = ((uint64_t)(uint32_t)__shfl((int)(x.mass_above >> 32), src, kWave) << 32) |
-                 (uint32_t)__shfl((int)x.mass_above, src, kWave);
+  x.above = shfl_u64(x.above, src);
   return x;
 }
 
@@ -419,8 +406,7 @@ __global__ __launch_bounds__(kSmpThreads) void k_smp_list(const Smp d) {
     to->mode = rec.mode;
     to->edge = rec.edge;
     to->above = rec.above;
-    to->mass_above = rec.mass_above;
-    to->mass = rec.mass;
+    to->all = rec.all;
   }
   if (rec.mode == kSmpSlow) return;
   const T* row = static_cast<const T*>(d.logits) + at.row * d.ld;
@@ -492,6 +478,60 @@ __device__ __forceinline__ uint64_t row_sum(RowShared& s, uint64_t v) {
   return v;
 }
 
+__device__ __forceinline__ uint64_t row_max(RowShared& s, uint64_t v) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  v = wave_max_u64(v);
+  __syncthreads();
+  if (lane == 0) s.red[wave] = v;
+  __syncthreads();
+  for (int w = 0; w < kRowWaves; ++w) v = umax64(v, s.red[w]);
+  return v;
+}
+// sum of this and lower threads' v; all: the workgroup's
+__device__ __forceinline__ uint64_t row_scan(RowShared& s, uint64_t v, uint64_t& all) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint64_t x = wave_scan_u64(v, lane);
+  __syncthreads();
+  if (lane == 63) s.red[wave] = x;
+  __syncthreads();
+  all = 0;
+#pragma unroll
+  for (int w = 0; w < kRowWaves; ++w) {
+    x += w < wave ? s.red[w] : 0u;
+    all += s.red[w];
+  }
+  return x;
+}
+// thread `at`'s x (whole workgroup)
+__device__ __forceinline__ uint64_t row_get(RowShared& s, uint64_t x, int at) {
+  __syncthreads();
+  if ((int)threadIdx.x == at) s.out[2] = x;
+  __syncthreads();
+  return s.out[2];
+}
+// The threads' x in falling order, n of them at most other than 0: bitonic, in as many
+// threads as n needs, within a wave by lane exchanges.
+__device__ __forceinline__ uint64_t row_sort(RowShared& s, uint64_t x, int n) {
+  const int tid = threadIdx.x;
+  int size = kWave;
+  while (size < n) size *= 2;
+  for (int m = 2; m <= size; m *= 2)
+    for (int o = m / 2; o > 0; o /= 2) {
+      uint64_t y;
+      if (o >= kWave) {                            // whole workgroup
+        __syncthreads();
+        s.bins[tid] = x;
+        __syncthreads();
+        y = s.bins[tid ^ o];
+      } else {
+        y = shfl_xor_u64(x, o);
+      }
+      const bool first = (tid & o) == 0, falls = (tid & m) == 0 || m == size;
+      x = first == falls ? umax64(x, y) : (x < y ? x : y);
+    }
+  return tid < size ? x : 0u;
+}
+
 // The first of the bins, from the top one down, at which the sum passes.
 template <typename F>
 __device__ __forceinline__ int row_find(RowShared& s, F reach, uint64_t& before) {
@@ -517,9 +557,9 @@ __device__ __forceinline__ int row_find(RowShared& s, F reach, uint64_t& before)
   return bin;
 }
 
-// Radix selection among 32-bit keys >= lo, 11 bits a round: the key at which the sum of
-// values, from the largest key down, passes; what lies before it, and at it alone.  0
-// where it never does.  each(f) calls f(key, value) for the thread's elements.
+// Radix selection among keys of so many bits, 11 a round: the key at which the sum of
+// values, from the largest key down, passes; what lies before it, and at it alone (0
+// where it never does).  each(f) calls f(key, value) for the thread's elements.
 template <typename E, typename F>
 __device__ __forceinline__ uint32_t row_select(RowShared& s, int bits, E each, F reach,
                                                uint64_t& before, uint64_t& at) {
@@ -540,7 +580,10 @@ __device__ __forceinline__ uint32_t row_select(RowShared& s, int bits, E each, F
     uint64_t in;
     const uint64_t base = before;
     const int bin = row_find(s, [&](uint64_t x) { return reach(base + x); }, in);
-    if (bin < 0) return 0u;                        // whole workgroup
+    if (bin < 0) {                                 // whole workgroup
+      at = 0;
+      return 0u;
+    }
     before = base + in;
     at = s.bins[bin];
     prefix |= (uint32_t)bin << shift;
@@ -570,16 +613,14 @@ __device__ __forceinline__ void row_draw(const Smp& d, RowShared& s, int64_t r, 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const uint64_t mine = lane < d.chunks ? sums[lane] : 0u;
   const uint64_t upto = wave_scan_u64(mine, lane);
-  const uint64_t Z = ((uint64_t)(uint32_t)__shfl((int)(upto >> 32), 63, kWave) << 32) |
-                     (uint32_t)__shfl((int)upto, 63, kWave);
+  const uint64_t Z = shfl_u64(upto, 63);
   const double goal = smp_goal(d, r, Z);
   auto over = [&](uint64_t x) { return (double)x > goal; };
   const uint64_t hit = __ballot(mine > 0 && over(upto)), some = __ballot(mine > 0);
   const bool none = hit == 0;                      // u is no number below 1
   const int c = none ? 63 - __builtin_clzll(some | 1u) : __builtin_ctzll(hit);
   const uint64_t b = upto - mine;
-  const uint64_t before = ((uint64_t)(uint32_t)__shfl((int)(b >> 32), c, kWave) << 32) |
-                          (uint32_t)__shfl((int)b, c, kWave);
+  const uint64_t before = shfl_u64(b, c);
   const int i0 = c * kSmpChunk + 4 * tid;
   uint32_t key[4];
   uint64_t wt[4], n = 0;
@@ -710,79 +751,126 @@ __global__ __launch_bounds__(kRowThreads) void k_smp_row(const Smp d) {
     return;
   }
   const SmpRec rec = d.rec[rb];
-  if (rec.mode == kSmpSlow) {
+  if (rec.mode == kSmpSlow || rec.n > (uint32_t)kSmpCap) {
     row_slow(d, s, r, row, wide, w, set);
     return;
   }
-  // ---- the candidates ----
-  const int n = (int)min(rec.n, (uint32_t)kSmpCap);
-  for (int i = tid; i < n; i += kRowThreads) cand[i] = d.list[rb * kSmpCap + i];   // its own ones
-  auto each = [&](auto f) {
-    for (int i = tid; i < n; i += kRowThreads) f((uint32_t)(cand[i] >> 32), (uint32_t)cand[i]);
-  };
-  // the edge's bin lies behind `above` tokens, which stay; a list begins at the top
-  const uint64_t above = rec.mode == kSmpEdge ? rec.above : 0u;
-  const uint64_t mass_above = rec.mode == kSmpEdge ? rec.mass_above : 0u;
+  // ---- the candidates that stay: down to the key `cut`, of those at it the ones whose
+  // index lies before tie_end ----
+  const int n = (int)rec.n;
+  const uint64_t* list = d.list + rb * kSmpCap;
+  // the edge's bin lies behind tokens that stay; a list begins at the top
+  const uint64_t num_above = rec.mode == kSmpEdge && set.k > 0 ? rec.above : 0u;
+  const uint64_t mass_above = rec.mode == kSmpEdge && set.k == 0 ? rec.above : 0u;
   uint32_t cut = 1u, tie_end = ~0u;
-  uint64_t before, at;
-  uint64_t sum = rec.mass;                         // of what top-k leaves
-  if (set.k > 0 && n > 0) {
-    const uint32_t x = row_select(s, 32, [&](auto f) {
-      each([&](uint32_t k, uint32_t) { f(k, 1u); });
-    }, [&](uint64_t x) { return above + x >= (uint64_t)set.k; }, before, at);
-    if (x != 0u) {                                 // else it leaves all that have a weight
-      cut = x;
-      sum = 0;
-      each([&](uint32_t k, uint32_t) { sum += k >= cut ? w.weight(k) : 0u; });
-      sum = row_sum(s, sum) + mass_above;
-    }
-  }
-  if (set.p < 1.f && n > 0) {
-    const double want = (double)set.p * (double)sum;
-    const uint32_t x = row_select(s, 32, [&](auto f) {
-      each([&](uint32_t k, uint32_t) {
-        if (k >= cut) f(k, w.weight(k));
-      });
-    }, [&](uint64_t x) { return (double)(mass_above + x) >= want; }, before, at);
-    if (x != 0u) {
-      cut = x;
-      const uint64_t one = w.weight(x), m = at / one;
-      const uint64_t stay = row_ties(want, mass_above + before, one, m);
-      if (stay < m)
-        tie_end = kIndexTop + 1 - row_select(s, 18, [&](auto f) {
-          each([&](uint32_t k, uint32_t i) {
-            if (k == cut) f(kIndexTop - i, 1u);
-          });
-        }, [&](uint64_t x) { return x >= stay; }, before, at);
-    }
-  }
   auto kept = [&](uint32_t k, uint32_t i) { return !(k < cut || (k == cut && i >= tie_end)); };
   auto stays = [&](uint32_t k, uint32_t i) -> uint64_t { return kept(k, i) ? heavy(k) : 0u; };
-  if (rec.mode == kSmpList) {
-    // the draw among the candidates: by index, the lowest first
-    uint64_t Z = 0;
-    each([&](uint32_t k, uint32_t i) { Z += stays(k, i); });
-    Z = row_sum(s, Z);
-    const double goal = smp_goal(d, r, Z);
-    auto by_index = [&](auto f) {
-      each([&](uint32_t k, uint32_t i) { f(kIndexTop - i, stays(k, i)); });
+  if (n <= kRowThreads) {
+    // in order, a thread each: what lies before a candidate is a prefix sum
+    uint64_t x = tid < n ? list[tid] : 0u;
+    x = row_sort(s, x != 0u ? (x & ~0xffffffffull) | (uint32_t)~(uint32_t)x : 0u, n);
+    const uint32_t key = (uint32_t)(x >> 32), idx = ~(uint32_t)x;
+    bool in = key != 0u;
+    if (set.k > 0) {
+      const int64_t last = set.k - 1 - (int64_t)num_above;   // of the k, among the candidates
+      const uint32_t kth = last < n ? (uint32_t)(row_get(s, x, (int)last) >> 32) : 1u;
+      in = in && key >= kth;                       // what ties with it stays
+    }
+    const uint64_t v = in ? w.weight(key) : 0u;
+    if (set.p < 1.f) {
+      uint64_t sum;
+      const uint64_t upto = row_scan(s, v, sum);
+      sum = set.k > 0 ? sum : rec.all;             // what top-k leaves
+      in = in && (double)(mass_above + upto - v) < (double)set.p * (double)sum;
+    }
+    const int stay = (int)row_sum(s, in ? 1u : 0u);
+    if (rec.mode == kSmpList) {
+      // the draw among them: by index, the lowest first
+      const bool take = in && w.x(key) >= log_mp;
+      x = row_sort(s, take ? ((uint64_t)(kIndexTop + 1 - idx) << 32) | key : 0u, n);
+      const uint64_t mine = x != 0u ? w.weight((uint32_t)x) : 0u;
+      uint64_t Z;
+      const uint64_t upto = row_scan(s, mine, Z);
+      const double goal = smp_goal(d, r, Z);
+      const bool none = !((double)Z > goal);       // the last one with a weight then
+      const bool hit = mine > 0 && (none ? upto == Z : (double)upto > goal && !((double)(upto - mine) > goal));
+      if (hit) smp_out(d, r, row, w, (int)(kIndexTop + 1 - (uint32_t)(x >> 32)), Z);
+      return;
+    }
+    if (stay > 0) {
+      const uint64_t y = row_get(s, x, stay - 1);
+      cut = (uint32_t)(y >> 32);
+      tie_end = ~(uint32_t)y + 1;
+    } else {
+      cut = ~0u;                                   // no candidate stays
+    }
+  } else {
+    uint32_t hi = 0, lo = ~0u;
+    for (int i = tid; i < n; i += kRowThreads) {   // its own ones from here on
+      const uint64_t x = list[i];
+      cand[i] = x;
+      hi = max(hi, (uint32_t)(x >> 32));
+      lo = min(lo, (uint32_t)(x >> 32));
+    }
+    // the bits in which the keys differ
+    hi = (uint32_t)row_max(s, hi);
+    lo = ~(uint32_t)row_max(s, (uint32_t)~lo);
+    const int bits = hi > lo ? 32 - __builtin_clz(hi - lo) : 1;
+    auto each = [&](auto f) {
+      for (int i = tid; i < n; i += kRowThreads) f((uint32_t)(cand[i] >> 32), (uint32_t)cand[i]);
     };
-    // a sum that is to exceed the goal, or, where none does, to be whole
-    const bool none = !((double)Z > goal);
-    const uint32_t x = row_select(s, 18, by_index, [&](uint64_t x) {
-      return none ? x >= Z : (double)x > goal;
-    }, before, at);
-    if (tid == 0) smp_out(d, r, row, w, (int)(kIndexTop - x), Z);
-    return;
+    uint64_t before, at, sum = rec.all;            // what top-k leaves
+    if (set.k > 0) {
+      const uint32_t x = row_select(s, bits, [&](auto f) {
+        each([&](uint32_t k, uint32_t) { f(k - lo, 1u); });
+      }, [&](uint64_t x) { return num_above + x >= (uint64_t)set.k; }, before, at);
+      if (at != 0u) cut = lo + x;
+      sum = 0;
+      each([&](uint32_t k, uint32_t) { sum += k >= cut ? w.weight(k) : 0u; });
+      sum = row_sum(s, sum);
+    }
+    if (set.p < 1.f) {
+      const double want = (double)set.p * (double)sum;
+      const uint32_t x = row_select(s, bits, [&](auto f) {
+        each([&](uint32_t k, uint32_t) {
+          if (k >= cut) f(k - lo, w.weight(k));
+        });
+      }, [&](uint64_t x) { return (double)(mass_above + x) >= want; }, before, at);
+      if (at != 0u) {
+        cut = lo + x;
+        const uint64_t one = w.weight(cut), m = at / one;
+        const uint64_t stay = row_ties(want, mass_above + before, one, m);
+        if (stay < m)
+          tie_end = kIndexTop + 1 - row_select(s, 18, [&](auto f) {
+            each([&](uint32_t k, uint32_t i) {
+              if (k == cut) f(kIndexTop - i, 1u);
+            });
+          }, [&](uint64_t x) { return x >= stay; }, before, at);
+      }
+    }
+    if (rec.mode == kSmpList) {
+      uint64_t Z = 0;
+      each([&](uint32_t k, uint32_t i) { Z += stays(k, i); });
+      Z = row_sum(s, Z);
+      const double goal = smp_goal(d, r, Z);
+      // a sum that is to exceed the goal, or, where none does, to be whole
+      const bool none = !((double)Z > goal);
+      const uint32_t x = row_select(s, 18, [&](auto f) {
+        each([&](uint32_t k, uint32_t i) { f(kIndexTop - i, stays(k, i)); });
+      }, [&](uint64_t x) { return none ? x >= Z : (double)x > goal; }, before, at);
+      if (tid == 0) smp_out(d, r, row, w, (int)(kIndexTop - x), Z);
+      return;
+    }
   }
-  // the chunks' sums with the candidates that stay
+  // ---- the chunks' sums with the candidates that stay, and the draw ----
   __syncthreads();
   if (tid < kSmpChunks) s.bins[tid] = tid < d.chunks ? sums[tid] : 0u;
   __syncthreads();
-  each([&](uint32_t k, uint32_t i) {
-    const uint64_t v = stays(k, i);
-    if (v != 0u) atomicAdd((unsigned long long*)&s.bins[i / kSmpChunk], (unsigned long long)v);
-  });
+  for (int i = tid; i < n; i += kRowThreads) {
+    const uint64_t x = list[i], v = stays((uint32_t)(x >> 32), (uint32_t)x);
+    if (v != 0u)
+      atomicAdd((unsigned long long*)&s.bins[(uint32_t)x / kSmpChunk], (unsigned long long)v);
+  }
   __syncthreads();
   row_draw(d, s, r, row, wide, w, s.bins, [&](uint32_t k, int i) -> uint64_t {
     if (k == 0u) return 0u;
@@ -872,8 +960,7 @@ extern "C" xp_status xp_sampler_create(int32_t V, int32_t max_rows, xp_sampler**
       {(void**)&s->d.err, 256},
       {(void**)&s->d.best, nb * kSmpChunks * 8},
       {(void**)&s->d.sums, nb * kSmpChunks * 8},
-      {(void**)&s->d.mass, nb * kSmpHist * 8},
-      {(void**)&s->d.count, nb * kSmpHist * 4},
+      {(void**)&s->d.hist, nb * kSmpHist * 8},
       {(void**)&s->d.rec, nb * sizeof(SmpRec)},
       {(void**)&s->d.list, nb * kSmpCap * 8},
   };
