@@ -380,9 +380,8 @@ xp_status xp_layer_forward_noalloc(const xp_layer_weights* w, int32_t batch, int
  *       of a page's KV head first the rows' e2m1 codes (head_dim / 2 bytes a row, dim 2 i
  *       in the low half of byte i), then the rows' exponents (head_dim / 32 bytes a row,
  *       byte i of dims 32 i .. 32 i + 31).  The value of an entry is its code's, 0, 0.5,
- *       1, 1.5, 2, 3, 4, 6 (codes 0 .. 7; 8 .. 15 the negatives), times 2^(exponent - 127),
- *       in bf16 (an infinity beyond its range, which only the exponents 253 and 254 reach);
- *       NaN where the exponent is 255
+ *       1, 1.5, 2, 3, 4, 6 (codes 0 .. 7; 8 .. 15 the negatives), times 2^(exponent - 127);
+ *       NaN where the exponent is above 252 (bf16 does not hold such values)
  *   table [..][table_ld] int32   the pages of each request, in order; key j of
  *       request b is row j % page_size of page table[b][j / page_size]
  *   a slot is page * page_size + row
@@ -535,8 +534,8 @@ xp_status xp_kv_read(xp_kv* kv, int32_t tokens, const int32_t* slots, const void
  * The same call gives the same bits; a request's summation order follows the
  * lengths of all requests of the call.
  * Errors: XP_EINVAL before any launch (null or misaligned pointers, sizes; also
- * where (tokens n_heads / n_kv / 32 + n) (keys / 64 + 8) n_kv reaches 2^31, keys the
- * lesser of max_len and the table's, twice that with shared prefixes: such a call is
+ * where (tokens n_heads / n_kv / 32 + n) (keys / 64 + 8) n_kv reaches 2^31 (16 in place
+ * of 32 over a 4-bit cache), keys the lesser of max_len and the table's, twice that with shared prefixes: such a call is
  * split, or made with a handle of a smaller max_len), XP_EHIP.
  */
 xp_status xp_kv_attn(xp_kv* kv, int32_t n, int32_t tokens, int32_t max_q, const void* q,

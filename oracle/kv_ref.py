@@ -108,7 +108,7 @@ def to_mxfp4(x):
 
 def mxfp4_values(codes, exps):
     v = E2M1[codes & 7] * np.where(codes & 8, -1.0, 1.0)
-    s = np.where(exps == 255, np.nan, 2.0 ** (exps.astype(F64) - 127))
+    s = np.where(exps > 252, np.nan, 2.0 ** (exps.astype(F64) - 127))
     return v * np.repeat(s, 32, axis=-1)
 
 

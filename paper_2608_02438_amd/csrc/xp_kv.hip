@@ -439,7 +439,7 @@ __global__ __launch_bounds__(256) void k_kv_read(const KvRead d) {
       const uint32_t x = *reinterpret_cast<const uint32_t*>(src);
       const uint8_t e =
           *reinterpret_cast<const uint8_t*>(src - 4 * c + kv_exp_at<HD>(slot, d.logP) + c / 4);
-      const float s = __uint_as_float((uint32_t)e << 23);
+      const float s = __uint_as_float((e > 252 ? 255u : (uint32_t)e) << 23);
       y[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, s, 0));
       y[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, s, 1));
       y[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(x, s, 2));
@@ -455,7 +455,7 @@ __global__ void k_kv_clear_err(uint32_t* err) {
 
 bool kv_units_fit(const xp_kv* kv, int64_t tokens, int64_t n, int groups, int64_t table_ld) {
   const int64_t keys = std::min<int64_t>(kv->max_pages, table_ld) * kv->P;
-  const int64_t ent = (tokens * kv->grp / 32 + n) * (groups > 0 ? 2 : 1);
+  const int64_t ent = (tokens * kv->grp / kv_least(kv) + n) * (groups > 0 ? 2 : 1);
   return ent * (keys / kKvTile + 8) * kv->nkv < ((int64_t)1 << 31);
 }
 

@@ -43,6 +43,10 @@ __device__ __forceinline__ float fsum_xor32(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
+__device__ __forceinline__ float fsum_xor16(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
 __device__ __forceinline__ int imin(int a, int b) { return a < b ? a : b; }
 __device__ __forceinline__ int imax(int a, int b) { return a > b ? a : b; }
 
@@ -890,7 +894,7 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
     u32x4* stage = lds + slot * SH::kStage + wave * (NG * 16 * CPR);   // its rows of K, then V
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
-      const float s = __uint_as_float(from.e[g] << 23);
+      const float s = __uint_as_float((from.e[g] > 252u ? 255u : from.e[g]) << 23);
       const int r = lane / 4;
       u32x4* row = stage + (16 * g + r) * CPR;
 #pragma unroll
@@ -1299,6 +1303,444 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
 }
 
 // ---------------------------------------------------------------------------
+// Few rows over a 4-bit cache: up to 16 of a tile (single tokens, short blocks).
+// A cache of 68 bytes a key (head_dim 128) leaves a third of the time a key that 8 bits
+// leave, so nothing may be done for rows that are not there, and little a key:
+//
+// * S^T = K Q^T on v_mfma_scale_f32_16x16x128_f8f6f4: its fp4 operand is a lane's 32
+//   codes of one block as they lie in memory, with the block's power of two, so K goes
+//   from the load into the product.  The queries are its e4m3 operand, in three parts:
+//   a row's largest element lies in [2^7, 2^8), the first part takes 4 bits, the second
+//   the next 4 (all that bf16 has, for elements above 2^-13 of the largest), the third
+//   what lies deeper; what is left is 2^-39 of the largest.
+// * V's power of two differs from key to key, the dimension that P V sums over, where
+//   the instruction takes one for 32: V is expanded to bf16 (exactly) on its way into
+//   the wave's LDS and comes back by transposing reads.
+// * O^T = V^T P^T on v_mfma_f32_16x16x32_bf16, P in two bf16 parts.  A lane has one row
+//   (l % 16) in S and in O; its numerators are the next product's operand.
+//
+// NW waves take a share's tiles of 64 keys in turn, each with its own statistics and
+// no barrier, the next tile on its way while one is worked on; at a segment's end their
+// results are added through LDS.
+// ---------------------------------------------------------------------------
+typedef int intx8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) char lds_char;
+constexpr int kFewRows = 16;
+
+__device__ __forceinline__ floatx4 mma16_bf16(u32x4 a, u32x4 b, floatx4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
+                                                 __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+// 32 e2m1 codes of A times 2^(ea - 127), 32 e4m3 values of B times 2^(eb - 127)
+__device__ __forceinline__ floatx4 mma16_f4f8(u32x4 a, intx8 b, floatx4 c, int ea, int eb) {
+  const intx8 x{(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, b, c, 4, 0, 0, ea, 0, eb);
+}
+// 4 keys of the lane's dim: 16 lanes read 4 rows of 16 dims
+__device__ __forceinline__ uint2 lds_tr16(uint32_t at) {
+  typedef short short4v __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) short4v lds_short4;
+  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(uintptr_t)at));
+}
+
+template <int HD, int NW, bool OWN>
+__global__ __launch_bounds__(NW* kWave, 2) void k_kv_few(const KvDev d) {
+  using SH = KvRows<HD, false>;                   // V's rows in LDS
+  constexpr int NT = HD / 16, RB = SH::RB, CPR = SH::CPR, QM = HD == 128 ? 3 : 2;
+  constexpr int RBM = kv_row_bytes(XP_MXFP4, HD);
+  constexpr int kRing = kKvTile * RB;             // bytes of LDS a wave
+  constexpr int kMerge = (4 * NT + 2) * kWave;    // floats that a wave hands over
+  static_assert(kMerge * 4 <= kRing, "merge in LDS");
+  __shared__ __align__(256) char lds[NW * kRing];
+  __shared__ KvEntry own_ent[OWN ? kOwnEntries : 1];
+  __shared__ int32_t own_sh[8];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int li = lane & 15, g = lane >> 4;
+  const int sidx = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+  if constexpr (OWN) {
+    if (wave == 0) plan_own(d, kFewRows, gridDim.x, sidx, own_ent, own_sh);
+    __syncthreads();
+  }
+  auto share = [&](int i) {
+    if constexpr (OWN) return __builtin_amdgcn_readfirstlane(own_sh[i]);
+    else return as_scalar(d.list.share + sidx)[i];
+  };
+  int f = share(0), e = share(1), kvh = share(2), j = share(3);
+  const int f1 = share(4);
+  if (f >= f1) return;                            // whole workgroup
+  // the lane's bytes within 16 rows: K a block of 32 codes (head_dim 64: the lanes of the
+  // second half have them again, for the second part of Q), V HD / 4 codes
+  const uint32_t ko = li * (HD / 2) + 16 * (HD == 128 ? g : g & 1);
+  const uint32_t keo = li * (HD / 32) + (HD == 128 ? g : g & 1);
+  const uint32_t vo = li * (HD / 2) + (HD / 8) * g;
+  const uint32_t veo = li * (HD / 32) + (HD == 128 ? g : g >> 1);
+  char* ring = lds + wave * kRing;
+  // V into LDS: row 16 n + li, chunks HD / 32 g + i; back: rows 4 g + (li / 4), block dt
+  // of 16 dims, 4 dims a lane
+  const uint32_t vw = lds_byte(ring) + li * RB, sw = SH::swz(li);
+  uint32_t vr;
+  {
+    const int r = 4 * g + (li >> 2);
+    vr = lds_byte(ring) + r * RB + 16 * (((li & 3) >> 1) ^ SH::swz(r)) + 8 * (li & 1);
+  }
+  const int P1 = (1 << d.logP) - 1;
+  const uint32_t exps = (uint32_t)(HD / 2) << d.logP;      // from a page's codes to its exponents
+  for (;;) {
+  int en[kKvEntryInts];
+#pragma unroll
+  for (int i = 0; i < kKvEntryInts; ++i) {
+    if constexpr (OWN) en[i] = __builtin_amdgcn_readfirstlane(reinterpret_cast<const int32_t*>(own_ent + e)[i]);
+    else en[i] = as_scalar(d.list.ent + e)[i];
+  }
+  const int tok0 = en[0], row0 = en[1], nrows = en[2], seq = en[3], p0 = en[4], prefix = en[5];
+  const int kfloor = en[6], kceil = en[7], ks_ = en[8], klo = en[9], khi = en[10], tiles = en[11];
+  const int a0 = en[12], n1 = en[13], b0 = en[14];
+  const int left = f1 - f + imin(j, 0);           // units of the share from tile max(j, 0) on
+  f += tiles - j;                                 // the segment's end
+  j = imax(j, 0);
+  const int nj = imin(tiles - j, left);
+  if (nj <= 0) return;                            // whole workgroup: the share ends before a tile
+  const bool whole = nj == tiles;
+  auto tile_key = [&](int t) { return kKvTile * (t < n1 ? a0 + t : b0 + t - n1); };
+
+  // ---- loads of a tile: 4 groups of 16 keys ----
+  const scalar_i32 tb = as_scalar(d.table + (int64_t)seq * d.table_ld);
+  const int64_t head = ((int64_t)kvh << d.logP) * RBM;
+  const uint32_t page_bytes = (uint32_t)(d.nkv * RBM) << d.logP;
+  const int kin = imax(klo, kfloor);
+  uint32_t bad = 0;
+  struct Tile {
+    u32x4 k[4], v[4];
+    uint32_t ke[4], ve[4];
+  };
+  auto fetch = [&](int t, Tile& x) __attribute__((always_inline)) {
+    const int k0 = tile_key(t);
+    const bool inner = ((k0 >= kin) & (k0 + kKvTile <= khi)) | ((k0 >= kfloor) & (k0 + kKvTile <= ks_));
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const int g0 = k0 + 16 * n, r = g0 & P1;
+      const uint32_t page = (uint32_t)tb[imin(g0 >> d.logP, d.cols - 1)];
+      const bool ok = page < (uint32_t)d.n_pages;
+      const int64_t at = head + (int64_t)((uint64_t)(ok ? page : 0u) * page_bytes);
+      const char *kc = d.kc + at + r * (HD / 2) + ko, *ke = d.kc + at + exps + r * (HD / 32) + keo;
+      const char *vc = d.vc + at + r * (HD / 2) + vo, *ve = d.vc + at + exps + r * (HD / 32) + veo;
+      if (inner) {
+        bad |= ok ? 0u : XP_DEVERR_PAGE;
+      } else {
+        const int from = imax(g0, kfloor), to = imin(g0 + 16, khi), key = g0 + li;
+        bad |= (!ok & (from < to) & ((to > klo) | (from < ks_))) ? XP_DEVERR_PAGE : 0u;
+        const bool any = (key >= kfloor) & (key < khi) & ((key >= klo) | (key < ks_));
+        kc = any ? kc : d.w.zero;
+        ke = any ? ke : d.w.zero;
+        vc = any ? vc : d.w.zero;
+        ve = any ? ve : d.w.zero;
+      }
+      x.k[n] = ld16_nt(kc);
+      if constexpr (HD == 128) {
+        x.v[n] = ld16_nt(vc);
+      } else {
+        typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+        const u32x2 y = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(vc));
+        x.v[n] = u32x4{y[0], y[1], 0u, 0u};
+      }
+      x.ke[n] = *reinterpret_cast<const uint8_t*>(ke);
+      x.ve[n] = *reinterpret_cast<const uint8_t*>(ve);
+    }
+  };
+  Tile ta, tc;
+  if (wave < nj) fetch(j + wave, ta);
+
+  // ---- the query rows ----
+  const bool rv = li < nrows;
+  KvSees sees;
+  intx8 qp[QM];
+  int qs[QM];
+  {
+    const int row = row0 + (rv ? li : 0), tk = row / d.grp;
+    const int64_t tok = tok0 + tk;
+    const uint16_t* q = d.q + tok * d.q_ld + (int64_t)(kvh * d.grp + (row - tk * d.grp)) * HD;
+    constexpr int NQ = HD / 64;                   // pieces of 16 dims: 16 g, and 64 + 16 g
+    float x[NQ][16];
+    float top = 0.f;
+    bool num = true;
+#pragma unroll
+    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const u32x4 y = ld16(q + 64 * n + 16 * g + 8 * c);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[n][8 * c + 2 * i] = __uint_as_float(y[i] << 16);
+          x[n][8 * c + 2 * i + 1] = __uint_as_float(y[i] & 0xffff0000u);
+        }
+      }
+#pragma unroll
+    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        num &= fabsf(x[n][i]) < INFINITY;
+        top = fmaxf(top, fabsf(x[n][i]));
+      }
+    top = fmax_xor16(num ? top : INFINITY);
+    top = fmax_xor32(top);
+    // 2^7 <= x < 2^8 for the largest; an infinity or NaN makes the row's scores NaN
+    const int eb = imax((int)(__float_as_uint(top) >> 23), 31);
+    const float up = __uint_as_float((uint32_t)(261 - imin(eb, 254)) << 23);
+    const bool odd = eb == 255;
+    intx8 part[3];
+    constexpr int kStep[2] = {5, 18};             // binades from a part to the next
+#pragma unroll
+    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[n][i] = odd ? 0.f : x[n][i] * up;
+#pragma unroll
+    for (int p = 0; p < 3; ++p)
+#pragma unroll
+      for (int n = 0; n < NQ; ++n)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          float* y = x[n] + 4 * c;
+          int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+          w = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
+          part[p][4 * n + c] = w;
+          if (p < 2) {
+            const xp_f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false);
+            const xp_f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+            const float m = (float)(1 << kStep[p]);
+            y[0] = (y[0] - lo[0]) * m;
+            y[1] = (y[1] - lo[1]) * m;
+            y[2] = (y[2] - hi[0]) * m;
+            y[3] = (y[3] - hi[1]) * m;
+          }
+        }
+    const int s0 = eb - 7, s1 = s0 - kStep[0], s2 = s1 - kStep[1];
+    if constexpr (HD == 128) {
+      qp[0] = part[0];
+      qp[1] = part[1];
+      qp[2] = part[2];
+      qs[0] = odd ? 255 : s0;
+      qs[1] = odd ? 255 : s1;
+      qs[2] = odd ? 255 : s2;
+    } else {                                      // two parts a product, 64 dims each
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        qp[0][c] = part[0][c];
+        qp[0][4 + c] = part[1][c];
+        qp[1][c] = part[2][c];
+        qp[1][4 + c] = 0;
+      }
+      qs[0] = odd ? 255 : (g < 2 ? s0 : s1);
+      qs[1] = odd ? 255 : s2;
+    }
+    const int p = prefix ? d.w.pos[tok] : p0 + tk;
+    const int hi = rv ? (d.causal ? imin(p + 1, kceil) : kceil) : kfloor;
+    const int lo = d.window > 0 ? imax(p - d.window + 1, kfloor) : kfloor;
+    sees = KvSees{lo, kfloor, (uint32_t)imax(hi - lo, 0),
+                  d.window > 0 ? (uint32_t)imax(imin(d.sinks, hi) - kfloor, 0) : 0u};
+  }
+  const int pmin = p0 + (prefix ? 0 : row0 / d.grp);
+  const int pmax = prefix ? en[15] : p0 + (row0 + nrows - 1) / d.grp;
+  const int whi = d.causal ? imin(pmin + 1, kceil) : kceil;
+  const int wlo = d.window > 0 ? imax(pmax - d.window + 1, kfloor) : kfloor;
+  const int wsink = d.window > 0 ? d.sinks : 0;
+
+  float m_run = -INFINITY, l_run = 0.f;           // the row's; l of this lane's keys
+  floatx4 o[NT];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) o[t] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+  auto work = [&](int t, Tile& x, Tile& next) __attribute__((always_inline)) {
+    const int k0 = tile_key(j + t);
+    if (t + NW < nj) fetch(j + t + NW, next);
+    const bool seen = k0 >= kfloor && k0 + kKvTile <= whi && (k0 >= wlo || k0 + kKvTile <= wsink);
+    // NaN blocks of V among keys that some row may not see leave the product
+    uint32_t odd = 0;                             // a bit a group: the lane's block of it is NaN
+    if (!seen) {
+#pragma unroll
+      for (int n = 0; n < 4; ++n) odd |= x.ve[n] > 252u ? 1u << n : 0u;
+    }
+    // ---- V to LDS ----
+    wave_lds_order();
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const float s = __uint_as_float((x.ve[n] > 252u ? (seen ? 255u : 0u) : x.ve[n]) << 23);
+#pragma unroll
+      for (int i = 0; i < HD / 32; ++i) {
+        const bool out = !seen && x.ve[n] > 252u;
+        *(lds_u32x4*)(uintptr_t)(vw + 16 * n * RB + 16 * ((HD / 32 * g + i) ^ sw)) =
+            f4_bf16x8(out ? 0u : x.v[n][i], s);
+      }
+    }
+    wave_lds_order();
+    // ---- scores ----
+    floatx4 s[4];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const int ke = x.ke[n] > 252u ? 255 : (int)x.ke[n];
+      s[n] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int p = QM - 1; p >= 0; --p) s[n] = mma16_f4f8(x.k[n], qp[p], s[n], ke, qs[p]);
+    }
+    if (!seen) {
+      const uint32_t a = (uint32_t)(k0 + 4 * g - sees.lo), b = (uint32_t)(k0 + 4 * g - sees.floor);
+#pragma unroll
+      for (int n = 0; n < 4; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          s[n][i] = ((a + 16 * n + i < sees.n) | (b + 16 * n + i < sees.s)) ? s[n][i] : -INFINITY;
+    }
+    // ---- softmax ----
+    constexpr float kLazy = 8.f;
+    float mt = s[0][0];
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mt = fmaxf(mt, s[n][i]);
+    mt = fmax_xor32(fmax_xor16(mt)) * d.scale2;
+    if (__ballot(mt > m_run + kLazy) != 0) {      // wave-uniform
+      const float mref = fmaxf(m_run, mt);
+      const float alpha = __builtin_amdgcn_exp2f(m_run - (mref == -INFINITY ? 0.f : mref));
+      l_run *= alpha;
+      m_run = mref;
+#pragma unroll
+      for (int u = 0; u < NT; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[u][i] *= alpha;
+    }
+    const float ref = m_run == -INFINITY ? 0.f : m_run;
+    u32x4 ph[2], pl[2];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], d.scale2, -ref));
+        l_run += s[n][i];
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float e0 = s[n][2 * i], e1 = s[n][2 * i + 1];
+        const uint32_t y = pk_bf16(e0, e1);
+        ph[n / 2][2 * (n % 2) + i] = y;
+        pl[n / 2][2 * (n % 2) + i] =
+            pk_bf16(e0 - __uint_as_float(y << 16), e1 - __uint_as_float(y & 0xFFFF0000u));
+      }
+    }
+    // ---- P V, 32 keys at a time ----
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      u32x4 v[NT];
+#pragma unroll
+      for (int u = 0; u < NT; ++u) {
+        const uint2 lo = lds_tr16((vr ^ (32 * u)) + 32 * h * RB);
+        const uint2 hi = lds_tr16((vr ^ (32 * u)) + (32 * h + 16) * RB);
+        v[u] = u32x4{lo.x, lo.y, hi.x, hi.y};
+      }
+#pragma unroll
+      for (int u = 0; u < NT; ++u) o[u] = mma16_bf16(v[u], pl[h], o[u]);
+#pragma unroll
+      for (int u = 0; u < NT; ++u) o[u] = mma16_bf16(v[u], ph[h], o[u]);
+    }
+    if (__builtin_expect(__ballot(odd != 0) != 0, 0)) {
+      // rows with a numerator for such a key are NaN in its block's dims.  The key li of
+      // group n, block of lane (li, g): its numerator is element li % 4 of s[n] in the
+      // lanes 16 (li / 4) + row
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        uint64_t who = __ballot((odd >> n) & 1u);
+        while (who != 0) {                        // wave-uniform
+          const int src = __builtin_ctzll(who);
+          who &= who - 1;
+          const int key = src & 15, part = src >> 4;
+          const float mine = key % 4 == 0 ? s[n][0] : (key % 4 == 1 ? s[n][1] : (key % 4 == 2 ? s[n][2] : s[n][3]));
+          const float pk = __shfl(mine, 16 * (key / 4) + li, kWave);
+#pragma unroll
+          for (int u = 0; u < NT; ++u) {
+            // the lane's HD / 4 dims from HD / 4 part on, all of their block's
+            if ((16 * u) / (HD / 4) == part && pk > 0.f)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) o[u][i] = NAN;
+          }
+        }
+      }
+    }
+  };
+#pragma unroll 1
+  for (int t = wave; t < nj; t += 2 * NW) {
+    work(t, ta, tc);
+    if (t + NW < nj) work(t + NW, tc, ta);
+  }
+  // ---- the waves' results ----
+  l_run = fsum_xor32(fsum_xor16(l_run));
+  __syncthreads();                                // every wave's reads of its ring done
+  float* mg = reinterpret_cast<float*>(lds) + wave * (kRing / 4) + lane;
+  mg[0] = m_run;
+  mg[kWave] = l_run;
+  floatx4* mo = reinterpret_cast<floatx4*>(ring + 2 * kWave * 4) + lane;
+#pragma unroll
+  for (int u = 0; u < NT; ++u) mo[u * kWave] = o[u];
+  __syncthreads();
+  // wave w adds the blocks w, w + NW, .. of 16 dims
+  {
+    float M = -INFINITY, wt[NW], l = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      wt[w] = reinterpret_cast<const float*>(lds)[w * (kRing / 4) + lane];
+      M = fmaxf(M, wt[w]);
+    }
+    const float Ms = M == -INFINITY ? 0.f : M;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      wt[w] = __builtin_amdgcn_exp2f(wt[w] - Ms);
+      l += wt[w] * reinterpret_cast<const float*>(lds)[w * (kRing / 4) + kWave + lane];
+    }
+    const int row = row0 + li, tk = row / d.grp;
+    const int64_t tok = tok0 + tk;
+    const int hd_ = kvh * d.grp + (row - tk * d.grp);
+    const bool done = whole && d.groups == 0;
+    const int64_t prow = whole ? d.row0 + ((int64_t)prefix * d.total_q + tok) * d.nh + hd_
+                               : d.part0 + (int64_t)(2 * sidx + (j == 0 ? 1 : 0)) * kFewRows + li;
+    const float inv = l == 0.f ? (sees_some(d, p0 + tk, kceil) ? NAN : 0.f) : 1.f / l;
+#pragma unroll
+    for (int u0 = 0; u0 < NT; u0 += NW) {
+      const int u = u0 + wave;
+      if (NT % NW != 0 && u >= NT) break;         // whole wave
+      floatx4 y{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        const floatx4 x = reinterpret_cast<const floatx4*>(lds + w * kRing + 2 * kWave * 4)[u * kWave + lane];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] += wt[w] * x[i];
+      }
+      if (rv && done) {
+        *reinterpret_cast<uint2*>(d.out + tok * d.out_ld + (int64_t)hd_ * HD + 16 * u + 4 * g) =
+            uint2{pk_bf16(y[0] * inv, y[1] * inv), pk_bf16(y[2] * inv, y[3] * inv)};
+      } else if (rv) {
+        *reinterpret_cast<floatx4*>(d.w.part + prow * HD + 16 * u + 4 * g) = y;
+      }
+    }
+    if (rv && wave == 0 && g == 0) {
+      if (!done) {
+        *reinterpret_cast<float2*>(d.w.ml + 2 * prow) = float2{M, l};
+      } else if (d.lse != nullptr) {
+        d.lse[tok * d.nh + hd_] =
+            l == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+      }
+    }
+  }
+  if (bad != 0) atomicOr(d.err, bad);
+  // ---- on to the next segment of the share ----
+  if (f >= f1) return;                            // whole workgroup
+  j = -kSegUnits;
+  if (++kvh == d.nkv) {
+    kvh = 0;
+    ++e;
+  }
+  __syncthreads();                                // the merge is read
+  }
+}
+
+// ---------------------------------------------------------------------------
 // Joining.  Part (m_i, l_i, O_i) of a row: O = sum 2^(m_i - M) O_i, l likewise,
 // M = max m_i, parts in order.  A workgroup per share and 1024 / head_dim rows, most of
 // which find nothing cut: 4 us, 12 to 17 with a tile of 128 or 256 rows for every
@@ -1442,13 +1884,16 @@ __global__ __launch_bounds__(256) void k_kv_join_rows(const KvDev d, const KvJoi
 static int kv_most(const xp_kv* kv) { return kv->hd == 64 ? 128 : 256; }
 static int kv_rows(const xp_kv* kv, int64_t rows) {
   const int most = kv_most(kv);
+  if (rows <= kFewRows && kv->dtype == XP_MXFP4) return kFewRows;   // k_kv_few
   return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : most;
 }
+constexpr int kFewWaves = 4;
 // Workgroups of a CU: 8 waves (12, see above), or as many as the rings leave room for (a
 // ring of two 32 KB stages twice).  128 rows over an 8-bit cache as two workgroups of 4
 // waves: 64 blocks of 32 over 8192 keys 405 us as one of 8, 378 so; 256 rows as two
 // tiles of them 3 to 7% slower.
 static int kv_wgs(const xp_kv* kv, int R) {
+  if (R == kFewRows) return 8 / kFewWaves;        // two waves a SIMD
   if (kv->hd == 64) return R >= 128 ? 3 : (R == 64 ? 2 : 4);
   const bool f8 = kv->dtype == XP_E4M3;
   return R >= 128 ? (f8 && R == 128 ? 2 : 1) : (f8 && R == 32 ? 4 : 2);
@@ -1459,11 +1904,12 @@ void kv_attn_sizes(const xp_kv* kv, int64_t* rows, int* entries, int* shares) {
   const int64_t all = (int64_t)kv->max_tokens * kv->grp;
   const int R = kv_rows(kv, all);
   *rows = 0;
-  for (int r = 32; r <= R; r *= 2) *rows = std::max(*rows, (int64_t)2 * kv_shares(kv, r) * r);
+  const int least = kv_least(kv);
+  for (int r = least; r <= R; r *= 2) *rows = std::max(*rows, (int64_t)2 * kv_shares(kv, r) * r);
   // every sequence (group) rounds its rows up to whole tiles
-  *entries = (int)((all + 31) / 32 + kv->max_batch);
+  *entries = (int)((all + least - 1) / least + kv->max_batch);
   *shares = 0;
-  for (int r = 32; r <= R; r *= 2) *shares = std::max(*shares, kv_shares(kv, r));
+  for (int r = least; r <= R; r *= 2) *shares = std::max(*shares, kv_shares(kv, r));
 }
 
 // one list's attention, in tiles of R rows
@@ -1479,7 +1925,18 @@ static hipError_t launch_list(const xp_kv* kv, int R, bool own, const KvDev& d, 
                          dim3((WR_) * (WK_) * kWave), 0, st, d);                                 \
   } while (0)
   const int fmt = kv->dtype;
-  if (kv->hd == 128 && fmt == XP_BF16) {
+  if (R == kFewRows) {
+#define XP_FEW(HD_, OWN_)                                                                       \
+  hipLaunchKernelGGL((k_kv_few<HD_, kFewWaves, OWN_>), dim3(shares), dim3(kFewWaves * kWave), 0, st, d)
+    if (kv->hd == 128) {
+      if (own) XP_FEW(128, true);
+      else XP_FEW(128, false);
+    } else {
+      if (own) XP_FEW(64, true);
+      else XP_FEW(64, false);
+    }
+#undef XP_FEW
+  } else if (kv->hd == 128 && fmt == XP_BF16) {
     if (R == 32) XP_KV(128, XP_BF16, 1, 2, 2, 2);
     else if (R == 64) XP_KV(128, XP_BF16, 2, 2, 2, 2);
     else if (R == 128) XP_KV(128, XP_BF16, 4, 2, 4, 1);
@@ -1535,7 +1992,7 @@ hipError_t launch_kv_attn(const xp_kv* kv, const KvAttnArgs& a, hipStream_t st) 
   p.window = a.window;
   p.sinks = a.sinks;
   p.groups = a.groups;
-  p.entries = (int)((int64_t)a.total_q * kv->grp / 32 + a.n);   // of a list: no more fit the tokens
+  p.entries = (int)((int64_t)a.total_q * kv->grp / kv_least(kv) + a.n);   // of a list: no more fit the tokens
   for (int k = 0; k < lists; ++k) {
     p.R[k] = R[k];
     p.shares[k] = kv_shares(kv, R[k]);

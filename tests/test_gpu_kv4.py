@@ -71,8 +71,6 @@ def test_write_and_read_back(hd, n_kv, P, tokens):
     for got, cache in ((gk, kc), (gv, vc)):
         want = _values(cache, P, hd).transpose(0, 2, 1, 3).reshape(-1, n_kv, hd)[order]
         want[order < 0] = 0
-        # exponents 253 and 254 of the first contents: beyond bf16's range is infinite
-        want = torch.tensor(want).to(torch.bfloat16).double().numpy()
         assert np.array_equal(got.double().cpu().numpy(), want, equal_nan=True)
     assert (wide[:, :16] == 9).all() and (wide[:, 16 + row:] == 9).all()
     only, none = kv.read(_i32(order), kc, vc, v=False)
@@ -119,9 +117,8 @@ def test_read_of_every_code_and_exponent():
     exps = np.arange(16 * 256 * 4).reshape(16, 1, 256, 4).astype(np.uint8)
     c = torch.tensor(R.pack_mxfp4(codes, exps)).cuda()
     k, v = kv.read(_i32(np.arange(4096)), c, c)
-    with np.errstate(over="ignore"):
-        want = torch.tensor(R.mxfp4_values(codes, exps)).reshape(4096, 1, 128).to(torch.bfloat16)
-    assert np.array_equal(k.double().cpu().numpy(), want.double().numpy(), equal_nan=True)
+    want = R.mxfp4_values(codes, exps).reshape(4096, 1, 128)
+    assert np.array_equal(k.double().cpu().numpy(), want, equal_nan=True)
     assert torch.equal(k.view(torch.int16), v.view(torch.int16))
     kv.close()
 
@@ -219,9 +216,9 @@ def test_attend4(name, hd, P):
 
 @pytest.mark.parametrize("hd", [64, 128])
 @pytest.mark.parametrize("ql", [[1, 1], [5, 16], [40, 90], [90, 70]])
-def test_unseen_keys_hold_nan_and_infinite_exponents(hd, ql):
+def test_unseen_keys_hold_nan(hd, ql):
     """Keys in front of the window, behind the last one and later than a token are NaN
-    (exponent 255) or so large that bf16 makes them infinite (253, 254)."""
+    (exponents above 252)."""
     kv_len, W = [150, 203], 100
     c = Call4(20 + sum(ql), kv_len, ql, heads=4, n_kv=2, hd=hd, P=64)
     for i, (b, j) in enumerate([(b, j) for b in range(2)
