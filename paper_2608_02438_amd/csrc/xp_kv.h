@@ -142,7 +142,7 @@ hipError_t launch_kv_read(const xp_kv* kv, int tokens, const int32_t* slots, con
 // `tokens` tokens and tables of table_ld pages
 bool kv_units_fit(const xp_kv* kv, int64_t tokens, int64_t n, int groups, int64_t table_ld);
 // rows of the smallest row tile
-inline int kv_least(const xp_kv* kv) { return kv->dtype == XP_MXFP4 ? 16 : 32; }
+inline int kv_least(const xp_kv* kv) { return kv->dtype == XP_MXFP4 ? 8 : 32; }
 // rows of partials and entries a handle needs
 void kv_attn_sizes(const xp_kv* kv, int64_t* rows, int* entries, int* shares);
 

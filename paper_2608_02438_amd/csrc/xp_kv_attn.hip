@@ -47,6 +47,14 @@ __device__ __forceinline__ float fsum_xor16(float x) {
   const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
+__device__ __forceinline__ uint32_t umax_xor16(uint32_t x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  return max(r[0], r[1]);
+}
+__device__ __forceinline__ uint32_t umax_xor32(uint32_t x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return max(r[0], r[1]);
+}
 __device__ __forceinline__ int imin(int a, int b) { return a < b ? a : b; }
 __device__ __forceinline__ int imax(int a, int b) { return a > b ? a : b; }
 
@@ -1303,7 +1311,7 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
 }
 
 // ---------------------------------------------------------------------------
-// Few rows over a 4-bit cache: up to 16 of a tile (single tokens, short blocks).
+// Few rows over a 4-bit cache: up to 8 or 16 of a tile (single tokens, short blocks).
 // A cache of 68 bytes a key (head_dim 128) leaves a third of the time a key that 8 bits
 // leave, so nothing may be done for rows that are not there, and little a key:
 //
@@ -1312,20 +1320,25 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
 //   from the load into the product.  The queries are its e4m3 operand, in three parts:
 //   a row's largest element lies in [2^7, 2^8), the first part takes 4 bits, the second
 //   the next 4 (all that bf16 has, for elements above 2^-13 of the largest), the third
-//   what lies deeper; what is left is 2^-39 of the largest.
+//   what lies deeper, where a row of the tile has such bits; what is left is 2^-39 of the
+//   largest.
 // * V's power of two differs from key to key, the dimension that P V sums over, where
 //   the instruction takes one for 32: V is expanded to bf16 (exactly) on its way into
 //   the wave's LDS and comes back by transposing reads.
-// * O^T = V^T P^T on v_mfma_f32_16x16x32_bf16, P in two bf16 parts.  A lane has one row
-//   (l % 16) in S and in O; its numerators are the next product's operand.
+// * O^T = V^T P^T on v_mfma_f32_16x16x32_bf16, P in two bf16 parts.  A lane has one
+//   column of S and of O; its numerators are the next product's operand.
+// * Up to 8 rows: a column is a row and a part, so that one product has the first two
+//   parts of Q, and one both parts of P (its 16 x 16 take 30 cycles whatever they hold).
 //
 // NW waves take a share's tiles of 64 keys in turn, each with its own statistics and
 // no barrier, the next tile on its way while one is worked on; at a segment's end their
-// results are added through LDS.
+// results are added through LDS.  A wave issues an instruction in 8 cycles at most, a SIMD
+// in 4: three waves of 168 registers.
 // ---------------------------------------------------------------------------
 typedef int intx8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) char lds_char;
-constexpr int kFewRows = 16;
+constexpr int kFewRows = 16;         // the larger row tile
+constexpr int kFewSimd = 3;          // waves of a SIMD
 
 __device__ __forceinline__ floatx4 mma16_bf16(u32x4 a, u32x4 b, floatx4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
@@ -1343,23 +1356,33 @@ __device__ __forceinline__ uint2 lds_tr16(uint32_t at) {
   return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(uintptr_t)at));
 }
 
-template <int HD, int NW, bool OWN>
-__global__ __launch_bounds__(NW* kWave, 2) void k_kv_few(const KvDev d) {
-  using SH = KvRows<HD, false>;                   // V's rows in LDS
-  constexpr int NT = HD / 16, RB = SH::RB, CPR = SH::CPR, QM = HD == 128 ? 3 : 2;
+// of the column 8 further in the lane's 16
+__device__ __forceinline__ float other_half(float x) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(x), 0x128, 0xF, 0xF, true));
+}
+
+template <int HD, int R, int NW, bool OWN>
+__global__ __launch_bounds__(NW* kWave, kFewSimd) void k_kv_few(const KvDev d) {
+  // rows of V in LDS, 16 bytes apart from the next: neither the 16-byte writes of 16 rows
+  // nor the transposing reads meet in a bank, and every address is one register and an
+  // offset
+  constexpr int NT = HD / 16, RB = 2 * HD + 16;
+  constexpr bool HALF = R == 8;                   // a column is a row and a part
+  // products of the first two parts, and of the third
+  constexpr int QM = HALF || HD == 64 ? 1 : 2, QD = HALF && HD == 64 ? 0 : 1;
   constexpr int RBM = kv_row_bytes(XP_MXFP4, HD);
-  constexpr int kRing = kKvTile * RB;             // bytes of LDS a wave
   constexpr int kMerge = (4 * NT + 2) * kWave;    // floats that a wave hands over
-  static_assert(kMerge * 4 <= kRing, "merge in LDS");
+  constexpr int kRing = kMerge * 4 > 32 * RB ? kMerge * 4 : 32 * RB;   // its LDS: V of half a tile
+  static_assert(kRing % 256 == 0, "a wave's LDS");
   __shared__ __align__(256) char lds[NW * kRing];
   __shared__ KvEntry own_ent[OWN ? kOwnEntries : 1];
   __shared__ int32_t own_sh[8];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int li = lane & 15, g = lane >> 4;
+  const int li = lane & 15, g = lane >> 4, ri = li & (R - 1);   // column, its keys; its row
   const int sidx = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
   if constexpr (OWN) {
-    if (wave == 0) plan_own(d, kFewRows, gridDim.x, sidx, own_ent, own_sh);
+    if (wave == 0) plan_own(d, R, gridDim.x, sidx, own_ent, own_sh);
     __syncthreads();
   }
   auto share = [&](int i) {
@@ -1376,14 +1399,10 @@ __global__ __launch_bounds__(NW* kWave, 2) void k_kv_few(const KvDev d) {
   const uint32_t vo = li * (HD / 2) + (HD / 8) * g;
   const uint32_t veo = li * (HD / 32) + (HD == 128 ? g : g >> 1);
   char* ring = lds + wave * kRing;
-  // V into LDS: row 16 n + li, chunks HD / 32 g + i; back: rows 4 g + (li / 4), block dt
-  // of 16 dims, 4 dims a lane
-  const uint32_t vw = lds_byte(ring) + li * RB, sw = SH::swz(li);
-  uint32_t vr;
-  {
-    const int r = 4 * g + (li >> 2);
-    vr = lds_byte(ring) + r * RB + 16 * (((li & 3) >> 1) ^ SH::swz(r)) + 8 * (li & 1);
-  }
+  // V into LDS: row 16 n + li, 16 bytes HD / 32 g + i; back: rows 4 g + li / 4, dims
+  // 16 u + 4 (li % 4) + 0..3 of the row, which make the lane's dim 16 u + li
+  const uint32_t vw = lds_byte(ring) + li * RB + HD / 2 * g;
+  const uint32_t vr = lds_byte(ring) + (4 * g + (li >> 2)) * RB + 8 * (li & 3);
   const int P1 = (1 << d.logP) - 1;
   const uint32_t exps = (uint32_t)(HD / 2) << d.logP;      // from a page's codes to its exponents
   for (;;) {
@@ -1404,66 +1423,72 @@ __global__ __launch_bounds__(NW* kWave, 2) void k_kv_few(const KvDev d) {
   const bool whole = nj == tiles;
   auto tile_key = [&](int t) { return kKvTile * (t < n1 ? a0 + t : b0 + t - n1); };
 
-  // ---- loads of a tile: 4 groups of 16 keys ----
+  // ---- loads of a tile: 4 groups of 16 keys, wherever their pages lie ----
+  // Keys that no row sees are loaded like the others: their scores are masked, and blocks
+  // of V that are NaN leave the product where a row may not see their key.
   const scalar_i32 tb = as_scalar(d.table + (int64_t)seq * d.table_ld);
-  const int64_t head = ((int64_t)kvh << d.logP) * RBM;
+  const uint64_t head = (uint64_t)((int64_t)kvh << d.logP) * RBM;
   const uint32_t page_bytes = (uint32_t)(d.nkv * RBM) << d.logP;
-  const int kin = imax(klo, kfloor);
   uint32_t bad = 0;
-  struct Tile {
-    u32x4 k[4], v[4];
-    uint32_t ke[4], ve[4];
-  };
-  auto fetch = [&](int t, Tile& x) __attribute__((always_inline)) {
+  u32x4 kx[4], vx[4];
+  uint32_t ke[4], ve[4];
+  int pg[4];                                      // the next tile's pages
+  auto pages = [&](int t) __attribute__((always_inline)) {
     const int k0 = tile_key(t);
-    const bool inner = ((k0 >= kin) & (k0 + kKvTile <= khi)) | ((k0 >= kfloor) & (k0 + kKvTile <= ks_));
+#pragma unroll
+    for (int n = 0; n < 4; ++n) pg[n] = tb[imin((k0 + 16 * n) >> d.logP, d.cols - 1)];
+  };
+  auto fetch = [&](auto isv, int t, u32x4 (&x)[4], uint32_t (&ex)[4]) __attribute__((always_inline)) {
+    constexpr bool V = decltype(isv)::value;
+    const char* const base = (V ? d.vc : d.kc) + head;
+    const uint32_t xo = V ? vo : ko, eo = V ? veo : keo;
+    const int k0 = tile_key(t);
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
       const int g0 = k0 + 16 * n, r = g0 & P1;
-      const uint32_t page = (uint32_t)tb[imin(g0 >> d.logP, d.cols - 1)];
-      const bool ok = page < (uint32_t)d.n_pages;
-      const int64_t at = head + (int64_t)((uint64_t)(ok ? page : 0u) * page_bytes);
-      const char *kc = d.kc + at + r * (HD / 2) + ko, *ke = d.kc + at + exps + r * (HD / 32) + keo;
-      const char *vc = d.vc + at + r * (HD / 2) + vo, *ve = d.vc + at + exps + r * (HD / 32) + veo;
-      if (inner) {
-        bad |= ok ? 0u : XP_DEVERR_PAGE;
-      } else {
-        const int from = imax(g0, kfloor), to = imin(g0 + 16, khi), key = g0 + li;
-        bad |= (!ok & (from < to) & ((to > klo) | (from < ks_))) ? XP_DEVERR_PAGE : 0u;
-        const bool any = (key >= kfloor) & (key < khi) & ((key >= klo) | (key < ks_));
-        kc = any ? kc : d.w.zero;
-        ke = any ? ke : d.w.zero;
-        vc = any ? vc : d.w.zero;
-        ve = any ? ve : d.w.zero;
+      uint32_t page = (uint32_t)pg[n];
+      if (page >= (uint32_t)d.n_pages) {          // wave-uniform
+        const int from = imax(g0, kfloor), to = imin(g0 + 16, khi);
+        bad |= ((from < to) & ((to > klo) | (from < ks_))) ? XP_DEVERR_PAGE : 0u;
+        page = 0;
       }
-      x.k[n] = ld16_nt(kc);
-      if constexpr (HD == 128) {
-        x.v[n] = ld16_nt(vc);
+      // wave-uniform addresses: scalar registers and the lane's bytes
+      uint64_t codes = (uint64_t)(uintptr_t)base + (uint64_t)page * page_bytes + (uint32_t)(r * (HD / 2));
+      uint64_t ep = codes + exps - (uint32_t)(r * (HD / 2 - HD / 32));
+      asm volatile("" : "+s"(codes), "+s"(ep));
+      if constexpr (HD == 128 || !V) {
+        x[n] = ld16_nt((const char*)(uintptr_t)codes + xo);
       } else {
         typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-        const u32x2 y = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(vc));
-        x.v[n] = u32x4{y[0], y[1], 0u, 0u};
+        const u32x2 y = __builtin_nontemporal_load(
+            reinterpret_cast<const u32x2*>((const char*)(uintptr_t)codes + xo));
+        x[n] = u32x4{y[0], y[1], 0u, 0u};
       }
-      x.ke[n] = *reinterpret_cast<const uint8_t*>(ke);
-      x.ve[n] = *reinterpret_cast<const uint8_t*>(ve);
+      ex[n] = *reinterpret_cast<const uint8_t*>((const char*)(uintptr_t)ep + eo);
     }
   };
-  Tile ta, tc;
-  if (wave < nj) fetch(j + wave, ta);
+  constexpr std::integral_constant<bool, false> isk{};
+  constexpr std::integral_constant<bool, true> isv{};
+  if (wave < nj) {
+    pages(j + wave);
+    fetch(isk, j + wave, kx, ke);
+    fetch(isv, j + wave, vx, ve);
+    pages(j + imin(wave + NW, nj - 1));
+  }
 
   // ---- the query rows ----
-  const bool rv = li < nrows;
+  const bool rv = ri < nrows;
   KvSees sees;
-  intx8 qp[QM];
-  int qs[QM];
+  intx8 qp[QM + QD];
+  int qs[QM + QD];
+  bool deep = false;                              // some row has a third part
   {
-    const int row = row0 + (rv ? li : 0), tk = row / d.grp;
+    const int row = row0 + (rv ? ri : 0), tk = row / d.grp;
     const int64_t tok = tok0 + tk;
     const uint16_t* q = d.q + tok * d.q_ld + (int64_t)(kvh * d.grp + (row - tk * d.grp)) * HD;
     constexpr int NQ = HD / 64;                   // pieces of 16 dims: 16 g, and 64 + 16 g
-    float x[NQ][16];
-    float top = 0.f;
-    bool num = true;
+    uint32_t x[NQ][8];
+    uint32_t top = 0;                             // the greatest magnitudes, two of 16 bits
 #pragma unroll
     for (int n = 0; n < NQ; ++n)
 #pragma unroll
@@ -1471,68 +1496,79 @@ __global__ __launch_bounds__(NW* kWave, 2) void k_kv_few(const KvDev d) {
         const u32x4 y = ld16(q + 64 * n + 16 * g + 8 * c);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          x[n][8 * c + 2 * i] = __uint_as_float(y[i] << 16);
-          x[n][8 * c + 2 * i + 1] = __uint_as_float(y[i] & 0xffff0000u);
+          x[n][4 * c + i] = y[i];
+          top = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(
+              __builtin_bit_cast(ushort2v, top), __builtin_bit_cast(ushort2v, y[i] & 0x7fff7fffu)));
         }
       }
-#pragma unroll
-    for (int n = 0; n < NQ; ++n)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        num &= fabsf(x[n][i]) < INFINITY;
-        top = fmaxf(top, fabsf(x[n][i]));
-      }
-    top = fmax_xor16(num ? top : INFINITY);
-    top = fmax_xor32(top);
+    const uint32_t most = umax_xor32(umax_xor16(max(top >> 16, top & 0xffffu)));
     // 2^7 <= x < 2^8 for the largest; an infinity or NaN makes the row's scores NaN
-    const int eb = imax((int)(__float_as_uint(top) >> 23), 31);
+    const bool odd = most >= 0x7f80u;
+    const int eb = imax((int)(most >> 7), 31), s0 = eb - 7, s1 = s0 - 5, s2 = s1 - 18;
     const float up = __uint_as_float((uint32_t)(261 - imin(eb, 254)) << 23);
-    const bool odd = eb == 255;
     intx8 part[3];
-    constexpr int kStep[2] = {5, 18};             // binades from a part to the next
+    uint32_t rest = 0;
 #pragma unroll
     for (int n = 0; n < NQ; ++n)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) x[n][i] = odd ? 0.f : x[n][i] * up;
+      for (int c = 0; c < 4; ++c) {
+        float y[4];
 #pragma unroll
-    for (int p = 0; p < 3; ++p)
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t w = odd ? 0u : x[n][2 * c + i / 2];
+          y[i] = __uint_as_float(i % 2 == 0 ? w << 16 : w & 0xffff0000u) * up;
+        }
 #pragma unroll
-      for (int n = 0; n < NQ; ++n)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          float* y = x[n] + 4 * c;
+        for (int p = 0; p < 3; ++p) {
           int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
           w = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
           part[p][4 * n + c] = w;
-          if (p < 2) {
+          if (p < 2) {                            // 5 and 18 binades from a part to the next
             const xp_f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false);
             const xp_f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
-            const float m = (float)(1 << kStep[p]);
+            const float m = p == 0 ? 0x1p5f : 0x1p18f;
             y[0] = (y[0] - lo[0]) * m;
             y[1] = (y[1] - lo[1]) * m;
             y[2] = (y[2] - hi[0]) * m;
             y[3] = (y[3] - hi[1]) * m;
           }
         }
-    const int s0 = eb - 7, s1 = s0 - kStep[0], s2 = s1 - kStep[1];
-    if constexpr (HD == 128) {
-      qp[0] = part[0];
-      qp[1] = part[1];
-      qp[2] = part[2];
-      qs[0] = odd ? 255 : s0;
-      qs[1] = odd ? 255 : s1;
-      qs[2] = odd ? 255 : s2;
-    } else {                                      // two parts a product, 64 dims each
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        qp[0][c] = part[0][c];
-        qp[0][4 + c] = part[1][c];
-        qp[1][c] = part[2][c];
-        qp[1][4 + c] = 0;
+        rest |= (uint32_t)part[2][4 * n + c] & 0x7f7f7f7fu;
       }
-      qs[0] = odd ? 255 : (g < 2 ? s0 : s1);
-      qs[1] = odd ? 255 : s2;
+    deep = __ballot(rest != 0) != 0;
+    const bool second = HALF && li >= 8;          // the columns of second parts
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      if constexpr (HD == 128 && !HALF) {
+        qp[0][c] = part[0][c];
+        qp[1][c] = part[1][c];
+        qp[2][c] = part[2][c];
+      } else if constexpr (HD == 128) {
+        qp[0][c] = second ? part[1][c] : part[0][c];
+        qp[1][c] = second ? 0 : part[2][c];
+      } else {                                    // two parts a product, 64 dims each
+        const int a = part[c / 4][c % 4], b = c < 4 ? part[2][c % 4] : 0;
+        if constexpr (HALF) {
+          qp[0][c] = second ? b : a;
+        } else {
+          qp[0][c] = a;
+          qp[1][c] = b;
+        }
+      }
     }
+    if constexpr (HD == 128 && !HALF) {
+      qs[0] = s0;
+      qs[1] = s1;
+      qs[2] = s2;
+    } else if constexpr (HD == 128) {
+      qs[0] = second ? s1 : s0;
+      qs[1] = s2;
+    } else {
+      qs[0] = second ? s2 : (g < 2 ? s0 : s1);
+      if constexpr (!HALF) qs[1] = s2;
+    }
+#pragma unroll
+    for (int i = 0; i < QM + QD; ++i) qs[i] = odd ? 255 : qs[i];
     const int p = prefix ? d.w.pos[tok] : p0 + tk;
     const int hi = rv ? (d.causal ? imin(p + 1, kceil) : kceil) : kfloor;
     const int lo = d.window > 0 ? imax(p - d.window + 1, kfloor) : kfloor;
@@ -1550,46 +1586,57 @@ __global__ __launch_bounds__(NW* kWave, 2) void k_kv_few(const KvDev d) {
 #pragma unroll
   for (int t = 0; t < NT; ++t) o[t] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-  auto work = [&](int t, Tile& x, Tile& next) __attribute__((always_inline)) {
+  auto v_write = [&](int h) __attribute__((always_inline)) {   // V of half a tile to LDS
+    wave_lds_order();
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      const float s = __uint_as_float(ve[2 * h + n] << 23);
+#pragma unroll
+      for (int i = 0; i < HD / 32; ++i)
+        *(lds_u32x4*)(uintptr_t)(vw + 16 * n * RB + 16 * i) = f4_bf16x8(vx[2 * h + n][i], s);
+    }
+    wave_lds_order();
+  };
+#pragma unroll 1
+  for (int t = wave; t < nj; t += NW) {
     const int k0 = tile_key(j + t);
-    if (t + NW < nj) fetch(j + t + NW, next);
+    const bool more = t + NW < nj;
+    // every row sees every key of the tile
     const bool seen = k0 >= kfloor && k0 + kKvTile <= whi && (k0 >= wlo || k0 + kKvTile <= wsink);
-    // NaN blocks of V among keys that some row may not see leave the product
-    uint32_t odd = 0;                             // a bit a group: the lane's block of it is NaN
-    if (!seen) {
+    // exponents above 252 are NaN; rarely there, so all are looked at together
+    if (__builtin_expect(__ballot(max(max(ke[0], ke[1]), max(ke[2], ke[3])) > 252u) != 0, 0)) {
 #pragma unroll
-      for (int n = 0; n < 4; ++n) odd |= x.ve[n] > 252u ? 1u << n : 0u;
+      for (int n = 0; n < 4; ++n) ke[n] = ke[n] > 252u ? 255u : ke[n];
     }
-    // ---- V to LDS ----
-    wave_lds_order();
-#pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      const float s = __uint_as_float((x.ve[n] > 252u ? (seen ? 255u : 0u) : x.ve[n]) << 23);
-#pragma unroll
-      for (int i = 0; i < HD / 32; ++i) {
-        const bool out = !seen && x.ve[n] > 252u;
-        *(lds_u32x4*)(uintptr_t)(vw + 16 * n * RB + 16 * ((HD / 32 * g + i) ^ sw)) =
-            f4_bf16x8(out ? 0u : x.v[n][i], s);
-      }
-    }
-    wave_lds_order();
     // ---- scores ----
     floatx4 s[4];
 #pragma unroll
-    for (int n = 0; n < 4; ++n) {
-      const int ke = x.ke[n] > 252u ? 255 : (int)x.ke[n];
-      s[n] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int n = 0; n < 4; ++n) s[n] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int p = QM - 1; p >= 0; --p) s[n] = mma16_f4f8(x.k[n], qp[p], s[n], ke, qs[p]);
+    for (int p = QM - 1; p >= 0; --p)
+#pragma unroll
+      for (int n = 0; n < 4; ++n) s[n] = mma16_f4f8(kx[n], qp[p], s[n], (int)ke[n], qs[p]);
+    if constexpr (QD > 0)
+      if (deep) {                                 // wave-uniform
+#pragma unroll
+        for (int n = 0; n < 4; ++n) s[n] = mma16_f4f8(kx[n], qp[QM], s[n], (int)ke[n], qs[QM]);
+      }
+    if constexpr (HALF) {                         // a row's parts
+#pragma unroll
+      for (int n = 0; n < 4; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[n][i] += other_half(s[n][i]);
     }
     if (!seen) {
-      const uint32_t a = (uint32_t)(k0 + 4 * g - sees.lo), b = (uint32_t)(k0 + 4 * g - sees.floor);
+      uint32_t a = (uint32_t)(k0 + 4 * g - sees.lo), b = (uint32_t)(k0 + 4 * g - sees.floor);
+      asm volatile("" : "+v"(a), "+v"(b));        // a branch of its own
 #pragma unroll
       for (int n = 0; n < 4; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           s[n][i] = ((a + 16 * n + i < sees.n) | (b + 16 * n + i < sees.s)) ? s[n][i] : -INFINITY;
     }
+    if (more) fetch(isk, j + t + NW, kx, ke);
     // ---- softmax ----
     constexpr float kLazy = 8.f;
     float mt = s[0][0];
@@ -1609,7 +1656,7 @@ __global__ __launch_bounds__(NW* kWave, 2) void k_kv_few(const KvDev d) {
         for (int i = 0; i < 4; ++i) o[u][i] *= alpha;
     }
     const float ref = m_run == -INFINITY ? 0.f : m_run;
-    u32x4 ph[2], pl[2];
+    u32x4 ph[2], pl[2];                           // the column's part; both parts
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
 #pragma unroll
@@ -1621,56 +1668,83 @@ __global__ __launch_bounds__(NW* kWave, 2) void k_kv_few(const KvDev d) {
       for (int i = 0; i < 2; ++i) {
         const float e0 = s[n][2 * i], e1 = s[n][2 * i + 1];
         const uint32_t y = pk_bf16(e0, e1);
-        ph[n / 2][2 * (n % 2) + i] = y;
-        pl[n / 2][2 * (n % 2) + i] =
-            pk_bf16(e0 - __uint_as_float(y << 16), e1 - __uint_as_float(y & 0xFFFF0000u));
+        const uint32_t z = pk_bf16(e0 - __uint_as_float(y << 16), e1 - __uint_as_float(y & 0xFFFF0000u));
+        ph[n / 2][2 * (n % 2) + i] = HALF && li >= 8 ? z : y;
+        if constexpr (!HALF) pl[n / 2][2 * (n % 2) + i] = z;
       }
     }
-    // ---- P V, 32 keys at a time ----
+    if (__builtin_expect(__ballot(max(max(ve[0], ve[1]), max(ve[2], ve[3])) > 252u) != 0, 0)) {
+      uint32_t odd = 0;                           // a bit a group: the lane's block is NaN
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      u32x4 v[NT];
-#pragma unroll
-      for (int u = 0; u < NT; ++u) {
-        const uint2 lo = lds_tr16((vr ^ (32 * u)) + 32 * h * RB);
-        const uint2 hi = lds_tr16((vr ^ (32 * u)) + (32 * h + 16) * RB);
-        v[u] = u32x4{lo.x, lo.y, hi.x, hi.y};
+      for (int n = 0; n < 4; ++n) {
+        if (ve[n] > 252u) {
+          // where a row may not see the key its NaN leaves the product
+          odd |= seen ? 0u : 1u << n;
+          ve[n] = seen ? 255u : 0u;
+          vx[n] = seen ? vx[n] : u32x4{0u, 0u, 0u, 0u};
+        }
       }
+      // Rows with a numerator for a key whose block is NaN are NaN in its dims.  Key li of
+      // group n, the dims of lane (li, g): the key's numerator is element li % 4 of s[n] in
+      // the lanes 16 (li / 4) + row.
+      uint32_t some = 0;
 #pragma unroll
-      for (int u = 0; u < NT; ++u) o[u] = mma16_bf16(v[u], pl[h], o[u]);
+      for (int n = 0; n < 4; ++n)
 #pragma unroll
-      for (int u = 0; u < NT; ++u) o[u] = mma16_bf16(v[u], ph[h], o[u]);
-    }
-    if (__builtin_expect(__ballot(odd != 0) != 0, 0)) {
-      // rows with a numerator for such a key are NaN in its block's dims.  The key li of
-      // group n, block of lane (li, g): its numerator is element li % 4 of s[n] in the
-      // lanes 16 (li / 4) + row
-#pragma unroll
+        for (int i = 0; i < 4; ++i) some |= s[n][i] > 0.f ? 1u << (4 * n + i) : 0u;
+#pragma unroll 1
       for (int n = 0; n < 4; ++n) {
         uint64_t who = __ballot((odd >> n) & 1u);
         while (who != 0) {                        // wave-uniform
-          const int src = __builtin_ctzll(who);
+          const int src = __builtin_ctzll(who), key = src & 15, part = src >> 4;
           who &= who - 1;
-          const int key = src & 15, part = src >> 4;
-          const float mine = key % 4 == 0 ? s[n][0] : (key % 4 == 1 ? s[n][1] : (key % 4 == 2 ? s[n][2] : s[n][3]));
-          const float pk = __shfl(mine, 16 * (key / 4) + li, kWave);
+          const uint32_t has = (uint32_t)__shfl((int)some, 16 * (key / 4) + li, kWave);
+          const bool hit = (has >> (4 * n + key % 4)) & 1u;
 #pragma unroll
-          for (int u = 0; u < NT; ++u) {
-            // the lane's HD / 4 dims from HD / 4 part on, all of their block's
-            if ((16 * u) / (HD / 4) == part && pk > 0.f)
+          for (int u = 0; u < NT; ++u)
+            if ((16 * u) / (HD / 4) == part && hit)
 #pragma unroll
               for (int i = 0; i < 4; ++i) o[u][i] = NAN;
-          }
         }
       }
     }
-  };
-#pragma unroll 1
-  for (int t = wave; t < nj; t += 2 * NW) {
-    work(t, ta, tc);
-    if (t + NW < nj) work(t + NW, tc, ta);
+    // ---- P V, 32 keys at a time ----
+    v_write(0);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      constexpr int NB = NT / 2;                  // blocks of dims at a time
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        u32x4 v[NB];
+#pragma unroll
+        for (int u = 0; u < NB; ++u) {
+          const uint2 lo = lds_tr16(vr + 32 * (c * NB + u)), hi = lds_tr16(vr + 32 * (c * NB + u) + 16 * RB);
+          v[u] = u32x4{lo.x, lo.y, hi.x, hi.y};
+        }
+        if (h == 0 && c == 1) {
+          v_write(1);
+          if (more) {
+            fetch(isv, j + t + NW, vx, ve);
+            pages(j + imin(t + 2 * NW, nj - 1));
+          }
+        }
+        if constexpr (!HALF) {
+#pragma unroll
+          for (int u = 0; u < NB; ++u) o[c * NB + u] = mma16_bf16(v[u], pl[h], o[c * NB + u]);
+        }
+#pragma unroll
+        for (int u = 0; u < NB; ++u) o[c * NB + u] = mma16_bf16(v[u], ph[h], o[c * NB + u]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
   }
   // ---- the waves' results ----
+  if constexpr (HALF) {                           // a row's parts
+#pragma unroll
+    for (int u = 0; u < NT; ++u)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[u][i] += other_half(o[u][i]);
+  }
   l_run = fsum_xor32(fsum_xor16(l_run));
   __syncthreads();                                // every wave's reads of its ring done
   float* mg = reinterpret_cast<float*>(lds) + wave * (kRing / 4) + lane;
@@ -1694,12 +1768,13 @@ __global__ __launch_bounds__(NW* kWave, 2) void k_kv_few(const KvDev d) {
       wt[w] = __builtin_amdgcn_exp2f(wt[w] - Ms);
       l += wt[w] * reinterpret_cast<const float*>(lds)[w * (kRing / 4) + kWave + lane];
     }
-    const int row = row0 + li, tk = row / d.grp;
+    const bool mine = li < imin(nrows, R);
+    const int row = row0 + (mine ? li : 0), tk = row / d.grp;
     const int64_t tok = tok0 + tk;
     const int hd_ = kvh * d.grp + (row - tk * d.grp);
     const bool done = whole && d.groups == 0;
     const int64_t prow = whole ? d.row0 + ((int64_t)prefix * d.total_q + tok) * d.nh + hd_
-                               : d.part0 + (int64_t)(2 * sidx + (j == 0 ? 1 : 0)) * kFewRows + li;
+                               : d.part0 + (int64_t)(2 * sidx + (j == 0 ? 1 : 0)) * R + li;
     const float inv = l == 0.f ? (sees_some(d, p0 + tk, kceil) ? NAN : 0.f) : 1.f / l;
 #pragma unroll
     for (int u0 = 0; u0 < NT; u0 += NW) {
@@ -1712,14 +1787,14 @@ __global__ __launch_bounds__(NW* kWave, 2) void k_kv_few(const KvDev d) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) y[i] += wt[w] * x[i];
       }
-      if (rv && done) {
+      if (mine && done) {
         *reinterpret_cast<uint2*>(d.out + tok * d.out_ld + (int64_t)hd_ * HD + 16 * u + 4 * g) =
             uint2{pk_bf16(y[0] * inv, y[1] * inv), pk_bf16(y[2] * inv, y[3] * inv)};
-      } else if (rv) {
+      } else if (mine) {
         *reinterpret_cast<floatx4*>(d.w.part + prow * HD + 16 * u + 4 * g) = y;
       }
     }
-    if (rv && wave == 0 && g == 0) {
+    if (mine && wave == 0 && g == 0) {
       if (!done) {
         *reinterpret_cast<float2*>(d.w.ml + 2 * prow) = float2{M, l};
       } else if (d.lse != nullptr) {
@@ -1884,7 +1959,7 @@ __global__ __launch_bounds__(256) void k_kv_join_rows(const KvDev d, const KvJoi
 static int kv_most(const xp_kv* kv) { return kv->hd == 64 ? 128 : 256; }
 static int kv_rows(const xp_kv* kv, int64_t rows) {
   const int most = kv_most(kv);
-  if (rows <= kFewRows && kv->dtype == XP_MXFP4) return kFewRows;   // k_kv_few
+  if (rows <= kFewRows && kv->dtype == XP_MXFP4) return rows <= 8 ? 8 : kFewRows;   // k_kv_few
   return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : most;
 }
 constexpr int kFewWaves = 4;
@@ -1893,7 +1968,7 @@ constexpr int kFewWaves = 4;
 // waves: 64 blocks of 32 over 8192 keys 405 us as one of 8, 378 so; 256 rows as two
 // tiles of them 3 to 7% slower.
 static int kv_wgs(const xp_kv* kv, int R) {
-  if (R == kFewRows) return 8 / kFewWaves;        // two waves a SIMD
+  if (R <= kFewRows) return 4 * kFewSimd / kFewWaves;
   if (kv->hd == 64) return R >= 128 ? 3 : (R == 64 ? 2 : 4);
   const bool f8 = kv->dtype == XP_E4M3;
   return R >= 128 ? (f8 && R == 128 ? 2 : 1) : (f8 && R == 32 ? 4 : 2);
@@ -1925,16 +2000,17 @@ static hipError_t launch_list(const xp_kv* kv, int R, bool own, const KvDev& d, 
                          dim3((WR_) * (WK_) * kWave), 0, st, d);                                 \
   } while (0)
   const int fmt = kv->dtype;
-  if (R == kFewRows) {
-#define XP_FEW(HD_, OWN_)                                                                       \
-  hipLaunchKernelGGL((k_kv_few<HD_, kFewWaves, OWN_>), dim3(shares), dim3(kFewWaves * kWave), 0, st, d)
-    if (kv->hd == 128) {
-      if (own) XP_FEW(128, true);
-      else XP_FEW(128, false);
-    } else {
-      if (own) XP_FEW(64, true);
-      else XP_FEW(64, false);
-    }
+  if (R <= kFewRows) {
+#define XP_FEW(HD_, R_)                                                                         \
+  do {                                                                                           \
+    const dim3 grid(shares), block(kFewWaves * kWave);                                           \
+    if (own) hipLaunchKernelGGL((k_kv_few<HD_, R_, kFewWaves, true>), grid, block, 0, st, d);    \
+    else hipLaunchKernelGGL((k_kv_few<HD_, R_, kFewWaves, false>), grid, block, 0, st, d);       \
+  } while (0)
+    if (kv->hd == 128 && R == 8) XP_FEW(128, 8);
+    else if (kv->hd == 128) XP_FEW(128, 16);
+    else if (R == 8) XP_FEW(64, 8);
+    else XP_FEW(64, 16);
 #undef XP_FEW
   } else if (kv->hd == 128 && fmt == XP_BF16) {
     if (R == 32) XP_KV(128, XP_BF16, 1, 2, 2, 2);
@@ -2045,7 +2121,7 @@ hipError_t launch_kv_attn(const xp_kv* kv, const KvAttnArgs& a, hipStream_t st) 
   if (a.groups == 0) {
     d.list = kv->a.list[0];
     if ((e = launch_list(kv, R[0], own, d, st)) != hipSuccess) return e;
-    const dim3 grid(kv_shares(kv, R[0]) - 1, R[0] * kv->hd / 1024);
+    const dim3 grid(kv_shares(kv, R[0]) - 1, (R[0] * kv->hd + 1023) / 1024);
     if (wide) hipLaunchKernelGGL(k_kv_join<128>, grid, dim3(256), 0, st, d, R[0]);
     else hipLaunchKernelGGL(k_kv_join<64>, grid, dim3(256), 0, st, d, R[0]);
     return hipGetLastError();
