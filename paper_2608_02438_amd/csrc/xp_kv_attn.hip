@@ -2077,7 +2077,9 @@ hipError_t launch_kv_attn(const xp_kv* kv, const KvAttnArgs& a, hipStream_t st) 
   p.kv_len = a.kv_len;
   p.group_start = a.group_start;
   p.shared_len = a.shared_len;
-  const int64_t most = (int64_t)a.total_q * kv->grp / R[0] + a.n;
+  int64_t most = (int64_t)a.total_q * kv->grp / R[0] + a.n;
+  // few rows: a tile has a token at least, so that 64 single tokens make their list themselves
+  if (R[0] <= kFewRows && kv->grp <= R[0]) most = std::min<int64_t>(most, a.total_q);
   const bool own = a.groups == 0 && most <= kOwnEntries;
   if (own) p.entries = (int)most;
   hipError_t e;
