@@ -524,7 +524,8 @@ xp_status xp_kv_read(xp_kv* kv, int32_t tokens, const int32_t* slots, const void
  * Keys that a token does not see do not enter its result, whatever they hold.
  * Scores and sums are fp32; the numerators enter the product with V as two bf16
  * parts, as one fp16 part (2^-11 of sum p |v| at most) with an 8-bit cache, and as one
- * bf16 part (2^-8) in calls of more than 64 rows over a bf16 one (max_q times the heads
+ * bf16 part (2^-8) in calls of more than 64 rows over a bf16 one, of more than 32 over a
+ * 4-bit one (max_q times the heads
  * of a group; with shared prefixes at least the mean tokens of a group times the heads,
  * or, for the keys behind prefixes that fill the largest row tiles, max_q alone).  So a
  * single token's result over a bf16 cache has the fewer bits in a call beside a prompt;

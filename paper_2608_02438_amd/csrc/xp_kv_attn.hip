@@ -379,6 +379,10 @@ struct KvRows {
   }
 };
 
+// the same of K's codes in 4 bits: 16-byte chunk c of row r at position c ^ swz4(r)
+template <int HD>
+__device__ __forceinline__ int kv_swz4(int r) { return HD == 128 ? (r >> 2) & 3 : (r >> 3) & 1; }
+
 __device__ __forceinline__ floatx16 mma32(u32x4 a, u32x4 b, floatx16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
                                                  __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -692,6 +696,11 @@ constexpr int kv_waves(int hd, int wr, int wk) { return hd == 64 && wr == 4 && w
 // 2^8 above), and those of 2^-21 of the greatest still have all 11 bits; the smaller
 // ones are off by at most 2^-25, where the sum is 2^7 at least.  Error 1.67e-3, where one
 // bf16 part had 2.2e-3 in 0 to 2% less time, two 1.66e-3 in 5 to 30% more.
+// Over a 4-bit cache, whose values span more than fp16 does, two bf16 parts up to 32 rows and
+// one above: memory bounds those calls no longer (32 blocks of 16 over 8192 keys 130 us with
+// one part, 163 with two).  K lies in LDS as in memory and becomes an operand behind it, V is
+// expanded on its way there: with both expanded, whose writes (64 bytes a cycle) and reads
+// are four times as long, the same 155 and 175 us.
 // Tiles wait in an LDS ring of NST stages filled by global_load_lds; the keys
 // that no row of the tile sees are loaded as zeros, whatever lies there.
 // Matrix pipe and vector pipe work side by side only if one wave's instructions
@@ -719,10 +728,16 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
   static_assert(NG * NW == 8 && NB * WK == 2, "waves");
   constexpr int PER = NG * IPG;                   // loads of a wave for a stage
   static_assert(F4 || (NST - 1) * PER < 64, "vmcnt field");
-  static_assert(!F4 || NST >= (WK == 2 ? 2 : 3), "4-bit: K of two (three) tiles");
+  // 4 bits: K as in memory (codes, then exponents), V expanded to bf16
+  static_assert(!F4 || NST == 3, "4-bit: the tile at work, the next, the one being stored");
+  constexpr int kCodes = HD / 2, kExps = HD / 32; // bytes of a row
+  constexpr int kK4 = kKvTile * (kCodes + kExps) / 16, kV0 = NST * kK4;   // K of a tile; V's beginning
   constexpr int kMerge = (HD / 2 + 2) * kWave;    // floats that a wave hands over
-  static_assert(WK == 1 || WR * kMerge * 4 <= NST * SH::kStage * 16, "merge in LDS");
-  __shared__ __align__(256) u32x4 lds[NST * SH::kStage];
+  constexpr int kRing = F4 ? kV0 + NST * SH::kHalf : NST * SH::kStage;
+  static_assert(F4 || WK == 1 || WR * kMerge * 4 <= kRing * 16, "merge in LDS");
+  constexpr int kMerges = WK == 2 ? WR * kMerge / 4 : 0;
+  __shared__ __align__(256) u32x4 lds[kRing > kMerges ? kRing : kMerges];
+  auto v_rows = [&](int stage, int r) { return lds + (F4 ? kV0 + stage * SH::kHalf : stage * SH::kStage + SH::kHalf) + r * CPR; };
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wr = wave % WR, wk = wave / WR;
@@ -752,7 +767,8 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
   {
     const int r = lane / CPR;
     lp = (uint32_t)(r * RB + 16 * ((lane % CPR) ^ SH::swz(r)));
-    ka = (uint32_t)(li * RB + 16 * (h ^ SH::swz(li)));
+    if constexpr (F4) ka = (uint32_t)(li * kCodes + 16 * (HD == 128 ? 2 * h ^ kv_swz4<HD>(li) : h ^ kv_swz4<HD>(li)));
+    else ka = (uint32_t)(li * RB + 16 * (h ^ SH::swz(li)));
     const int rv = F8 ? 4 * h + ((lane >> 1) & 3) + 8 * ((lane >> 3) & 1) : 4 * h + ((lane & 15) >> 2);
     const int cv = F8 ? (lane >> 4) & 1 : 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
     va = (uint32_t)(rv * RB + 16 * (cv ^ SH::swz(rv)) + 8 * (lane & 1));
@@ -789,7 +805,8 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
     const uint16_t* qs = d.q + tok * d.q_ld + (int64_t)(kvh * d.grp + (row - tk * d.grp)) * HD;
 #pragma unroll
     for (int ks = 0; ks < NKS; ++ks)
-      qf[ks] = ld16(qs + (F8 ? 32 * (ks >> 1) + 16 * h + 8 * (ks & 1) : 16 * ks + 8 * h));
+      qf[ks] = ld16(qs + (F8 ? 32 * (ks >> 1) + 16 * h + 8 * (ks & 1)
+                             : (F4 ? HD / 2 * h + 8 * ks : 16 * ks + 8 * h)));
     const int p = prefix ? d.w.pos[tok] : p0 + tk;
     const int hi = rv ? (d.causal ? imin(p + 1, kceil) : kceil) : kfloor;
     const int lo = d.window > 0 ? imax(p - d.window + 1, kfloor) : kfloor;
@@ -809,18 +826,25 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
   const scalar_i32 tb = as_scalar(d.table + (int64_t)seq * d.table_ld);
   // the first page's rows of this KV head, and the bytes from page to page
   constexpr int RBM = kv_row_bytes(FMT, HD);      // bytes of a row in memory
-  const char* heads = (wave < NW / 2 ? d.kc : d.vc) + (((int64_t)kvh << d.logP) * RBM);
+  const int64_t head0 = ((int64_t)kvh << d.logP) * RBM;
+  const char* heads = (wave < NW / 2 ? d.kc : d.vc) + head0;
   const uint32_t page_bytes = (uint32_t)(d.nkv * RBM) << d.logP;
   const int kin = imax(klo, kfloor);              // from here to khi, or to ks_, some row sees all
   uint32_t bad = 0;                               // a page outside the cache was asked for
-  auto pages = [&](int t, int (&pg)[NG]) {        // page ids of the wave's rows of tile t
+  // 4 bits: a lane's units of a tile, 16 or 8 bytes of codes, 16 or 8 rows of a wave each
+  constexpr int kUnit = HD == 128 && NW <= 4 ? 16 : 8, kUnits = kKvTile * kCodes / (NW * kWave * kUnit);
+  constexpr int kUPR = kCodes / kUnit, kURows = kWave / kUPR;   // units of a row, rows of a wave
+  static_assert(!F4 || (kUnits >= 1 && kURows <= 16), "units");
+  auto row4 = [&](int u) { return (u * NW + wave) * kURows; };
+  constexpr int NPG = F4 ? kUnits : NG;
+  auto pages = [&](int t, int (&pg)[NPG]) {       // page ids of the wave's rows of tile t
 #pragma unroll
-    for (int g = 0; g < NG; ++g)
-      pg[g] = tb[imin((tile_key(t) + 16 * ((wave * NG + g) & 3)) >> d.logP, d.cols - 1)];
+    for (int g = 0; g < NPG; ++g)
+      pg[g] = tb[imin((tile_key(t) + (F4 ? row4(g) : 16 * ((wave * NG + g) & 3))) >> d.logP, d.cols - 1)];
   };
   // tile t to a slot; a segment's first tiles by the general way alone (a tile all of
   // whose keys some row sees needs no test of its keys, but costs a copy of the code)
-  auto issue = [&](auto first, int t, int slot, const int (&pg)[NG]) __attribute__((always_inline)) {
+  auto issue = [&](auto first, int t, int slot, const int (&pg)[NPG]) __attribute__((always_inline)) {
     const int k0 = tile_key(t);
     const bool inner = !decltype(first)::value &&
         (((k0 >= kin) & (k0 + kKvTile <= khi)) | ((k0 >= kfloor) & (k0 + kKvTile <= ks_)));
@@ -866,56 +890,72 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
   // loads still under way when iteration t has what it needs: K of tile t + 1, V of t
   constexpr int kWaitV = (NST - 2) * PER, kWaitK = (NB == 1 ? NST - 2 : NST - 3) * PER;
   static_assert(F4 || kWaitK >= 0, "stages");
-  // A 4-bit cache's tiles come through registers and are expanded to bf16 (exactly) on
-  // their way into the ring, so that everything behind it is a bf16 cache's.  A lane
-  // takes HD / 4 values of row lane / 4 of each 16 and their exponent.  The waves that
-  // load V store tile t + 1 in iteration t, those that load K tile t + 2, and have the
-  // tile after it under way meanwhile.
+  // A 4-bit cache's tiles come through registers: K's codes and exponents go to LDS as
+  // they are and become bf16 operands behind it, V is expanded to bf16 (both exactly) on
+  // its way there.  In iteration t every wave stores its part of tile t + 2 and has tile
+  // t + 3 under way.  Keys that no row sees come like the others: their scores are masked
+  // and their V is looked through for NaN, as where only some row does not see them.
   struct Held {
-    u32x4 x[NG];
-    uint32_t e[NG];
+    u32x4 k[kUnits], v[kUnits];
+    uint32_t ke[kUnits], ve[kUnits];
   };
-  auto fetch = [&](int t, const int (&pg)[NG], Held& to) __attribute__((always_inline)) {
+  const int ur = lane / kUPR, uc = lane % kUPR;   // the lane's row and unit of a wave's
+  const int ub = uc * kUnit / 16;                 // its block of 32
+  const uint32_t xo = ur * kCodes + kUnit * uc, eo = ur * kExps + ub;
+  auto fetch = [&](int t, const int (&pg)[NPG], Held& to) __attribute__((always_inline)) {
     const int k0 = tile_key(t);
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      const int g0 = k0 + 16 * ((wave * NG + g) & 3), key = g0 + lane / 4, r = key & P1;
-      const uint32_t page = (uint32_t)pg[g];
-      const bool ok = page < (uint32_t)d.n_pages;
-      const int from = imax(g0, kfloor), to_ = imin(g0 + 16, khi);
-      bad |= (!ok & (from < to_) & ((to_ > klo) | (from < ks_))) ? XP_DEVERR_PAGE : 0u;
-      const char* base = heads + (uint64_t)(ok ? page : 0u) * page_bytes;
-      const bool any = (key >= kfloor) & (key < khi) & ((key >= klo) | (key < ks_));
-      const char* x = any ? base + r * (HD / 2) + (HD / 8) * (lane & 3) : d.w.zero;
-      const char* e = any ? base + ((HD / 2) << d.logP) + r * (HD / 32) + (lane & 3) * HD / 128
-                          : d.w.zero;
-      if constexpr (HD == 128) {
-        to.x[g] = ld16(x);
-      } else {
-        const uint2 y = *reinterpret_cast<const uint2*>(x);
-        to.x[g] = u32x4{y.x, y.y, 0u, 0u};
+    for (int u = 0; u < kUnits; ++u) {
+      const int g0 = k0 + row4(u), r = g0 & P1;
+      uint32_t page = (uint32_t)pg[u];
+      if (page >= (uint32_t)d.n_pages) {          // wave-uniform
+        const int from = imax(g0, kfloor), upto = imin(g0 + kURows, khi);
+        bad |= ((from < upto) & ((upto > klo) | (from < ks_))) ? XP_DEVERR_PAGE : 0u;
+        page = 0;
       }
-      to.e[g] = *reinterpret_cast<const uint8_t*>(e);
+      // wave-uniform addresses: scalar registers and the lane's bytes
+      const uint64_t at = (uint64_t)head0 + (uint64_t)page * page_bytes + (uint32_t)(r * kCodes);
+      const uint64_t ex = at + ((uint32_t)kCodes << d.logP) - (uint32_t)(r * (kCodes - kExps));
+      uint64_t kx = (uint64_t)(uintptr_t)d.kc + at, vx = (uint64_t)(uintptr_t)d.vc + at;
+      uint64_t ke = (uint64_t)(uintptr_t)d.kc + ex, ve = (uint64_t)(uintptr_t)d.vc + ex;
+      asm volatile("" : "+s"(kx), "+s"(vx), "+s"(ke), "+s"(ve));
+      if constexpr (kUnit == 16) {
+        to.k[u] = ld16((const char*)(uintptr_t)kx + xo);
+        to.v[u] = ld16((const char*)(uintptr_t)vx + xo);
+      } else {
+        const uint2 y = *reinterpret_cast<const uint2*>((const char*)(uintptr_t)kx + xo);
+        const uint2 z = *reinterpret_cast<const uint2*>((const char*)(uintptr_t)vx + xo);
+        to.k[u] = u32x4{y.x, y.y, 0u, 0u};
+        to.v[u] = u32x4{z.x, z.y, 0u, 0u};
+      }
+      to.ke[u] = *reinterpret_cast<const uint8_t*>((const char*)(uintptr_t)ke + eo);
+      to.ve[u] = *reinterpret_cast<const uint8_t*>((const char*)(uintptr_t)ve + eo);
     }
   };
   auto put = [&](int slot, const Held& from) __attribute__((always_inline)) {
-    u32x4* stage = lds + slot * SH::kStage + wave * (NG * 16 * CPR);   // its rows of K, then V
+    char* kst = reinterpret_cast<char*>(lds + slot * kK4);
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      const float s = __uint_as_float((from.e[g] > 252u ? 255u : from.e[g]) << 23);
-      const int r = lane / 4;
-      u32x4* row = stage + (16 * g + r) * CPR;
+    for (int u = 0; u < kUnits; ++u) {
+      const int r = row4(u) + ur;
+      const u32x4 x = from.k[u];
+      if constexpr (kUnit == 16)
+        *reinterpret_cast<u32x4*>(kst + r * kCodes + 16 * (uc ^ kv_swz4<HD>(r))) = x;
+      else
+        *reinterpret_cast<uint2*>(kst + r * kCodes + 16 * ((uc >> 1) ^ kv_swz4<HD>(r)) + 8 * (uc & 1)) = uint2{x[0], x[1]};
+      // exponents above 252 are NaN
+      kst[kKvTile * kCodes + r * kExps + ub] = (char)(from.ke[u] > 252u ? 255u : from.ke[u]);
+      const float s = __uint_as_float((from.ve[u] > 252u ? 255u : from.ve[u]) << 23);
+      u32x4* row = v_rows(slot, r);
 #pragma unroll
-      for (int i = 0; i < HD / 32; ++i)
-        row[(HD / 32 * (lane & 3) + i) ^ SH::swz(r)] = f4_bf16x8(from.x[g][i], s);
+      for (int i = 0; i < kUnit / 4; ++i)
+        row[(kUnit / 4 * uc + i) ^ SH::swz(r)] = f4_bf16x8(from.v[u][i], s);
     }
   };
-  const int lead = F4 ? is_k : ahead;             // tiles that the wave's loads run ahead
-  constexpr int NPG = F4 ? 2 : NST;
   Held held;
-  int pg[NG], pg0[NPG][NG];
+  constexpr int NFST = F4 ? 2 : NST;              // tiles whose pages are asked for at once
+  int pg[NPG], pg0[NFST][NPG];
 #pragma unroll
-  for (int t = 0; t < NPG; ++t) pages(j + imin(t, nj - 1), pg0[t]);
+  for (int t = 0; t < NFST; ++t) pages(j + imin(t, nj - 1), pg0[t]);
   pages(j + imin(F4 ? 2 : NST - 1 + ahead, nj - 1), pg);
   // The query rows are waited for here: with loads to LDS under way the compiler waits
   // for all of them before it uses a register that was loaded.
@@ -926,11 +966,9 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
     fetch(j, pg0[0], first);
     fetch(j + imin(1, nj - 1), pg0[1], held);
     put(0, first);
-    if (is_k) {                                   // whole wave
-      put(1, held);
-      fetch(j + imin(2, nj - 1), pg, held);
-      pages(j + imin(3, nj - 1), pg);
-    }
+    put(1, held);
+    fetch(j + imin(2, nj - 1), pg, held);
+    pages(j + imin(3, nj - 1), pg);
   } else {
 #pragma unroll
     for (int t = 0; t < NST; ++t)
@@ -950,7 +988,25 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
   };
   // K operands of the block at row r of a stage
   u32x4 kf[NKS];
+  float kscale[2] = {};
   auto k_read = [&](int stage, int r) __attribute__((always_inline)) {
+    if constexpr (F4) {
+      uint32_t kx = ka + lds_byte(lds + stage * kK4) + r * kCodes;
+      uint32_t ex = lds_byte(lds + stage * kK4) + kKvTile * kCodes + (r + li) * kExps;
+      asm volatile("" : "+v"(kx), "+v"(ex));
+      kf[0] = *(const lds_u32x4*)(uintptr_t)kx;
+      if constexpr (HD == 128) {
+        kf[1] = *(const lds_u32x4*)(uintptr_t)(kx ^ 16);
+        const uint32_t y = *(const __attribute__((address_space(3))) uint32_t*)(uintptr_t)ex >> (16 * h);
+        kscale[0] = __uint_as_float(y << 23 & 0x7f800000u);
+        kscale[1] = __uint_as_float(y << 15 & 0x7f800000u);
+      } else {
+        const uint32_t y = *(const __attribute__((address_space(3))) uint16_t*)(uintptr_t)ex >> (8 * h);
+        kscale[0] = __uint_as_float(y << 23 & 0x7f800000u);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      return;
+    }
     uint32_t kx = ka + lds_byte(lds + stage * SH::kStage + r * CPR);
     asm volatile("" : "+v"(kx));                  // opaque: no address is kept for the next block
 #pragma unroll
@@ -966,12 +1022,13 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
         return f8_bf16x8(x.x, x.y);
       }
     }
-    return kf[i];
+    if constexpr (F4) return f4_bf16x8(kf[i / 4][i % 4], kscale[i / 4]);
+    else return kf[i];
   };
   // V operands of a block, and the numerators (as bf16 parts) of this one and the next
   u32x4 v[2][ND], ph[2][2], pl[2][2];
   auto v_read = [&](int stage, int r) __attribute__((always_inline)) {
-    uint32_t vx = va + lds_byte(lds + stage * SH::kStage + SH::kHalf + r * CPR);
+    uint32_t vx = va + lds_byte(v_rows(stage, r));
     asm volatile("" : "+v"(vx));
     uint32_t xa[ND], xb[ND];
 #pragma unroll
@@ -989,7 +1046,7 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
   };
   // infinities or NaN among the block's V
   auto odd_values = [&](int stage, int r) __attribute__((always_inline)) {
-    const u32x4* Vs = lds + stage * SH::kStage + SH::kHalf + r * CPR;
+    const u32x4* Vs = v_rows(stage, r);
     constexpr int N = 32 * CPR / kWave, U = N < 4 ? N : 4;   // reads of a lane, at a time
     KvOdd<F8> odd;
 #pragma unroll 1
@@ -1138,10 +1195,10 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
   auto begin = [&](int t, int stage) __attribute__((always_inline)) {
     if constexpr (F4) {
       lds_barrier();
-      if (t + 1 + lead < nj) put((stage + 1 + lead) % NST, held);
-      if (t + 2 + lead < nj) {
-        fetch(j + t + 2 + lead, pg, held);
-        pages(j + imin(t + 3 + lead, nj - 1), pg);
+      if (t + 2 < nj) put(stage == 0 ? NST - 1 : stage - 1, held);
+      if (t + 3 < nj) {
+        fetch(j + t + 3, pg, held);
+        pages(j + imin(t + 4, nj - 1), pg);
       }
       return;
     }
@@ -2023,8 +2080,8 @@ static hipError_t launch_list(const xp_kv* kv, int R, bool own, const KvDev& d, 
     else if (R == 128) XP_KV(128, XP_E4M3, 4, 1, 4, 1);
     else XP_KV(128, XP_E4M3, 8, 1, 8, 1);
   } else if (kv->hd == 128) {
-    if (R == 32) XP_KV(128, XP_MXFP4, 1, 2, 2, 2);
-    else if (R == 64) XP_KV(128, XP_MXFP4, 2, 2, 2, 2);
+    if (R == 32) XP_KV(128, XP_MXFP4, 1, 2, 3, 2);
+    else if (R == 64) XP_KV(128, XP_MXFP4, 2, 2, 3, 1);
     else if (R == 128) XP_KV(128, XP_MXFP4, 4, 2, 3, 1);
     else XP_KV(128, XP_MXFP4, 8, 1, 3, 1);
   } else if (fmt == XP_BF16) {
@@ -2036,8 +2093,8 @@ static hipError_t launch_list(const xp_kv* kv, int R, bool own, const KvDev& d, 
     else if (R == 64) XP_KV(64, XP_E4M3, 2, 2, 4, 1);
     else XP_KV(64, XP_E4M3, 4, 1, 6, 1);
   } else {
-    if (R == 32) XP_KV(64, XP_MXFP4, 1, 2, 2, 2);
-    else if (R == 64) XP_KV(64, XP_MXFP4, 2, 2, 2, 2);
+    if (R == 32) XP_KV(64, XP_MXFP4, 1, 2, 3, 2);
+    else if (R == 64) XP_KV(64, XP_MXFP4, 2, 2, 3, 1);
     else XP_KV(64, XP_MXFP4, 4, 1, 3, 1);
   }
 #undef XP_KV

@@ -51,3 +51,8 @@ class Call4(Call):
             self.dgs = t(np.array(starts), torch.int32)
             self.dgl = t(np.array([g[2] for g in self.groups]), torch.int32)
         return kv
+
+
+def parts_of4(rows):
+    # the bf16 parts of the numerators: two in calls of up to 32 rows, else one
+    return 2 if rows <= 32 else 1

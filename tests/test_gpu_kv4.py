@@ -4,8 +4,8 @@ import numpy as np
 import pytest
 
 import oracle as O
-from _kv import bf16, parts_of
-from _kv4 import Call4
+from _kv import bf16
+from _kv4 import Call4, parts_of4
 
 R = O.kv_ref
 pytestmark = pytest.mark.gpu
@@ -210,7 +210,7 @@ def test_attend4(name, hd, P):
         lse = torch.zeros((c.total, c.heads), device="cuda")
         out = c.run(kv, lse=lse, **m)
         assert kv.device_errors() == 0
-        c.check(out, lse, parts=parts_of(c.rows()), **m)
+        c.check(out, lse, parts=parts_of4(c.rows()), **m)
     kv.close()
 
 
@@ -237,7 +237,7 @@ def test_unseen_keys_hold_nan(hd, ql):
     print(f"masked exponents: hd={hd} ql={ql}", flush=True)
     out = c.run(kv, window=W, sinks=5).double().cpu().numpy()
     with np.errstate(invalid="ignore"):
-        want = c.oracle(causal=True, window=W, sinks=5, parts=parts_of(c.rows()))
+        want = c.oracle(causal=True, window=W, sinks=5, parts=parts_of4(c.rows()))
     for b in want:
         o, _, eb, _ = want[b]
         m = ql[b]
@@ -260,7 +260,7 @@ def test_nan_values_of_later_tokens(ql):
     c.v = R.mxfp4_values(*c.bits[1])
     kv = c.device()
     out = c.run(kv).double().cpu().numpy()
-    want = c.oracle(causal=True, parts=parts_of(c.rows()))
+    want = c.oracle(causal=True, parts=parts_of4(c.rows()))
     for b in want:
         o, _, eb, _ = want[b]
         got = out[c.cu[b]:c.cu[b + 1]]
@@ -338,7 +338,7 @@ def test_captured_calls_replay_with_new_lengths(ql):
         out.zero_()
         g.replay()
         torch.cuda.synchronize()
-        c.check(out, causal=True, parts=parts_of(c.rows()))
+        c.check(out, causal=True, parts=parts_of4(c.rows()))
         assert c.run(kv).equal(out)
     kv.close()
 
