@@ -24,7 +24,7 @@ namespace xp {
 constexpr int kSmpMaxV = 1 << 18;
 constexpr int kSmpChunk = 4096;                    // tokens of a chunk
 constexpr int kSmpChunks = kSmpMaxV / kSmpChunk;
-constexpr int kSmpBatch = 512;                     // rows that go through the launches together
+constexpr int kSmpBatch = 128;                     // rows that go through the launches together
 // passes over the vocabulary: a workgroup has some chunks of a row, a thread 16 tokens of each
 constexpr int kSmpThreads = 256;
 constexpr int kSmpPer = kSmpChunk / kSmpThreads;
@@ -66,6 +66,7 @@ struct Smp {
   uint64_t* best;                    // [rows][kSmpChunks] the largest key, lowest index
   uint64_t* sums;                    // [rows][kSmpChunks] kept weights
   uint64_t* hist;                    // [rows][kSmpHist] tokens (top-k) or weights of a bin
+  uint64_t* part;                    // [rows][kSmpChunks][kSmpHist] weights of every chunk's bins
   SmpRec* rec;                       // [rows]
   uint64_t* list;                    // [rows][kSmpCap] key, index
 };
@@ -84,6 +85,10 @@ __device__ __forceinline__ float smp_value(uint32_t key) {
 struct SmpRow {
   double inv_t, top;
   uint32_t top_key;
+  float top_f, bin_t;
+  __device__ __forceinline__ SmpRow(float t, uint32_t key)
+      : inv_t(1.0 / (double)t), top((double)smp_value(key)), top_key(key), top_f(smp_value(key)),
+        bin_t(16.f / t) {}
   __device__ __forceinline__ double x(uint32_t key) const {
     return key == top_key ? 0.0 : ((double)smp_value(key) - top) * inv_t;
   }
@@ -112,10 +117,12 @@ struct SmpRow {
   __device__ __forceinline__ uint64_t weight(uint32_t key) const {
     return key != 0u ? weight_at(x(key)) : 0u;
   }
-  // bins of l from the largest down; kSmpHist and more have no weight
-  __device__ __forceinline__ int bin_at(double y) const {
-    const double b = y * -16.0;
-    return b < (double)kSmpHist ? (int)b : kSmpHist;
+  // Bins of l from the largest down, 1 / 16 of (m - l) / T each: differences, products and
+  // truncation in fp32 never fall where l falls, which is all that bins have to do.  From
+  // kSmpHist on (and for keys of no token) there is no weight.
+  __device__ __forceinline__ int bin(uint32_t key) const {
+    const float b = key == top_key ? 0.f : (top_f - smp_value(key)) * bin_t;
+    return b < (float)kSmpHist ? (int)b : kSmpHist;
   }
 };
 
@@ -293,15 +300,20 @@ __global__ __launch_bounds__(kSmpThreads) void k_smp_mass(const Smp d) {
   if (d.temp[at.row] == 0) return;
   const T* row = static_cast<const T*>(d.logits) + at.row * d.ld;
   const bool wide = reinterpret_cast<uintptr_t>(row) % (4 * sizeof(T)) == 0;
+  uint32_t next[kSmpPer];                          // the next chunk's, on their way
+  smp_chunk(d, row, wide, at.c0, next);
   const SmpSet set(d, at.row);
   const uint32_t top_key = (uint32_t)(smp_best(d, at.r) >> 32);
   if (top_key == 0u) return;
-  const SmpRow w{1.0 / (double)set.t, (double)smp_value(top_key), top_key};
-  if (!set.cuts()) {
-    const double log_mp = set.log_min();
-    for (int c = at.c0; c < at.c1; ++c) {
-      uint32_t key[kSmpPer];
-      smp_chunk(d, row, wide, c, key);
+  const SmpRow w(set.t, top_key);
+  const bool cuts = set.cuts(), tokens = set.k > 0;
+  const double log_mp = set.log_min();
+  for (int c = at.c0; c < at.c1; ++c) {
+    uint32_t key[kSmpPer];
+#pragma unroll
+    for (int i = 0; i < kSmpPer; ++i) key[i] = next[i];
+    if (c + 1 < at.c1) smp_chunk(d, row, wide, c + 1, next);
+    if (!cuts) {
       uint64_t sum = 0;
 #pragma unroll
       for (int i = 0; i < kSmpPer; ++i) {
@@ -316,29 +328,24 @@ __global__ __launch_bounds__(kSmpThreads) void k_smp_mass(const Smp d) {
         d.sums[at.r * kSmpChunks + c] = sum;
       }
       __syncthreads();
+      continue;
     }
-    return;
-  }
-  for (int b = tid; b < kSmpHist; b += kSmpThreads) hist[b] = 0;
-  __syncthreads();
-  const bool tokens = set.k > 0;
-  for (int c = at.c0; c < at.c1; ++c) {
-    uint32_t key[kSmpPer];
-    smp_chunk(d, row, wide, c, key);
+    for (int b = tid; b < kSmpHist; b += kSmpThreads) hist[b] = 0;
+    __syncthreads();
 #pragma unroll
     for (int i = 0; i < kSmpPer; ++i) {
-      const double y = w.x(key[i]);
-      const int b = w.bin_at(y);
-      if (key[i] != 0u && b < kSmpHist) {
-        const uint64_t v = tokens ? 1u : w.weight_at(y);
-        atomicAdd((unsigned long long*)&hist[b], (unsigned long long)v);
-      }
+      const int b = w.bin(key[i]);
+      if (b < kSmpHist)
+        atomicAdd((unsigned long long*)&hist[b],
+                  (unsigned long long)(tokens ? 1u : w.weight_at(w.x(key[i]))));
+    }
+    __syncthreads();
+    for (int b = tid; b < kSmpHist; b += kSmpThreads) {
+      const uint64_t v = hist[b];
+      if (v != 0u) atomicAdd((unsigned long long*)&d.hist[at.r * kSmpHist + b], (unsigned long long)v);
+      if (!tokens) d.part[(at.r * kSmpChunks + c) * kSmpHist + b] = v;
     }
   }
-  __syncthreads();
-  for (int b = tid; b < kSmpHist; b += kSmpThreads)
-    if (hist[b] != 0u)
-      atomicAdd((unsigned long long*)&d.hist[at.r * kSmpHist + b], (unsigned long long)hist[b]);
 }
 
 // What the histogram says: the bin in which the threshold lies.
@@ -398,6 +405,10 @@ __global__ __launch_bounds__(kSmpThreads) void k_smp_list(const Smp d) {
   if (d.temp[at.row] == 0) return;
   const SmpSet set(d, at.row);
   if (!set.cuts()) return;
+  const T* row = static_cast<const T*>(d.logits) + at.row * d.ld;
+  const bool wide = reinterpret_cast<uintptr_t>(row) % (4 * sizeof(T)) == 0;
+  uint32_t next[kSmpPer];                          // the next chunk's, on their way
+  smp_chunk(d, row, wide, at.c0, next);
   const uint32_t top_key = (uint32_t)(smp_best(d, at.r) >> 32);
   if (top_key == 0u) return;
   const SmpRec rec = smp_decide(d, at.r, set);     // every wave the same
@@ -409,22 +420,29 @@ __global__ __launch_bounds__(kSmpThreads) void k_smp_list(const Smp d) {
     to->all = rec.all;
   }
   if (rec.mode == kSmpSlow) return;
-  const T* row = static_cast<const T*>(d.logits) + at.row * d.ld;
-  const bool wide = reinterpret_cast<uintptr_t>(row) % (4 * sizeof(T)) == 0;
-  const SmpRow w{1.0 / (double)set.t, (double)smp_value(top_key), top_key};
+  const SmpRow w(set.t, top_key);
   const double log_mp = set.log_min();
+  // the chunks' bins hold the weights before the edge, unless min-p may take some of them
+  const bool held = set.k == 0 && !(set.mp > 0.f);
   for (int c = at.c0; c < at.c1; ++c) {
     uint32_t key[kSmpPer];
-    smp_chunk(d, row, wide, c, key);
+#pragma unroll
+    for (int i = 0; i < kSmpPer; ++i) key[i] = next[i];
+    if (c + 1 < at.c1) smp_chunk(d, row, wide, c + 1, next);
     uint64_t sum = 0;
     uint32_t pick = 0;                             // a bit a candidate
+    if (rec.mode == kSmpEdge && held)
+      for (int b = tid; b < rec.edge; b += kSmpThreads)
+        sum += d.part[(at.r * kSmpChunks + c) * kSmpHist + b];
 #pragma unroll
     for (int i = 0; i < kSmpPer; ++i) {
-      const double y = w.x(key[i]);
-      const int b = key[i] != 0u ? w.bin_at(y) : kSmpHist;
+      const int b = w.bin(key[i]);
       const bool cand = rec.mode == kSmpList ? b <= rec.edge : b == rec.edge;
       pick |= cand && b < kSmpHist ? 1u << i : 0u;
-      if (rec.mode == kSmpEdge && b < rec.edge && y >= log_mp) sum += w.weight_at(y);
+      if (rec.mode == kSmpEdge && !held && b < rec.edge) {
+        const double y = w.x(key[i]);
+        sum += y >= log_mp ? w.weight_at(y) : 0u;
+      }
     }
     const uint32_t n = __popc(pick);
     uint32_t upto = n;
@@ -741,7 +759,7 @@ __global__ __launch_bounds__(kRowThreads) void k_smp_row(const Smp d) {
   const bool wide = reinterpret_cast<uintptr_t>(row) % (4 * sizeof(T)) == 0;
   const SmpSet set(d, r);
   if (set.bad && tid == 0) atomicOr(d.err, set.bad);
-  const SmpRow w{1.0 / (double)set.t, (double)smp_value(top_key), top_key};
+  const SmpRow w(set.t, top_key);
   const double log_mp = set.log_min();
   const uint64_t* sums = d.sums + rb * kSmpChunks;
   auto heavy = [&](uint32_t key) -> uint64_t { return w.x(key) >= log_mp ? w.weight(key) : 0u; };
@@ -873,11 +891,8 @@ __global__ __launch_bounds__(kRowThreads) void k_smp_row(const Smp d) {
   }
   __syncthreads();
   row_draw(d, s, r, row, wide, w, s.bins, [&](uint32_t k, int i) -> uint64_t {
-    if (k == 0u) return 0u;
-    const double y = w.x(k);
-    const int b = w.bin_at(y);
-    const bool in = b < rec.edge || (b == rec.edge && kept(k, (uint32_t)i));
-    return in && y >= log_mp ? w.weight_at(y) : 0u;
+    const int b = w.bin(k);
+    return b < kSmpHist && (b < rec.edge || (b == rec.edge && kept(k, (uint32_t)i))) ? heavy(k) : 0u;
   });
 }
 
@@ -961,6 +976,7 @@ extern "C" xp_status xp_sampler_create(int32_t V, int32_t max_rows, xp_sampler**
       {(void**)&s->d.best, nb * kSmpChunks * 8},
       {(void**)&s->d.sums, nb * kSmpChunks * 8},
       {(void**)&s->d.hist, nb * kSmpHist * 8},
+      {(void**)&s->d.part, nb * kSmpChunks * kSmpHist * 8},
       {(void**)&s->d.rec, nb * sizeof(SmpRec)},
       {(void**)&s->d.list, nb * kSmpCap * 8},
   };
