@@ -89,9 +89,10 @@ struct SmpRow {
   __device__ __forceinline__ SmpRow(float t, uint32_t key)
       : inv_t(1.0 / (double)t), top((double)smp_value(key)), top_key(key), top_f(smp_value(key)),
         bin_t(16.f / t) {}
-  __device__ __forceinline__ double x(uint32_t key) const {
-    return key == top_key ? 0.0 : ((double)smp_value(key) - top) * inv_t;
+  __device__ __forceinline__ double xl(float l) const {
+    return l == top_f ? 0.0 : ((double)l - top) * inv_t;
   }
+  __device__ __forceinline__ double x(uint32_t key) const { return xl(smp_value(key)); }
   // e^x 2^45 to the nearest integer: 2^k e^f with |f| <= ln 2 / 2, e^f by its series up
   // to f^11 (2^-47 off), the integer from the sum with 2^52
   __device__ __forceinline__ uint64_t weight_at(double y) const {
@@ -119,9 +120,9 @@ struct SmpRow {
   }
   // Bins of l from the largest down, 1 / 16 of (m - l) / T each: differences, products and
   // truncation in fp32 never fall where l falls, which is all that bins have to do.  From
-  // kSmpHist on (and for keys of no token) there is no weight.
-  __device__ __forceinline__ int bin(uint32_t key) const {
-    const float b = key == top_key ? 0.f : (top_f - smp_value(key)) * bin_t;
+  // kSmpHist on (and for -inf and NaN) there is no weight.
+  __device__ __forceinline__ int bin(float l) const {
+    const float b = l == top_f ? 0.f : (top_f - l) * bin_t;
     return b < (float)kSmpHist ? (int)b : kSmpHist;
   }
 };
@@ -184,11 +185,9 @@ __device__ __forceinline__ uint64_t wave_scan_u64(uint64_t v, int lane) {
   return v;
 }
 
-// four tokens' keys from index i0 on; 0 past the vocabulary
+// four tokens' logits from index i0 on; -inf past the vocabulary
 template <typename T>
-__device__ __forceinline__ void smp_load(const Smp& d, const T* row, bool wide, int i0,
-                                         uint32_t (&key)[4]) {
-  float l[4];
+__device__ __forceinline__ void smp_logits(const Smp& d, const T* row, bool wide, int i0, float (&l)[4]) {
   if (wide && i0 + 4 <= d.V) {
     if constexpr (sizeof(T) == 2) {
       const uint2 x = *reinterpret_cast<const uint2*>(row + i0);
@@ -205,6 +204,12 @@ __device__ __forceinline__ void smp_load(const Smp& d, const T* row, bool wide, 
 #pragma unroll
     for (int q = 0; q < 4; ++q) l[q] = i0 + q < d.V ? to_f32<T>(row[i0 + q]) : -INFINITY;
   }
+}
+template <typename T>
+__device__ __forceinline__ void smp_load(const Smp& d, const T* row, bool wide, int i0,
+                                         uint32_t (&key)[4]) {
+  float l[4];
+  smp_logits(d, row, wide, i0, l);
 #pragma unroll
   for (int q = 0; q < 4; ++q) key[q] = smp_key(l[q]);
 }
@@ -239,13 +244,13 @@ __device__ __forceinline__ int smp_index(int chunk, int i) {
 }
 template <typename T>
 __device__ __forceinline__ void smp_chunk(const Smp& d, const T* row, bool wide, int chunk,
-                                          uint32_t (&key)[kSmpPer]) {
+                                          float (&l)[kSmpPer]) {
 #pragma unroll
   for (int i = 0; i < kSmpPer / 4; ++i) {
-    uint32_t x[4];
-    smp_load(d, row, wide, smp_index(chunk, i), x);
+    float x[4];
+    smp_logits(d, row, wide, smp_index(chunk, i), x);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) key[4 * i + q] = x[q];
+    for (int q = 0; q < 4; ++q) l[4 * i + q] = x[q];
   }
 }
 // the row's largest key and its lowest index, from the chunks' (every wave for itself)
@@ -267,17 +272,18 @@ __global__ __launch_bounds__(kSmpThreads) void k_smp_max(const Smp d) {
     if (tid == 0) d.rec[at.r] = SmpRec{};
   }
   for (int c = at.c0; c < at.c1; ++c) {
-    uint32_t key[kSmpPer];
-    smp_chunk(d, row, wide, c, key);
-    uint32_t top = 0;
-    int idx = 0;
+    float l[kSmpPer];
+    smp_chunk(d, row, wide, c, l);
+    float top = -INFINITY;
+    int at_i = 0;
 #pragma unroll
-    for (int i = 0; i < kSmpPer; ++i) {            // indices ascend
-      const bool more = key[i] > top;
-      top = more ? key[i] : top;
-      idx = more ? smp_index(c, i / 4) + i % 4 : idx;
+    for (int i = 0; i < kSmpPer; ++i) {            // indices ascend; NaN is never more
+      const bool more = l[i] > top;
+      top = more ? l[i] : top;
+      at_i = more ? i : at_i;
     }
-    const uint64_t best = wave_max_u64(((uint64_t)top << 32) | (uint32_t)~idx);
+    const int idx = smp_index(c, at_i / 4) + at_i % 4;
+    const uint64_t best = wave_max_u64(((uint64_t)smp_key(top) << 32) | (uint32_t)~idx);
     if (lane == 0) red[wave] = best;
     __syncthreads();
     if (tid == 0) {
@@ -300,7 +306,7 @@ __global__ __launch_bounds__(kSmpThreads) void k_smp_mass(const Smp d) {
   if (d.temp[at.row] == 0) return;
   const T* row = static_cast<const T*>(d.logits) + at.row * d.ld;
   const bool wide = reinterpret_cast<uintptr_t>(row) % (4 * sizeof(T)) == 0;
-  uint32_t next[kSmpPer];                          // the next chunk's, on their way
+  float next[kSmpPer];                             // the next chunk's, on their way
   smp_chunk(d, row, wide, at.c0, next);
   const SmpSet set(d, at.row);
   const uint32_t top_key = (uint32_t)(smp_best(d, at.r) >> 32);
@@ -309,37 +315,37 @@ __global__ __launch_bounds__(kSmpThreads) void k_smp_mass(const Smp d) {
   const bool cuts = set.cuts(), tokens = set.k > 0;
   const double log_mp = set.log_min();
   for (int c = at.c0; c < at.c1; ++c) {
-    uint32_t key[kSmpPer];
+    float l[kSmpPer];
 #pragma unroll
-    for (int i = 0; i < kSmpPer; ++i) key[i] = next[i];
+    for (int i = 0; i < kSmpPer; ++i) l[i] = next[i];
     if (c + 1 < at.c1) smp_chunk(d, row, wide, c + 1, next);
     if (!cuts) {
       uint64_t sum = 0;
 #pragma unroll
       for (int i = 0; i < kSmpPer; ++i) {
-        const double y = w.x(key[i]);
-        sum += key[i] != 0u && y >= log_mp ? w.weight_at(y) : 0u;
+        const double y = w.xl(l[i]);               // NaN for NaN: no weight
+        sum += y >= log_mp ? w.weight_at(y) : 0u;
       }
       sum = wave_sum_u64(sum);
       if (lane == 0) red[wave] = sum;
-      __syncthreads();
+      lds_barrier();
       if (tid == 0) {
         for (int x = 1; x < kSmpThreads / kWave; ++x) sum += red[x];
         d.sums[at.r * kSmpChunks + c] = sum;
       }
-      __syncthreads();
+      lds_barrier();
       continue;
     }
     for (int b = tid; b < kSmpHist; b += kSmpThreads) hist[b] = 0;
-    __syncthreads();
+    lds_barrier();
 #pragma unroll
     for (int i = 0; i < kSmpPer; ++i) {
-      const int b = w.bin(key[i]);
+      const int b = w.bin(l[i]);
       if (b < kSmpHist)
         atomicAdd((unsigned long long*)&hist[b],
-                  (unsigned long long)(tokens ? 1u : w.weight_at(w.x(key[i]))));
+                  (unsigned long long)(tokens ? 1u : w.weight_at(w.xl(l[i]))));
     }
-    __syncthreads();
+    lds_barrier();
     for (int b = tid; b < kSmpHist; b += kSmpThreads) {
       const uint64_t v = hist[b];
       if (v != 0u) atomicAdd((unsigned long long*)&d.hist[at.r * kSmpHist + b], (unsigned long long)v);
@@ -407,7 +413,7 @@ __global__ __launch_bounds__(kSmpThreads) void k_smp_list(const Smp d) {
   if (!set.cuts()) return;
   const T* row = static_cast<const T*>(d.logits) + at.row * d.ld;
   const bool wide = reinterpret_cast<uintptr_t>(row) % (4 * sizeof(T)) == 0;
-  uint32_t next[kSmpPer];                          // the next chunk's, on their way
+  float next[kSmpPer];                             // the next chunk's, on their way
   smp_chunk(d, row, wide, at.c0, next);
   const uint32_t top_key = (uint32_t)(smp_best(d, at.r) >> 32);
   if (top_key == 0u) return;
@@ -425,9 +431,9 @@ __global__ __launch_bounds__(kSmpThreads) void k_smp_list(const Smp d) {
   // the chunks' bins hold the weights before the edge, unless min-p may take some of them
   const bool held = set.k == 0 && !(set.mp > 0.f);
   for (int c = at.c0; c < at.c1; ++c) {
-    uint32_t key[kSmpPer];
+    float l[kSmpPer];
 #pragma unroll
-    for (int i = 0; i < kSmpPer; ++i) key[i] = next[i];
+    for (int i = 0; i < kSmpPer; ++i) l[i] = next[i];
     if (c + 1 < at.c1) smp_chunk(d, row, wide, c + 1, next);
     uint64_t sum = 0;
     uint32_t pick = 0;                             // a bit a candidate
@@ -436,11 +442,11 @@ __global__ __launch_bounds__(kSmpThreads) void k_smp_list(const Smp d) {
         sum += d.part[(at.r * kSmpChunks + c) * kSmpHist + b];
 #pragma unroll
     for (int i = 0; i < kSmpPer; ++i) {
-      const int b = w.bin(key[i]);
+      const int b = w.bin(l[i]);
       const bool cand = rec.mode == kSmpList ? b <= rec.edge : b == rec.edge;
       pick |= cand && b < kSmpHist ? 1u << i : 0u;
       if (rec.mode == kSmpEdge && !held && b < rec.edge) {
-        const double y = w.x(key[i]);
+        const double y = w.xl(l[i]);
         sum += y >= log_mp ? w.weight_at(y) : 0u;
       }
     }
@@ -454,7 +460,7 @@ __global__ __launch_bounds__(kSmpThreads) void k_smp_list(const Smp d) {
     sum = wave_sum_u64(sum);
     if (lane == 63) num[wave] = upto;
     if (lane == 0) red[wave] = sum;
-    __syncthreads();
+    lds_barrier();
     if (tid == 0) {
       uint32_t all = 0;
       for (int x = 0; x < kSmpThreads / kWave; ++x) all += num[x];
@@ -462,15 +468,15 @@ __global__ __launch_bounds__(kSmpThreads) void k_smp_list(const Smp d) {
       for (int x = 1; x < kSmpThreads / kWave; ++x) sum += red[x];
       d.sums[at.r * kSmpChunks + c] = sum;
     }
-    __syncthreads();
+    lds_barrier();
     uint32_t to = base + upto - n;
     for (int x = 0; x < wave; ++x) to += num[x];
 #pragma unroll
     for (int i = 0; i < kSmpPer; ++i)
       if (((pick >> i) & 1u) && to < (uint32_t)kSmpCap)
         d.list[at.r * kSmpCap + to++] =
-            ((uint64_t)key[i] << 32) | (uint32_t)(smp_index(c, i / 4) + i % 4);
-    __syncthreads();
+            ((uint64_t)smp_key(l[i]) << 32) | (uint32_t)(smp_index(c, i / 4) + i % 4);
+    lds_barrier();
   }
 }
 
@@ -891,7 +897,7 @@ __global__ __launch_bounds__(kRowThreads) void k_smp_row(const Smp d) {
   }
   __syncthreads();
   row_draw(d, s, r, row, wide, w, s.bins, [&](uint32_t k, int i) -> uint64_t {
-    const int b = w.bin(k);
+    const int b = w.bin(smp_value(k));
     return b < kSmpHist && (b < rec.edge || (b == rec.edge && kept(k, (uint32_t)i))) ? heavy(k) : 0u;
   });
 }
@@ -902,7 +908,8 @@ __global__ void k_smp_clear_err(uint32_t* err) {
 
 template <typename T>
 static hipError_t launch_sample(Smp d, int rows, int cus, hipStream_t st) {
-  // as many chunks a workgroup as leave four workgroups a CU
+  // as many chunks a workgroup as leave four workgroups a CU: 64 rows of 38 chunks in 1216
+  // workgroups of two took 7 + 18 + 15 us, of one 7 + 18 + 18, in 832 of three 8 + 21 + 18
   d.per_wg = std::max(1, std::min(d.chunks, rows * d.chunks / (4 * cus)));
   const dim3 grid(rows * ((d.chunks + d.per_wg - 1) / d.per_wg)), block(kSmpThreads);
   hipError_t e;

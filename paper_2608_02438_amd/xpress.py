@@ -380,60 +380,76 @@ def rope(q, pos, sections, theta, k=None, g_q=None, g_k=None, eps=1e-6, rot_dim=
     Returns (q_out, k_out)."""
     import torch
     L = load_library()
-    hd, dev, dt = q.shape[-1], q.device, q.dtype
-    code = {torch.float32: XP_F32, torch.bfloat16: XP_BF16}.get(dt)
-    if code is None or q.dim() != 3 or not q.is_cuda:
+    dt, index = q.dtype, q.get_device()
+    code = XP_BF16 if dt == torch.bfloat16 else (XP_F32 if dt == torch.float32 else None)
+    if code is None or q.dim() != 3 or index < 0:
         raise ValueError("q: expected a bf16 or float32 device tensor [tokens][heads][head_dim]")
-    tokens = q.shape[0]
-    sections = [int(x) for x in sections]
-    if not 1 <= len(sections) <= 4 or min(sections) < 0:
-        raise ValueError("sections: pairs of 1 to 4 axes")
-    if rot_dim is not None and rot_dim != 2 * sum(sections):
-        raise ValueError(f"rot_dim={rot_dim} is not twice the sum of sections={sections}")
-    if (pos.dtype != torch.int32 or pos.device != dev or pos.dim() != 2
-            or tuple(pos.shape) != (len(sections), tokens)
-            or (tokens > 1 and pos.stride(1) != 1)
-            or (len(sections) > 1 and pos.stride(0) < tokens)):
-        raise ValueError(f"pos: expected int32 [{len(sections)}][{tokens}] with contiguous rows "
-                         f"on {dev}")
+    tokens, _, hd = q.shape
+    key = (hd, code, tuple(sections), bool(interleaved), theta, eps)
+    shape = _rope_shapes.get(key)
+    if shape is None:
+        shape = _rope_shapes[key] = _rope_shape(*key)
+    axes = len(sections)
+    if rot_dim is not None and rot_dim != shape.rot_dim:
+        raise ValueError(f"rot_dim={rot_dim} is not twice the sum of sections={list(sections)}")
+    if (pos.dtype != torch.int32 or pos.get_device() != index or pos.dim() != 2
+            or pos.shape[0] != axes or pos.shape[1] != tokens
+            or (tokens > 1 and pos.stride(1) != 1) or (axes > 1 and pos.stride(0) < tokens)):
+        raise ValueError(f"pos: expected int32 [{axes}][{tokens}] with contiguous rows on {q.device}")
 
-    def rows(name, t, like):
-        if (t.dtype != dt or t.device != dev or t.dim() != 3 or t.shape[0] != tokens
-                or t.shape[2] != hd or (like is not None and t.shape != like.shape)):
-            raise ValueError(f"{name}: expected {dt} [{tokens}][heads][{hd}] rows on {dev}")
-        heads = t.shape[1]
+    def rows(name, t, heads):
+        s = t.shape
+        if (t.dtype != dt or t.get_device() != index or len(s) != 3 or s[0] != tokens or s[2] != hd
+                or (heads is not None and s[1] != heads)):
+            raise ValueError(f"{name}: expected {dt} [{tokens}][heads][{hd}] rows on {q.device}")
         if t.is_contiguous():
-            return t.data_ptr(), heads * hd
-        if t.stride(2) != 1 or (heads > 1 and t.stride(1) != hd):
-            raise ValueError(f"{name}: expected contiguous [{heads}][{hd}] rows")
-        return t.data_ptr(), t.stride(0) if tokens > 1 else heads * hd
+            return t.data_ptr(), s[1] * hd
+        if t.stride(2) != 1 or (s[1] > 1 and t.stride(1) != hd):
+            raise ValueError(f"{name}: expected contiguous [{s[1]}][{hd}] rows")
+        return t.data_ptr(), t.stride(0) if tokens > 1 else s[1] * hd
 
-    args, out = [], []
-    for name, x, g, y in (("q", q, g_q, q_out), ("k", k, g_k, k_out)):
+    def side(name, x, g, y):
         if x is None:
             if g is not None or y is not None:
                 raise ValueError(f"g_{name}, {name}_out need {name}")
-            args += [None, 0, 0, None, None, 0]
-            out.append(None)
-            continue
-        if g is not None and (g.dtype != dt or g.device != dev or tuple(g.shape) != (hd,)
-                              or not g.is_contiguous()):
-            raise ValueError(f"g_{name}: expected a contiguous {dt} [{hd}] tensor on {dev}")
+            return None, (None, 0, 0, None, None, 0)
+        if g is not None and (g.dtype != dt or g.get_device() != index or g.dim() != 1
+                              or g.shape[0] != hd or not g.is_contiguous()):
+            raise ValueError(f"g_{name}: expected a contiguous {dt} [{hd}] tensor on {q.device}")
+        xr = rows(name, x, None)
         if y is None:
-            y = _empty_on(stream, x.shape, dt, dev)
-        args += [*rows(name, x, None), x.shape[1], _ptr(g), *rows(name + "_out", y, x)]
-        out.append(y)
-    s = _RopeShape(head_dim=hd, rot_dim=2 * sum(sections), axes=len(sections),
-                   sections=(ctypes.c_int32 * 4)(*sections), interleaved=1 if interleaved else 0,
-                   dtype=code, theta=theta, eps=eps)
+            y = _empty_on(stream, x.shape, dt, q.device)
+        return y, (*xr, x.shape[1], None if g is None else g.data_ptr(),
+                   *rows(name + "_out", y, x.shape[1]))
+
+    (q_out, qa), (k_out, ka) = side("q", q, g_q, q_out), side("k", k, g_k, k_out)
     if tokens == 0:
-        return tuple(out)
-    with torch.cuda.device(dev):
-        _check(L.xp_rope(ctypes.byref(s), tokens, pos.data_ptr(),
-                         pos.stride(0) if len(sections) > 1 else tokens, *args, _stream(stream)),
-               f"xp_rope: head_dim={hd} (64, 128, 256), sections={sections} (their sum a multiple of "
-               f"8 up to {hd // 2}), theta={theta}, eps={eps}, 16-byte aligned rows")
-    return tuple(out)
+        return q_out, k_out
+    pld = pos.stride(0) if axes > 1 else tokens
+    if torch.cuda.current_device() == index:
+        st = L.xp_rope(ctypes.byref(shape), tokens, pos.data_ptr(), pld, *qa, *ka, _stream(stream))
+    else:
+        with torch.cuda.device(index):
+            st = L.xp_rope(ctypes.byref(shape), tokens, pos.data_ptr(), pld, *qa, *ka, _stream(stream))
+    if st != XP_OK:
+        raise XpError(st, f"xp_rope: head_dim={hd} (64, 128, 256), sections={list(sections)} (their sum "
+                      f"a multiple of 8 up to {hd // 2}), theta={theta}, eps={eps}, rows 16-byte aligned")
+    return q_out, k_out
+
+
+_rope_shapes: Dict[tuple, object] = {}
+
+
+def _rope_shape(hd, code, sections, interleaved, theta, eps):
+    """The xp_rope_shape record, kept for later calls."""
+    sections = [int(x) for x in sections]
+    if not 1 <= len(sections) <= 4 or min(sections) < 0:
+        raise ValueError("sections: pairs of 1 to 4 axes")
+    if len(_rope_shapes) >= 64:
+        _rope_shapes.clear()
+    return _RopeShape(head_dim=hd, rot_dim=2 * sum(sections), axes=len(sections),
+                      sections=(ctypes.c_int32 * 4)(*sections), interleaved=1 if interleaved else 0,
+                      dtype=code, theta=theta, eps=eps)
 
 
 def layer_weights_struct(weights: Dict[str, object], H: int, n_heads: int, n_kv: int, ffn: int,
@@ -682,20 +698,19 @@ class PagedKV:
         c = self._cache(k_cache, v_cache, k_scale, v_scale)
         if k is False and v is False:
             raise ValueError("k, v: one of them is read at least")
-        out, args = [], []
-        for name, t in (("k", k), ("v", v)):
-            if t is False:
-                out.append(None)
-                args += [None, 0]
-                continue
-            if t is None:
-                t = _empty_on(stream, (n, self.n_kv, self.head_dim), self._torch.bfloat16,
-                              self.device)
-            args += [t.data_ptr(), self._rows(name, t, self.n_kv, n)]
-            out.append(t)
+        shape = (n, self.n_kv, self.head_dim)
+        if k is None and v is None:
+            kv = _empty_on(stream, (2, *shape), self._torch.bfloat16, self.device)
+            k, v, at, row = kv[0], kv[1], kv.data_ptr(), self.n_kv * self.head_dim
+            args = (at, row, at + 2 * n * row, row)
+        else:
+            k, v = (_empty_on(stream, shape, self._torch.bfloat16, self.device) if t is None
+                    else (None if t is False else t) for t in (k, v))
+            args = (*((None, 0) if k is None else (k.data_ptr(), self._rows("k", k, self.n_kv, n))),
+                    *((None, 0) if v is None else (v.data_ptr(), self._rows("v", v, self.n_kv, n))))
         if n:
-            self._call("xp_kv_read", n, sl, *c, args[0], args[1], args[2], args[3], stream=stream)
-        return tuple(out)
+            self._call("xp_kv_read", n, sl, *c, *args, stream=stream)
+        return k, v
 
     def _attend(self, name, groups, q, k_cache, v_cache, table, kv_len, cu_q, max_q, causal,
                 window, sinks, scale, k_scale, v_scale, out, lse, stream):
@@ -784,10 +799,28 @@ class Sampler:
         if s != XP_OK:
             raise XpError(s, "xp_sampler_create: " + L.xp_sampler_last_error(None).decode())
         self._h, self._L, self._torch = h, L, torch
+        self._codes = {torch.float32: XP_F32, torch.bfloat16: XP_BF16}
+        self._raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
-    def _check(self, name, s):
+    def _call(self, name, *args, stream=None):
+        if self._torch.cuda.current_device() == self._index:
+            st = self._raw(self._index) if stream is None and self._raw else _stream(stream)
+            s = getattr(self._L, name)(self._h, *args, st)
+        else:
+            with self._torch.cuda.device(self._index):
+                s = getattr(self._L, name)(self._h, *args, _stream(stream))
         if s != XP_OK:
             raise XpError(s, f"{name}: " + self._L.xp_sampler_last_error(self._h).decode())
+
+    def _flat(self, name, t, dtype, n):
+        """The address of a contiguous device vector of n elements, None where none is given."""
+        if t is None:
+            return None
+        if (t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous()
+                or t.get_device() != self._index):
+            raise ValueError(f"{name}: expected a contiguous {dtype} tensor of {n} elements on "
+                             f"{self.device}")
+        return t.data_ptr()
 
     def sample(self, logits, temp=None, temperature=None, top_k=None, top_p=None, min_p=None,
                u=None, out=None, logprob=None, stream=None):
@@ -795,40 +828,27 @@ class Sampler:
         int32 `out` (allocated when None), which is returned; their log probabilities to
         `logprob` (float32) where given.  temp (uint8): 0 = greedy; None = all greedy."""
         torch = self._torch
-        code = {torch.float32: XP_F32, torch.bfloat16: XP_BF16}.get(logits.dtype)
-        n = logits.shape[0]
+        code, n = self._codes.get(logits.dtype), logits.shape[0]
         if (code is None or logits.dim() != 2 or logits.shape[1] != self.V
                 or logits.get_device() != self._index or (self.V > 1 and logits.stride(1) != 1)):
             raise ValueError(f"logits: expected float32 or bf16 [rows][{self.V}], rows contiguous, "
                              f"on {self.device}")
         if out is None:
             out = _empty_on(stream, (n,), torch.int32, self.device)
-        ptr = []
-        for name, t, dt in (("temp", temp, torch.uint8), ("temperature", temperature, torch.float32),
-                            ("top_k", top_k, torch.int32), ("top_p", top_p, torch.float32),
-                            ("min_p", min_p, torch.float32), ("u", u, torch.float32),
-                            ("out", out, torch.int32), ("logprob", logprob, torch.float32)):
-            if t is None:
-                ptr.append(None)
-                continue
-            if (t.dtype != dt or tuple(t.shape) != (n,) or not t.is_contiguous()
-                    or t.get_device() != self._index):
-                raise ValueError(f"{name}: expected a contiguous {dt} tensor of {n} elements on "
-                                 f"{self.device}")
-            ptr.append(t.data_ptr())
+        f32, i32, flat = torch.float32, torch.int32, self._flat
+        ptr = (flat("temp", temp, torch.uint8, n), flat("temperature", temperature, f32, n),
+               flat("top_k", top_k, i32, n), flat("top_p", top_p, f32, n),
+               flat("min_p", min_p, f32, n), flat("u", u, f32, n), flat("out", out, i32, n),
+               flat("logprob", logprob, f32, n))
         if n:
-            with torch.cuda.device(self._index):
-                self._check("xp_sample", self._L.xp_sample(
-                    self._h, n, code, logits.data_ptr(), logits.stride(0) if n > 1 else self.V,
-                    *ptr, _stream(stream)))
+            self._call("xp_sample", n, code, logits.data_ptr(),
+                       logits.stride(0) if n > 1 else self.V, *ptr, stream=stream)
         return out
 
     def device_errors(self, stream=None) -> int:
         """The XP_DEVERR_* bits set since the last read; synchronizes."""
         v = ctypes.c_uint32(0)
-        with self._torch.cuda.device(self._index):
-            self._check("xp_sampler_device_errors", self._L.xp_sampler_device_errors(
-                self._h, ctypes.byref(v), _stream(stream)))
+        self._call("xp_sampler_device_errors", ctypes.byref(v), stream=stream)
         return int(v.value)
 
     def close(self):
