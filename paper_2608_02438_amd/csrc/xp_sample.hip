@@ -47,7 +47,7 @@ enum SmpMode {
   kSmpPlain = 0,                     // no threshold of l: the chunks' sums are final
   kSmpList = 1,                      // the candidates are all tokens that can stay
   kSmpEdge = 2,                      // tokens before the edge's bin stay, those of it are candidates
-  kSmpSlow = 3                       // too many candidates: the row by radix selection
+  kSmpSlow = 3                       // too many candidates, or no bins: the row by radix selection
 };
 
 struct Smp {
@@ -158,6 +158,8 @@ struct SmpSet {
     k = k < d.V ? k : 0;
   }
   __device__ __forceinline__ bool cuts() const { return k > 0 || p < 1.f; }
+  // the bins' fp32 holds 16 / t, and every difference of logits that has a weight
+  __device__ __forceinline__ bool bins() const { return t >= 0x1p-120f && t <= 0x1p120f; }
   __device__ __forceinline__ double log_min() const { return mp > 0.f ? log((double)mp) : -INFINITY; }
 };
 
@@ -358,6 +360,11 @@ __global__ __launch_bounds__(kSmpThreads) void k_smp_mass(const Smp d) {
 __device__ __forceinline__ SmpRec smp_decide(const Smp& d, int64_t r, const SmpSet& set) {
   constexpr int N = kSmpHist / kWave;
   const int lane = threadIdx.x & 63;
+  if (!set.bins()) {
+    SmpRec x{};
+    x.mode = kSmpSlow;
+    return x;
+  }
   uint64_t v[N], sum = 0;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
@@ -677,7 +684,7 @@ __device__ __forceinline__ void row_draw(const Smp& d, RowShared& s, int64_t r, 
 }
 
 // Rows with more candidates than the list holds (many equal logits, or top-k of tens of
-// thousands with top-p): radix selection over the row itself.
+// thousands with top-p), or a temperature past the bins' fp32: radix selection over the row.
 template <typename T>
 __device__ __forceinline__ void row_slow(const Smp& d, RowShared& s, int64_t r, const T* row, bool wide,
                                       const SmpRow& w, const SmpSet& set) {

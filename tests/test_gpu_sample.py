@@ -162,6 +162,23 @@ def test_uniforms_and_temperatures_at_their_ends():
     s.close()
 
 
+@pytest.mark.parametrize("T,scale", [(2.0 ** -126, 2.0 ** -126), (2.0 ** -130, 2.0 ** -128),
+                                     (2.0 ** -121, 2.0 ** -120), (2.0 ** 121, 2.0 ** 122),
+                                     (3e38, 2.0 ** 126)])
+def test_temperatures_near_the_ends_of_fp32(T, scale):
+    """Where 1 / T, or a difference of logits that has a weight, passes fp32's range."""
+    V = 5000
+    c = Rows(21, 24, V, greedy=0)
+    c.T[:] = T
+    c.logits = (c.logits.double() / 8 * scale).float()
+    assert bool(c.logits.isfinite().all())
+    s = _sampler(V, 24)
+    ids, lp = c.run(s)
+    assert s.device_errors() == 0
+    c.check(ids, lp)
+    s.close()
+
+
 def test_settings_out_of_range_are_replaced_and_reported():
     import torch
     from paper_2608_02438_amd import xpress as X
