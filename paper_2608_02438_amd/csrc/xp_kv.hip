@@ -271,6 +271,16 @@ __device__ __forceinline__ float f8_quotient(float x, float s, float inv) {
   return q > 448.f ? 448.f : (q < -448.f ? -448.f : q);
 }
 
+// a thread's item where a grid's x holds 2^22 workgroups (its threads are counted in 32 bits)
+constexpr int kKvGridX = 1 << 22;
+__device__ __forceinline__ int64_t kv_item() {
+  return ((int64_t)blockIdx.z * kKvGridX + blockIdx.x) * 256 + threadIdx.x;
+}
+static dim3 kv_items_grid(int64_t items, unsigned y) {
+  const int64_t wgs = (items + 255) / 256;
+  return dim3((unsigned)std::min<int64_t>(wgs, kKvGridX), y, (unsigned)((wgs + kKvGridX - 1) / kKvGridX));
+}
+
 struct KvWrite {
   const uint16_t *k, *v;
   int64_t k_ld, v_ld;
@@ -313,7 +323,7 @@ template <int HD, int FMT>
 __global__ __launch_bounds__(256) void k_kv_write(const KvWrite d) {
   constexpr bool F8 = FMT == XP_E4M3, F4 = FMT == XP_MXFP4;
   constexpr int VE = F8 ? 16 : 8, CH = HD / VE;   // values, chunks of a row
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t i = kv_item();
   if (i >= d.items) return;
   const bool isv = blockIdx.y == 1;
   const int c = (int)(i % CH);
@@ -409,7 +419,7 @@ __device__ __forceinline__ float product_for_bf16(float x, float s) {
 template <int HD, int FMT>
 __global__ __launch_bounds__(256) void k_kv_read(const KvRead d) {
   constexpr int CH = HD / 8;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t i = kv_item();
   if (i >= d.items) return;
   const bool isv = blockIdx.y == 1 || d.k == nullptr;
   const int c = (int)(i % CH);
@@ -483,7 +493,7 @@ hipError_t launch_kv_write(const xp_kv* kv, int tokens, const uint16_t* k, const
   d.ks = k_scale;
   d.vs = v_scale;
   d.err = kv->err;
-  const dim3 grid((unsigned)((d.items + 255) / 256), 2);
+  const dim3 grid = kv_items_grid(d.items, 2);
 #define XP_KV(HD_, FMT_) hipLaunchKernelGGL((k_kv_write<HD_, FMT_>), grid, dim3(256), 0, st, d)
   if (kv->hd == 128) {
     if (kv->dtype == XP_BF16) XP_KV(128, XP_BF16);
@@ -516,7 +526,7 @@ hipError_t launch_kv_read(const xp_kv* kv, int tokens, const int32_t* slots, con
   d.k_ld = k_ld;
   d.v_ld = v_ld;
   d.err = kv->err;
-  const dim3 grid((unsigned)((d.items + 255) / 256), k != nullptr && v != nullptr ? 2 : 1);
+  const dim3 grid = kv_items_grid(d.items, k != nullptr && v != nullptr ? 2 : 1);
 #define XP_KV(HD_, FMT_) hipLaunchKernelGGL((k_kv_read<HD_, FMT_>), grid, dim3(256), 0, st, d)
   if (kv->hd == 128) {
     if (kv->dtype == XP_BF16) XP_KV(128, XP_BF16);

@@ -407,6 +407,32 @@ def test_pages_past_four_gigabytes():
     kv.close()
 
 
+def test_more_than_2_30_chunks_of_rows():
+    """Rows of 1024 heads: 17 GB of them, more workgroups than one dimension of a grid has."""
+    import torch
+    n_kv, P, tokens = 1024, 16, 2 ** 16 + 40
+    kv = _handle(n_kv, P, 8, max_tokens=tokens)
+    c = [torch.full(kv.cache_shape, 255, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    slots = torch.full((tokens,), -1, dtype=torch.int32, device="cuda")
+    at = [0, 5, 2 ** 16 - 1, 2 ** 16, tokens - 1]
+    to = [3, 17, 127, 64, 40]
+    slots[at] = _i32(to)
+    k = torch.zeros((tokens, n_kv, 128), dtype=torch.bfloat16, device="cuda")
+    rng = np.random.default_rng(3)
+    k[at] = _bf(rng.normal(size=(len(at), n_kv, 128)))
+    kv.write(k, k, slots, *c)
+    want = R.mxfp4_values(*R.to_mxfp4(k[at].double().cpu().numpy()))
+    for cache in c:
+        got = _values(cache, P, 128)[np.array(to) // P, :, np.array(to) % P]
+        assert np.array_equal(got, want)
+    k.fill_(7.0)
+    kv.read(slots, *c, k=k, v=False)
+    assert np.array_equal(k[at].double().cpu().numpy(), want)
+    assert int((k != 0).any(-1).any(-1).sum()) == len(at)
+    assert kv.device_errors() == 0
+    kv.close()
+
+
 @pytest.mark.parametrize("window,sinks", [(0, 0), (64, 16)])
 def test_layer_over_4_bit_pages(window, sinks):
     """The context layer writes its block's rows in 4 bits and attends to them: against
