@@ -525,10 +525,9 @@ xp_status xp_kv_read(xp_kv* kv, int32_t tokens, const int32_t* slots, const void
  * Scores and sums are fp32; the numerators enter the product with V as two bf16
  * parts, as one fp16 part (2^-11 of sum p |v| at most) with an 8-bit cache, and as one
  * bf16 part (2^-8) in calls of more than 64 rows over a bf16 one, of more than 32 over a
- * 4-bit one (max_q times the heads
- * of a group; with shared prefixes at least the mean tokens of a group times the heads,
+ * 4-bit one (rows: max_q times the heads of a group; with shared prefixes at least the mean tokens of a group times the heads,
  * or, for the keys behind prefixes that fill the largest row tiles, max_q alone).  So a
- * single token's result over a bf16 cache has the fewer bits in a call beside a prompt;
+ * single token's result over a bf16 or 4-bit cache has the fewer bits in a call beside a prompt;
  * two calls keep them.
  * Pages outside [0, n_pages) where a key is read are replaced by 0 and set
  * XP_DEVERR_PAGE; lengths outside [0, max_len] are clamped (XP_DEVERR_LENGTH).

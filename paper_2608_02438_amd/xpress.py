@@ -443,8 +443,8 @@ _rope_shapes: Dict[tuple, object] = {}
 def _rope_shape(hd, code, sections, interleaved, theta, eps):
     """The xp_rope_shape record, kept for later calls."""
     sections = [int(x) for x in sections]
-    if not 1 <= len(sections) <= 4 or min(sections) < 0:
-        raise ValueError("sections: pairs of 1 to 4 axes")
+    if not 1 <= len(sections) <= 4 or not all(0 <= x <= hd for x in sections):
+        raise ValueError(f"sections: pairs of 1 to 4 axes, {hd // 2} of them at most")
     if len(_rope_shapes) >= 64:
         _rope_shapes.clear()
     return _RopeShape(head_dim=hd, rot_dim=2 * sum(sections), axes=len(sections),
