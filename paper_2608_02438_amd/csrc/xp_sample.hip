@@ -356,56 +356,56 @@ __global__ __launch_bounds__(kSmpThreads) void k_smp_mass(const Smp d) {
   }
 }
 
-// What the histogram says: the bin in which the threshold lies.
-__device__ __forceinline__ SmpRec smp_decide(const Smp& d, int64_t r, const SmpSet& set) {
-  constexpr int N = kSmpHist / kWave;
-  const int lane = threadIdx.x & 63;
+// What the histogram says: the bin in which the threshold lies (whole workgroup, two bins
+// a thread; by every wave for itself 0.7 us more).
+struct SmpDecide {
+  uint64_t red[kSmpThreads / kWave];
+  SmpRec rec;
+};
+__device__ __forceinline__ SmpRec smp_decide(const Smp& d, int64_t r, const SmpSet& set, SmpDecide& s) {
+  static_assert(kSmpHist == 2 * kSmpThreads, "two bins a thread");
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const bool by_k = set.k > 0;
+  SmpRec x{};
   if (!set.bins()) {
-    SmpRec x{};
     x.mode = kSmpSlow;
     return x;
   }
-  uint64_t v[N], sum = 0;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    v[i] = d.hist[r * kSmpHist + N * lane + i];
-    sum += v[i];
+  const uint64_t* bins = d.hist + r * kSmpHist + 2 * tid;
+  const uint64_t v[2] = {bins[0], bins[1]};
+  uint64_t before = wave_scan_u64(v[0] + v[1], lane);
+  if (lane == 63) s.red[wave] = before;
+  if (tid == 0) {
+    // where no bin reaches it, top-k leaves every token that has a weight: the bins' all, or
+    // what top-p cuts of them
+    x.mode = set.p >= 1.f ? kSmpEdge : kSmpSlow;
+    x.edge = kSmpHist;
+    s.rec = x;
   }
-  uint64_t before = wave_scan_u64(sum, lane);
-  SmpRec x{};
-  x.all = shfl_u64(before, 63);
-  before -= sum;
-  const bool by_k = set.k > 0;
+  lds_barrier();
+  before -= v[0] + v[1];
+  for (int w = 0; w < kSmpThreads / kWave; ++w) {
+    x.all += s.red[w];
+    before += w < wave ? s.red[w] : 0u;
+  }
   const double want = (double)set.p * (double)x.all;
-  bool mine = false;
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
+  for (int i = 0; i < 2; ++i) {                    // one bin of all hits
     const uint64_t upto = before + v[i];
-    const bool hit = by_k ? before < (uint64_t)set.k && upto >= (uint64_t)set.k
-                          : (double)before < want && (double)upto >= want;
-    if (hit && !mine) {
-      mine = true;
-      x.edge = N * lane + i;
+    if (by_k ? before < (uint64_t)set.k && upto >= (uint64_t)set.k
+             : (double)before < want && (double)upto >= want) {
+      x.edge = 2 * tid + i;
       x.above = before;
       // top-p alone: whether the candidates are too many shows when they are counted
       x.mode = !by_k ? kSmpEdge
                      : (upto <= (uint64_t)kSmpCap ? kSmpList
                         : (v[i] <= (uint64_t)kSmpCap && set.p >= 1.f ? kSmpEdge : kSmpSlow));
+      s.rec = x;
     }
     before = upto;
   }
-  const uint64_t who = __ballot(mine);
-  if (who == 0) {
-    // top-k leaves every token that has a weight: the bins' all, or what top-p cuts of them
-    x.mode = set.p >= 1.f ? kSmpEdge : kSmpSlow;
-    x.edge = kSmpHist;
-    return x;
-  }
-  const int src = __builtin_ctzll(who);
-  x.mode = __shfl(x.mode, src, kWave);
-  x.edge = __shfl(x.edge, src, kWave);
-  x.above = shfl_u64(x.above, src);
-  return x;
+  lds_barrier();
+  return s.rec;
 }
 
 // Rows with a threshold of l: the candidates, and the sums of what stays before them.
@@ -413,6 +413,7 @@ template <typename T>
 __global__ __launch_bounds__(kSmpThreads) void k_smp_list(const Smp d) {
   __shared__ uint64_t red[kSmpThreads / kWave];
   __shared__ uint32_t num[kSmpThreads / kWave], base;
+  __shared__ SmpDecide dec;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const SmpPlace at = smp_place(d);
   if (d.temp[at.row] == 0) return;
@@ -424,7 +425,7 @@ __global__ __launch_bounds__(kSmpThreads) void k_smp_list(const Smp d) {
   smp_chunk(d, row, wide, at.c0, next);
   const uint32_t top_key = (uint32_t)(smp_best(d, at.r) >> 32);
   if (top_key == 0u) return;
-  const SmpRec rec = smp_decide(d, at.r, set);     // every wave the same
+  const SmpRec rec = smp_decide(d, at.r, set, dec);
   if (at.c0 == 0 && tid == 0) {
     SmpRec* to = d.rec + at.r;                     // rec.n counts meanwhile
     to->mode = rec.mode;
@@ -561,6 +562,19 @@ __device__ __forceinline__ uint64_t row_sort(RowShared& s, uint64_t x, int n) {
       x = first == falls ? umax64(x, y) : (x < y ? x : y);
     }
   return tid < size ? x : 0u;
+}
+
+// The same of a wave's 64.
+__device__ __forceinline__ uint64_t wave_sort(uint64_t x, int lane) {
+#pragma unroll
+  for (int m = 2; m <= kWave; m *= 2)
+#pragma unroll
+    for (int o = m / 2; o > 0; o /= 2) {
+      const uint64_t y = shfl_xor_u64(x, o);
+      const bool first = (lane & o) == 0, falls = (lane & m) == 0 || m == kWave;
+      x = first == falls ? umax64(x, y) : (x < y ? x : y);
+    }
+  return x;
 }
 
 // The first of the bins, from the top one down, at which the sum passes.
@@ -796,8 +810,34 @@ __global__ __launch_bounds__(kRowThreads) void k_smp_row(const Smp d) {
   uint32_t cut = 1u, tie_end = ~0u;
   auto kept = [&](uint32_t k, uint32_t i) { return !(k < cut || (k == cut && i >= tie_end)); };
   auto stays = [&](uint32_t k, uint32_t i) -> uint64_t { return kept(k, i) ? heavy(k) : 0u; };
-  if (n <= kRowThreads) {
-    // in order, a thread each: what lies before a candidate is a prefix sum
+  if (rec.mode == kSmpList && n <= kWave) {
+    // a wave has them all, and needs no barrier (12 -> 5.2 us): top-k decides, as in every list
+    if (tid >= kWave) return;
+    uint64_t x = tid < n ? list[tid] : 0u;
+    x = wave_sort(x != 0u ? (x & ~0xffffffffull) | (uint32_t)~(uint32_t)x : 0u, tid);
+    const uint32_t key = (uint32_t)(x >> 32), idx = ~(uint32_t)x;
+    const uint32_t kth = set.k <= n ? __shfl(key, set.k - 1, kWave) : 1u;
+    bool in = key != 0u && key >= kth;             // what ties with the k-th stays
+    const uint64_t v = in ? w.weight(key) : 0u;
+    uint64_t upto = wave_scan_u64(v, tid);
+    const double want = (double)set.p * (double)shfl_u64(upto, 63);
+    in = in && (set.p >= 1.f || (double)(upto - v) < want) && w.x(key) >= log_mp;
+    // by index, the lowest first
+    x = wave_sort(in ? ((uint64_t)(kIndexTop + 1 - idx) << 32) | key : 0u, tid);
+    const uint64_t mine = x != 0u ? w.weight((uint32_t)x) : 0u;
+    upto = wave_scan_u64(mine, tid);
+    const uint64_t Z = shfl_u64(upto, 63);
+    const double goal = smp_goal(d, r, Z);
+    const bool none = !((double)Z > goal);
+    const bool hit = mine > 0 && (none ? upto == Z : (double)upto > goal && !((double)(upto - mine) > goal));
+    if (hit) smp_out(d, r, row, w, (int)(kIndexTop + 1 - (uint32_t)(x >> 32)), Z);
+    return;
+  }
+  // In order, a thread each, what lies before a candidate is a prefix sum: two sorts, where
+  // radix selection takes two rounds for every threshold and two for the draw.  64 rows of
+  // 200 candidates 17 us against 19, of 400 20.5 against 19, of 800 24.5 against 20; with
+  // both thresholds 25.8 against 28.9.
+  if (n <= (set.k > 0 && set.p < 1.f ? kRowThreads : kRowThreads / 4)) {
     uint64_t x = tid < n ? list[tid] : 0u;
     x = row_sort(s, x != 0u ? (x & ~0xffffffffull) | (uint32_t)~(uint32_t)x : 0u, n);
     const uint32_t key = (uint32_t)(x >> 32), idx = ~(uint32_t)x;
