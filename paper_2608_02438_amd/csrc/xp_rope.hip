@@ -11,7 +11,10 @@
 // A wave has a token (a part of its heads where there are few tokens): its lanes form
 // the token's cosines and sines once, a pair each, and hand them round through LDS.
 // A head is HD / 16 lanes of 16 values: 8 of the pairs' first halves and their 8
-// partners, so that no value changes lanes.  Bound by memory where there are many tokens.
+// partners, so that no value changes lanes.  Bound by memory where there are many tokens:
+// 8191 tokens of 40 heads, three axes (168 MB), 37 to 41 us where the inputs alternate, 4.1 to
+// 4.5 TB/s, 29 where the caches still hold some of them; one token 2.9 us.  Tokens split among
+// more waves, each with fewer heads, took 49 to 52 us (the sines again).
 #include <algorithm>
 #include <cmath>
 
