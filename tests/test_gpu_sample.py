@@ -115,6 +115,54 @@ def test_equal_logits(V, levels):
     s.close()
 
 
+@pytest.mark.parametrize("k", [63, 64, 65, 255, 256, 257, 1023, 1024, 1025, 3000, 16384, 16385])
+@pytest.mark.parametrize("p", [1.0, 0.9])
+def test_top_k_of_any_size(k, p):
+    """As many candidates as a wave, a sort or a list holds, and one more or less: of rows in
+    which the k-th stands alone, and of rows of few levels, where many tie with it."""
+    V = 40000
+    c = Rows(k, 6, V, greedy=0)
+    c.logits[3:] = (c.logits[3:] * 64).round() / 64
+    c.k[:], c.p[:] = k, p
+    c.m[::2] = 0.0
+    s = _sampler(V, 6)
+    ids, lp = c.run(s)
+    assert s.device_errors() == 0
+    c.check(ids, lp)
+    s.close()
+
+
+def test_two_graphs_of_one_sampler():
+    """Two captured calls of different rows share the workspace; replayed in turn, with eager
+    calls between."""
+    import torch
+    V = 30000
+    s = _sampler(V, 20)
+    cs = [Rows(31, 20, V), Rows(32, 7, V, "bf16", greedy=0)]
+    args, outs, graphs = [c.args() for c in cs], [], []
+    for c, a in zip(cs, args):
+        out = torch.zeros(c.n, dtype=torch.int32, device="cuda")
+        lp = torch.zeros(c.n, device="cuda")
+        s.sample(c.logits, out=out, logprob=lp, **a)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            s.sample(c.logits, out=out, logprob=lp, **a)
+        outs.append((out, lp))
+        graphs.append(g)
+    for i in (0, 1, 1, 0, 1, 0):
+        for c, a in zip(cs, args):                     # other uniforms for both, on the device
+            c.u[:] = np.random.default_rng(100 + i).random(c.n).astype(np.float32)
+            a["u"].copy_(torch.tensor(c.u))
+        out, lp = outs[i]
+        out.zero_()
+        graphs[i].replay()
+        cs[1 - i].run(s)
+        cs[i].check(out.cpu().numpy(), lp.cpu().numpy())
+    assert s.device_errors() == 0
+    s.close()
+
+
 def test_masked_nan_and_infinite_logits():
     import torch
     from paper_2608_02438_amd import xpress as X
