@@ -16,8 +16,9 @@
 // once, from the caches after the first, and what bounds them is what each does before its
 // first and after its last token (settings, bins, scans, barriers): one row of 151936 logits
 // 3.5 + 5.5 + 8 + 6 us, 64 rows with every kind of filter 7.5 + 19 + 15 + 21.  The weights of
-// all tokens of 64 rows take 7 us, and 1216 workgroups of 118 to 128 registers are a fifth
-// more than run at once; with fewer registers they spill (74 to 148 us in all in place of 64).
+// all tokens of 64 rows take 7 us.  With fewer registers (118 to 128) more workgroups would
+// run at once, but spill (74 to 148 us in all in place of 64); by half chunks, in 82 to 92
+// and without spilling, 66.5.
 #include <stdarg.h>
 #include <stdio.h>
 
