@@ -534,9 +534,10 @@ xp_status xp_kv_read(xp_kv* kv, int32_t tokens, const int32_t* slots, const void
  * The same call gives the same bits; a request's summation order follows the
  * lengths of all requests of the call.
  * Errors: XP_EINVAL before any launch (null or misaligned pointers, sizes; also
- * where (tokens n_heads / n_kv / 32 + n) (keys / 64 + 8) n_kv reaches 2^31 (8 in place
- * of 32 over a 4-bit cache), keys the lesser of max_len and the table's, twice that with shared prefixes: such a call is
- * split, or made with a handle of a smaller max_len), XP_EHIP.
+ * where (tokens n_heads / n_kv / 32 + n) (keys / 64 + 8) n_kv reaches 2^31 (over a 4-bit
+ * cache 8 or 16 in place of 32 where max_q times the heads of a group is at most that),
+ * keys the lesser of max_len and the table's, twice that with shared prefixes: such a call
+ * is split, or made with a handle of a smaller max_len), XP_EHIP.
  */
 xp_status xp_kv_attn(xp_kv* kv, int32_t n, int32_t tokens, int32_t max_q, const void* q,
                      int64_t q_ld, const int32_t* cu_q, const int32_t* kv_len,

@@ -140,9 +140,14 @@ hipError_t launch_kv_read(const xp_kv* kv, int tokens, const int32_t* slots, con
                           uint16_t* v, int64_t k_ld, int64_t v_ld, hipStream_t st);
 // the units of the attention's work list, counted in 32 bits, for n sequences of
 // `tokens` tokens and tables of table_ld pages
-bool kv_units_fit(const xp_kv* kv, int64_t tokens, int64_t n, int groups, int64_t table_ld);
-// rows of the smallest row tile
-inline int kv_least(const xp_kv* kv) { return kv->dtype == XP_MXFP4 ? 8 : 32; }
+// in calls of so many tokens a sequence
+bool kv_units_fit(const xp_kv* kv, int64_t tokens, int64_t n, int groups, int64_t table_ld,
+                  int64_t max_q);
+// the fewest rows of a row tile in calls of so many rows a sequence, in any call
+inline int kv_least(const xp_kv* kv, int64_t rows) {
+  return kv->dtype != XP_MXFP4 || rows > 16 ? 32 : (rows <= 8 ? 8 : 16);
+}
+inline int kv_least(const xp_kv* kv) { return kv_least(kv, 0); }
 // rows of partials and entries a handle needs
 void kv_attn_sizes(const xp_kv* kv, int64_t* rows, int* entries, int* shares);
 

@@ -468,9 +468,10 @@ __global__ void k_kv_clear_err(uint32_t* err) {
   if (threadIdx.x == 0) *err = 0u;
 }
 
-bool kv_units_fit(const xp_kv* kv, int64_t tokens, int64_t n, int groups, int64_t table_ld) {
+bool kv_units_fit(const xp_kv* kv, int64_t tokens, int64_t n, int groups, int64_t table_ld,
+                  int64_t max_q) {
   const int64_t keys = std::min<int64_t>(kv->max_pages, table_ld) * kv->P;
-  const int64_t ent = (tokens * kv->grp / kv_least(kv) + n) * (groups > 0 ? 2 : 1);
+  const int64_t ent = (tokens * kv->grp / kv_least(kv, max_q * kv->grp) + n) * (groups > 0 ? 2 : 1);
   return ent * (keys / kKvTile + 8) * kv->nkv < ((int64_t)1 << 31);
 }
 
@@ -836,7 +837,7 @@ static xp_status kv_attn(xp_kv* kv, const KvAttnArgs& a, void* stream) {
                    "of range", a.causal, a.window, a.sinks, (double)a.scale);
   const xp_status s = kv_cache_args(kv, a.kc, a.vc, a.k_scale, a.v_scale);
   if (s != XP_OK) return s;
-  if (!kv_units_fit(kv, a.total_q, a.n, a.groups, a.table_ld))
+  if (!kv_units_fit(kv, a.total_q, a.n, a.groups, a.table_ld, a.max_q))
     return kv_fail(kv, XP_EINVAL, "the call's tokens and max_len reach 2^31 key tiles");
   const xp_status ds = kv_device(kv);
   if (ds != XP_OK || a.n == 0 || a.total_q == 0) return ds;

@@ -1398,7 +1398,7 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
 // ---------------------------------------------------------------------------
 typedef int intx8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) char lds_char;
-constexpr int kFewRows = 16;         // the larger row tile
+constexpr int kFewRows = 16;         // the larger row tile (kv_least)
 constexpr int kFewSimd = 3;          // waves of a SIMD
 
 __device__ __forceinline__ floatx4 mma16_bf16(u32x4 a, u32x4 b, floatx4 c) {
@@ -2020,7 +2020,7 @@ __global__ __launch_bounds__(256) void k_kv_join_rows(const KvDev d, const KvJoi
 static int kv_most(const xp_kv* kv) { return kv->hd == 64 ? 128 : 256; }
 static int kv_rows(const xp_kv* kv, int64_t rows) {
   const int most = kv_most(kv);
-  if (rows <= kFewRows && kv->dtype == XP_MXFP4) return rows <= 8 ? 8 : kFewRows;   // k_kv_few
+  if (kv_least(kv, rows) < 32) return kv_least(kv, rows);   // k_kv_few
   return rows <= 32 ? 32 : rows <= 64 ? 64 : rows <= 128 ? 128 : most;
 }
 constexpr int kFewWaves = 4;
@@ -2129,7 +2129,7 @@ hipError_t launch_kv_attn(const xp_kv* kv, const KvAttnArgs& a, hipStream_t st) 
   p.window = a.window;
   p.sinks = a.sinks;
   p.groups = a.groups;
-  p.entries = (int)((int64_t)a.total_q * kv->grp / kv_least(kv) + a.n);   // of a list: no more fit the tokens
+  p.entries = (int)((int64_t)a.total_q * kv->grp / kv_least(kv, rows) + a.n);   // of a list: no more fit the tokens
   for (int k = 0; k < lists; ++k) {
     p.R[k] = R[k];
     p.shares[k] = kv_shares(kv, R[k]);

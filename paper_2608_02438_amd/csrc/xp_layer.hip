@@ -1511,7 +1511,7 @@ extern "C" xp_status xp_layer_forward_paged(xp_layer* L, xp_kv* kv, int32_t batc
   if (kv->nh != L->nh || kv->nkv != L->nkv || kv->hd != kHd)
     return layer_fail(L, XP_EINVAL, "the cache has heads %d/%d x %d, the layer %d/%d x %d", kv->nh,
                       kv->nkv, kv->hd, L->nh, L->nkv, kHd);
-  if (!kv_units_fit(kv, batch * B, batch, 0, table_ld))
+  if (!kv_units_fit(kv, batch * B, batch, 0, table_ld, B))
     return layer_fail(L, XP_EINVAL, "the call's tokens and the tables' pages reach 2^31 key tiles");
   if (window < 0 || window > kKvMaxLen || sinks < 0 || sinks > kKvMaxLen)
     return layer_fail(L, XP_EINVAL, "window=%d or sinks=%d out of range 0..2^22", window, sinks);

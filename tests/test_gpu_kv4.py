@@ -433,6 +433,38 @@ def test_more_than_2_30_chunks_of_rows():
     kv.close()
 
 
+def test_a_long_prompt_in_a_handle_of_long_contexts():
+    """65536 new tokens where contexts may reach 2^20 keys: as over the other caches (whose
+    row tiles have 32 rows at least) the call is made, not refused."""
+    import torch
+    from paper_2608_02438_amd.xpress import PagedKV, XpError
+    T, P, hd, nh, n_kv, W = 65536, 256, 128, 32, 8, 40
+    kv = PagedKV(nh, n_kv, P, T // P, 1, T, 1 << 20, cache_dtype="mxfp4")
+    g = torch.Generator(device="cuda").manual_seed(2)
+    q = torch.randn((T, nh, hd), generator=g, device="cuda").bfloat16()
+    k, v = (torch.randn((T, n_kv, hd), generator=g, device="cuda").bfloat16() for _ in range(2))
+    c = [torch.zeros(kv.cache_shape, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    table = torch.full((1, (1 << 20) // P), -1, dtype=torch.int32, device="cuda")
+    table[0, :T // P] = torch.arange(T // P, device="cuda")
+    slots = torch.arange(T, dtype=torch.int32, device="cuda")
+    kv.write(k, v, slots, *c)
+    kc, vc = (x.double().cpu().numpy() for x in kv.read(slots, *c))
+    out = kv.attend(q, *c, table, _i32([T]), cu_q=_i32([0, T]), max_q=T, window=W)
+    assert kv.device_errors() == 0
+    for t in (0, 1, 63, 64, 40000, T - 1):
+        a = max(t - W + 1, 0)
+        o, _, spread, score = R.attend(q[t:t + 1].double().cpu().numpy(), kc[a:t + 1], vc[a:t + 1])
+        # tests/_kv.py's bound, one bf16 part
+        d = 2 * ((hd + 12) * 2.0 ** -23 * score + 2.0 ** -22) + W * 2.0 ** -23 + 2.0 ** -20
+        e = d[..., None] + 2.0 ** -8
+        err = np.abs(out[t:t + 1].double().cpu().numpy() - o)
+        assert (err <= 2.0 ** -8 * (np.abs(o) + e * spread) + e * spread + 1e-30).all()
+    # tiles of 8 rows: their list would not fit 32 bits
+    with pytest.raises(XpError):
+        kv.attend(q, *c, table, _i32([T]), cu_q=_i32([0, T]), max_q=2, window=W)
+    kv.close()
+
+
 @pytest.mark.parametrize("window,sinks", [(0, 0), (64, 16)])
 def test_layer_over_4_bit_pages(window, sinks):
     """The context layer writes its block's rows in 4 bits and attends to them: against
