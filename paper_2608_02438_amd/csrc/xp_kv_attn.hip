@@ -621,11 +621,11 @@ __device__ __forceinline__ int wave_scan(int v, int lane) {
   return v;
 }
 
-// A work list of at most 64 entries, made by one wave of every workgroup for itself, a
-// lane per sequence and then per entry: small calls spare a launch and the way of the
-// list through memory (one token over 100 keys 17.2 -> 14.6 us, 48 in a window 72.5 -> 70.8).
-// Entries to ent, the share's beginning to sh[0..3] (and its global copy, for
-// k_kv_join) and its end to sh[4].
+// A work list of at most 64 entries of at most 64 sequences, made by one wave of every
+// workgroup for itself, a lane per sequence and then per entry: small calls spare a launch
+// and the way of the list through memory (one token over 100 keys 17.2 -> 14.6 us, 48 in a
+// window 72.5 -> 70.8).  Entries to ent, the share's beginning to sh[0..3] (and its global
+// copy, for k_kv_join) and its end to sh[4].
 constexpr int kOwnEntries = kWave;
 __device__ __forceinline__ void plan_own(const KvDev& d, int R, int shares, int sidx, KvEntry* ent,
                                          int32_t* sh) {
@@ -2145,7 +2145,9 @@ hipError_t launch_kv_attn(const xp_kv* kv, const KvAttnArgs& a, hipStream_t st) 
   int64_t most = (int64_t)a.total_q * kv->grp / R[0] + a.n;
   // few rows: a tile has a token at least, so that 64 single tokens make their list themselves
   if (R[0] <= kFewRows && kv->grp <= R[0]) most = std::min<int64_t>(most, a.total_q);
-  const bool own = a.groups == 0 && most <= kOwnEntries;
+  // plan_own has a lane for a request and one for an entry: requests without tokens have a
+  // lane, but no entry
+  const bool own = a.groups == 0 && a.n <= kOwnEntries && most <= kOwnEntries;
   if (own) p.entries = (int)most;
   hipError_t e;
   if (!own) {

@@ -298,6 +298,96 @@ def test_attend4_shared(name, hd):
     kv.close()
 
 
+def _slots_call(seed, n, active, ql=1, **kw):
+    """n request slots of which `active` have ql new tokens; some of the idle ones keep keys."""
+    rng = np.random.default_rng(seed)
+    keys = rng.integers(1, 300, size=n)
+    q = [ql if b in active else 0 for b in range(n)]
+    kv_len = [int(keys[b]) + q[b] if q[b] else int(keys[b]) * (b % 3 == 0 and n <= 300)
+              for b in range(n)]
+    return Call4(seed, kv_len, q, **kw)
+
+
+SLOTS = {                            # slots, those with tokens, tokens of each
+    "64 of 65": (65, [b for b in range(65) if b != 3], 1),
+    "the last of 65": (65, [64], 1),
+    "35 of 96": (96, [5, 20, 63] + list(range(64, 96)), 1),
+    "40 of 200": (200, [0, 62] + list(range(64, 200, 4))[:34] + [190, 194, 198, 199], 1),
+    "blocks, 30 of 100": (100, [3, 40] + list(range(66, 94)), 2),
+    "blocks, 12 of 300": (300, [64, 65, 100, 128, 191, 192, 255, 256, 257, 290, 298, 299], 4),
+    "64 of 64": (64, list(range(64)), 1),
+    "100 of 100": (100, list(range(100)), 1),
+    "64 of 4096": (4096, list(range(63, 4096, 64)), 1),
+}
+
+
+@pytest.mark.parametrize("name", SLOTS)
+@pytest.mark.parametrize("hd,heads,n_kv", [(128, 8, 2), (64, 4, 1), (128, 16, 1), (64, 32, 2)])
+def test_request_slots_without_tokens(name, hd, heads, n_kv):
+    """Few tokens of many request slots, most of them behind the 64th: every token's row is
+    written, the rows behind the last one are not."""
+    import torch
+    n, active, ql = SLOTS[name]
+    c = _slots_call(n + hd + heads, n, active, ql, heads=heads, n_kv=n_kv, hd=hd, P=32)
+    kv = c.device(max_tokens=c.total + 3)
+    q = torch.cat([c.dq, torch.ones((3, heads, hd), dtype=torch.bfloat16, device="cuda")])
+    for m in (dict(causal=True), dict(causal=True, window=40, sinks=2)):
+        for tokens in ((c.total, c.total + 3) if m == dict(causal=True) else (c.total,)):
+            print(f"slots: {name} hd={hd} heads={heads}/{n_kv} tokens={tokens} {m}", flush=True)
+            out = torch.full((c.total + 3, heads, hd), 777.0, dtype=torch.bfloat16, device="cuda")
+            lse = torch.full((c.total + 3, heads), 777.0, device="cuda")
+            c.run(kv, q=q[:tokens], out=out[:tokens], lse=lse[:tokens], **m)
+            assert kv.device_errors() == 0
+            c.check(out, lse, parts=parts_of4(c.rows()), **m)
+            assert (out[c.total:] == 777).all() and (lse[c.total:] == 777).all()
+    kv.close()
+
+
+@pytest.mark.parametrize("heads,n_kv", [(8, 2), (16, 1)])
+def test_a_captured_step_over_slots(heads, n_kv):
+    """A step captured for 96 request slots is replayed as other slots become active."""
+    import torch
+    n = 96
+    sets = [list(range(40)), list(range(56, 96)), list(range(1, 80, 2)), [95] + list(range(39))]
+    calls = [_slots_call(7, n, s, heads=heads, n_kv=n_kv, P=16) for s in sets]
+    need = max(c.width for c in calls)
+    kv = calls[0].device(max_len=need * 16)
+    tokens = calls[0].total
+    table = torch.zeros((n, need), dtype=torch.int32, device="cuda")
+    pages = max(c.n_pages for c in calls)
+    handle = Call4(1, [16 * (pages - 3)], [1], heads=heads, n_kv=n_kv, P=16).device(
+        max_batch=n, max_tokens=tokens, max_len=need * 16)
+    kv.close()
+    kc, vc = (torch.zeros(handle.cache_shape, dtype=torch.uint8, device="cuda") for _ in range(2))
+    q, cu, lens = torch.empty_like(calls[0].dq), _i32(np.zeros(n + 1)), _i32(np.zeros(n))
+    out, lse = torch.empty_like(q), torch.empty((tokens, heads), device="cuda")
+    step = lambda: handle.attend(q, kc, vc, table, lens, cu_q=cu, max_q=1, out=out, lse=lse)  # noqa: E731
+
+    def load(c):
+        c.device().close()
+        assert c.total == tokens
+        kc[:c.n_pages], vc[:c.n_pages] = c.dk, c.dv
+        table[:, :c.width] = c.dtable
+        q.copy_(c.dq), cu.copy_(c.dcu), lens.copy_(c.dkv)
+        out.fill_(777.0), lse.fill_(777.0)
+    load(calls[0])
+    step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    for i in (0, 1, 2, 3, 1, 0):
+        load(calls[i])
+        g.replay()
+        torch.cuda.synchronize()
+        assert handle.device_errors() == 0
+        calls[i].check(out, lse, causal=True, parts=parts_of4(calls[i].rows()))
+        got = out.clone()
+        step()
+        assert out.equal(got)
+    handle.close()
+
+
 def test_many_sequences_and_strided_rows():
     import torch
     ql = [(150, 1, 16, 33, 0, 2)[i % 6] for i in range(70)]
