@@ -329,6 +329,94 @@ def test_targets_for_verification():
     s.close()
 
 
+# (rows, V): with 256 CUs a workgroup has rows * chunks / 1024 chunks of 4096 tokens of a
+# row, and the last of a row what is left; rows go through the launches 128 at a time
+@pytest.mark.parametrize("rows,V,ld,offset", [
+    (64, 151936, None, 0),               # two chunks a workgroup
+    (64, 135001, 135003, 1),             # two, one in the last; unaligned rows
+    (100, 151936, None, 0),              # three, two in the last
+    (128, 250000, None, 0),              # seven, six in the last
+    (129, 5000, None, 0), (300, 40000, 40001, 0),   # a batch of one row, of 44
+    (131, 151936, None, 0)])             # four chunks and two in the last, then one
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_chunks_of_a_workgroup_and_batches_of_rows(rows, V, ld, offset, dtype):
+    """Rows, settings and logits all different."""
+    print(f"sample: rows={rows} V={V} {dtype}", flush=True)
+    c = Rows(rows + V, rows, V, dtype, ld=ld, offset=offset)
+    s = _sampler(V, rows)
+    ids, lp = c.run(s)
+    assert s.device_errors() == 0
+    c.check(ids, lp)
+    ids = s.sample(c.logits).cpu().numpy()
+    assert np.array_equal(ids, c.logits.float().cpu().numpy().argmax(-1))
+    for kw, drop in ((dict(top_k=None, top_p=None), dict(k=0, p=1.0)), (dict(top_k=None), dict(k=0)),
+                     (dict(top_p=None, min_p=None), dict(p=1.0, min_p=0.0))):
+        if rows * V < 10 ** 7:
+            ids, lp = c.run(s, **kw)
+            c.check(ids, lp, **drop)
+    s.close()
+
+
+@pytest.mark.parametrize("rows,V", [(9, 4999), (9, 151936), (70, 151936)])
+@pytest.mark.parametrize("k,p", [(20, 0.8), (20, 1.0), (1000, 0.8), (1000, 0.999), (1000, 1.0), (0, 0.8)])
+def test_rows_of_few_tokens_with_a_weight(rows, V, k, p):
+    """One to a few tokens far ahead of the others at low temperatures: fewer than k of them
+    have a weight."""
+    import torch
+    c = Rows(rows + V + k, rows, V, greedy=0)
+    rng = np.random.default_rng(k)
+    l = c.logits.cpu().numpy()
+    for r in range(rows):
+        at = rng.choice(V, size=(1, 2, 5, 15, 19, 20, 21, 30, 500)[r % 9], replace=False)
+        l[r, at] = 40 + rng.random(at.size)
+    c.logits = _t(l, torch.float32)
+    c.T[:] = rng.uniform(0.2, 0.7, size=rows)
+    c.k[:], c.p[:] = k, p
+    print(f"peaked rows: rows={rows} V={V} k={k} p={p}", flush=True)
+    s = _sampler(V, rows)
+    ids, lp = c.run(s)
+    assert s.device_errors() == 0
+    c.check(ids, lp)
+    s.close()
+
+
+def test_anchors_and_greedy_targets_of_a_block():
+    """A first token and greedy targets go from the sampler into refine and verify."""
+    import oracle as O
+    import synth
+    import torch
+    from paper_2608_02438_amd.xpress import device_tensor, refiner_from_arrays
+    w = synth.configs.TINY_F32
+    batch, B, V = 3, w.B, w.V
+    w = synth.scaled(w, index=w.index + 900, batch=batch)
+    weights, inp = synth.make_weights(w), synth.make_inputs(w)
+    ref = refiner_from_arrays(weights, w.H, w.r, V, B, batch)
+    s = _sampler(V, batch * (B + 1))
+    rng = np.random.default_rng(9)
+    first = rng.normal(size=(batch, V)).astype(np.float32)
+    anchor = s.sample(_t(first, torch.float32))
+    seeds = rng.integers(0, V, size=(batch, B)).astype(np.int32)
+    out = ref.refine_block(device_tensor(inp.h), anchor, seed_ids=device_tensor(seeds), K=w.K)
+    P = O.Params.from_arrays(weights)
+    res = O.refine_batch(P, inp.h, first.argmax(-1).astype(np.int32), inp.temp, inp.u_draft, w.K,
+                         seed_ids=seeds)
+    want = np.stack([r.ids for r in res.refined])
+    assert np.array_equal(out.ids.cpu().numpy(), want)
+    target = rng.normal(size=(batch, B + 1, V)).astype(np.float32)
+    for b, n in enumerate((0, B // 2, B)):                # tokens that the target agrees with
+        target[b, np.arange(n), want[b, :n]] = 9.0
+        if n < B:
+            target[b, n, want[b, n]] = -9.0
+    t = s.sample(_t(target.reshape(-1, V), torch.float32)).view(batch, B + 1)
+    n, nxt = ref.verify_block(out.ids, t)
+    best = target.argmax(-1)
+    for b, accepted in enumerate((0, B // 2, B)):
+        assert (int(n[b]), int(nxt[b])) == O.verify_greedy(want[b], best[b])
+        assert int(n[b]) == accepted
+    ref.close()
+    s.close()
+
+
 def test_calls_reject_bad_arguments():
     import torch
     from paper_2608_02438_amd import xpress as X
