@@ -298,6 +298,41 @@ def test_attend4_shared(name, hd):
     kv.close()
 
 
+def _behind_prefixes(groups, each, shared, own):
+    """Single tokens of `each` requests behind every one of so many prefixes."""
+    kv = [shared + 16 * g + 1 + (own * (i + 1)) % 97 for g in range(groups) for i in range(each)]
+    return kv, [1] * len(kv), [(g * each, (g + 1) * each, shared + 16 * g) for g in range(groups)]
+
+
+SHARED4_TWO = {                      # both lists' tiles have up to 32 rows
+    "one group": SHARED4["one group"], "odd prefix": SHARED4["odd prefix"],
+    "16 prefixes": (*_behind_prefixes(16, 4, 48, 31), dict(heads=8, n_kv=2)),
+    "2 prefixes": (*_behind_prefixes(2, 8, 400, 17), dict(heads=4, n_kv=1)),
+    "a head each": (*_behind_prefixes(5, 8, 160, 23), dict(heads=2, n_kv=2)),
+    "blocks": ([300, 340, 220], [5, 4, 3], [(0, 2, 192), (2, 3, 64)], dict(heads=4, n_kv=2)),
+}
+
+
+@pytest.mark.parametrize("name", SHARED4_TWO)
+@pytest.mark.parametrize("hd", [64, 128])
+def test_attend4_shared_numerators_of_two_parts(name, hd):
+    """Calls whose rows a prefix are 32 at most keep both parts of every numerator."""
+    import torch
+    kv_len, ql, groups, kw = SHARED4_TWO[name]
+    c = Call4(len(name) + 60, kv_len, ql, groups=groups, hd=hd, P=16, spread=2,
+              sigma_q=0.5, **kw)
+    rows = max(max(ql), sum(ql) // len(groups)) * (c.heads // c.n_kv)
+    assert parts_of4(rows) == 2
+    kv = c.device(shared=True)
+    for m in (dict(causal=True), dict(causal=True, window=150, sinks=20), dict(causal=False)):
+        print(f"shared4, two parts: {name} hd={hd} {m}", flush=True)
+        lse = torch.full((c.total, c.heads), 777.0, device="cuda")
+        out = c.run(kv, shared=True, lse=lse, **m)
+        assert kv.device_errors() == 0
+        c.check(out, lse, parts=2, **m)
+    kv.close()
+
+
 def _slots_call(seed, n, active, ql=1, **kw):
     """n request slots of which `active` have ql new tokens; some of the idle ones keep keys."""
     rng = np.random.default_rng(seed)
