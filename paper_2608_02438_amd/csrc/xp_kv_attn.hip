@@ -1378,11 +1378,13 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
 //
 // * S^T = K Q^T on v_mfma_scale_f32_16x16x128_f8f6f4: its fp4 operand is a lane's 32
 //   codes of one block as they lie in memory, with the block's power of two, so K goes
-//   from the load into the product.  The queries are its e4m3 operand, in three parts:
-//   a row's largest element lies in [2^7, 2^8), the first part takes 4 bits, the second
-//   the next 4 (all that bf16 has, for elements above 2^-13 of the largest), the third
-//   what lies deeper, where a row of the tile has such bits; what is left is 2^-39 of the
-//   largest.
+//   from the load into the product.  The queries are its e4m3 operand, in two parts: a
+//   row's largest element lies in [2^7, 2^8), the first part takes 4 bits, the second the
+//   next 4: all that bf16 has, for elements down to 2^-14 of the largest.
+// * Where a row of the tile has smaller ones (beside a key whose block for the largest is
+//   as small, they are the score), K is expanded to bf16 in registers and the queries come
+//   as they are, through LDS: 6% of such tiles of 4 normal rows, which take a tenth longer
+//   (a third fp8 part instead: registers that the loads need, 16 rows 2 to 5% slower).
 // * V's power of two differs from key to key, the dimension that P V sums over, where
 //   the instruction takes one for 32: V is expanded to bf16 (exactly) on its way into
 //   the wave's LDS and comes back by transposing reads.
@@ -1433,13 +1435,17 @@ __global__ __launch_bounds__(NW* kWave, kFewSimd) void k_kv_few(const KvDev d) {
   // offset
   constexpr int NT = HD / 16, RB = 2 * HD + 16;
   constexpr bool HALF = R == 8;                   // a column is a row and a part
-  // products of the first two parts, and of the third
-  constexpr int QM = HALF || HD == 64 ? 1 : 2, QD = HALF && HD == 64 ? 0 : 1;
+  constexpr int QM = HALF || HD == 64 ? 1 : 2;    // products of the queries' two parts
+  constexpr int kDeepest = 14;                    // binades that the parts hold
   constexpr int RBM = kv_row_bytes(XP_MXFP4, HD);
   constexpr int kMerge = (4 * NT + 2) * kWave;    // floats that a wave hands over
   constexpr int kRing = kMerge * 4 > 32 * RB ? kMerge * 4 : 32 * RB;   // its LDS: V of half a tile
   static_assert(kRing % 256 == 0, "a wave's LDS");
   __shared__ __align__(256) char lds[NW * kRing];
+  // the queries, where parts do not hold them: 16 bytes behind every row of V, where that is
+  // enough (4 KB of their own cost 2% of a call's time)
+  constexpr bool kBehind = R * HD / 8 <= 32 * NW;
+  __shared__ __align__(16) u32x4 own_q[kBehind ? 1 : R * HD / 8];
   __shared__ KvEntry own_ent[OWN ? kOwnEntries : 1];
   __shared__ int32_t own_sh[8];
   const int lane = threadIdx.x & 63;
@@ -1544,16 +1550,25 @@ __global__ __launch_bounds__(NW* kWave, kFewSimd) void k_kv_few(const KvDev d) {
   // ---- the query rows ----
   const bool rv = ri < nrows;
   KvSees sees;
-  intx8 qp[QM + QD];
-  int qs[QM + QD];
-  bool deep = false;                              // some row has a third part
+  // dims 8 c .. 8 c + 7 of row ri, as they are
+  auto raw_q = [&](int c) __attribute__((always_inline)) {
+    c += ri * (HD / 8);
+    if constexpr (kBehind)
+      return reinterpret_cast<u32x4*>(lds + c / 32 * kRing + c % 32 * RB + 2 * HD);
+    else
+      return own_q + c;
+  };
+  intx8 qp[QM];
+  int qs[QM];
+  bool raw = false;                               // some row has elements that are in no part
   {
     const int row = row0 + (rv ? ri : 0), tk = row / d.grp;
     const int64_t tok = tok0 + tk;
     const uint16_t* q = d.q + tok * d.q_ld + (int64_t)(kvh * d.grp + (row - tk * d.grp)) * HD;
     constexpr int NQ = HD / 64;                   // pieces of 16 dims: 16 g, and 64 + 16 g
     uint32_t x[NQ][8];
-    uint32_t top = 0;                             // the greatest magnitudes, two of 16 bits
+    uint32_t top = 0;                             // the greatest magnitudes, two of 16 bits,
+    ushort2v low = {0xffff, 0xffff};              // the least but 0, less 1
 #pragma unroll
     for (int n = 0; n < NQ; ++n)
 #pragma unroll
@@ -1564,15 +1579,27 @@ __global__ __launch_bounds__(NW* kWave, kFewSimd) void k_kv_few(const KvDev d) {
           x[n][4 * c + i] = y[i];
           top = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(
               __builtin_bit_cast(ushort2v, top), __builtin_bit_cast(ushort2v, y[i] & 0x7fff7fffu)));
+          low = __builtin_elementwise_min(
+              low, __builtin_bit_cast(ushort2v, y[i] & 0x7fff7fffu) - ushort2v{1, 1});
         }
       }
     const uint32_t most = umax_xor32(umax_xor16(max(top >> 16, top & 0xffffu)));
     // 2^7 <= x < 2^8 for the largest; an infinity or NaN makes the row's scores NaN
     const bool odd = most >= 0x7f80u;
-    const int eb = imax((int)(most >> 7), 31), s0 = eb - 7, s1 = s0 - 5, s2 = s1 - 18;
+    const int eb = imax((int)(most >> 7), kDeepest + 1);
+    const int s0 = eb - 7, s1 = s0 - 5;
     const float up = __uint_as_float((uint32_t)(261 - imin(eb, 254)) << 23);
-    intx8 part[3];
-    uint32_t rest = 0;
+    raw = __ballot((int)min(low[0], low[1]) + 1 < (eb - kDeepest) << 7) != 0;
+    if (__builtin_expect(raw, 0)) {               // wave-uniform; every wave writes the same
+#pragma unroll
+      for (int n = 0; n < NQ; ++n)
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+          if (li < R)
+            *raw_q(8 * n + 2 * g + c) = u32x4{x[n][4 * c], x[n][4 * c + 1], x[n][4 * c + 2], x[n][4 * c + 3]};
+      wave_lds_order();
+    }
+    intx8 part[2];
 #pragma unroll
     for (int n = 0; n < NQ; ++n)
 #pragma unroll
@@ -1584,56 +1611,42 @@ __global__ __launch_bounds__(NW* kWave, kFewSimd) void k_kv_few(const KvDev d) {
           y[i] = __uint_as_float(i % 2 == 0 ? w << 16 : w & 0xffff0000u) * up;
         }
 #pragma unroll
-        for (int p = 0; p < 3; ++p) {
+        for (int p = 0; p < 2; ++p) {
           int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
           w = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
           part[p][4 * n + c] = w;
-          if (p < 2) {                            // 5 and 18 binades from a part to the next
+          if (p == 0) {                           // 5 binades to the next
             const xp_f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false);
             const xp_f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
-            const float m = p == 0 ? 0x1p5f : 0x1p18f;
-            y[0] = (y[0] - lo[0]) * m;
-            y[1] = (y[1] - lo[1]) * m;
-            y[2] = (y[2] - hi[0]) * m;
-            y[3] = (y[3] - hi[1]) * m;
+            y[0] = (y[0] - lo[0]) * 0x1p5f;
+            y[1] = (y[1] - lo[1]) * 0x1p5f;
+            y[2] = (y[2] - hi[0]) * 0x1p5f;
+            y[3] = (y[3] - hi[1]) * 0x1p5f;
           }
         }
-        rest |= (uint32_t)part[2][4 * n + c] & 0x7f7f7f7fu;
       }
-    deep = __ballot(rest != 0) != 0;
     const bool second = HALF && li >= 8;          // the columns of second parts
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
       if constexpr (HD == 128 && !HALF) {
         qp[0][c] = part[0][c];
         qp[1][c] = part[1][c];
-        qp[2][c] = part[2][c];
       } else if constexpr (HD == 128) {
         qp[0][c] = second ? part[1][c] : part[0][c];
-        qp[1][c] = second ? 0 : part[2][c];
-      } else {                                    // two parts a product, 64 dims each
-        const int a = part[c / 4][c % 4], b = c < 4 ? part[2][c % 4] : 0;
-        if constexpr (HALF) {
-          qp[0][c] = second ? b : a;
-        } else {
-          qp[0][c] = a;
-          qp[1][c] = b;
-        }
+      } else {                                    // both parts, 64 dims each
+        qp[0][c] = second ? 0 : part[c / 4][c % 4];
       }
     }
     if constexpr (HD == 128 && !HALF) {
       qs[0] = s0;
       qs[1] = s1;
-      qs[2] = s2;
     } else if constexpr (HD == 128) {
       qs[0] = second ? s1 : s0;
-      qs[1] = s2;
     } else {
-      qs[0] = second ? s2 : (g < 2 ? s0 : s1);
-      if constexpr (!HALF) qs[1] = s2;
+      qs[0] = g < 2 ? s0 : s1;
     }
 #pragma unroll
-    for (int i = 0; i < QM + QD; ++i) qs[i] = odd ? 255 : qs[i];
+    for (int i = 0; i < QM; ++i) qs[i] = odd ? 255 : qs[i];
     const int p = prefix ? d.w.pos[tok] : p0 + tk;
     const int hi = rv ? (d.causal ? imin(p + 1, kceil) : kceil) : kfloor;
     const int lo = d.window > 0 ? imax(p - d.window + 1, kfloor) : kfloor;
@@ -1681,11 +1694,18 @@ __global__ __launch_bounds__(NW* kWave, kFewSimd) void k_kv_few(const KvDev d) {
     for (int p = QM - 1; p >= 0; --p)
 #pragma unroll
       for (int n = 0; n < 4; ++n) s[n] = mma16_f4f8(kx[n], qp[p], s[n], (int)ke[n], qs[p]);
-    if constexpr (QD > 0)
-      if (deep) {                                 // wave-uniform
+    if (__builtin_expect(raw, 0)) {               // wave-uniform: in their place
 #pragma unroll
-        for (int n = 0; n < 4; ++n) s[n] = mma16_f4f8(kx[n], qp[QM], s[n], (int)ke[n], qs[QM]);
+      for (int n = 0; n < 4; ++n) s[n] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const u32x4 x = *raw_q(4 * (g & (HD / 32 - 1)) + t);
+        const u32x4 y = li < R && g < HD / 32 ? x : u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+          s[n] = mma16_bf16(f4_bf16x8(kx[n][t], __uint_as_float(ke[n] << 23)), y, s[n]);
       }
+    }
     if constexpr (HALF) {                         // a row's parts
 #pragma unroll
       for (int n = 0; n < 4; ++n)

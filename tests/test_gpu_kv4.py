@@ -270,6 +270,59 @@ def test_nan_values_of_later_tokens(ql):
     kv.close()
 
 
+@pytest.mark.parametrize("far", [14, 20, 27, 60, 100])
+@pytest.mark.parametrize("hd,heads,n_kv,ql", [(128, 8, 2, [1, 1, 2]), (64, 8, 2, [1, 1, 2]),
+                                              (128, 16, 1, [1, 1, 1]), (64, 12, 3, [1, 4, 3]),
+                                              (128, 8, 1, [4, 2, 3]), (64, 4, 2, [16, 7, 16])])
+def test_queries_of_far_apart_magnitudes(hd, heads, n_kv, ql, far):
+    """Queries with 32 elements 2^far above the others and keys as far below there: all of
+    them count for the scores, as where they are alike."""
+    import torch
+    c = Call4(far + hd, [130, 64, 333], ql, heads=heads, n_kv=n_kv, hd=hd, P=16)
+    c.q[:, ::2, 32:64] *= 2.0 ** far                          # the others' rows beside them
+    codes, exps = c.bits[0]
+    exps[..., 1] -= far
+    c.k = R.mxfp4_values(codes, exps)
+    assert np.isfinite(c.k).all() and np.array_equal(bf16(c.q), c.q)
+    kv = c.device()
+    for m in (dict(causal=True), dict(causal=False, window=90, sinks=7)):
+        print(f"far-apart queries: hd={hd} heads={heads}/{n_kv} ql={ql} 2^{far} {m}", flush=True)
+        lse = torch.zeros((c.total, c.heads), device="cuda")
+        out = c.run(kv, lse=lse, **m)
+        assert kv.device_errors() == 0
+        c.check(out, lse, parts=parts_of4(c.rows()), **m)
+    kv.close()
+
+
+@pytest.mark.parametrize("tiny", [0.0, 2.0 ** -40])
+@pytest.mark.parametrize("hd,heads,n_kv", [(128, 8, 2), (64, 8, 2), (128, 16, 1), (64, 12, 1)])
+def test_infinite_queries_and_nan_keys_beside_tiny_elements(hd, heads, n_kv, tiny):
+    """A row with an infinity, NaN in keys behind the last one and before the window: with
+    and without elements far below their row's greatest, the other rows are the oracle's."""
+    c = Call4(hd + heads, [130, 77], [1, 1], heads=heads, n_kv=n_kv, hd=hd, P=16)
+    if tiny:
+        c.q[..., 3] = tiny
+    for x in (0, 1):
+        for b, n in enumerate(c.kv):
+            for j in [*range(3, n - 50), *range(n, -(-n // 16) * 16)]:
+                c.exponent(x, c.table[b, j // 16], j % 16, 255)
+    bad = [(0, 1, np.inf), (1, heads - 1, -np.inf), (1, 0, np.nan)]
+    want = c.oracle(causal=True, window=50, sinks=3, parts=parts_of4(c.rows()))
+    for t, h, v in bad:
+        c.q[t, h, 7] = v
+    kv = c.device()
+    print(f"infinite queries: hd={hd} heads={heads}/{n_kv} tiny={tiny}", flush=True)
+    out = c.run(kv, window=50, sinks=3).double().cpu().numpy()
+    assert kv.device_errors() == 0
+    for b in want:
+        o, _, eb, _ = want[b]
+        ok = np.array([(b, h) not in [x[:2] for x in bad] for h in range(heads)])
+        got = out[c.cu[b]:c.cu[b + 1]]
+        assert (np.abs(got - o) <= eb)[:, ok].all()
+        assert np.isnan(got[:, ~ok]).all()
+    kv.close()
+
+
 SHARED4 = {
     "one group": ([700, 650, 900], [1, 1, 1], [(0, 3, 512)], dict(heads=8, n_kv=2)),
     "blocks": ([300, 280, 90, 400, 330], [16, 16, 16, 16, 16], [(0, 2, 256), (2, 3, 0), (3, 5, 320)],
