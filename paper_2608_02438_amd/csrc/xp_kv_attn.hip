@@ -1403,7 +1403,6 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
 // its way through LDS, exponentials) and by 384 segments' beginnings and ends.
 // ---------------------------------------------------------------------------
 typedef int intx8 __attribute__((ext_vector_type(8)));
-typedef __attribute__((address_space(3))) char lds_char;
 constexpr int kFewRows = 16;         // the larger row tile (kv_least)
 constexpr int kFewSimd = 3;          // waves of a SIMD
 
