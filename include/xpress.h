@@ -507,7 +507,8 @@ xp_status xp_kv_read(xp_kv* kv, int32_t tokens, const int32_t* slots, const void
  *               tokens from cu_q[n] on are left as they are.
  *   max_q       the most tokens of a request, up to max_tokens.  It sizes the row
  *               tiles and chooses the numerators' parts (below): a wrong one costs
- *               time, one that is too large may cost the second part
+ *               time, one that is too large may cost the second part, and one that is
+ *               too small for a long prompt over a 4-bit cache may be refused (Errors)
  *   kv_len      [n] int32: keys of request b, the new tokens' own among them
  *   causal      1 or 0 (the drafter's bidirectional block)
  *   window      0: none; W: a token at position p sees keys j > p - W only
@@ -665,8 +666,8 @@ const char* xp_sampler_last_error(const xp_sampler* s);
  * Logits of -inf (masked tokens) and NaN are never taken; a row that holds nothing else
  * gives id -1, log probability -inf, and sets XP_DEVERR_EMPTY.  Tokens at +inf share all
  * of the weight.  Weights e^{(l - max) / T} are formed in 64 bits and summed exactly in
- * units of 2^-45; tokens below 2^-46 of the greatest weight have none.  The same call
- * gives the same tokens.
+ * units of 2^-45; tokens below 2^-46 of the greatest weight have none.  Sums are compared
+ * with p and u times others in fp64.  The same call gives the same tokens.
  * Errors: XP_EINVAL before any launch, XP_EHIP.
  */
 xp_status xp_sample(xp_sampler* s, int32_t rows, int32_t dtype, const void* logits, int64_t ld,

@@ -1398,7 +1398,7 @@ __global__ __launch_bounds__(WR* WK* kWave, kv_waves(HD, WR, WK)) void k_kv_attn
 // results are added through LDS.  A wave issues an instruction in 8 cycles at best, a SIMD
 // in 4.3: three waves of 168 registers (two, each with two tiles under way, 107 to 118 us
 // where three take 94; 1 or 2 waves a workgroup the same, 3, 6, 8 and 12 take 110 to 150).
-// 48 single tokens over 512 .. 16384 keys, 439 MB: 88 to 93 us, 4.7 to 5 TB/s; the 32-row
+// 48 single tokens over 512 .. 16384 keys, 439 MB: 91 to 95 us, 4.6 to 4.8 TB/s; the 32-row
 // engine above took 225.  Bound by memory, by the vector instructions (V's expansion and
 // its way through LDS, exponentials) and by 384 segments' beginnings and ends.
 // ---------------------------------------------------------------------------

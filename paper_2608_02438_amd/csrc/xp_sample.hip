@@ -7,8 +7,10 @@
 //
 // A sample hangs on where u falls between sums over the vocabulary, so the weights are
 // formed in 64 bits and then held as integers, 2^45 for the largest: sums of up to 2^18
-// of them fit 63 bits and are exact, the same whatever their order, and of any two sums
-// that are compared neither is rounded.  What 2^-46 of the largest weight can move is
+// of them are 2^63 at most and exact, the same whatever their order.  They are compared
+// with p or u times another sum in fp64: from 2^53 on (256 tokens of the largest weight)
+// both sides are rounded, by 2^-53 of themselves, which never puts sums out of order, so
+// that exactly one token passes.  What that, and 2^-46 of the largest weight, can move is
 // far below the 2^-24 by which uniforms differ.
 //
 // Four launches: the largest logits; weights or a histogram of them; the tokens in the bin
@@ -56,7 +58,8 @@ enum SmpMode {
   kSmpPlain = 0,                     // no threshold of l: the chunks' sums are final
   kSmpList = 1,                      // the candidates are all tokens that can stay
   kSmpEdge = 2,                      // tokens before the edge's bin stay, those of it are candidates
-  kSmpSlow = 3                       // too many candidates, or no bins: the row by radix selection
+  kSmpSlow = 3                       // too many candidates, no bins, or top-p among fewer than k
+                                     // tokens with a weight: the row by radix selection
 };
 
 struct Smp {
@@ -707,7 +710,9 @@ __device__ __forceinline__ void row_draw(const Smp& d, RowShared& s, int64_t r, 
 }
 
 // Rows with more candidates than the list holds (many equal logits, or top-k of tens of
-// thousands with top-p), or a temperature past the bins' fp32: radix selection over the row.
+// thousands with top-p), with top-p where fewer than k tokens have a weight (within 32 T of
+// the largest logit: peaked rows), or a temperature past the bins' fp32: radix selection over
+// the row, which one workgroup walks about eight times.
 template <typename T>
 __device__ __forceinline__ void row_slow(const Smp& d, RowShared& s, int64_t r, const T* row, bool wide,
                                       const SmpRow& w, const SmpSet& set) {
